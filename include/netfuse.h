@@ -186,6 +186,90 @@ nf_status netfuse_attention_relpos(const void* Q, const void* K, const void* V, 
                                    float scale, nf_dtype dt, void* stream);
 
 /*
+ * Decoders (the operators above merge encoders): attention of prompts, then of the tokens that follow over a cache of keys and
+ * values, and that cache.  Attention has no weights, so merging M models multiplies the number of independent problems by M here
+ * too (Section 3.1, "Operations with input-weight local computations"); the slopes of a distance bias are per model.
+ *
+ * Common to these calls
+ *   - Rows: element (m, b, s, head, t) of Q lives at ptr[m*q_stride_m + (b*N + s)*q_stride_row + head*d + t] (N = S or T), of K and V
+ *     likewise with kv_heads heads and kv_stride_*; the three may point into one packed buffer.  Query head h reads key head
+ *     h / (heads / kv_heads); heads is a multiple of kv_heads.  O[M][B*N][heads*d] is dense and must not alias an input.
+ *   - Cache: Kc and Vc [M][B][kv_heads][C][d] dense, C the capacity.  len[M][B]: entries that each sequence holds, in slots 0 ... len-1,
+ *     the same number for every head.  pos[M][B][kv_heads][C] int: position of each entry, or NULL: its slot.  weight[...] float: attention
+ *     weight that each entry has collected.  What lies in other slots is neither read nor written.
+ *   - start[M][B] int: position of the first new token of each sequence, or NULL: len.
+ *   - Scores: s_ij = f(scale * q_i . k_j) - slope[m][head] * |position_i - position_j|,  f(x) = cap * tanh(x / cap), or x for cap = 0.
+ *     slope: float[M][heads], finite, or NULL.  cap: 0, or 1e-30 ... 1e30.
+ *   - What a row does not see has no part in it whatever it holds, infinities and NaN too.  A row that sees nothing gives 0.
+ *   - Integer operands are DEVICE arrays that the kernels bound: a length, count or number of nodes below 0 counts as 0, above its range as the
+ *     largest.  No call changes len or start: after an append the caller adds the counts, after an eviction it takes min(len, budget).
+ *   - NF_EUNSUPPORTED for d > 256.
+ */
+
+/*
+ * Attention of prompts:  row i of sequence (m, b) sees key j if  i, j < len[m][b],  and with causal != 0  j <= i or j < prefix[m][b],
+ * and with doc  doc[m][b][i] == doc[m][b][j] >= 0.  Positions are 0 ... S-1.
+ *   len, prefix: int[M][B] or NULL (all S rows; no prefix).  prefix only with causal.   doc: int[M][B][S] or NULL.
+ * Rows at and past len are written as 0.
+ */
+nf_status netfuse_attention_prompt(const void* Q, const void* K, const void* V, const float* slope, const int* len,
+                                   const int* prefix, const int* doc, void* O, int M, int B, int S, int heads, int kv_heads,
+                                   int d, long q_stride_m, long q_stride_row, long kv_stride_m, long kv_stride_row, int causal,
+                                   float scale, float cap, nf_dtype dt, void* stream);
+
+/*
+ * Attention of a tree of T <= 64 drafted tokens per sequence over the cache (NF_EUNSUPPORTED for more).  Node t sees every entry of the cache,
+ * itself and its ancestors; its position is start + the number of its ancestors.
+ *   parent: int[M][B][T], the parent of each node: a lower node, or anything else for a root; NULL: node t-1 (a chain, T = 1 a single token).
+ *   nodes: int[M][B], how many of the T are there, or NULL: all.  Rows past it are written as 0.
+ *   lse: float[M][B*T][heads] or NULL: log of the sum of exp(s_ij) over the keys that a row sees (-infinity if none), for netfuse_cache_weigh.
+ *   workspace: 16-byte aligned device memory of at least netfuse_attention_tree_workspace(...) bytes (-1 for sizes that the call refuses;
+ *   may be 0: then NULL will do).  Calls that may run at the same time need one each, two captured graphs that may too.
+ */
+long long netfuse_attention_tree_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt);
+nf_status netfuse_attention_tree(const void* Q, const void* K, const void* V, const void* Kc, const void* Vc, const int* pos,
+                                 const int* len, const int* start, const int* parent, const int* nodes, const float* slope,
+                                 void* O, float* lse, void* workspace, long long workspace_bytes, int M, int B, int T, int C,
+                                 int heads, int kv_heads, int d, long q_stride_m, long q_stride_row, long kv_stride_m,
+                                 long kv_stride_row, float scale, float cap, nf_dtype dt, void* stream);
+
+/*
+ * New rows into the cache (a prompt's, or the accepted path of a tree): entry len + i takes row index[m][b][i] of the T rows of K and V,
+ * position start + i and weight 0, for i < count[m][b].
+ *   index: int[M][B][n] or NULL (row i; n = T then).   count: int[M][B] or NULL (all n).   pos, weight: or NULL (not kept).
+ * An entry that would lie past C, or whose row number is not one of the T, is not written.
+ */
+nf_status netfuse_cache_append(const void* K, const void* V, const int* index, const int* count, const int* len, const int* start,
+                               void* Kc, void* Vc, int* pos, float* weight, int M, int B, int T, int n, int C, int kv_heads, int d,
+                               long kv_stride_m, long kv_stride_row, nf_dtype dt, void* stream);
+
+/*
+ * Attention weight of the entries, summed over the new tokens, after they were appended (len, start, index and count as for
+ * netfuse_cache_append, Q and lse the rows of netfuse_attention_tree): token i < count[m][b] has row index[m][b][i] and position start + i and sees slots
+ * j <= len + i, and
+ *   weight_out[m][b][g][j] = weight[m][b][g][j] + sum over these tokens and the query heads h of key head g of exp(s_ij - lse_ih)
+ * for all C slots (a slot that no token sees keeps its value; a row number that is not one of the T and a row whose lse is -infinity add nothing).
+ * weight_out may be weight.
+ */
+nf_status netfuse_cache_weigh(const void* Q, const float* lse, const int* index, const int* count, const void* Kc, const int* pos,
+                              const int* len, const int* start, const float* slope, const float* weight, float* weight_out, int M,
+                              int B, int T, int n, int C, int heads, int kv_heads, int d, long q_stride_m, long q_stride_row,
+                              float scale, float cap, nf_dtype dt, void* stream);
+
+/*
+ * Eviction: every head of a sequence that holds more than `budget` entries gives up len - budget of them: those of lowest weight, the lower
+ * slot first among equals, and any at positions start - recent and later only once no others are left (NaN counts as the largest weight).
+ * The free slots below budget, in rising order, take the entries that stay in slots budget ... len-1, in rising order: keys and values in place,
+ * position and weight from pos, weight to pos_out, weight_out, of which slots 0 ... min(len, budget)-1 are written.
+ *   pos, pos_out: both, or both NULL with recent = 0.   pos_out may be pos, weight_out may be weight.   0 < budget <= C.
+ *   workspace: as for netfuse_attention_tree, of netfuse_cache_evict_workspace(...) bytes.
+ */
+long long netfuse_cache_evict_workspace(int M, int B, int C, int kv_heads, int budget);
+nf_status netfuse_cache_evict(void* Kc, void* Vc, const int* pos, const float* weight, const int* len, const int* start, int* pos_out,
+                              float* weight_out, void* workspace, long long workspace_bytes, int M, int B, int C, int kv_heads,
+                              int d, int budget, int recent, nf_dtype dt, void* stream);
+
+/*
  * Non-trainable operators merge by concatenation (Section 3.1, "Non-trainable operations"), so
  * these act per channel of the channel-merged tensor; Ctot = M*C.
  * Max pooling: x[B][Ctot][H][W] -> y[B][Ctot][Ho][Wo], window k x k, Ho = (H + 2 pad - k)/stride + 1;

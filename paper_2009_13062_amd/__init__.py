@@ -29,7 +29,9 @@ EXPORTS = ("netfuse_linear", "netfuse_conv2d", "netfuse_layernorm", "netfuse_bat
            "netfuse_bn_fold", "netfuse_attention", "netfuse_maxpool2d", "netfuse_avgpool_global",
            "netfuse_merge_transpose", "netfuse_linear_pack_weight", "netfuse_linear_packed",
            "netfuse_time_next_launch", "netfuse_linear_packed_supported", "netfuse_linear_ragged",
-           "netfuse_attention_relpos", "netfuse_probe_mfma", "netfuse_probe_hbm_read", "netfuse_strerror")
+           "netfuse_attention_relpos", "netfuse_probe_mfma", "netfuse_probe_hbm_read", "netfuse_attention_prompt",
+           "netfuse_attention_tree_workspace", "netfuse_attention_tree", "netfuse_cache_append", "netfuse_cache_weigh",
+           "netfuse_cache_evict_workspace", "netfuse_cache_evict", "netfuse_strerror")
 
 
 class NetFuseError(RuntimeError):
@@ -62,8 +64,16 @@ def _load() -> ctypes.CDLL:
     lib.netfuse_linear_ragged.argtypes = [vp, vp, fp, vp, i, i, i, ctypes.POINTER(ctypes.c_int), i, i, vp]
     lib.netfuse_probe_mfma.argtypes = [vp, i, ctypes.POINTER(ctypes.c_double), vp]
     lib.netfuse_probe_hbm_read.argtypes = [vp, ctypes.c_longlong, vp, vp]
+    ll = ctypes.c_longlong
+    lib.netfuse_attention_prompt.argtypes = [vp] * 3 + [fp] + [vp] * 4 + [i] * 6 + [l] * 4 + [i, f, f, i, vp]
+    lib.netfuse_attention_tree_workspace.argtypes = [i] * 8
+    lib.netfuse_attention_tree.argtypes = [vp] * 10 + [fp, vp, fp, vp, ll] + [i] * 7 + [l] * 4 + [f, f, i, vp]
+    lib.netfuse_cache_append.argtypes = [vp] * 8 + [vp, fp] + [i] * 7 + [l, l, i, vp]
+    lib.netfuse_cache_weigh.argtypes = [vp, fp] + [vp] * 6 + [fp] * 3 + [i] * 8 + [l, l, f, f, i, vp]
+    lib.netfuse_cache_evict_workspace.argtypes = [i] * 5
+    lib.netfuse_cache_evict.argtypes = [vp] * 3 + [fp] + [vp] * 3 + [fp, vp, ll] + [i] * 7 + [i, vp]
     for name in EXPORTS[:-1]:
-        getattr(lib, name).restype = ctypes.c_int
+        getattr(lib, name).restype = ll if name.endswith("_workspace") else ctypes.c_int
     lib.netfuse_strerror.argtypes = [ctypes.c_int]
     lib.netfuse_strerror.restype = ctypes.c_char_p
     return lib
@@ -378,3 +388,7 @@ def merge_transpose(src, M, to_channel, out=None, stream=None):
     _check("netfuse_merge_transpose", lib.netfuse_merge_transpose(
         _ptr(src), _ptr(dst, src), M, rows, H, int(bool(to_channel)), _dt(src), _stream(stream)))
     return dst
+
+
+from .decoder import (attention_prompt, attention_tree, attention_tree_workspace, cache_append, cache_evict,  # noqa: E402,F401
+                      cache_evict_workspace, cache_weigh)

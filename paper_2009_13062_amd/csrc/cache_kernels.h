@@ -1,0 +1,201 @@
+// The cache of merged decoders: rows appended, entries evicted.
+#pragma once
+#include "decoder.h"
+
+namespace nf {
+
+struct AppendArgs {
+  const void* K; const void* V; const int* index; const int* count; const int* len; const int* start;
+  void* Kc; void* Vc; int* pos; float* weight;
+  int M, B, T, n, C, kv, units;                            // units: pieces of type U per row and head
+  long stride_m, stride_row;                               // in pieces
+};
+
+// Copies of U at a time (16 bytes where rows and strides allow, one element otherwise).  A workgroup takes `rows` new rows of one sequence;
+// consecutive threads take consecutive pieces of a head's row, on both sides.
+template <typename U>
+__global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, int rows, int blocks_per_seq) {
+  const long mb = blockIdx.x / blocks_per_seq;
+  const int i0 = (int)(blockIdx.x % blocks_per_seq) * rows;
+  const int b = (int)(mb % a.B);
+  const long m = mb / a.B;
+  const int cnt = a.count ? clamp_len(a.count[mb], a.n) : a.n, L = clamp_len(a.len[mb], a.C);
+  const int end = min(min(i0 + rows, cnt), a.C - L);       // entries past the capacity are not written
+  const int per_row = a.kv * a.units;
+  for (int i = i0 + (int)threadIdx.x / per_row, c = (int)threadIdx.x % per_row; i < end;) {
+    const int row = a.index ? a.index[mb * a.n + i] : i;
+    if (row >= 0 && row < a.T) {
+      const int g = c / a.units, u = c % a.units;
+      const long from = m * a.stride_m + ((long)b * a.T + row) * a.stride_row + c;
+      const long slot = (mb * a.kv + g) * a.C + L + i;
+      ((U*)a.Kc)[slot * a.units + u] = ((const U*)a.K)[from];
+      ((U*)a.Vc)[slot * a.units + u] = ((const U*)a.V)[from];
+      if (u == 0) {
+        if (a.pos) a.pos[slot] = (a.start ? a.start[mb] : L) + i;
+        if (a.weight) a.weight[slot] = 0.f;
+      }
+    }
+    c += 256;
+    i += c / per_row;
+    c %= per_row;
+  }
+}
+
+struct EvictArgs {
+  void* Kc; void* Vc; const int* pos; const float* weight; const int* len; const int* start; int* pos_out; float* weight_out; int* ws;
+  int M, B, C, kv, units, budget, recent, most;            // most: pairs that a head can have, min(budget, C - budget)
+};
+
+// Bits of a weight in the order of its value: -0 counts as 0, NaN as the largest.
+__device__ __forceinline__ uint32_t weight_order(float w) {
+  if (w != w) return 0xffffffffu;
+  const uint32_t u = __float_as_uint(w + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// Exclusive sum over the 1024 threads of a workgroup, `total` their sum.  Every thread has to come here.
+__device__ __forceinline__ int block_scan(int v, int* wave_sums, int& total) {
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int x = v;
+#pragma unroll
+  for (int o = 1; o < kWave; o *= 2) {
+    const int y = __shfl_up(x, o, kWave);
+    if (lane >= o) x += y;
+  }
+  if (lane == kWave - 1) wave_sums[wave] = x;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    const int s = wave_sums[w];
+    before += w < wave ? s : 0;
+    total += s;
+  }
+  __syncthreads();
+  return before + x - v;
+}
+
+// Which entries of one head leave: one workgroup finds the n-th smallest (guarded, weight) by digits of 11, 11 and 10 bits of the weight's order,
+// then walks the slots in order, giving entries equal to it to the lowest slots, and writes the list of free slots below the budget and
+// that of the entries above it that stay (equally many).  Counts in LDS: whole numbers, so their order does not matter.
+__global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
+  __shared__ int hist[2048];
+  __shared__ int wave_sums[16];
+  __shared__ int found[3];
+  const int tid = threadIdx.x;
+  const long head = blockIdx.x, mb = head / a.kv;
+  const int L = clamp_len(a.len[mb], a.C);
+  const int keep = min(L, a.budget), n = L - keep;
+  const long long bound = (long long)(a.start ? a.start[mb] : L) - a.recent;     // guarded from this position on
+  const float* w = a.weight + head * a.C;
+  const int* pos = a.pos ? a.pos + head * a.C : nullptr;
+  int* const count = a.ws + head * (1 + 2 * (long)a.most);
+  int* const holes = count + 1;
+  int* const movers = holes + a.most;
+  auto is_guarded = [&](int j) { return a.recent > 0 && (long long)pos[j] >= bound; };
+  if (n == 0) {                                            // uniform
+    if (tid == 0) *count = 0;
+    for (int j = tid; j < keep; j += 1024) {
+      if (a.weight_out != a.weight) a.weight_out[head * a.C + j] = w[j];
+      if (pos && a.pos_out != a.pos) a.pos_out[head * a.C + j] = pos[j];
+    }
+    return;
+  }
+  int open = 0, total;
+  for (int j = tid; j < L; j += 1024) open += !is_guarded(j);
+  block_scan(open, wave_sums, open);
+  const bool guards = n > open;                            // all the others leave and some guarded entries too
+  int want = guards ? n - open : n;                        // so many of the group with is_guarded == guards, from the smallest
+  uint32_t prefix = 0;
+  for (int shift = 21, bits = 11; bits > 0;) {
+    for (int d = tid; d < 2048; d += 1024) hist[d] = 0;
+    __syncthreads();
+    for (int j = tid; j < L; j += 1024) {
+      const uint32_t o = weight_order(w[j]);
+      if (is_guarded(j) == guards && (shift + bits == 32 || (o >> (shift + bits)) == prefix)) atomicAdd(&hist[(o >> shift) & ((1u << bits) - 1)], 1);
+    }
+    __syncthreads();
+    const int c0 = hist[2 * tid], c1 = hist[2 * tid + 1];
+    const int before = block_scan(c0 + c1, wave_sums, total);
+    if (before < want && want <= before + c0) found[0] = 2 * tid, found[1] = before;
+    if (before + c0 < want && want <= before + c0 + c1) found[0] = 2 * tid + 1, found[1] = before + c0;
+    __syncthreads();
+    prefix = (prefix << bits) | (uint32_t)found[0];
+    want -= found[1];                                      // at least 1 of the entries with this prefix
+    __syncthreads();
+    bits = shift == 21 ? 11 : shift == 10 ? 10 : 0;
+    shift = shift == 21 ? 10 : 0;
+  }
+  int equal_before = 0, holes_before = 0, movers_before = 0;
+  for (int j0 = 0; j0 < L; j0 += 4096) {                   // 4 slots in a row per thread
+    uint32_t o[4];
+    bool in[4], guarded[4];
+    int equal = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = j0 + 4 * tid + e;
+      in[e] = j < L;
+      o[e] = in[e] ? weight_order(w[j]) : 0;
+      guarded[e] = in[e] && is_guarded(j);
+      equal += in[e] && guarded[e] == guards && o[e] == prefix;
+    }
+    int rank = equal_before + block_scan(equal, wave_sums, total);
+    equal_before += total;
+    bool leaves[4];
+    int mine = 0;                                          // holes in the low half, movers in the high half
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = j0 + 4 * tid + e;
+      const bool same = guarded[e] == guards;
+      leaves[e] = in[e] && (same ? o[e] < prefix || (o[e] == prefix && rank < want) : guards);
+      rank += in[e] && same && o[e] == prefix;
+      if (in[e]) mine += j < keep ? (leaves[e] ? 1 : 0) : (leaves[e] ? 0 : 1 << 16);
+    }
+    int at = block_scan(mine, wave_sums, total);
+    int hole = holes_before + (at & 0xffff), mover = movers_before + (at >> 16);
+    holes_before += total & 0xffff;
+    movers_before += total >> 16;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = j0 + 4 * tid + e;
+      if (!in[e]) continue;
+      if (j < keep) {
+        if (leaves[e]) holes[hole++] = j;
+        else {
+          if (a.weight_out != a.weight) a.weight_out[head * a.C + j] = w[j];
+          if (pos && a.pos_out != a.pos) a.pos_out[head * a.C + j] = pos[j];
+        }
+      } else if (!leaves[e]) {
+        movers[mover++] = j;
+      }
+    }
+  }
+  if (tid == 0) *count = holes_before;
+}
+
+// The pairs of the lists: rows of keys and values, position and weight.  Sources lie at or above the budget, targets below it, each once.
+template <typename U>
+__global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int rows, int blocks_per_head) {
+  const long head = blockIdx.x / blocks_per_head;
+  const int* count = a.ws + head * (1 + 2 * (long)a.most);
+  const int* holes = count + 1;
+  const int* movers = holes + a.most;
+  const int i0 = (int)(blockIdx.x % blocks_per_head) * rows, end = min(i0 + rows, *count);
+  U* Kh = (U*)a.Kc + head * a.C * a.units;
+  U* Vh = (U*)a.Vc + head * a.C * a.units;
+  for (int i = i0 + (int)threadIdx.x / a.units, u = (int)threadIdx.x % a.units; i < end;) {
+    const long to = holes[i], from = movers[i];
+    Kh[to * a.units + u] = Kh[from * a.units + u];
+    Vh[to * a.units + u] = Vh[from * a.units + u];
+    if (u == 0) {
+      a.weight_out[head * a.C + to] = a.weight[head * a.C + from];
+      if (a.pos) a.pos_out[head * a.C + to] = a.pos[head * a.C + from];
+    }
+    u += 256;
+    i += u / a.units;
+    u %= a.units;
+  }
+}
+
+}  // namespace nf

@@ -1,0 +1,44 @@
+// What the kernels of merged decoders share: their operands, scores and masks.
+//
+// Score of query i and key j:  f(scale q_i . k_j) - slope |position_i - position_j|,  f(x) = cap tanh(x / cap) or x.  A key that a row does not
+// see is left out by a select on its weight (and on its values where these could be infinite or NaN), never by adding to its score.
+#pragma once
+#include <type_traits>
+
+#include "nf_common.h"
+
+namespace nf {
+
+constexpr float kLowestScore = -3.402823466e38f;          // running maxima start here: finite, so that a difference of two is no NaN
+
+struct DecArgs {
+  const void* Q; const void* K; const void* V;          // new rows: [M][B * N] of heads * d and kv * d, strides below
+  const void* Kc; const void* Vc;                       // cache [M][B][kv][C][d]; null for prompts
+  const float* slope;                                   // [M][heads] or null
+  const int* len; const int* prefix; const int* doc;    // [M][B], [M][B], [M][B][N], each or null
+  const int* start; const int* parent; const int* nodes; const int* pos;
+  void* O; float* lse; float* ws;
+  int M, B, N, C, heads, kv, d, causal;
+  long q_stride_m, q_stride_row, kv_stride_m, kv_stride_row;
+  float scale, cap, inv_cap;                            // inv_cap = 1 / cap, 0 without a cap
+};
+
+__device__ __forceinline__ int clamp_len(int v, int top) { return min(max(v, 0), top); }
+
+// f of the score, the exact way: tanhf in natural units.
+__device__ __forceinline__ float capped(float x, const DecArgs& a) { return a.cap != 0.f ? a.cap * tanhf(x * a.inv_cap) : x; }
+
+// The nodes that node t of a tree sees, itself among them, a bit each.  Ancestors have lower numbers, so the walk ends after at most t steps
+// whatever `parent` holds, and the distance from t to node u of its path is the number of path nodes above u: popcount(path >> u) - 1.
+__device__ __forceinline__ uint64_t tree_path(const int* parent, int t) {
+  if (!parent) return (2ull << t) - 1;
+  uint64_t path = 1ull << t;
+  for (int u = t;;) {
+    const int p = parent[u];
+    if (p < 0 || p >= u) return path;
+    path |= 1ull << p;
+    u = p;
+  }
+}
+
+}  // namespace nf

@@ -20,6 +20,7 @@
 #include "gemm_mfma.h"
 #include "generic_kernels.h"
 #include "nf_common.h"
+#include "nf_host.h"
 #include "norm_kernels.h"
 #include "probe_kernels.h"
 
@@ -27,23 +28,7 @@ using namespace nf;
 
 namespace {
 
-inline bool is_dtype(int dt) { return dt == NF_F32 || dt == NF_BF16; }
 inline bool is_act(int a) { return a == NF_ACT_NONE || a == NF_ACT_RELU || a == NF_ACT_GELU; }
-inline bool aligned(const void* p, size_t a) { return p == nullptr || ((uintptr_t)p % a) == 0; }
-
-// product of non-negative ints, saturating at LLONG_MAX
-inline long long prod(std::initializer_list<long long> v) {
-  long long r = 1;
-  for (long long x : v) {
-    if (x < 0) return -1;
-    if (x != 0 && r > LLONG_MAX / x) return LLONG_MAX;
-    r *= x;
-  }
-  return r;
-}
-constexpr long long kMaxElems = (1LL << 62);     // element counts must stay below this
-constexpr long long kMaxGrid = 0x7fffffffLL;
-
 }  // namespace
 
 namespace nf {
