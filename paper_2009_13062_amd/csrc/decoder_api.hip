@@ -8,6 +8,7 @@
 #include "cache_kernels.h"
 #include "decoder.h"
 #include "decoder_generic.h"
+#include "decoder_launch.h"
 #include "nf_host.h"
 #include "nf_launch.h"
 
@@ -29,6 +30,15 @@ bool rows_ok(int M, long long rows, long long width, long stride_m, long stride_
 }
 
 bool heads_ok(int heads, int kv_heads, int d) { return heads > 0 && kv_heads > 0 && d > 0 && heads % kv_heads == 0; }
+
+// What the tiled kernels take: rows in 16-byte pieces, row numbers in an int.
+bool tiles_sizes(int N, int heads, int kv_heads, int d, nf_dtype dt) {
+  return dt == NF_BF16 && d % 8 == 0 && d <= 128 && (long long)N * (heads / kv_heads) <= INT_MAX / 2;
+}
+bool tiles_ok(const DecArgs& a, nf_dtype dt) {
+  return tiles_sizes(a.N, a.heads, a.kv, a.d, dt) && a.q_stride_m % 8 == 0 && a.q_stride_row % 8 == 0 && a.kv_stride_m % 8 == 0 && a.kv_stride_row % 8 == 0 &&
+         aligned(a.Q, 16) && aligned(a.K, 16) && aligned(a.V, 16) && aligned(a.Kc, 16) && aligned(a.Vc, 16) && aligned(a.O, 8);
+}
 
 template <bool TREE>
 nf_status launch_rows(const DecArgs& a, nf_dtype dt, hipStream_t s) {
@@ -69,12 +79,17 @@ nf_status netfuse_attention_prompt(const void* Q, const void* K, const void* V, 
   a.M = M; a.B = B; a.N = S; a.heads = heads; a.kv = kv_heads; a.d = d; a.causal = causal != 0;
   a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.kv_stride_m = kv_stride_m; a.kv_stride_row = kv_stride_row;
   a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
+  if (tiles_ok(a, dt)) return launch_prompt_tiles(a, (hipStream_t)stream);
   return launch_rows<false>(a, dt, (hipStream_t)stream);
 }
 
 long long netfuse_attention_tree_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt) {
   if (M <= 0 || B <= 0 || T <= 0 || T > 64 || C <= 0 || !heads_ok(heads, kv_heads, d) || d > 256 || !is_dtype(dt)) return -1;
-  return 0;
+  if (!tiles_sizes(T, heads, kv_heads, d, dt)) return 0;
+  const int chunk = tree_chunk(T * (heads / kv_heads)), splits = (int)(((long long)C + chunk - 1) / chunk);
+  if (splits == 1) return 0;                               // no cache is shared out
+  const long long bytes = prod({M, B, heads, T, splits, 4LL * (tree_features(d) + 2)});      // a row's sums, its maximum and its total per chunk
+  return bytes >= kMaxElems ? -1 : bytes;
 }
 
 nf_status netfuse_attention_tree(const void* Q, const void* K, const void* V, const void* Kc, const void* Vc, const int* pos,
@@ -104,6 +119,10 @@ nf_status netfuse_attention_tree(const void* Q, const void* K, const void* V, co
   a.M = M; a.B = B; a.N = T; a.C = C; a.heads = heads; a.kv = kv_heads; a.d = d;
   a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.kv_stride_m = kv_stride_m; a.kv_stride_row = kv_stride_row;
   a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
+  if (tiles_ok(a, dt)) {
+    const int chunk = tree_chunk(T * (heads / kv_heads));
+    return launch_tree_tiles(a, chunk, (int)(((long long)C + chunk - 1) / chunk), (hipStream_t)stream);
+  }
   return launch_rows<true>(a, dt, (hipStream_t)stream);
 }
 

@@ -1,0 +1,46 @@
+// bfloat16 attention of prompts and trees: instances and launches of decoder_tiles.h.
+#include <atomic>
+
+#include "decoder_launch.h"
+#include "decoder_tiles.h"
+#include "nf_host.h"
+#include "nf_launch.h"
+
+namespace nf {
+namespace {
+
+template <int D, int KB, int KS, int RB, bool TREE>
+nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
+  constexpr int kRows = 4 / KS * RB * 32, kBytes = DecLds<D, KB, KS == 1 ? 2 : 1>::kBytes;
+  const long long R = (long long)a.N * (a.heads / a.kv), row_blocks = (R + kRows - 1) / kRows;
+  const long long total = prod({a.M, a.B, a.kv, row_blocks, splits});
+  if (total > kMaxGrid) return NF_EUNSUPPORTED;
+  const auto kernel = decoder_tiles_kernel<D, KB, KS, RB, TREE>;
+  static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
+  if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) != hipSuccess) return NF_ELAUNCH;
+    opted_in.store(true, std::memory_order_release);
+  }
+  nf_launch(kernel, dim3((unsigned)total), dim3(256), kBytes, s, a, (int)row_blocks, splits, chunk);
+  return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH;
+}
+
+}  // namespace
+
+nf_status launch_prompt_tiles(const DecArgs& a, hipStream_t s) {
+  return a.d <= 64 ? go<64, 64, 1, 1, false>(a, 1, 0, s) : go<128, 64, 1, 1, false>(a, 1, 0, s);
+}
+
+nf_status launch_tree_tiles(const DecArgs& a, int chunk, int splits, hipStream_t s) {
+  const int R = a.N * (a.heads / a.kv);
+  nf_status st;
+  if (a.d <= 64) st = R <= 32 ? go<64, 128, 4, 1, true>(a, splits, chunk, s) : R <= 64 ? go<64, 128, 2, 1, true>(a, splits, chunk, s) : go<64, 64, 1, 1, true>(a, splits, chunk, s);
+  else st = R <= 32 ? go<128, 128, 4, 1, true>(a, splits, chunk, s) : R <= 64 ? go<128, 128, 2, 1, true>(a, splits, chunk, s) : go<128, 64, 1, 1, true>(a, splits, chunk, s);
+  if (st != NF_OK || splits == 1) return st;
+  const long long blocks = (prod({a.M, a.B, a.heads, a.N}) + 3) / 4;
+  if (a.d <= 64) nf_launch((decoder_join_kernel<bf16_t, 64, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk);
+  else nf_launch((decoder_join_kernel<bf16_t, 128, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk);
+  return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH;
+}
+
+}  // namespace nf
