@@ -23,6 +23,14 @@ struct DecArgs {
   float scale, cap, inv_cap;                            // inv_cap = 1 / cap, 0 without a cap
 };
 
+struct WeighArgs {
+  const void* Q; const float* lse; const int* index; const int* count; const void* Kc; const int* pos; const int* len; const int* start;
+  const float* slope; const float* weight; float* out;
+  int M, B, T, n, C, heads, kv, d;
+  long q_stride_m, q_stride_row;
+  float scale, cap, inv_cap;
+};
+
 __device__ __forceinline__ int clamp_len(int v, int top) { return min(max(v, 0), top); }
 
 // f of the score, the exact way: tanhf in natural units.

@@ -31,13 +31,17 @@ bool rows_ok(int M, long long rows, long long width, long stride_m, long stride_
 
 bool heads_ok(int heads, int kv_heads, int d) { return heads > 0 && kv_heads > 0 && d > 0 && heads % kv_heads == 0; }
 
-// What the tiled kernels take: rows in 16-byte pieces, row numbers in an int.
-bool tiles_sizes(int N, int heads, int kv_heads, int d, nf_dtype dt) {
-  return dt == NF_BF16 && d % 8 == 0 && d <= 128 && (long long)N * (heads / kv_heads) <= INT_MAX / 2;
+// What the kernels on the matrix pipe take: rows in 16-byte pieces, row numbers in an int.
+bool pieces_sizes(int N, int heads, int kv_heads, int d, nf_dtype dt) {
+  return d % (dt == NF_F32 ? 4 : 8) == 0 && d <= 256 && (long long)N * (heads / kv_heads) <= INT_MAX / 2;
 }
-bool tiles_ok(const DecArgs& a, nf_dtype dt) {
-  return tiles_sizes(a.N, a.heads, a.kv, a.d, dt) && a.q_stride_m % 8 == 0 && a.q_stride_row % 8 == 0 && a.kv_stride_m % 8 == 0 && a.kv_stride_row % 8 == 0 &&
-         aligned(a.Q, 16) && aligned(a.K, 16) && aligned(a.V, 16) && aligned(a.Kc, 16) && aligned(a.Vc, 16) && aligned(a.O, 8);
+bool pieces_strides(long stride_m, long stride_row, nf_dtype dt) {
+  const int n = dt == NF_F32 ? 4 : 8;
+  return stride_m % n == 0 && stride_row % n == 0;
+}
+bool pieces_ok(const DecArgs& a, nf_dtype dt) {
+  return pieces_sizes(a.N, a.heads, a.kv, a.d, dt) && pieces_strides(a.q_stride_m, a.q_stride_row, dt) && pieces_strides(a.kv_stride_m, a.kv_stride_row, dt) &&
+         aligned(a.Q, 16) && aligned(a.K, 16) && aligned(a.V, 16) && aligned(a.Kc, 16) && aligned(a.Vc, 16) && aligned(a.O, 16);
 }
 
 template <bool TREE>
@@ -79,13 +83,13 @@ nf_status netfuse_attention_prompt(const void* Q, const void* K, const void* V, 
   a.M = M; a.B = B; a.N = S; a.heads = heads; a.kv = kv_heads; a.d = d; a.causal = causal != 0;
   a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.kv_stride_m = kv_stride_m; a.kv_stride_row = kv_stride_row;
   a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
-  if (tiles_ok(a, dt)) return launch_prompt_tiles(a, (hipStream_t)stream);
+  if (pieces_ok(a, dt)) return dt == NF_BF16 && d <= 128 ? launch_prompt_tiles(a, (hipStream_t)stream) : launch_prompt_stream(a, dt, (hipStream_t)stream);
   return launch_rows<false>(a, dt, (hipStream_t)stream);
 }
 
 long long netfuse_attention_tree_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt) {
   if (M <= 0 || B <= 0 || T <= 0 || T > 64 || C <= 0 || !heads_ok(heads, kv_heads, d) || d > 256 || !is_dtype(dt)) return -1;
-  if (!tiles_sizes(T, heads, kv_heads, d, dt)) return 0;
+  if (!pieces_sizes(T, heads, kv_heads, d, dt)) return 0;
   const int chunk = tree_chunk(T * (heads / kv_heads)), splits = (int)(((long long)C + chunk - 1) / chunk);
   if (splits == 1) return 0;                               // no cache is shared out
   const long long bytes = prod({M, B, heads, T, splits, 4LL * (tree_features(d) + 2)});      // a row's sums, its maximum and its total per chunk
@@ -119,9 +123,10 @@ nf_status netfuse_attention_tree(const void* Q, const void* K, const void* V, co
   a.M = M; a.B = B; a.N = T; a.C = C; a.heads = heads; a.kv = kv_heads; a.d = d;
   a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.kv_stride_m = kv_stride_m; a.kv_stride_row = kv_stride_row;
   a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
-  if (tiles_ok(a, dt)) {
-    const int chunk = tree_chunk(T * (heads / kv_heads));
-    return launch_tree_tiles(a, chunk, (int)(((long long)C + chunk - 1) / chunk), (hipStream_t)stream);
+  if (pieces_ok(a, dt)) {
+    const int rows = T * (heads / kv_heads), chunk = tree_chunk(rows), splits = (int)(((long long)C + chunk - 1) / chunk);
+    const nf_status st = dt == NF_BF16 && d <= 128 && rows > 32 ? launch_tree_tiles(a, chunk, splits, (hipStream_t)stream) : launch_tree_stream(a, chunk, splits, dt, (hipStream_t)stream);
+    return st != NF_OK || splits == 1 ? st : launch_tree_join(a, chunk, splits, dt, (hipStream_t)stream);
   }
   return launch_rows<true>(a, dt, (hipStream_t)stream);
 }
@@ -174,7 +179,9 @@ nf_status netfuse_cache_weigh(const void* Q, const float* lse, const int* index,
   if (d > 256) return NF_EUNSUPPORTED;
   WeighArgs a = {Q, lse, index, count, Kc, pos, len, start, slope, weight, weight_out, M, B, T, n, C, heads, kv_heads, d,
                  q_stride_m, q_stride_row, scale, cap, cap != 0.f ? 1.f / cap : 0.f};
-  const int per_head = (C + 255) / 256;
+  if (pieces_sizes(n, heads, kv_heads, d, dt) && pieces_strides(q_stride_m, q_stride_row, dt) && aligned(Q, 16) && aligned(Kc, 16))
+    return launch_weigh_tiles(a, dt, (hipStream_t)stream);
+  const int per_head = (int)((C + 255LL) / 256);
   const long long blocks = prod({M, B, kv_heads, per_head});
   if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;

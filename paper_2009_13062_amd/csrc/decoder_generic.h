@@ -101,14 +101,6 @@ __global__ __launch_bounds__(256) void decoder_rows_kernel(DecArgs a) {
   if (TREE && a.lse && lane == 0) a.lse[(mb * a.N + i) * a.heads + h] = lrun == 0.f ? -INFINITY : mrun + logf(lrun);
 }
 
-struct WeighArgs {
-  const void* Q; const float* lse; const int* index; const int* count; const void* Kc; const int* pos; const int* len; const int* start;
-  const float* slope; const float* weight; float* out;
-  int M, B, T, n, C, heads, kv, d;
-  long q_stride_m, q_stride_row;
-  float scale, cap, inv_cap;
-};
-
 // One thread per slot; its key row is read again for every token and head.
 template <typename T>
 __global__ __launch_bounds__(256) void weigh_rows_kernel(WeighArgs a, int blocks_per_head) {

@@ -1,0 +1,77 @@
+// Attention of prompts and trees without LDS stages, weights of cached keys: instances and launches of decoder_stream.h and weigh_kernels.h.
+#include <atomic>
+
+#include "decoder_launch.h"
+#include "decoder_stream.h"
+#include "nf_host.h"
+#include "nf_launch.h"
+#include "weigh_kernels.h"
+
+namespace nf {
+namespace {
+
+inline nf_status launched() { return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH; }
+
+template <typename T, int D, int RT, int KS, bool TREE>
+nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
+  constexpr int kRows = 4 / KS * RT * 16, kBytes = stream_lds_bytes(RT, KS, D / 16);
+  const long long R = (long long)a.N * (a.heads / a.kv), row_blocks = (R + kRows - 1) / kRows;
+  const long long total = prod({a.M, a.B, a.kv, row_blocks, splits});
+  if (total > kMaxGrid) return NF_EUNSUPPORTED;
+  const auto kernel = decoder_stream_kernel<T, D, RT, KS, TREE>;
+  static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
+  if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) != hipSuccess) return NF_ELAUNCH;
+    opted_in.store(true, std::memory_order_release);
+  }
+  nf_launch(kernel, dim3((unsigned)total), dim3(256), kBytes, s, a, (int)row_blocks, splits, chunk);
+  return launched();
+}
+
+template <typename T, int D>
+nf_status tree(const DecArgs& a, int splits, int chunk, hipStream_t s) {
+  const int R = a.N * (a.heads / a.kv);
+  return R <= 16 ? go<T, D, 1, 4, true>(a, splits, chunk, s) : R <= 32 ? go<T, D, 1, 2, true>(a, splits, chunk, s) : go<T, D, 1, 1, true>(a, splits, chunk, s);
+}
+
+template <typename T, int D>
+nf_status weigh(const WeighArgs& a, hipStream_t s) {
+  constexpr int kKeys = 4 * weigh_keys<T, D>();
+  const int per_head = (int)(((long long)a.C + kKeys - 1) / kKeys);
+  const long long blocks = prod({a.M, a.B, a.kv, per_head});
+  if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
+  nf_launch((weigh_tiles_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head);
+  return launched();
+}
+
+}  // namespace
+
+nf_status launch_prompt_stream(const DecArgs& a, nf_dtype dt, hipStream_t s) {
+  if (dt == NF_F32) return a.d <= 64 ? go<float, 64, 1, 1, false>(a, 1, 0, s) : a.d <= 128 ? go<float, 128, 1, 1, false>(a, 1, 0, s) : go<float, 256, 1, 1, false>(a, 1, 0, s);
+  return go<bf16_t, 256, 1, 1, false>(a, 1, 0, s);         // smaller heads are decoder_tiles.h's
+}
+
+nf_status launch_tree_stream(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s) {
+  if (dt == NF_F32) return a.d <= 64 ? tree<float, 64>(a, splits, chunk, s) : a.d <= 128 ? tree<float, 128>(a, splits, chunk, s) : tree<float, 256>(a, splits, chunk, s);
+  return a.d <= 64 ? tree<bf16_t, 64>(a, splits, chunk, s) : a.d <= 128 ? tree<bf16_t, 128>(a, splits, chunk, s) : tree<bf16_t, 256>(a, splits, chunk, s);
+}
+
+nf_status launch_tree_join(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s) {
+  const long long blocks = (prod({a.M, a.B, a.heads, a.N}) + 3) / 4;
+  if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
+#define NF_JOIN(T, D, LOG2) nf_launch((decoder_join_kernel<T, D, LOG2>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk)
+  if (dt == NF_F32) {
+    if (a.d <= 64) NF_JOIN(float, 64, false); else if (a.d <= 128) NF_JOIN(float, 128, false); else NF_JOIN(float, 256, false);
+  } else {
+    if (a.d <= 64) NF_JOIN(bf16_t, 64, true); else if (a.d <= 128) NF_JOIN(bf16_t, 128, true); else NF_JOIN(bf16_t, 256, true);
+  }
+#undef NF_JOIN
+  return launched();
+}
+
+nf_status launch_weigh_tiles(const WeighArgs& a, nf_dtype dt, hipStream_t s) {
+  if (dt == NF_F32) return a.d <= 64 ? weigh<float, 64>(a, s) : a.d <= 128 ? weigh<float, 128>(a, s) : weigh<float, 256>(a, s);
+  return a.d <= 64 ? weigh<bf16_t, 64>(a, s) : a.d <= 128 ? weigh<bf16_t, 128>(a, s) : weigh<bf16_t, 256>(a, s);
+}
+
+}  // namespace nf

@@ -33,14 +33,8 @@ nf_status launch_prompt_tiles(const DecArgs& a, hipStream_t s) {
 
 nf_status launch_tree_tiles(const DecArgs& a, int chunk, int splits, hipStream_t s) {
   const int R = a.N * (a.heads / a.kv);
-  nf_status st;
-  if (a.d <= 64) st = R <= 32 ? go<64, 128, 4, 1, true>(a, splits, chunk, s) : R <= 64 ? go<64, 128, 2, 1, true>(a, splits, chunk, s) : go<64, 64, 1, 1, true>(a, splits, chunk, s);
-  else st = R <= 32 ? go<128, 128, 4, 1, true>(a, splits, chunk, s) : R <= 64 ? go<128, 128, 2, 1, true>(a, splits, chunk, s) : go<128, 64, 1, 1, true>(a, splits, chunk, s);
-  if (st != NF_OK || splits == 1) return st;
-  const long long blocks = (prod({a.M, a.B, a.heads, a.N}) + 3) / 4;
-  if (a.d <= 64) nf_launch((decoder_join_kernel<bf16_t, 64, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk);
-  else nf_launch((decoder_join_kernel<bf16_t, 128, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk);
-  return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH;
+  if (a.d <= 64) return R <= 64 ? go<64, 128, 2, 1, true>(a, splits, chunk, s) : go<64, 64, 1, 1, true>(a, splits, chunk, s);
+  return R <= 64 ? go<128, 128, 2, 1, true>(a, splits, chunk, s) : go<128, 64, 1, 1, true>(a, splits, chunk, s);
 }
 
 }  // namespace nf
