@@ -31,6 +31,18 @@ struct WeighArgs {
   float scale, cap, inv_cap;
 };
 
+// Loads of whole tiles go through a buffer resource over the rows from the tile's first key on: a key or feature that is not there gets an
+// offset outside it and comes back as 0.  (A load under a condition is a branch, and the compiler then waits for one load at a time.)  Offsets are 32 bits
+// of bytes: the host takes other kernels where 64 rows do not fit.
+typedef uint32_t dec_u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t dec_u32x2_t __attribute__((ext_vector_type(2)));
+constexpr unsigned kDecOob = 0x80000000u;
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void* first) { return __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)kDecOob, 0x00020000); }
+__device__ __forceinline__ uint4 rows_load16(__amdgpu_buffer_rsrc_t r, unsigned off) {
+  const dec_u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+
 __device__ __forceinline__ int clamp_len(int v, int top) { return min(max(v, 0), top); }
 
 // f of the score, the exact way: tanhf in natural units.

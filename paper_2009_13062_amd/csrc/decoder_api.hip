@@ -40,7 +40,8 @@ bool pieces_strides(long stride_m, long stride_row, nf_dtype dt) {
   return stride_m % n == 0 && stride_row % n == 0;
 }
 bool pieces_ok(const DecArgs& a, nf_dtype dt) {
-  return pieces_sizes(a.N, a.heads, a.kv, a.d, dt) && pieces_strides(a.q_stride_m, a.q_stride_row, dt) && pieces_strides(a.kv_stride_m, a.kv_stride_row, dt) &&
+  // 64 rows of keys within 31 bits of bytes: a tile's offsets
+  return a.kv_stride_row < (1L << 31) / 64 / (dt == NF_F32 ? 4 : 2) && pieces_sizes(a.N, a.heads, a.kv, a.d, dt) && pieces_strides(a.q_stride_m, a.q_stride_row, dt) && pieces_strides(a.kv_stride_m, a.kv_stride_row, dt) &&
          aligned(a.Q, 16) && aligned(a.K, 16) && aligned(a.V, 16) && aligned(a.Kc, 16) && aligned(a.Vc, 16) && aligned(a.O, 16);
 }
 

@@ -174,11 +174,10 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
     if (st >= win_at + kWindow) {
       win_at = st;
       win_any = win_all = 0;
-#pragma unroll
+#pragma unroll 4
       for (int t = 0; t < 8; ++t) {
-        const int j = st * kStep + t * kWave + lane;
-        const int v = j < L ? doc[j] : -1;
-        const uint64_t any = __ballot(v >= lo && v <= hi), all = __ballot(v == lo);
+        const int j = st * kStep + t * kWave + lane, v = doc[min(j, L - 1)];
+        const uint64_t any = __ballot((j < L) & (v >= lo) & (v <= hi)), all = __ballot((j < L) & (v == lo));
 #pragma unroll
         for (int u = 0; u < kPerBallot; ++u) {
           const uint64_t part = kPerBallot == 1 ? ~0ull : ((1ull << kStep % kWave) - 1) << (u * kStep) % kWave;
@@ -207,37 +206,43 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
   int key_reg = 0;                                         // position or document of key `lane` of the step
   auto load_keys = [&](int st) {
     const bool own_step = TREE && st >= cached_steps;
-    const T* kb = own_step ? Kp : Kh;
-    const long row = own_step ? a.kv_stride_row : stride;
-    const int base = own_step ? (st - cached_steps) * kStep : key_start + st * kStep, limit = own_step ? a.N : L;
+    const int base = own_step ? (st - cached_steps) * kStep : key_start + st * kStep, limit = (own_step ? a.N : L) - base;
+    const long rows = own_step ? a.kv_stride_row : stride;
+    const auto rk = rows_from((own_step ? Kp : Kh) + base * rows);
+    const unsigned row = (unsigned)(rows * (long)sizeof(T));
 #pragma unroll
-    for (int k = 0; k < NK; ++k)
+    for (int k = 0; k < NK; ++k) {
+      const unsigned from = 16 * k + l16 < limit ? (16 * k + l16) * row + g4 * 16 : kDecOob;
 #pragma unroll
-      for (int sl = 0; sl < SL; ++sl) {
-        const int key = base + 16 * k + l16, f = sl * Sh::kSliceF + g4 * Sh::kPiece;
-        kreg[k][sl] = make_uint4(0, 0, 0, 0);
-        if (key < limit && f < a.d) kreg[k][sl] = *reinterpret_cast<const uint4*>(kb + (long)key * row + f);
-      }
+      for (int sl = 0; sl < SL; ++sl) kreg[k][sl] = rows_load16(rk, sl * Sh::kSliceF + g4 * Sh::kPiece < a.d ? from + sl * 64 : kDecOob);
+    }
     if (keyed) {
-      const int key = base + lane;
-      if (TREE) key_reg = own_step ? __shfl(node_at, key % kWave, kWave) : key < limit && lane < kStep ? (a.pos ? a.pos[head * a.C + key] : key) : 0;
-      else key_reg = key < limit && lane < kStep ? doc[key] : -1;
+      const int key = base + lane, there = base + min(lane, limit - 1);
+      if (TREE) key_reg = own_step ? __shfl(node_at, key % kWave, kWave) : a.pos ? a.pos[head * a.C + there] : key;
+      else key_reg = lane < limit ? doc[there] : -1;
     }
   };
   auto load_values = [&](int st) {
     const bool own_step = TREE && st >= cached_steps;
-    const T* vb = own_step ? Vp : Vh;
-    const long row = own_step ? a.kv_stride_row : stride;
-    const int base = own_step ? (st - cached_steps) * kStep : key_start + st * kStep, limit = own_step ? a.N : L;
+    const int base = own_step ? (st - cached_steps) * kStep : key_start + st * kStep, limit = (own_step ? a.N : L) - base;
+    const long rows = own_step ? a.kv_stride_row : stride;
+    const auto rv = rows_from((own_step ? Vp : Vh) + base * rows);
+    const unsigned row = (unsigned)(rows * (long)sizeof(T));
 #pragma unroll
-    for (int e = 0; e < NK * 4; ++e)
+    for (int e = 0; e < NK * 4; ++e) {
+      const int key = 16 * (e / 4) + 4 * g4 + e % 4;
+      const unsigned from = key < limit ? key * row + l16 * (Sh::kVWords * 4) : kDecOob;
 #pragma unroll
       for (int c = 0; c < VC; ++c) {
-        const int key = base + 16 * (e / 4) + 4 * g4 + e % 4, f = c * 16 * VF + l16 * VF;
-#pragma unroll
-        for (int w = 0; w < Sh::kVWords; ++w) vreg[e][c].w[w] = 0;
-        if (key < limit && f < a.d) vreg[e][c] = *reinterpret_cast<const Words<Sh::kVWords>*>(__builtin_assume_aligned(vb + (long)key * row + f, Sh::kVWords * 4));
+        const unsigned off = c * 16 * VF + l16 * VF < a.d ? from + c * (64 * Sh::kVWords) : kDecOob;
+        if constexpr (Sh::kVWords == 4) {
+          vreg[e][c] = __builtin_bit_cast(Words<4>, rows_load16(rv, off));
+        } else {
+          const dec_u32x2_t v = __builtin_amdgcn_raw_buffer_load_b64(rv, (int)off, 0, 0);
+          vreg[e][c] = __builtin_bit_cast(Words<Sh::kVWords>, v);
+        }
       }
+    }
   };
 
   f32x4_t o_acc[RT][NB];                                   // element r of block i: feature (i / VF) 16 VF + VF (4 g4 + r) + i % VF of row l16
@@ -282,8 +287,7 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
           float x = s[rt][k][r];
           if (capped_scores) {
             if constexpr (kBf) {
-              const float u = x * (a.scale * a.inv_cap);
-              x = (fabsf(u) < kTanhSeries ? tanh_series(u) : tanh_exp(u)) * (a.cap * kLog2e);
+              x = tanh_either(x * (a.scale * a.inv_cap)) * (a.cap * kLog2e);
             } else {
               x = a.cap * tanhf(x * a.scale * a.inv_cap);
             }
@@ -307,10 +311,10 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const int key = base + 16 * k + 4 * g4 + r;
-            bool seen = own_step ? key < 64 && ((path[rt] >> (key & 63)) & 1) : key < end[rt];
+            bool seen = own_step ? (key < 64) & (int)((path[rt] >> (key & 63)) & 1) : key < end[rt];
             if (!TREE && doc) {
               const int of = __shfl(key_now, 16 * k + 4 * g4 + r, kWave);  // by every lane
-              seen = seen && of == docr[rt];
+              seen &= of == docr[rt];
             }
             s[rt][k][r] = seen ? s[rt][k][r] : -INFINITY;
           }
@@ -348,7 +352,7 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
 #pragma unroll
         for (int c = 0; c < VC; ++c)
 #pragma unroll
-          for (int w = 0; w < Sh::kVWords; ++w) odd = odd || (kBf ? bf16_odd(vreg[e][c].w[w]) : (vreg[e][c].w[w] & 0x7f800000u) == 0x7f800000u);
+          for (int w = 0; w < Sh::kVWords; ++w) odd |= (kBf ? bf16_odd(vreg[e][c].w[w]) : (vreg[e][c].w[w] & 0x7f800000u) == 0x7f800000u);
     }
     if constexpr (kBf) {
       auto product = [&](auto pick, auto fold) {           // pick: what of a dword of two keys' values counts, fold: where a block's result goes

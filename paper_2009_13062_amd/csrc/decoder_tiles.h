@@ -28,14 +28,13 @@ template <int D, int KB, int STAGES> struct DecLds {
   static constexpr int kVPitch = D + 32;                   // the 4 keys x 64 bytes of a transposing read tile the 64 banks
   static constexpr int kOffV = STAGES * KB * kKPitch * 2;
   static constexpr int kOffKey = kOffV + STAGES * KB * kVPitch * 2;       // position or document of each key
-  static constexpr int kOffP = kOffKey + STAGES * KB * 4;                 // 16 keys' weights of each wavefront's 32 rows
-  static constexpr int kOffFlag = kOffP + 4 * 32 * 16 * 2;                // tile whose values are not all finite, per stage
+  static constexpr int kOffFlag = kOffKey + STAGES * KB * 4;              // tile whose values are not all finite, per stage
   static constexpr int kBytes = kOffFlag + 16;
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
-// cap tanh(x / cap) in log2 units for x = dot * scale: u = x / cap.  Near 0 by its series (the other form loses its bits there).
+// tanh(u): near 0 by its series (the other form loses its bits there), relative error below 2^-20 either way.
 __device__ __forceinline__ float tanh_series(float u) {
   const float w = u * u;
   float p = fmaf(w, 0.021869488536155203f, -0.05396825396825397f);
@@ -48,9 +47,13 @@ __device__ __forceinline__ float tanh_exp(float u) {
   return copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), u);
 }
 constexpr float kTanhSeries = 0.25f;
+__device__ __forceinline__ float tanh_either(float u) {
+  const float t = tanh_series(u), e = tanh_exp(u);
+  return fabsf(u) < kTanhSeries ? t : e;
+}
 
 // Either half of a dword an infinity or NaN of bfloat16
-__device__ __forceinline__ bool bf16_odd(uint32_t x) { return (x & 0x7f80u) == 0x7f80u || (x & 0x7f800000u) == 0x7f800000u; }
+__device__ __forceinline__ bool bf16_odd(uint32_t x) { return ((x & 0x7f80u) == 0x7f80u) | ((x & 0x7f800000u) == 0x7f800000u); }
 
 template <int D, int KB, int KS, int RB, bool TREE>
 __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
@@ -69,7 +72,6 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int half = lane / 32, lq = lane % 32, l16 = lane % 16;
-  lds_bf16_t* const Pw = (lds_bf16_t*)(dec_smem + Lds::kOffP) + wave * 32 * 16;
   const int rg = wave % RG, key0 = wave / RG * (KB / KS);  // of a tile
 
   unsigned id = xcd_remap(blockIdx.x, gridDim.x);
@@ -188,15 +190,14 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
   auto look = [&](int j0) {
     win_at = j0;
     win_any = win_all = 0;
-#pragma unroll
+#pragma unroll 4
     for (int t = 0; t < 16; ++t) {
       bool any = false, all = true;
 #pragma unroll
       for (int u = 0; u < KB / kWave; ++u) {
-        const int j = j0 + t * KB + u * kWave + lane;
-        const int v = j < L ? doc[j] : -1;
-        any = any || (v >= blo && v <= bhi);
-        all = all && v == blo;
+        const int j = j0 + t * KB + u * kWave + lane, v = doc[min(j, L - 1)];
+        any |= (j < L) & (v >= blo) & (v <= bhi);
+        all &= (j < L) & (v == blo);
       }
       win_any |= (__any(any) ? 1u : 0u) << t;
       win_all |= (__all(all) && blo == bhi ? 1u : 0u) << t;
@@ -228,24 +229,24 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
 
   uint4 kreg[kPer], vreg[kPer];
   int key_reg = 0;
+  const int my_key = tid / (D / 8), my_f = tid % (D / 8) * 8;             // first piece of this thread: the others are 256 / (D / 8) keys apart
   auto fetch = [&](int j0) {
     const bool own_tile = TREE && j0 == kTreeTile;
-    const bf16_t* kb = own_tile ? Kp : Kh;
-    const bf16_t* vb = own_tile ? Vp : Vh;
+    const int base = own_tile ? 0 : j0, limit = (own_tile ? a.N : L) - base;
     const long st = own_tile ? a.kv_stride_row : stride;
-    const int base = own_tile ? 0 : j0, limit = own_tile ? a.N : L;
+    const auto rk = rows_from((own_tile ? Kp : Kh) + base * st), rv = rows_from((own_tile ? Vp : Vh) + base * st);
+    const unsigned row = (unsigned)(st * 2), from = my_key * row + my_f * 2;
 #pragma unroll
     for (int t = 0; t < kPer; ++t) {
-      const int c = tid + t * 256, key = base + c / (D / 8), f = c % (D / 8) * 8;
-      kreg[t] = vreg[t] = make_uint4(0, 0, 0, 0);
-      if (key < limit && f < a.d) {
-        kreg[t] = *reinterpret_cast<const uint4*>(kb + (long)key * st + f);
-        vreg[t] = *reinterpret_cast<const uint4*>(vb + (long)key * st + f);
-      }
+      const bool in = my_key + t * (2048 / D) < limit && my_f < a.d;
+      const unsigned off = in ? from + t * (2048 / D) * row : kDecOob;
+      kreg[t] = rows_load16(rk, off);
+      vreg[t] = rows_load16(rv, off);
     }
     if (keyed && tid < KB) {
-      const int key = base + tid;
-      key_reg = TREE ? (own_tile ? node_at : key < limit ? (a.pos ? a.pos[head * a.C + key] : key) : 0) : key < limit ? doc[key] : -1;
+      const int key = base + tid, there = min(tid, limit - 1) + base;
+      key_reg = TREE ? (own_tile ? node_at : a.pos ? a.pos[head * a.C + there] : key) : doc[there];
+      if (!TREE && tid >= limit) key_reg = -1;
     }
   };
   auto commit = [&](int stage, bool check, int number) {
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
       const int c = tid + t * 256, key = c / (D / 8), f = c % (D / 8) * 8;
       lds_store16(Ks + (stage * KB + key) * Lds::kKPitch + f, kreg[t]);
       lds_store16(Vs + (stage * KB + key) * Lds::kVPitch + f, vreg[t]);
-      if (check) odd = odd || bf16_odd(vreg[t].x) || bf16_odd(vreg[t].y) || bf16_odd(vreg[t].z) || bf16_odd(vreg[t].w);
+      if (check) odd |= bf16_odd(vreg[t].x) | bf16_odd(vreg[t].y) | bf16_odd(vreg[t].z) | bf16_odd(vreg[t].w);
     }
     if (check && odd) Flag[stage] = number;
   };
@@ -274,6 +275,9 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
   }
   const bool capped_scores = a.cap != 0.f, biased = a.slope != nullptr;
   const float sc = a.scale * kLog2e;
+  const float to_u = a.scale * a.inv_cap, back = a.cap * kLog2e, u2 = to_u * to_u;
+  const float cap1 = sc * u2 * -0.3333333333333333f, cap2 = sc * u2 * u2 * 0.13333333333333333f, cap3 = sc * u2 * u2 * u2 * -0.05396825396825397f;
+  const float cap_small = fabsf(to_u) > 1e-4f && fabsf(to_u) < 1e4f ? kTanhSeries / fabsf(to_u) : 0.f;      // powers of others leave float32
   const bool raw = !capped_scores && !biased && sc > 0.f;  // scale and maximum enter the exponent in one fma
 
   if (tid < kStages) Flag[tid] = 0;
@@ -298,9 +302,9 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
       fetch(next);
     }
     const bool skip = !TREE && a.causal && tile > w_hi && tile >= first;          // no row of this wavefront sees the tile
-    if (!skip) {
+    const bool odd_tile = !was_whole && Flag[cur] == number;                      // uniform over the workgroup
+    if (!skip || odd_tile) {
       const lds_bf16_t* Kc = Ks + (cur * KB + key0) * Lds::kKPitch;
-      const lds_bf16_t* Vc = Vs + (cur * KB + key0) * Lds::kVPitch;
       const lds_int_t* Kk = Key + cur * KB + key0;
       const int base = (tile == kTreeTile ? 0 : tile) + key0 + 4 * half;          // register r of block sb is key base + 32 sb + 8 (r / 4) + r % 4
       f32x16_t s[RB][NSB];
@@ -322,25 +326,25 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
         if (capped_scores) {                               // uniform
-          const float to_u = a.scale * a.inv_cap, back = a.cap * kLog2e;
           float top = 0.f;
 #pragma unroll
           for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              s[rb][sb][r] *= to_u;
-              top = fmaxf(top, fabsf(s[rb][sb][r]));
-            }
-          const bool small = __all(top < kTanhSeries);
+            for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(s[rb][sb][r]));
+          if (__all(top < cap_small)) {                    // as a rule: the series in the unscaled score, its last term below 2^-21
 #pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
+            for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const float u = s[rb][sb][r];
-              float t = tanh_series(u);
-              if (!small) t = fabsf(u) < kTanhSeries ? t : tanh_exp(u);
-              s[rb][sb][r] = t * back;
-            }
+              for (int r = 0; r < 16; ++r) {
+                const float w = s[rb][sb][r] * s[rb][sb][r];
+                s[rb][sb][r] *= fmaf(fmaf(fmaf(w, cap3, cap2), w, cap1), w, sc);
+              }
+          } else {
+#pragma unroll
+            for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) s[rb][sb][r] = tanh_either(s[rb][sb][r] * to_u) * back;
+          }
         } else if (!raw) {
 #pragma unroll
           for (int sb = 0; sb < NSB; ++sb)
@@ -435,51 +439,75 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
         }
       }
 
-      if (mask && Flag[cur] == number) {
-        // values that are not finite in a masked tile: 16 keys' weights at a time through LDS, then key by key
+      const lds_bf16_t* Vc = Vs + (cur * KB + key0) * Lds::kVPitch;
+      if (odd_tile) {
+        // which keys hold such a value: a key per lane
+        bool odd = false;
+        if (lane < KB / KS) {
+#pragma unroll 1
+          for (int f = 0; f < a.d; ++f) odd |= (Vc[lane * Lds::kVPitch + f] & 0x7f80) == 0x7f80;
+        }
+        const uint64_t odd_keys = __ballot(odd);
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb)
+        for (int rb = 0; rb < RB; ++rb) {
+          uint32_t lo = 0, hi = 0;                         // keys under a weight that is not 0: this half's, then both
 #pragma unroll
           for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
             for (int st = 0; st < 2; ++st) {
-              const bf16x8_t p = pf[rb][sb][st];           // keys 4 half + 0..3 and 8 + 4 half + 0..3 of the step
-              const uint4 w = __builtin_bit_cast(uint4, p);
-              __builtin_amdgcn_wave_barrier();
-              lds_store8(Pw + lq * 16 + 4 * half, w.x, w.y);
-              lds_store8(Pw + lq * 16 + 8 + 4 * half, w.z, w.w);
-              __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-              for (int k = 0; k < 16; ++k) {
-                const float pk = bf16_to_f32(Pw[lq * 16 + k]);
-                const lds_bf16_t* vr = Vc + (sb * 32 + st * 16 + k) * Lds::kVPitch + 4 * half;
+              const uint4 w = __builtin_bit_cast(uint4, pf[rb][sb][st]);
+              const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-                for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-                  for (int r = 0; r < 16; ++r) {
-                    const float v = bf16_to_f32(vr[tb * 32 + 8 * (r / 4) + r % 4]);
-                    o_acc[rb][tb][r] = pk != 0.f ? fmaf(pk, v, o_acc[rb][tb][r]) : o_acc[rb][tb][r];
-                  }
+              for (int e = 0; e < 8; ++e) {
+                const uint32_t bit = (ws[e / 2] >> (e % 2 * 16) & 0x7fffu) != 0 ? 1u << (16 * st + 8 * (e / 4) + e % 4) : 0u;
+                if (sb == 0) lo |= bit; else hi |= bit;
               }
             }
-      } else {
-        // O^T += V^T P^T.  In a 16-lane group, lane i points at key row i / 4, features 4 (i % 4) .. + 3 of a 4 x 16 block and receives the
-        // 4 keys of feature i; slots 0-3 of step (sb, st) are keys 32 sb + 16 st + 4 half + 0..3, slots 4-7 the same + 8.
+          lo <<= 4 * half;
+          hi <<= 4 * half;
+          lo |= __shfl_xor(lo, 32, kWave);
+          hi |= __shfl_xor(hi, 32, kWave);
+          const uint64_t under = (uint64_t)hi << 32 | lo;
+#pragma unroll 1
+          for (uint64_t left = odd_keys; left; left &= left - 1) {
+            const int k = __builtin_ctzll(left);
+            const bool takes = (under >> k) & 1;
+            const lds_bf16_t* vr = Vc + k * Lds::kVPitch + 4 * half;
 #pragma unroll
-        for (int sb = 0; sb < NSB; ++sb)
+            for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-          for (int st = 0; st < 2; ++st)
+              for (int r = 0; r < 16; ++r) {
+                const uint32_t v = vr[tb * 32 + 8 * (r / 4) + r % 4];
+                o_acc[rb][tb][r] += takes & ((v & 0x7f80) == 0x7f80) ? __uint_as_float(v << 16) : 0.f;
+              }
+          }
+        }
+        __syncthreads();
 #pragma unroll
-            for (int tb = 0; tb < TB; ++tb) {
-              const lds_bf16_t* vp = Vc + (sb * 32 + st * 16 + 4 * half + l16 / 4) * Lds::kVPitch + tb * 32 + ((lane / 16) % 2) * 16 + (l16 % 4) * 4;
-              const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)vp);
-              const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vp + 8 * Lds::kVPitch));
-              const s16x8_t both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-              for (int rb = 0; rb < RB; ++rb)
-                o_acc[rb][tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, both), pf[rb][sb][st], o_acc[rb][tb], 0, 0, 0);
-            }
+        for (int t = 0; t < kPer; ++t) {                   // the product runs on the others
+          lds_bf16_t* const v = Vs + (cur * KB + my_key + t * (2048 / D)) * Lds::kVPitch + my_f;
+#pragma unroll 1
+          for (int e = 0; e < 8; ++e)
+            if ((v[e] & 0x7f80) == 0x7f80) v[e] = 0;
+        }
+        __syncthreads();
       }
+      // O^T += V^T P^T.  In a 16-lane group, lane i points at key row i / 4, features 4 (i % 4) .. + 3 of a 4 x 16 block and receives the
+      // 4 keys of feature i; slots 0-3 of step (sb, st) are keys 32 sb + 16 st + 4 half + 0..3, slots 4-7 the same + 8.
+#pragma unroll
+      for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+        for (int st = 0; st < 2; ++st)
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb) {
+            const lds_bf16_t* vp = Vc + (sb * 32 + st * 16 + 4 * half + l16 / 4) * Lds::kVPitch + tb * 32 + ((lane / 16) % 2) * 16 + (l16 % 4) * 4;
+            const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)vp);
+            const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vp + 8 * Lds::kVPitch));
+            const s16x8_t both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+            for (int rb = 0; rb < RB; ++rb)
+              o_acc[rb][tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, both), pf[rb][sb][st], o_acc[rb][tb], 0, 0, 0);
+          }
     }
     if (kStages == 1) __syncthreads();                     // the stage is free
     ++number;

@@ -34,7 +34,7 @@ __global__ __launch_bounds__(256) void weigh_tiles_kernel(WeighArgs a, int block
 #pragma unroll
   for (int k = 0; k < NK; ++k) sum[k] = 0.f;
   if (j0 < held) {
-    const T* Kh = (const T*)a.Kc + head * a.C * a.d;
+    const auto rk = rows_from((const T*)a.Kc + (head * a.C + j0) * a.d);
     uint4 kf[NK][SL];
     int at[NK];
 #pragma unroll
@@ -43,10 +43,10 @@ __global__ __launch_bounds__(256) void weigh_tiles_kernel(WeighArgs a, int block
 #pragma unroll
       for (int sl = 0; sl < SL; ++sl) {
         const int f = sl * Sh::kSliceF + g4 * Sh::kPiece;
-        kf[k][sl] = make_uint4(0, 0, 0, 0);
-        if (key < held && f < a.d) kf[k][sl] = *reinterpret_cast<const uint4*>(Kh + (long)key * a.d + f);
+        kf[k][sl] = rows_load16(rk, (key < held) & (f < a.d) ? ((16 * k + l16) * a.d + f) * (unsigned)sizeof(T) : kDecOob);
       }
-      at[k] = a.slope && a.pos && key < held ? a.pos[head * a.C + key] : key;
+      at[k] = key;
+      if (a.slope && a.pos) at[k] = a.pos[head * a.C + min(key, held - 1)];
     }
     const int rows = cnt * group;
     lds_f32_t* const tab = (lds_f32_t*)&table[wave][0][0];
@@ -90,8 +90,7 @@ __global__ __launch_bounds__(256) void weigh_tiles_kernel(WeighArgs a, int block
             float x = s[k][e];
             if (a.cap != 0.f) {
               if constexpr (kBf) {
-                const float u = x * (a.scale * a.inv_cap);
-                x = (fabsf(u) < kTanhSeries ? tanh_series(u) : tanh_exp(u)) * (a.cap * kLog2e);
+                x = tanh_either(x * (a.scale * a.inv_cap)) * (a.cap * kLog2e);
               } else {
                 x = a.cap * tanhf(x * a.scale * a.inv_cap);
               }
