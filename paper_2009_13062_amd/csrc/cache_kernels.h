@@ -53,8 +53,8 @@ __device__ __forceinline__ uint32_t weight_order(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Exclusive sum over the 1024 threads of a workgroup, `total` their sum.  Every thread has to come here.
-__device__ __forceinline__ int block_scan(int v, int* wave_sums, int& total) {
+// Exclusive sum over the NT threads of a workgroup, `total` their sum.  Every thread has to come here; wave_sums must not be in use by another sum.
+template <int NT> __device__ __forceinline__ int block_sum(int v, int* wave_sums, int& total) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   int x = v;
 #pragma unroll
@@ -67,22 +67,47 @@ __device__ __forceinline__ int block_scan(int v, int* wave_sums, int& total) {
   int before = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < 16; ++w) {
+  for (int w = 0; w < NT / kWave; ++w) {
     const int s = wave_sums[w];
     before += w < wave ? s : 0;
     total += s;
   }
-  __syncthreads();
   return before + x - v;
 }
+// The same where wave_sums is used again.
+template <int NT> __device__ __forceinline__ int block_scan(int v, int* wave_sums, int& total) {
+  const int r = block_sum<NT>(v, wave_sums, total);
+  __syncthreads();
+  return r;
+}
 
-// Which entries of one head leave: one workgroup finds the n-th smallest (guarded, weight) by digits of 11, 11 and 10 bits of the weight's order,
+// One digit of the search: hist holds how many candidates have each of 2048 digits; the digit of the want-th of them, and want among those that share it.
+template <int NT> __device__ __forceinline__ int pick_digit(const int* hist, int* wave_sums, int* found, int& want) {
+  constexpr int kBins = 2048 / NT;
+  int c[kBins], sum = 0, total;
+#pragma unroll
+  for (int i = 0; i < kBins; ++i) {
+    c[i] = hist[kBins * threadIdx.x + i];
+    sum += c[i];
+  }
+  int before = block_sum<NT>(sum, wave_sums, total);
+#pragma unroll
+  for (int i = 0; i < kBins; ++i) {
+    if (before < want && want <= before + c[i]) found[0] = kBins * threadIdx.x + i, found[1] = before;
+    before += c[i];
+  }
+  __syncthreads();
+  want -= found[1];                                        // at least 1 of the entries with this digit
+  return found[0];
+}
+
+// Which entries of one head leave, caches of any size: one workgroup finds the n-th smallest (guarded, weight) by digits of 11, 11 and 10 bits of the weight's order,
 // then walks the slots in order, giving entries equal to it to the lowest slots, and writes the list of free slots below the budget and
 // that of the entries above it that stay (equally many).  Counts in LDS: whole numbers, so their order does not matter.
 __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
   __shared__ int hist[2048];
   __shared__ int wave_sums[16];
-  __shared__ int found[3];
+  __shared__ int found[2];
   const int tid = threadIdx.x;
   const long head = blockIdx.x, mb = head / a.kv;
   const int L = clamp_len(a.len[mb], a.C);
@@ -104,7 +129,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
   }
   int open = 0, total;
   for (int j = tid; j < L; j += 1024) open += !is_guarded(j);
-  block_scan(open, wave_sums, open);
+  block_scan<1024>(open, wave_sums, open);
   const bool guards = n > open;                            // all the others leave and some guarded entries too
   int want = guards ? n - open : n;                        // so many of the group with is_guarded == guards, from the smallest
   uint32_t prefix = 0;
@@ -116,14 +141,8 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
       if (is_guarded(j) == guards && (shift + bits == 32 || (o >> (shift + bits)) == prefix)) atomicAdd(&hist[(o >> shift) & ((1u << bits) - 1)], 1);
     }
     __syncthreads();
-    const int c0 = hist[2 * tid], c1 = hist[2 * tid + 1];
-    const int before = block_scan(c0 + c1, wave_sums, total);
-    if (before < want && want <= before + c0) found[0] = 2 * tid, found[1] = before;
-    if (before + c0 < want && want <= before + c0 + c1) found[0] = 2 * tid + 1, found[1] = before + c0;
-    __syncthreads();
-    prefix = (prefix << bits) | (uint32_t)found[0];
-    want -= found[1];                                      // at least 1 of the entries with this prefix
-    __syncthreads();
+    prefix = (prefix << bits) | (uint32_t)pick_digit<1024>(hist, wave_sums, found, want);
+    __syncthreads();                                       // all three are used again
     bits = shift == 21 ? 11 : shift == 10 ? 10 : 0;
     shift = shift == 21 ? 10 : 0;
   }
@@ -140,7 +159,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
       guarded[e] = in[e] && is_guarded(j);
       equal += in[e] && guarded[e] == guards && o[e] == prefix;
     }
-    int rank = equal_before + block_scan(equal, wave_sums, total);
+    int rank = equal_before + block_scan<1024>(equal, wave_sums, total);
     equal_before += total;
     bool leaves[4];
     int mine = 0;                                          // holes in the low half, movers in the high half
@@ -152,7 +171,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
       rank += in[e] && same && o[e] == prefix;
       if (in[e]) mine += j < keep ? (leaves[e] ? 1 : 0) : (leaves[e] ? 0 : 1 << 16);
     }
-    int at = block_scan(mine, wave_sums, total);
+    int at = block_scan<1024>(mine, wave_sums, total);
     int hole = holes_before + (at & 0xffff), mover = movers_before + (at >> 16);
     holes_before += total & 0xffff;
     movers_before += total >> 16;
@@ -172,6 +191,113 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
     }
   }
   if (tid == 0) *count = holes_before;
+}
+
+// The same for caches of up to NT E slots, which are read once: a thread holds the weights' order of E slots in a row, turned round through LDS, and
+// E bits for what may leave.  The lists are those of the kernel above.
+template <int NT, int E> struct EvictLds {
+  static constexpr int kOffGuard = NT * E * 4, kOffHist = kOffGuard + NT * E / 8, kOffSums = kOffHist + 3 * 2048 * 4, kBytes = kOffSums + 7 * 16 * 4;
+};
+template <int NT, int E>
+__global__ __launch_bounds__(NT) void evict_select_held_kernel(EvictArgs a) {
+  using Lds = EvictLds<NT, E>;
+  static_assert(E >= 4 && E <= 32 && (E & (E - 1)) == 0, "whole 16-byte pieces, a bit each");
+  extern __shared__ __align__(16) unsigned char evict_smem[];
+  uint32_t* const order = (uint32_t*)evict_smem;
+  uint32_t* const guard = (uint32_t*)(evict_smem + Lds::kOffGuard);
+  int* const hist = (int*)(evict_smem + Lds::kOffHist);
+  int* const wave_sums = (int*)(evict_smem + Lds::kOffSums);
+  int* const found = wave_sums + 6 * 16;
+  const int tid = threadIdx.x, lane = tid % kWave;
+  const long head = blockIdx.x, mb = head / a.kv;
+  const int L = clamp_len(a.len[mb], a.C), keep = min(L, a.budget), n = L - keep;
+  const long long bound = (long long)(a.start ? a.start[mb] : L) - a.recent;     // guarded from this position on
+  const float* w = a.weight + head * a.C;
+  const int* pos = a.pos ? a.pos + head * a.C : nullptr;
+  float* const w_out = a.weight_out != a.weight ? a.weight_out + head * a.C : nullptr;
+  int* const p_out = pos && a.pos_out != a.pos ? a.pos_out + head * a.C : nullptr;
+  int* const count = a.ws + head * (1 + 2 * (long)a.most);
+  int* const holes = count + 1;
+  int* const movers = holes + a.most;
+  for (int d = tid; d < 3 * 2048; d += NT) hist[d] = 0;
+  // piece c of thread t's E slots lies at piece c ^ (t mod E / 4): reads by owner then spread over the banks
+#pragma unroll 16
+  for (int i = 0; i < E; ++i) {
+    const int j = i * NT + tid, there = min(j, max(L - 1, 0));
+    const float x = w[there];
+    const int p = pos ? pos[there] : 0;
+    const int owner = j / E, e = j % E;
+    order[owner * E + ((e / 4) ^ (owner & (E / 4 - 1))) * 4 + e % 4] = weight_order(x);
+    const uint64_t g = __ballot(a.recent > 0 && (long long)p >= bound);
+    if (lane == 0) *reinterpret_cast<uint64_t*>(guard + j / 32) = g;
+    if (j < keep) {                                        // slots that another entry moves into are written again by the next kernel
+      if (w_out) w_out[j] = x;
+      if (p_out) p_out[j] = p;
+    }
+  }
+  if (n == 0) {                                            // uniform
+    if (tid == 0) *count = 0;
+    return;
+  }
+  __syncthreads();
+  uint32_t o[E];
+#pragma unroll
+  for (int c = 0; c < E / 4; ++c) {
+    const uint4 v = *reinterpret_cast<const uint4*>(order + tid * E + (c ^ (tid & (E / 4 - 1))) * 4);
+    o[4 * c] = v.x;
+    o[4 * c + 1] = v.y;
+    o[4 * c + 2] = v.z;
+    o[4 * c + 3] = v.w;
+  }
+  const int j0 = tid * E, mine = min(max(L - j0, 0), E);   // entries of this thread
+  const uint32_t in = mine == 32 ? ~0u : (1u << mine) - 1;
+  const uint32_t guarded = (guard[j0 / 32] >> (j0 % 32)) & in;
+  int open, total;
+  block_sum<NT>(__popc(in & ~guarded), wave_sums, open);
+  const bool guards = n > open;                            // all the others leave and some guarded entries too
+  int want = guards ? n - open : n;
+  const uint32_t may = guards ? guarded : in & ~guarded;
+  uint32_t prefix = 0;
+#pragma unroll
+  for (int round = 0; round < 3; ++round) {
+    const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bits = round == 2 ? 10 : 11;
+    int* const h = hist + round * 2048;
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (((may >> e) & 1) && (round == 0 || (o[e] >> (shift + bits) % 32) == prefix)) atomicAdd(&h[(o[e] >> shift) & ((1u << bits) - 1)], 1);
+    __syncthreads();
+    prefix = (prefix << bits) | (uint32_t)pick_digit<NT>(h, wave_sums + 16 * (1 + round), found + 2 * round, want);
+  }
+  uint32_t less = 0, equal = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    less |= (o[e] < prefix ? 1u : 0u) << e;
+    equal |= (o[e] == prefix ? 1u : 0u) << e;
+  }
+  equal &= may;
+  int rank = block_sum<NT>(__popc(equal), wave_sums + 16 * 4, total);
+  uint32_t leaves = (less & may) | (guards ? in & ~guarded : 0u);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const uint32_t bit = equal & (1u << e);
+    leaves |= rank < want ? bit : 0u;
+    rank += bit != 0;
+  }
+  const int below = min(max(keep - j0, 0), E);             // slots of this thread below the budget
+  const uint32_t low = below == 32 ? ~0u : (1u << below) - 1;
+  uint32_t hole_bits = leaves & low, mover_bits = in & ~leaves & ~low;
+  const int at = block_sum<NT>(__popc(hole_bits) | __popc(mover_bits) << 16, wave_sums + 16 * 5, total);  // at most 2^14 of each
+  const int pairs = total & 0xffff;
+  int* const list = (int*)order;                           // every thread has its own by now: holes, then movers, NT E / 2 at most each
+  int hole = at & 0xffff, mover = NT * E / 2 + (at >> 16);
+  for (; hole_bits; hole_bits &= hole_bits - 1) list[hole++] = j0 + __builtin_ctz(hole_bits);
+  for (; mover_bits; mover_bits &= mover_bits - 1) list[mover++] = j0 + __builtin_ctz(mover_bits);
+  __syncthreads();
+  for (int i = tid; i < pairs; i += NT) {
+    holes[i] = list[i];
+    movers[i] = list[NT * E / 2 + i];
+  }
+  if (tid == 0) *count = pairs;
 }
 
 // The pairs of the lists: rows of keys and values, position and weight.  Sources lie at or above the budget, targets below it, each once.

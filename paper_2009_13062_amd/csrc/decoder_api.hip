@@ -4,6 +4,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "cache_kernels.h"
 #include "decoder.h"
@@ -56,6 +57,19 @@ nf_status launch_rows(const DecArgs& a, nf_dtype dt, hipStream_t s) {
     if (a.d <= 64) NF_ROWS(bf16_t, 1); else if (a.d <= 128) NF_ROWS(bf16_t, 2); else NF_ROWS(bf16_t, 4);
   }
 #undef NF_ROWS
+  return launched();
+}
+
+template <int NT, int E>
+nf_status select_held(const EvictArgs& a, long long heads, hipStream_t s) {
+  constexpr int kBytes = EvictLds<NT, E>::kBytes;
+  const auto kernel = evict_select_held_kernel<NT, E>;
+  static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
+  if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) != hipSuccess) return NF_ELAUNCH;
+    opted_in.store(true, std::memory_order_release);
+  }
+  nf_launch(kernel, dim3((unsigned)heads), dim3(NT), kBytes, s, a);
   return launched();
 }
 
@@ -215,12 +229,15 @@ nf_status netfuse_cache_evict(void* Kc, void* Vc, const int* pos, const float* w
   EvictArgs a = {Kc, Vc, pos, weight, len, start, pos_out, weight_out, (int*)workspace, M, B, C, kv_heads,
                  (int)(d * esz / (wide ? 16 : esz)), budget, recent, std::min(budget, C - budget)};
   const long long heads = prod({M, B, kv_heads});
-  const int rows = std::max(1, 1024 / a.units);                            // about 4 pieces per thread and tensor
+  const int rows = std::max(1, 256 / a.units);                             // a piece of each tensor per thread
   const int per_head = std::max(1, (a.most + rows - 1) / rows);
   const long long blocks = prod({heads, per_head});
   if (heads > kMaxGrid || blocks > kMaxGrid) return NF_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
-  nf_launch(evict_select_kernel, dim3((unsigned)heads), dim3(1024), 0, s, a);
+  const nf_status st = C <= 1024 ? select_held<256, 4>(a, heads, s) : C <= 4096 ? select_held<256, 16>(a, heads, s) : C <= 8192 ? select_held<1024, 8>(a, heads, s)
+                       : C <= 32768 ? select_held<1024, 32>(a, heads, s) : NF_EUNSUPPORTED;
+  if (st == NF_ELAUNCH) return st;
+  if (st == NF_EUNSUPPORTED) nf_launch(evict_select_kernel, dim3((unsigned)heads), dim3(1024), 0, s, a);
   if (a.most > 0) {
 #define NF_MOVE(U) nf_launch((evict_move_kernel<U>), dim3((unsigned)blocks), dim3(256), 0, s, a, rows, per_head)
     if (wide) NF_MOVE(uint4); else if (esz == 4) NF_MOVE(uint32_t); else NF_MOVE(uint16_t);

@@ -11,8 +11,7 @@
 // wavefront; K of the next step is in flight while V of this one is used.
 //
 // float32: scores in natural units, expf and tanhf, weights unrounded.  bfloat16: log2 units, weights rounded to bfloat16 (half a step of 2^-8 each).
-// Masks, chunks of a cache and workspace as in decoder_tiles.h.  Values that are infinite or NaN in a masked step: the second product runs on the
-// finite ones, and three products of indicators say which rows meet +infinity, -infinity and NaN under a weight that is not 0.
+// Masks, chunks of a cache and workspace as in decoder_tiles.h.
 #pragma once
 #include "decoder.h"
 #include "decoder_tiles.h"
@@ -345,96 +344,79 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
       }
     }
 
-    bool odd = false;
     if (mask) {
+      // values that are infinite or NaN: 0 times them would reach the rows that do not see them, so each row takes them from the keys that have a
+      // weight and the product runs on the others.  Key e of a lane's group g is passed round group by group.
 #pragma unroll
-      for (int e = 0; e < NK * 4; ++e)
+      for (int e = 0; e < NK * 4; ++e) {
+        bool odd = false;
 #pragma unroll
         for (int c = 0; c < VC; ++c)
 #pragma unroll
-          for (int w = 0; w < Sh::kVWords; ++w) odd |= (kBf ? bf16_odd(vreg[e][c].w[w]) : (vreg[e][c].w[w] & 0x7f800000u) == 0x7f800000u);
+          for (int w = 0; w < Sh::kVWords; ++w) odd |= kBf ? bf16_odd(vreg[e][c].w[w]) : (vreg[e][c].w[w] & 0x7f800000u) == 0x7f800000u;
+        const uint64_t where = __ballot(odd);
+        if (where == 0) continue;                          // uniform
+#pragma unroll 1
+        for (int from = 0; from < 4; ++from) {
+          if (!((where >> (16 * from)) & 0xffff)) continue;
+          bool takes[RT];
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) takes[rt] = __shfl(s[rt][e / 4][e % 4], 16 * from + l16, kWave) != 0.f;
+#pragma unroll
+          for (int c = 0; c < VC; ++c)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+              for (int w = 0; w < Sh::kVWords; ++w) {
+                const uint32_t x = __shfl(vreg[e][c].w[w], 16 * from + 4 * g4 + r, kWave);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+                  if constexpr (kBf) {
+                    o_acc[rt][c * VF + 2 * w][r] += takes[rt] & ((x & 0x7f80u) == 0x7f80u) ? __uint_as_float(x << 16) : 0.f;
+                    o_acc[rt][c * VF + 2 * w + 1][r] += takes[rt] & ((x & 0x7f800000u) == 0x7f800000u) ? __uint_as_float(x & 0xffff0000u) : 0.f;
+                  } else {
+                    o_acc[rt][c * VF + w][r] += takes[rt] & ((x & 0x7f800000u) == 0x7f800000u) ? __uint_as_float(x) : 0.f;
+                  }
+                }
+              }
+        }
+#pragma unroll
+        for (int c = 0; c < VC; ++c)
+#pragma unroll
+          for (int w = 0; w < Sh::kVWords; ++w) {
+            const uint32_t x = vreg[e][c].w[w];
+            if constexpr (kBf) vreg[e][c].w[w] = ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
+            else vreg[e][c].w[w] = (x & 0x7f800000u) == 0x7f800000u ? 0u : x;
+          }
+      }
     }
     if constexpr (kBf) {
-      auto product = [&](auto pick, auto fold) {           // pick: what of a dword of two keys' values counts, fold: where a block's result goes
 #pragma unroll
-        for (int k = 0; k < NK; k += 2) {
-          bf16x8_t pf[RT];
-#pragma unroll
-          for (int rt = 0; rt < RT; ++rt)
-            pf[rt] = __builtin_bit_cast(bf16x8_t, make_uint4(pack_bf16x2(s[rt][k][0], s[rt][k][1]), pack_bf16x2(s[rt][k][2], s[rt][k][3]),
-                                                             pack_bf16x2(s[rt][k + 1][0], s[rt][k + 1][1]), pack_bf16x2(s[rt][k + 1][2], s[rt][k + 1][3])));
-#pragma unroll
-          for (int i = 0; i < NB; ++i) {
-            uint32_t x[4];
-#pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-              const uint32_t p = vreg[4 * k + e][i / VF].w[i % VF / 2], q = vreg[4 * k + e + 1][i / VF].w[i % VF / 2];
-              x[e / 2] = pick(__builtin_amdgcn_perm(q, p, i % 2 ? 0x07060302u : 0x05040100u));
-            }
-            const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt) fold(rt, i, vf, pf[rt]);
-          }
-        }
-      };
-      if (__any(odd)) {
-        product([](uint32_t x) { return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u); },
-                [&](int rt, int i, bf16x8_t vf, bf16x8_t pf) { o_acc[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o_acc[rt][i], 0, 0, 0); });
+      for (int k = 0; k < NK; k += 2) {
+        bf16x8_t pf[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
+          pf[rt] = __builtin_bit_cast(bf16x8_t, make_uint4(pack_bf16x2(s[rt][k][0], s[rt][k][1]), pack_bf16x2(s[rt][k][2], s[rt][k][3]),
+                                                           pack_bf16x2(s[rt][k + 1][0], s[rt][k + 1][1]), pack_bf16x2(s[rt][k + 1][2], s[rt][k + 1][3])));
 #pragma unroll
-          for (int k = 0; k < NK; ++k)
+        for (int i = 0; i < NB; ++i) {
+          uint32_t x[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[rt][k][r] = s[rt][k][r] != 0.f ? 1.f : 0.f;
-#pragma unroll 1
-        for (int kind = 0; kind < 3; ++kind) {             // +infinity, -infinity, NaN
-          auto is = [&](uint32_t h) { return kind == 0 ? h == 0x7f80u : kind == 1 ? h == 0xff80u : (h & 0x7fffu) > 0x7f80u; };
-          const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
-          product([&](uint32_t x) {
-                    asm volatile("" : "+v"(x));            // not taken out of the loop over the kinds: hundreds of registers
-                    return (is(x & 0xffffu) ? 0x3f80u : 0u) | (is(x >> 16) ? 0x3f800000u : 0u);
-                  },
-                  [&](int rt, int i, bf16x8_t vf, bf16x8_t pf) {
-                    const f32x4_t n = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+          for (int e = 0; e < 8; e += 2)
+            x[e / 2] = __builtin_amdgcn_perm(vreg[4 * k + e + 1][i / VF].w[i % VF / 2], vreg[4 * k + e][i / VF].w[i % VF / 2], i % 2 ? 0x07060302u : 0x05040100u);
+          const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) o_acc[rt][i][r] = n[r] > 0.f ? o_acc[rt][i][r] + what : o_acc[rt][i][r];
-                  });
+          for (int rt = 0; rt < RT; ++rt) o_acc[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[rt], o_acc[rt][i], 0, 0, 0);
         }
-      } else {
-        product([](uint32_t x) { return x; },
-                [&](int rt, int i, bf16x8_t vf, bf16x8_t pf) { o_acc[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, o_acc[rt][i], 0, 0, 0); });
       }
     } else {
-      auto product = [&](auto pick, auto fold) {
 #pragma unroll
-        for (int e = 0; e < NK * 4; ++e)
+      for (int e = 0; e < NK * 4; ++e)
 #pragma unroll
-          for (int i = 0; i < NB; ++i) {
-            const float v = pick(__uint_as_float(vreg[e][i / VF].w[i % VF]));
+        for (int i = 0; i < NB; ++i)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) fold(rt, i, v, s[rt][e / 4][e % 4]);
-          }
-      };
-      if (__any(odd)) {
-        product([](float v) { return fabsf(v) < INFINITY ? v : 0.f; },
-                [&](int rt, int i, float v, float p) { o_acc[rt][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p, o_acc[rt][i], 0, 0, 0); });
-#pragma unroll 1
-        for (int kind = 0; kind < 3; ++kind) {
-          const float what = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : __uint_as_float(0x7fc00000u);
-          product([&](float v) {
-                    asm volatile("" : "+v"(v));
-                    return kind == 2 ? (v != v ? 1.f : 0.f) : v == what ? 1.f : 0.f;
-                  },
-                  [&](int rt, int i, float v, float p) {
-                    const f32x4_t n = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p != 0.f ? 1.f : 0.f, f32x4_t{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) o_acc[rt][i][r] = n[r] > 0.f ? o_acc[rt][i][r] + what : o_acc[rt][i][r];
-                  });
-        }
-      } else {
-        product([](float v) { return v; },
-                [&](int rt, int i, float v, float p) { o_acc[rt][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, p, o_acc[rt][i], 0, 0, 0); });
-      }
+          for (int rt = 0; rt < RT; ++rt)
+            o_acc[rt][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vreg[e][i / VF].w[i % VF]), s[rt][e / 4][e % 4], o_acc[rt][i], 0, 0, 0);
     }
     st = next;
   }

@@ -57,13 +57,19 @@ nf_status launch_tree_stream(const DecArgs& a, int chunk, int splits, nf_dtype d
 }
 
 nf_status launch_tree_join(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s) {
-  const long long blocks = (prod({a.M, a.B, a.heads, a.N}) + 3) / 4;
+  const long long rows = prod({a.M, a.B, a.heads, a.N});
+  const int features = tree_features(a.d);
+  // up to 8 chunks a row is a few loads of one group of lanes, above that a workgroup's
+  const bool shared = splits > 8;
+  const long long blocks = shared ? rows : (rows * (features / 4) + 255) / 256;
   if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
-#define NF_JOIN(T, D, LOG2) nf_launch((decoder_join_kernel<T, D, LOG2>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk)
+#define NF_JOIN(T, D, LOG2)                                                                                                              \
+  if (shared) nf_launch((decoder_join_kernel<T, D, LOG2, 1024 / D>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk);         \
+  else nf_launch((decoder_join_kernel<T, D, LOG2, 1>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk)
   if (dt == NF_F32) {
-    if (a.d <= 64) NF_JOIN(float, 64, false); else if (a.d <= 128) NF_JOIN(float, 128, false); else NF_JOIN(float, 256, false);
+    if (features == 64) { NF_JOIN(float, 64, false); } else if (features == 128) { NF_JOIN(float, 128, false); } else { NF_JOIN(float, 256, false); }
   } else {
-    if (a.d <= 64) NF_JOIN(bf16_t, 64, true); else if (a.d <= 128) NF_JOIN(bf16_t, 128, true); else NF_JOIN(bf16_t, 256, true);
+    if (features == 64) { NF_JOIN(bf16_t, 64, true); } else if (features == 128) { NF_JOIN(bf16_t, 128, true); } else { NF_JOIN(bf16_t, 256, true); }
   }
 #undef NF_JOIN
   return launched();

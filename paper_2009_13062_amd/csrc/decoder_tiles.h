@@ -586,40 +586,76 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
   }
 }
 
-// Sums of the chunks of one row: a wavefront per row, D / 64 features per lane.  Maxima and sums in log2 units where LOG2, natural ones otherwise.
-template <typename T, int D, bool LOG2>
+// Sums of the chunks of one row: D / 4 lanes hold its features, 4 each, and SHARE such groups of lanes take every SHARE-th chunk.  Maxima and sums in log2
+// units where LOG2, natural ones otherwise.
+template <typename T, int D, bool LOG2, int SHARE>
 __global__ __launch_bounds__(256) void decoder_join_kernel(DecArgs a, int splits, int chunk) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x % kWave;
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes, kRows = kGroups / SHARE;
+  static_assert(SHARE == 1 || SHARE == kGroups, "a group per row, or all of them on one");
+  const int lane = threadIdx.x % kLanes, grp = threadIdx.x / kLanes;
   const int group = a.heads / a.kv, R = a.N * group;
-  const long row = (long)blockIdx.x * 4 + threadIdx.x / kWave;
+  const long row = (long)blockIdx.x * kRows + (SHARE == 1 ? grp : 0);
   if (row >= (long)a.M * a.B * a.kv * R) return;
   const long head = row / R, mb = head / a.kv;
   const int r = (int)(row % R), i = r / group, h = (int)(head % a.kv) * group + r % group;
   const int parts = (clamp_len(a.len[mb], a.C) + chunk - 1) / chunk;
-  if (parts <= 1) return;                                  // written already
-  const float* o = a.ws + row * splits * D;
+  if (parts <= 1) return;                                  // written already; uniform where groups share a row
+  const float* o = a.ws + row * splits * D + lane * 4;
   const float2* ml = reinterpret_cast<const float2*>(a.ws + (long)a.M * a.B * a.kv * R * splits * D) + row * splits;
-  float top = kLowestScore;
-  for (int k = lane; k < parts; k += kWave) top = fmaxf(top, ml[k].x);
-  top = wave_max(top);
-  float acc[E], sum = 0.f;
+  const int first = SHARE == 1 ? 0 : grp;
+  f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  float top = kLowestScore, sum = 0.f;
+  for (int k0 = first; k0 < parts; k0 += 8 * SHARE) {      // 8 loads of each kind at a time
+    float2 p[8];
+    f32x4_t v[8];
 #pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = 0.f;
-#pragma unroll 4
-  for (int k = 0; k < parts; ++k) {
-    const float2 p = ml[k];
-    const float c = LOG2 ? __builtin_amdgcn_exp2f(p.x - top) : expf(p.x - top);
-    sum = fmaf(p.y, c, sum);
+    for (int u = 0; u < 8; ++u) {
+      const int k = min(k0 + u * SHARE, parts - 1);
+      p[u] = ml[k];
+      v[u] = *reinterpret_cast<const f32x4_t*>(o + (long)k * D);
+    }
+    float most = top;
 #pragma unroll
-    for (int e = 0; e < E; ++e) acc[e] = fmaf(o[(long)k * D + lane + 64 * e], c, acc[e]);
+    for (int u = 0; u < 8; ++u) most = fmaxf(most, p[u].x);
+    const float old = LOG2 ? __builtin_amdgcn_exp2f(top - most) : expf(top - most);
+    top = most;
+    sum *= old;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc[e] *= old;
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float c = k0 + u * SHARE < parts ? (LOG2 ? __builtin_amdgcn_exp2f(p[u].x - top) : expf(p[u].x - top)) : 0.f;
+      sum = fmaf(p[u].y, c, sum);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[u][e], c, acc[e]);
+    }
+  }
+  if constexpr (SHARE > 1) {
+    __shared__ __align__(16) float of[kGroups][D];
+    __shared__ float2 stat[kGroups];
+    *reinterpret_cast<f32x4_t*>(&of[grp][lane * 4]) = acc;
+    if (lane == 0) stat[grp] = make_float2(top, sum);
+    __syncthreads();
+    if (grp != 0) return;
+    top = kLowestScore;
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) top = fmaxf(top, stat[k].x);
+    acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < kGroups; ++k) {
+      const float c = LOG2 ? __builtin_amdgcn_exp2f(stat[k].x - top) : expf(stat[k].x - top);
+      sum = fmaf(stat[k].y, c, sum);
+      const f32x4_t v = *reinterpret_cast<const f32x4_t*>(&of[k][lane * 4]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[e], c, acc[e]);
+    }
   }
   const bool none = sum == 0.f || (a.nodes && i >= clamp_len(a.nodes[mb], a.N));
-  T* Op = (T*)a.O + (mb * a.N + i) * ((long)a.heads * a.d) + (long)h * a.d;
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int f = lane + 64 * e;
-    if (f < a.d) store_f32(Op + f, none ? 0.f : acc[e] / sum);
+  T* Op = (T*)a.O + (mb * a.N + i) * ((long)a.heads * a.d) + (long)h * a.d + lane * 4;
+  if (lane * 4 < a.d) {
+    if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(Op) = none ? make_uint2(0, 0) : make_uint2(pack_bf16x2(acc[0] / sum, acc[1] / sum), pack_bf16x2(acc[2] / sum, acc[3] / sum));
+    else *reinterpret_cast<f32x4_t*>(Op) = none ? f32x4_t{0.f, 0.f, 0.f, 0.f} : f32x4_t{acc[0] / sum, acc[1] / sum, acc[2] / sum, acc[3] / sum};
   }
   if (a.lse && lane == 0) a.lse[(mb * a.N + i) * a.heads + h] = none ? -INFINITY : LOG2 ? (top + __builtin_amdgcn_logf(sum)) * kLn2 : top + logf(sum);
 }
