@@ -38,8 +38,8 @@ typedef uint32_t dec_u32x4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t dec_u32x2_t __attribute__((ext_vector_type(2)));
 constexpr unsigned kDecOob = 0x80000000u;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rows_from(const void* first) { return __builtin_amdgcn_make_buffer_rsrc((void*)first, 0, (int)kDecOob, 0x00020000); }
-__device__ __forceinline__ uint4 rows_load16(__amdgpu_buffer_rsrc_t r, unsigned off) {
-  const dec_u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, 0);
+template <int AUX = 0> __device__ __forceinline__ uint4 rows_load16(__amdgpu_buffer_rsrc_t r, unsigned off) {
+  const dec_u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(r, (int)off, 0, AUX);
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 

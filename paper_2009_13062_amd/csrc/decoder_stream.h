@@ -47,11 +47,14 @@ template <typename T> __device__ __forceinline__ f32x4_t slice_product(const uin
 }
 
 template <typename T, int D, int RT, int KS, bool TREE>
-__global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
+__global__ __launch_bounds__(256, D <= 128 ? 3 : 2) void decoder_stream_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
   using Sh = StreamShape<T, D>;
   constexpr bool kBf = Sh::kBf;
   constexpr int NK = Sh::NK, NB = Sh::NB, VF = Sh::VF, VC = Sh::VC, SL = Sh::kSlices, kStep = 16 * NK, RG = 4 / KS;
   constexpr int kRows = RG * RT * 16;                      // per workgroup
+  // A cache that one workgroup's rows are all of is read once: its values go past the caches (two of 100003 keys 131 -> 122 us; keys, whose 128-byte lines take
+  // two loads, do not: one token over 8192 110 -> 119).
+  constexpr int kOnce = TREE && KS > 1 ? 2 : 0;
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int g4 = lane / 16, l16 = lane % 16, rg = wave % RG, share = wave / RG;
@@ -86,80 +89,10 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
   const long stride = TREE ? a.d : a.kv_stride_row;
   const float unit = kBf ? kLog2e : 1.f;
 
-  // ---- this lane's rows
-  int token[RT], end[RT], mine[RT], docr[RT];
-  uint64_t path[RT];
-  float slope[RT];
-  uint4 qf[RT][SL];
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt) {
-    const int r = r0 + (rg * RT + rt) * 16 + l16;
-    const int i = min(r, R - 1) / group, h = g * group + (min(r, R - 1) - i * group);
-    token[rt] = i;
-    const T* q = (const T*)a.Q + m * a.q_stride_m + ((long)b * a.N + i) * a.q_stride_row + (long)h * a.d;
-#pragma unroll
-    for (int sl = 0; sl < SL; ++sl) {
-      const int f = sl * Sh::kSliceF + g4 * Sh::kPiece;
-      qf[rt][sl] = make_uint4(0, 0, 0, 0);
-      if (r < R && f < a.d) qf[rt][sl] = *reinterpret_cast<const uint4*>(q + f);
-    }
-    slope[rt] = biased ? a.slope[m * a.heads + h] * unit : 0.f;
-  }
   const int w0 = r0 + rg * RT * 16;                        // first row of the wavefront
   const int w_lo = min(w0, R - 1) / group, w_hi = min(w0 + RT * 16 - 1, R - 1) / group;
-  int node_at = 0, lo = 0, hi = 0, key_end;
-  if constexpr (TREE) {
-    int par = lane - 1;                                    // paths of all nodes at once, as in decoder_tiles.h
-    if (a.parent && a.N > 1) {
-      par = lane < a.N ? a.parent[mb * a.N + lane] : -1;
-      par = par < lane ? par : -1;
-    }
-    uint64_t all = 1ull << lane;
-    for (int step = 1; step < a.N; step *= 2) {
-      const int from = max(par, 0);
-      const uint32_t x = __shfl((uint32_t)all, from, kWave), y = __shfl((uint32_t)(all >> 32), from, kWave);
-      const int up = __shfl(par, from, kWave);
-      if (par >= 0) {
-        all |= ((uint64_t)y << 32) | x;
-        par = up;
-      }
-    }
-    const int begin = a.start ? a.start[mb] : L;
-    node_at = begin + __popcll(all) - 1;
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const uint32_t x = __shfl((uint32_t)all, token[rt], kWave), y = __shfl((uint32_t)(all >> 32), token[rt], kWave);
-      path[rt] = ((uint64_t)y << 32) | x;
-      mine[rt] = begin + __popcll(path[rt]) - 1;
-      end[rt] = L;
-      docr[rt] = 0;
-    }
-    key_end = min(L, (split + 1) * chunk);
-  } else {
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int i = token[rt];
-      path[rt] = 0;
-      mine[rt] = i;
-      docr[rt] = doc ? doc[i] : 0;
-      end[rt] = i >= L || docr[rt] < 0 ? 0 : a.causal ? max(i + 1, first) : L;
-    }
-    key_end = w0 >= R || w_lo >= L ? 0 : a.causal ? min(max(w_hi + 1, first), L) : L;
-    if (doc) {
-      lo = 0x7fffffff;
-      hi = -1;
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-        if (end[rt] > 0) lo = min(lo, docr[rt]), hi = max(hi, docr[rt]);
-#pragma unroll
-      for (int o = 1; o < kWave; o *= 2) {
-        lo = min(lo, __shfl_xor(lo, o, kWave));
-        hi = max(hi, __shfl_xor(hi, o, kWave));
-      }
-      lo = __builtin_amdgcn_readfirstlane(lo);
-      hi = __builtin_amdgcn_readfirstlane(hi);
-    }
-  }
+  int node_at = 0, lo = 0, hi = 0;                         // position of node `lane`, documents of this wavefront's rows
+  const int key_end = TREE ? min(L, (split + 1) * chunk) : w0 >= R || w_lo >= L ? 0 : a.causal ? min(max(w_hi + 1, first), L) : L;
 
   // ---- the steps of this wavefront: of its chunk of the cache, then of the tree; every KS-th is its own
   const int key_start = TREE ? split * chunk : 0;
@@ -216,8 +149,8 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
       for (int sl = 0; sl < SL; ++sl) kreg[k][sl] = rows_load16(rk, sl * Sh::kSliceF + g4 * Sh::kPiece < a.d ? from + sl * 64 : kDecOob);
     }
     if (keyed) {
-      const int key = base + lane, there = base + min(lane, limit - 1);
-      if (TREE) key_reg = own_step ? __shfl(node_at, key % kWave, kWave) : a.pos ? a.pos[head * a.C + there] : key;
+      const int there = base + min(lane, limit - 1);
+      if (TREE) key_reg = a.pos && !own_step ? a.pos[head * a.C + there] : there;
       else key_reg = lane < limit ? doc[there] : -1;
     }
   };
@@ -235,14 +168,88 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
       for (int c = 0; c < VC; ++c) {
         const unsigned off = c * 16 * VF + l16 * VF < a.d ? from + c * (64 * Sh::kVWords) : kDecOob;
         if constexpr (Sh::kVWords == 4) {
-          vreg[e][c] = __builtin_bit_cast(Words<4>, rows_load16(rv, off));
+          vreg[e][c] = __builtin_bit_cast(Words<4>, rows_load16<kOnce>(rv, off));
         } else {
-          const dec_u32x2_t v = __builtin_amdgcn_raw_buffer_load_b64(rv, (int)off, 0, 0);
+          const dec_u32x2_t v = __builtin_amdgcn_raw_buffer_load_b64(rv, (int)off, 0, kOnce);
           vreg[e][c] = __builtin_bit_cast(Words<Sh::kVWords>, v);
         }
       }
     }
   };
+
+  int st = share;
+  const bool early = TREE || !doc;                         // the first keys are on their way before anything else is looked up
+  if (early && st < steps) load_keys(st);
+
+  // ---- this lane's rows
+  int token[RT], end[RT], mine[RT], docr[RT];
+  uint64_t path[RT];
+  float slope[RT];
+  uint4 qf[RT][SL];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    const int r = r0 + (rg * RT + rt) * 16 + l16;
+    const int i = min(r, R - 1) / group, h = g * group + (min(r, R - 1) - i * group);
+    token[rt] = i;
+    const T* q = (const T*)a.Q + m * a.q_stride_m + ((long)b * a.N + i) * a.q_stride_row + (long)h * a.d;
+#pragma unroll
+    for (int sl = 0; sl < SL; ++sl) {
+      const int f = sl * Sh::kSliceF + g4 * Sh::kPiece;
+      qf[rt][sl] = make_uint4(0, 0, 0, 0);
+      if (r < R && f < a.d) qf[rt][sl] = *reinterpret_cast<const uint4*>(q + f);
+    }
+    slope[rt] = biased ? a.slope[m * a.heads + h] * unit : 0.f;
+  }
+  if constexpr (TREE) {
+    int par = lane - 1;                                    // paths of all nodes at once, as in decoder_tiles.h
+    if (a.parent && a.N > 1) {
+      par = lane < a.N ? a.parent[mb * a.N + lane] : -1;
+      par = par < lane ? par : -1;
+    }
+    uint64_t all = 1ull << lane;
+    for (int step = 1; step < a.N; step *= 2) {
+      const int from = max(par, 0);
+      const uint32_t x = __shfl((uint32_t)all, from, kWave), y = __shfl((uint32_t)(all >> 32), from, kWave);
+      const int up = __shfl(par, from, kWave);
+      if (par >= 0) {
+        all |= ((uint64_t)y << 32) | x;
+        par = up;
+      }
+    }
+    const int begin = a.start ? a.start[mb] : L;
+    node_at = begin + __popcll(all) - 1;
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const uint32_t x = __shfl((uint32_t)all, token[rt], kWave), y = __shfl((uint32_t)(all >> 32), token[rt], kWave);
+      path[rt] = ((uint64_t)y << 32) | x;
+      mine[rt] = begin + __popcll(path[rt]) - 1;
+      end[rt] = L;
+      docr[rt] = 0;
+    }
+  } else {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int i = token[rt];
+      path[rt] = 0;
+      mine[rt] = i;
+      docr[rt] = doc ? doc[i] : 0;
+      end[rt] = i >= L || docr[rt] < 0 ? 0 : a.causal ? max(i + 1, first) : L;
+    }
+    if (doc) {
+      lo = 0x7fffffff;
+      hi = -1;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+        if (end[rt] > 0) lo = min(lo, docr[rt]), hi = max(hi, docr[rt]);
+#pragma unroll
+      for (int o = 1; o < kWave; o *= 2) {
+        lo = min(lo, __shfl_xor(lo, o, kWave));
+        hi = max(hi, __shfl_xor(hi, o, kWave));
+      }
+      lo = __builtin_amdgcn_readfirstlane(lo);
+      hi = __builtin_amdgcn_readfirstlane(hi);
+    }
+  }
 
   f32x4_t o_acc[RT][NB];                                   // element r of block i: feature (i / VF) 16 VF + VF (4 g4 + r) + i % VF of row l16
   float mrun[RT], lrun[RT];
@@ -255,8 +262,10 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
   }
   const float sc = a.scale * unit;
 
-  int st = seek(share);
-  if (st < steps) load_keys(st);
+  if (!early) {
+    st = seek(share);
+    if (st < steps) load_keys(st);
+  }
   while (st < steps) {
     const bool mask = !whole(st), own_step = TREE && st >= cached_steps;
     const int base = own_step ? (st - cached_steps) * kStep : key_start + st * kStep;
@@ -272,7 +281,7 @@ __global__ __launch_bounds__(256, 2) void decoder_stream_kernel(DecArgs a, int r
       for (int k = 0; k < NK; ++k)
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) s[rt][k] = slice_product<T>(kreg[k][sl], qf[rt][sl], s[rt][k]);
-    const int key_now = key_reg;
+    const int key_now = own_step ? __shfl(node_at, (base + lane) % kWave, kWave) : key_reg;
     const int next = seek(st + KS);
     if (next < steps) load_keys(next);
 
