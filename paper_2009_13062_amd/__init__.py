@@ -136,7 +136,9 @@ try:
     _address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
     _native.bind(_check, _address(lib.netfuse_linear), _address(lib.netfuse_linear_packed), _address(lib.netfuse_layernorm),
                  _address(lib.netfuse_attention), _address(lib.netfuse_attention_relpos), _address(lib.netfuse_conv2d))
-except ImportError:
+    _native.bind_decoder(*[_address(getattr(lib, "netfuse_" + f)) for f in (
+        "attention_prompt", "attention_tree", "attention_tree_workspace", "cache_append", "cache_weigh", "cache_evict", "cache_evict_workspace")])
+except (ImportError, AttributeError):                        # not built, for another torch or Python, or from older sources
     _native = None
 if _raw_stream is None or _device is None:
     _native = None

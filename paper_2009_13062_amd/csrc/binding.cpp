@@ -21,6 +21,13 @@ decltype(&netfuse_layernorm) f_layernorm;
 decltype(&netfuse_attention) f_attention;
 decltype(&netfuse_attention_relpos) f_relpos;
 decltype(&netfuse_conv2d) f_conv2d;
+decltype(&netfuse_attention_prompt) f_prompt;
+decltype(&netfuse_attention_tree) f_tree;
+decltype(&netfuse_attention_tree_workspace) f_tree_workspace;
+decltype(&netfuse_cache_append) f_append;
+decltype(&netfuse_cache_weigh) f_weigh;
+decltype(&netfuse_cache_evict) f_evict;
+decltype(&netfuse_cache_evict_workspace) f_evict_workspace;
 PyObject* g_error;                           // callable (entry point, status) that raises
 
 const c10::DispatchKeySet kWrapped({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper,
@@ -243,6 +250,264 @@ PyObject* conv2d(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- decoders: every operand's shape, type and device is checked here, and what is not as it should be goes to decoder.py for its error
+
+const at::Tensor* strided(PyObject* o, at::ScalarType st, int device) {
+  if (!THPVariable_CheckExact(o)) return nullptr;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  if (!t.defined() || !t.is_cuda() || t.layout() != at::kStrided || t.key_set().has_any(kWrapped) || !t.has_storage() || t.scalar_type() != st ||
+      t.device().index() != device)
+    return nullptr;
+  return &t;
+}
+// A contiguous operand of this type and shape, or None where it may be missing.
+bool dense(PyObject* o, at::ScalarType st, at::IntArrayRef shape, int device, bool needed, void** p) {
+  *p = nullptr;
+  if (o == Py_None) return !needed;
+  const at::Tensor* t = strided(o, st, device);
+  if (!t || t->sizes() != shape || !t->is_contiguous()) return false;
+  *p = t->data_ptr();
+  return true;
+}
+struct Rows {
+  const void* p;
+  long model, row;
+};
+// [M][N][width] with a contiguous last dimension; the stride of a dimension of one element says nothing.
+bool rows(const at::Tensor* t, int64_t M, int64_t N, int64_t width, Rows* r) {
+  if (!t || t->dim() != 3 || t->size(0) != M || t->size(1) != N || t->size(2) != width || (width > 1 && t->stride(2) != 1)) return false;
+  r->p = t->data_ptr();
+  r->row = N > 1 ? t->stride(1) : width;
+  r->model = M > 1 ? t->stride(0) : (N - 1) * r->row + width;
+  return true;
+}
+bool number(PyObject* o, float* v) {
+  if (!PyFloat_CheckExact(o)) return false;
+  *v = (float)PyFloat_AS_DOUBLE(o);
+  return true;
+}
+bool scale_of(PyObject* o, int d, float* v) {
+  if (o == Py_None) {
+    *v = (float)std::pow((double)d, -0.5);
+    return true;
+  }
+  return number(o, v);
+}
+// The type of the rows and the current device.
+bool types(PyObject* o, PyObject* device_, at::ScalarType* st, int* device) {
+  if (!THPVariable_CheckExact(o) || !whole(device_, device)) return false;
+  *st = THPVariable_Unpack(o).scalar_type();
+  return *st == at::kFloat || *st == at::kBFloat16;
+}
+struct Cache {
+  int M, B, kv, C, d;
+  void* p;
+};
+bool cache(PyObject* o, at::ScalarType st, int device, Cache* c) {
+  const at::Tensor* t = strided(o, st, device);
+  if (!t || t->dim() != 5 || !t->is_contiguous() || !size(t->size(0), &c->M) || !size(t->size(1), &c->B) || !size(t->size(2), &c->kv) || !size(t->size(3), &c->C) ||
+      !size(t->size(4), &c->d) || t->numel() == 0)
+    return false;
+  c->p = t->data_ptr();
+  return true;
+}
+// Rows of a batch of c.B sequences: T of them each.
+bool batch(const at::Tensor* t, const Cache& c, int* T) { return t && t->dim() == 3 && t->size(1) > 0 && t->size(1) % c.B == 0 && size(t->size(1) / c.B, T); }
+
+// Q, K, V, B, S, heads, kv_heads, causal, scale, cap, slope, length, prefix, doc, out, device, stream
+PyObject* attention_prompt(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, B, S, heads, kv, M, d;
+    float scale, cap;
+    void *slope, *len, *prefix, *doc, *s;
+    if (n != 17 || !types(a[0], a[15], &st, &device)) return not_taken();
+    const at::Tensor *Q = strided(a[0], st, device), *K = strided(a[1], st, device), *V = strided(a[2], st, device);
+    if (!Q || Q->dim() != 3 || !whole(a[3], &B) || !whole(a[4], &S) || !whole(a[5], &heads) || B <= 0 || S <= 0 || heads <= 0 || !size(Q->size(0), &M) || M <= 0 ||
+        Q->size(2) % heads || !size(Q->size(2) / heads, &d) || d <= 0 || !PyBool_Check(a[7]) || !scale_of(a[8], d, &scale) || !number(a[9], &cap) || !stream_of(a[16], &s))
+      return not_taken();
+    kv = heads;
+    if (a[6] != Py_None && (!whole(a[6], &kv) || kv <= 0)) return not_taken();
+    Rows q, k, v;
+    const int64_t N = (int64_t)B * S;
+    if (!rows(Q, M, N, (int64_t)heads * d, &q) || !rows(K, M, N, (int64_t)kv * d, &k) || !rows(V, M, N, (int64_t)kv * d, &v) || k.model != v.model || k.row != v.row ||
+        !dense(a[10], at::kFloat, {M, heads}, device, false, &slope) || !dense(a[11], at::kInt, {M, B}, device, false, &len) ||
+        !dense(a[12], at::kInt, {M, B}, device, false, &prefix) || !dense(a[13], at::kInt, {M, B, S}, device, false, &doc))
+      return not_taken();
+    void* given;
+    if (!dense(a[14], st, {M, N, (int64_t)heads * d}, device, false, &given)) return not_taken();
+    const int causal = a[7] == Py_True;
+    const nf_dtype dt = type_of(*Q);
+    return produce("netfuse_attention_prompt", a[14], {M, N, (int64_t)heads * d}, Q->options(), [=](void* y) {
+      return f_prompt(q.p, k.p, v.p, (const float*)slope, (const int*)len, (const int*)prefix, (const int*)doc, y, M, B, S, heads, kv, d, q.model, q.row, k.model, k.row, causal, scale, cap,
+                      dt, s);
+    });
+  });
+}
+
+// Q, K, V, Kc, Vc, length, start, parent, nodes, pos, slope, scale, cap, out, lse, workspace, device, stream
+PyObject* attention_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, T, heads;
+    float scale, cap;
+    void *vc, *len, *start, *parent, *nodes, *pos, *slope, *given, *lse, *ws = nullptr, *s;
+    Cache c;
+    if (n != 18 || !types(a[0], a[16], &st, &device) || !cache(a[3], st, device, &c) || !dense(a[4], st, {c.M, c.B, c.kv, c.C, c.d}, device, true, &vc)) return not_taken();
+    const at::Tensor *Q = strided(a[0], st, device), *K = strided(a[1], st, device), *V = strided(a[2], st, device);
+    if (!batch(Q, c, &T) || Q->size(2) % c.d || !size(Q->size(2) / c.d, &heads) || !scale_of(a[11], c.d, &scale) || !number(a[12], &cap) || !stream_of(a[17], &s)) return not_taken();
+    Rows q, k, v;
+    const int64_t N = (int64_t)c.B * T, W = (int64_t)heads * c.d;
+    if (!rows(Q, c.M, N, W, &q) || !rows(K, c.M, N, (int64_t)c.kv * c.d, &k) || !rows(V, c.M, N, (int64_t)c.kv * c.d, &v) || k.model != v.model || k.row != v.row ||
+        !dense(a[5], at::kInt, {c.M, c.B}, device, true, &len) || !dense(a[6], at::kInt, {c.M, c.B}, device, false, &start) ||
+        !dense(a[7], at::kInt, {c.M, c.B, T}, device, false, &parent) || !dense(a[8], at::kInt, {c.M, c.B}, device, false, &nodes) ||
+        !dense(a[9], at::kInt, {c.M, c.B, c.kv, c.C}, device, false, &pos) || !dense(a[10], at::kFloat, {c.M, heads}, device, false, &slope) ||
+        !dense(a[13], st, {c.M, N, W}, device, false, &given) || !dense(a[14], at::kFloat, {c.M, N, heads}, device, false, &lse))
+      return not_taken();
+    const nf_dtype dt = type_of(*Q);
+    long long bytes = f_tree_workspace(c.M, c.B, T, c.C, heads, c.kv, c.d, dt);
+    if (bytes < 0) return not_taken();
+    at::Tensor room;
+    const bool mine = a[15] == Py_None && bytes > 0;
+    if (a[15] != Py_None) {
+      if (!THPVariable_CheckExact(a[15])) return not_taken();
+      const at::Tensor& w = THPVariable_Unpack(a[15]);
+      if (!w.defined() || !w.is_cuda() || w.layout() != at::kStrided || w.key_set().has_any(kWrapped) || !w.has_storage() || !w.is_contiguous() || w.device().index() != device) return not_taken();
+      ws = w.data_ptr();
+      bytes = w.numel() * (long long)w.element_size();
+    }
+    return produce("netfuse_attention_tree", a[13], {c.M, N, W}, Q->options(), [&](void* y) {
+      if (mine) {
+        room = at::empty({bytes}, Q->options().dtype(at::kByte));
+        ws = room.data_ptr();
+      }
+      return f_tree(q.p, k.p, v.p, c.p, vc, (const int*)pos, (const int*)len, (const int*)start, (const int*)parent, (const int*)nodes, (const float*)slope, y, (float*)lse, ws, bytes, c.M, c.B, T,
+                    c.C, heads, c.kv, c.d, q.model, q.row, k.model, k.row, scale, cap, dt, s);
+    });
+  });
+}
+
+// A call that has no output of its own: True where it was made.
+template <class F>
+PyObject* made(const char* fn, F&& call) {
+  nf_status st;
+  {
+    Unlocked unlocked;
+    st = call();
+  }
+  at::Tensor none;
+  return done(fn, st, Py_True, none);
+}
+
+// K, V, Kc, Vc, pos, weight, length, start, index, count, device, stream
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, T, m;
+    void *vc, *pos, *weight, *len, *start, *index, *count, *s;
+    Cache c;
+    if (n != 12 || !types(a[0], a[10], &st, &device) || !cache(a[2], st, device, &c) || !dense(a[3], st, {c.M, c.B, c.kv, c.C, c.d}, device, true, &vc) || !stream_of(a[11], &s)) return not_taken();
+    const at::Tensor *K = strided(a[0], st, device), *V = strided(a[1], st, device);
+    if (!batch(K, c, &T)) return not_taken();
+    m = T;
+    if (a[8] != Py_None) {
+      const at::Tensor* i = strided(a[8], at::kInt, device);
+      if (!i || i->dim() != 3 || !size(i->size(2), &m)) return not_taken();
+    }
+    Rows k, v;
+    const int64_t N = (int64_t)c.B * T, W = (int64_t)c.kv * c.d;
+    if (!rows(K, c.M, N, W, &k) || !rows(V, c.M, N, W, &v) || k.model != v.model || k.row != v.row || !dense(a[4], at::kInt, {c.M, c.B, c.kv, c.C}, device, false, &pos) ||
+        !dense(a[5], at::kFloat, {c.M, c.B, c.kv, c.C}, device, false, &weight) || !dense(a[6], at::kInt, {c.M, c.B}, device, true, &len) ||
+        !dense(a[7], at::kInt, {c.M, c.B}, device, false, &start) || !dense(a[8], at::kInt, {c.M, c.B, m}, device, false, &index) ||
+        !dense(a[9], at::kInt, {c.M, c.B}, device, false, &count))
+      return not_taken();
+    const nf_dtype dt = type_of(*K);
+    return made("netfuse_cache_append", [=] {
+      return f_append(k.p, v.p, (const int*)index, (const int*)count, (const int*)len, (const int*)start, c.p, vc, (int*)pos, (float*)weight, c.M, c.B, T, m, c.C, c.kv, c.d, k.model, k.row, dt, s);
+    });
+  });
+}
+
+// Q, lse, Kc, weight, length, start, index, count, pos, slope, scale, cap, out, device, stream
+PyObject* cache_weigh(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, T, m, heads;
+    float scale, cap;
+    void *lse, *weight, *len, *start, *index, *count, *pos, *slope, *given, *s;
+    Cache c;
+    if (n != 15 || !types(a[0], a[13], &st, &device) || !cache(a[2], st, device, &c) || !stream_of(a[14], &s)) return not_taken();
+    const at::Tensor* Q = strided(a[0], st, device);
+    if (!batch(Q, c, &T) || Q->size(2) % c.d || !size(Q->size(2) / c.d, &heads) || !scale_of(a[10], c.d, &scale) || !number(a[11], &cap)) return not_taken();
+    m = T;
+    if (a[6] != Py_None) {
+      const at::Tensor* i = strided(a[6], at::kInt, device);
+      if (!i || i->dim() != 3 || !size(i->size(2), &m)) return not_taken();
+    }
+    Rows q;
+    const int64_t N = (int64_t)c.B * T;
+    const at::DimVector shape({c.M, c.B, c.kv, c.C});
+    if (!rows(Q, c.M, N, (int64_t)heads * c.d, &q) || !dense(a[1], at::kFloat, {c.M, N, heads}, device, true, &lse) || !dense(a[3], at::kFloat, shape, device, true, &weight) ||
+        !dense(a[4], at::kInt, {c.M, c.B}, device, true, &len) || !dense(a[5], at::kInt, {c.M, c.B}, device, false, &start) ||
+        !dense(a[6], at::kInt, {c.M, c.B, m}, device, false, &index) || !dense(a[7], at::kInt, {c.M, c.B}, device, false, &count) || !dense(a[8], at::kInt, shape, device, false, &pos) ||
+        !dense(a[9], at::kFloat, {c.M, heads}, device, false, &slope) || !dense(a[12], at::kFloat, shape, device, false, &given))
+      return not_taken();
+    const nf_dtype dt = type_of(*Q);
+    return produce("netfuse_cache_weigh", a[12], shape, Q->options().dtype(at::kFloat), [=](void* y) {
+      return f_weigh(q.p, (const float*)lse, (const int*)index, (const int*)count, c.p, (const int*)pos, (const int*)len, (const int*)start, (const float*)slope, (const float*)weight, (float*)y, c.M, c.B,
+                     T, m, c.C, heads, c.kv, c.d, q.model, q.row, scale, cap, dt, s);
+    });
+  });
+}
+
+// Kc, Vc, pos, weight, length, budget, start, recent, pos_out, weight_out, device, stream (a workspace of the caller's is decoder.py's)
+PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, budget, recent;
+    void *vc, *pos, *weight, *len, *start, *pos_out, *weight_out, *s;
+    Cache c;
+    if (n != 12 || !types(a[0], a[10], &st, &device) || !cache(a[0], st, device, &c) || !dense(a[1], st, {c.M, c.B, c.kv, c.C, c.d}, device, true, &vc) || !whole(a[5], &budget) ||
+        !whole(a[7], &recent) || !stream_of(a[11], &s))
+      return not_taken();
+    const at::DimVector shape({c.M, c.B, c.kv, c.C});
+    if (!dense(a[2], at::kInt, shape, device, false, &pos) || !dense(a[3], at::kFloat, shape, device, true, &weight) || !dense(a[4], at::kInt, {c.M, c.B}, device, true, &len) ||
+        !dense(a[6], at::kInt, {c.M, c.B}, device, false, &start) || !dense(a[8], at::kInt, shape, device, false, &pos_out) || !dense(a[9], at::kFloat, shape, device, true, &weight_out))
+      return not_taken();
+    const at::Tensor& K = THPVariable_Unpack(a[0]);
+    const nf_dtype dt = type_of(K);
+    const long long bytes = f_evict_workspace(c.M, c.B, c.C, c.kv, budget);
+    if (bytes < 0) return not_taken();
+    at::Tensor room;
+    return made("netfuse_cache_evict", [&] {
+      room = at::empty({bytes}, K.options().dtype(at::kByte));
+      return f_evict(c.p, vc, (const int*)pos, (const float*)weight, (const int*)len, (const int*)start, (int*)pos_out, (float*)weight_out, room.data_ptr(), bytes, c.M, c.B, c.C, c.kv, c.d, budget,
+                     recent, dt, s);
+    });
+  });
+}
+
+// bind_decoder: the addresses of prompt, tree and its workspace, append, weigh, evict and its workspace
+PyObject* bind_decoder(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 7) {
+    PyErr_SetString(PyExc_TypeError, "bind_decoder takes seven addresses");
+    return nullptr;
+  }
+  void* p[7];
+  for (int i = 0; i < 7; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  f_prompt = (decltype(f_prompt))p[0];
+  f_tree = (decltype(f_tree))p[1];
+  f_tree_workspace = (decltype(f_tree_workspace))p[2];
+  f_append = (decltype(f_append))p[3];
+  f_weigh = (decltype(f_weigh))p[4];
+  f_evict = (decltype(f_evict))p[5];
+  f_evict_workspace = (decltype(f_evict_workspace))p[6];
+  Py_RETURN_NONE;
+}
+
 // bind(error, linear, linear_packed, layernorm, attention, attention_relpos, conv2d): the addresses of the entry points
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 7) {
@@ -267,7 +532,7 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind), FAST(linear), FAST(linear_packed), FAST(layernorm), FAST(attention_packed), FAST(attention_relpos_packed),
-                         FAST(conv2d), {nullptr, nullptr, 0, nullptr}};
+                         FAST(conv2d), FAST(bind_decoder), FAST(attention_prompt), FAST(attention_tree), FAST(cache_append), FAST(cache_weigh), FAST(cache_evict), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

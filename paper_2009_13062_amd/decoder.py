@@ -85,6 +85,11 @@ def attention_prompt(Q, K, V, B, S, heads, kv_heads=None, causal=True, scale=Non
 
     Scores are cap*tanh(scale*qk/cap) (cap 0: scale*qk) minus slope[m, head] * distance.  Row i sees key j if both lie below length[m, b], and, where
     causal, j <= i or j < prefix[m, b], and, with doc[m, b, S], both belong to the same document >= 0.  Rows that see nothing are 0."""
+    if nf._native is not None and stream is None and type(Q) is nf._Tensor and Q.is_cuda:
+        device = nf._device()
+        O = nf._native.attention_prompt(Q, K, V, B, S, heads, kv_heads, causal, scale, cap, slope, length, prefix, doc, out, device, nf._raw_stream(device))
+        if O is not None:
+            return O
     if Q.dim() != 3:
         raise ValueError("Q must be [M, B*S, heads*d]")
     kv_heads = heads if kv_heads is None else kv_heads
@@ -129,6 +134,11 @@ def attention_tree(Q, K, V, Kc, Vc, length, start=None, parent=None, nodes=None,
     start[m, b] (None: length) plus the number of its ancestors, an entry's is pos[m, b, kv_heads, C] (None: its slot).  nodes[m, b]: how many nodes there
     are; rows past it are 0.  lse: a float32 [M, B*T, heads] tensor that receives the logarithms of the sums, for cache_weigh.
     workspace: attention_tree_workspace(...) bytes, a call's own if None."""
+    if nf._native is not None and stream is None and type(Q) is nf._Tensor and Q.is_cuda:
+        device = nf._device()
+        O = nf._native.attention_tree(Q, K, V, Kc, Vc, length, start, parent, nodes, pos, slope, scale, cap, out, lse, workspace, device, nf._raw_stream(device))
+        if O is not None:
+            return O
     (M, B, kv_heads, C, d), kc, vc = _cache_shape(Kc, Vc, Q.dtype)
     if Q.dim() != 3 or Q.shape[0] != M or Q.shape[1] % B or Q.shape[2] % d:
         raise ValueError("Q must be [M, B*T, heads*d]")
@@ -153,6 +163,10 @@ def attention_tree(Q, K, V, Kc, Vc, length, start=None, parent=None, nodes=None,
 def cache_append(K, V, Kc, Vc, pos, weight, length, start=None, index=None, count=None, stream=None):
     """Entry length + i of each cache takes row index[m, b, i] (None: row i) of K and V[M, B*T, kv_heads*d], position start + i and weight 0, for
     i < count[m, b] (None: all).  pos int32 and weight float32 [M, B, kv_heads, C], or None where they are not kept.  `length` stays as it is."""
+    if nf._native is not None and stream is None and type(K) is nf._Tensor and K.is_cuda:
+        device = nf._device()
+        if nf._native.cache_append(K, V, Kc, Vc, pos, weight, length, start, index, count, device, nf._raw_stream(device)) is not None:
+            return
     (M, B, kv_heads, C, d), kc, vc = _cache_shape(Kc, Vc, K.dtype)
     if K.dim() != 3 or K.shape[0] != M or K.shape[1] % B:
         raise ValueError("K must be [M, B*T, kv_heads*d]")
@@ -170,6 +184,11 @@ def cache_append(K, V, Kc, Vc, pos, weight, length, start=None, index=None, coun
 def cache_weigh(Q, lse, Kc, weight, length, start=None, index=None, count=None, pos=None, slope=None, scale=None, cap=0.0, out=None, stream=None):
     """weight[M, B, kv_heads, C] plus the attention weight that the appended tokens gave to each entry (length, start, index and count as they were for
     cache_append; Q and lse as of attention_tree, with its pos, slope, scale and cap).  out may be weight."""
+    if nf._native is not None and stream is None and type(Q) is nf._Tensor and Q.is_cuda:
+        device = nf._device()
+        W = nf._native.cache_weigh(Q, lse, Kc, weight, length, start, index, count, pos, slope, scale, cap, out, device, nf._raw_stream(device))
+        if W is not None:
+            return W
     if Kc.dim() != 5:
         raise ValueError("a cache is [M, B, kv_heads, C, d]")
     M, B, kv_heads, C, d = Kc.shape
@@ -204,11 +223,15 @@ def cache_evict(Kc, Vc, pos, weight, length, budget, start=None, recent=0, pos_o
     """Cuts every cache that holds more than `budget` entries back to it: the entries of lowest weight leave (the lower slot among equals), those at positions
     start - recent and later last, and the free slots below budget take the entries that stay above it.  Keys and values move in place; position and
     weight too, or into pos_out and weight_out, which are returned.  `length` stays as it is: the caller takes length.clamp_(max=budget)."""
+    pos_out, weight_out = (pos if pos_out is None else pos_out), (weight if weight_out is None else weight_out)
+    if nf._native is not None and stream is None and workspace is None and type(Kc) is nf._Tensor and Kc.is_cuda:
+        device = nf._device()
+        if nf._native.cache_evict(Kc, Vc, pos, weight, length, budget, start, recent, pos_out, weight_out, device, nf._raw_stream(device)) is not None:
+            return pos_out, weight_out
     if weight is None or length is None:
         raise ValueError("weight and length are required")
     (M, B, kv_heads, C, d), kc, vc = _cache_shape(Kc, Vc, Kc.dtype)
     shape = (M, B, kv_heads, C)
-    pos_out, weight_out = (pos if pos_out is None else pos_out), (weight if weight_out is None else weight_out)
     small = (_dense(pos, "pos", shape, torch.int32), _dense(weight, "weight", shape, torch.float32), _dense(length, "length", (M, B), torch.int32),
              _dense(start, "start", (M, B), torch.int32), _dense(pos_out, "pos_out", shape, torch.int32), _dense(weight_out, "weight_out", shape, torch.float32))
     need = max(0, nf.lib.netfuse_cache_evict_workspace(M, B, C, kv_heads, budget))
