@@ -9,7 +9,7 @@ namespace nf {
 // eighth of it; below 512 keys a chunk is not worth its own start.
 inline int tree_chunk(int rows) {
   int chunk = 512;
-  while (chunk < 16LL * rows && chunk < 1 << 20) chunk *= 2;
+  while (chunk < 16LL * rows && chunk < 1024) chunk *= 2;
   return chunk;
 }
 inline int tree_features(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }

@@ -31,6 +31,9 @@ nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
 template <typename T, int D>
 nf_status tree(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   const int R = a.N * (a.heads / a.kv);
+  if constexpr (D == 128) {
+    if (R > 16 && R <= 64) return R <= 32 ? go<T, D, 2, 4, true>(a, splits, chunk, s) : go<T, D, 2, 2, true>(a, splits, chunk, s);
+  }
   return R <= 16 ? go<T, D, 1, 4, true>(a, splits, chunk, s) : R <= 32 ? go<T, D, 1, 2, true>(a, splits, chunk, s) : go<T, D, 1, 1, true>(a, splits, chunk, s);
 }
 

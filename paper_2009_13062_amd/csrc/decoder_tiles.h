@@ -17,19 +17,26 @@
 // what is merged with it nor on the capacity.  Where a sequence fills more than one chunk, partial sums go to the workspace and a second kernel joins them.
 #pragma once
 #include "decoder.h"
-#include "gemm_mfma.h"
+#include "gemm_dma.h"
 
 namespace nf {
 
 typedef int int4v_t __attribute__((ext_vector_type(4)));
 
-template <int D, int KB, int STAGES> struct DecLds {
-  static constexpr int kKPitch = D + 8;                    // 16-byte fragment reads of 32 keys spread over the banks
-  static constexpr int kVPitch = D + 32;                   // the 4 keys x 64 bytes of a transposing read tile the 64 banks
-  static constexpr int kOffV = STAGES * KB * kKPitch * 2;
-  static constexpr int kOffKey = kOffV + STAGES * KB * kVPitch * 2;       // position or document of each key
-  static constexpr int kOffFlag = kOffKey + STAGES * KB * 4;              // tile whose values are not all finite, per stage
+// 16 bytes per lane from `off` of the resource to the lane's place in 1 KB of LDS
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, lds_u8_t* to, unsigned off) { __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, (int)off, 0, 0, 0); }
+
+template <int D, int KB, int NS> struct DecLds {
+  static constexpr int kRow = D * 2, kTile = KB * kRow;    // bytes of a row, of the keys or values of a stage
+  static constexpr int kPieces = D / 8, kRowsPerLoad = 1024 / kRow;
+  static constexpr int kOffV = NS * kTile;
+  static constexpr int kOffKey = 2 * NS * kTile;           // position or document of each key
+  static constexpr int kOffFlag = kOffKey + NS * KB * 4;   // tile whose values are not all finite
   static constexpr int kBytes = kOffFlag + 16;
+  // Piece c of row r lies at c ^ swz(r).  K: 16 lanes that read one piece each of 16 neighbouring rows meet all 16 groups of 4 banks; V: the 4 rows x 64
+  // bytes of 32 lanes of a transposing read tile the 64 banks.
+  __device__ static __forceinline__ int swz_k(int r) { return D == 64 ? (r / 2) % 8 : r % 16; }
+  __device__ static __forceinline__ int swz_v(int r) { return D == 64 ? (r / 2) % 2 * 4 : r % 4 * 4; }
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -55,18 +62,34 @@ __device__ __forceinline__ float tanh_either(float u) {
 // Either half of a dword an infinity or NaN of bfloat16
 __device__ __forceinline__ bool bf16_odd(uint32_t x) { return ((x & 0x7f80u) == 0x7f80u) | ((x & 0x7f800000u) == 0x7f800000u); }
 
-template <int D, int KB, int KS, int RB, bool TREE>
-__global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
-  constexpr int RG = 4 / KS, kStages = KS == 1 ? 2 : 1, TB = D / 32;
+// Order of the N operands of a product that come from LDS, READS reads and MF matrix instructions each: four operands are asked for ahead of the
+// instruction that takes them.  (Left to itself the compiler asks for one and waits for it.)
+template <int N, int READS, int MF> __device__ __forceinline__ void keep_ahead() {
+  constexpr int kAhead = N < 4 ? N : 4;
+  __builtin_amdgcn_sched_group_barrier(0x100, kAhead * READS, 0);
+#pragma unroll
+  for (int i = 0; i < N - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, MF, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x8, kAhead * MF, 0);
+}
+
+// `Q` is a.Q once more: a pointer that is declared not to alias is what keeps the compiler from waiting for every load into LDS before a transposing read.
+template <int D, int KB, int KS, int RB, int NS, bool TREE>
+__device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __restrict__ Q, int row_blocks, int splits, int chunk) {
+  constexpr int RG = 4 / KS, TB = D / 32;
   constexpr int kRows = RG * RB * 32;                      // per workgroup
   constexpr int NSB = KB / KS / 32;                        // 32-key blocks of a tile per wavefront
-  constexpr int kPer = KB * D / 8 / 256;                   // 16-byte pieces per thread and tensor
-  using Lds = DecLds<D, KB, kStages>;
+  using Lds = DecLds<D, KB, NS>;
+  constexpr int kPer = Lds::kTile / 1024 / 4;              // loads per wavefront, tensor and tile
+  static_assert(Lds::kTile % 4096 == 0 && NSB >= 1 && NS >= 2, "whole loads, whole blocks");
   extern __shared__ __align__(16) unsigned char dec_smem[];
-  lds_bf16_t* const Ks = (lds_bf16_t*)dec_smem;
-  lds_bf16_t* const Vs = (lds_bf16_t*)(dec_smem + Lds::kOffV);
+  typedef lds_u8_t lds_byte_t;
   typedef __attribute__((address_space(3))) int lds_int_t;
   typedef __attribute__((address_space(3))) int4v_t lds_int4_t;
+  lds_byte_t* const Ks = (lds_byte_t*)dec_smem;
+  lds_byte_t* const Vs = Ks + Lds::kOffV;
   lds_int_t* const Key = (lds_int_t*)(dec_smem + Lds::kOffKey);
   lds_int_t* const Flag = (lds_int_t*)(dec_smem + Lds::kOffFlag);
   const int tid = threadIdx.x, lane = tid % kWave;
@@ -112,7 +135,7 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
     const int r = r0 + (rg * RB + rb) * 32 + lq;
     const int i = min(r, R - 1) / group, h = g * group + (min(r, R - 1) - i * group);
     token[rb] = i;
-    const bf16_t* q = (const bf16_t*)a.Q + m * a.q_stride_m + ((long)b * a.N + i) * a.q_stride_row + (long)h * a.d;
+    const bf16_t* q = Q + m * a.q_stride_m + ((long)b * a.N + i) * a.q_stride_row + (long)h * a.d;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
       uint4 v = make_uint4(0, 0, 0, 0);
@@ -123,7 +146,7 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
   }
 
   int node_at = 0;                                         // position of node `lane`
-  int blo = 0, bhi = 0, block_end = 0;                     // documents and last key of the workgroup's rows
+  int lo = 0, hi = 0, wlo = 0, whi = 0, block_end = 0;     // documents of the workgroup's rows and of this wavefront's, end of the keys that they see
   if constexpr (TREE) {
     // paths of all nodes at once, a node per lane: each step doubles the ancestors that a path holds
     int par = lane - 1;
@@ -134,10 +157,10 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
     uint64_t all = 1ull << lane;
     for (int step = 1; step < a.N; step *= 2) {
       const int from = max(par, 0);
-      const uint32_t lo = __shfl((uint32_t)all, from, kWave), hi = __shfl((uint32_t)(all >> 32), from, kWave);
+      const uint32_t x = __shfl((uint32_t)all, from, kWave), y = __shfl((uint32_t)(all >> 32), from, kWave);
       const int up = __shfl(par, from, kWave);
       if (par >= 0) {
-        all |= ((uint64_t)hi << 32) | lo;
+        all |= ((uint64_t)y << 32) | x;
         par = up;
       }
     }
@@ -145,13 +168,15 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
     node_at = begin + __popcll(all) - 1;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
-      const uint32_t lo = __shfl((uint32_t)all, token[rb], kWave), hi = __shfl((uint32_t)(all >> 32), token[rb], kWave);
-      path[rb] = ((uint64_t)hi << 32) | lo;
+      const uint32_t x = __shfl((uint32_t)all, token[rb], kWave), y = __shfl((uint32_t)(all >> 32), token[rb], kWave);
+      path[rb] = ((uint64_t)y << 32) | x;
       mine[rb] = begin + __popcll(path[rb]) - 1;
       end[rb] = L;
       docr[rb] = 0;
     }
   } else {
+    wlo = 0x7fffffff;
+    whi = -1;
 #pragma unroll
     for (int rb = 0; rb < RB; ++rb) {
       const int i = token[rb];
@@ -160,47 +185,53 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
       docr[rb] = doc ? doc[i] : 0;
       const bool valid = i < L && docr[rb] >= 0;
       end[rb] = !valid ? 0 : a.causal ? max(i + 1, first) : L;
+      wlo = min(wlo, valid ? docr[rb] : 0x7fffffff);
+      whi = max(whi, valid ? docr[rb] : -1);
     }
-    const int i_lo = r0 / group, i_hi = min(min(r0 + kRows, R) - 1, R - 1) / group;
-    block_end = i_lo >= L ? 0 : a.causal ? min(max(i_hi + 1, first), L) : L;
+    const int i_lo = r0 / group, i_hi = min(r0 + kRows, R) - 1;
+    block_end = i_lo >= L ? 0 : a.causal ? min(max(i_hi / group + 1, first), L) : L;
     if (doc) {
-      blo = 0x7fffffff;
-      bhi = -1;
-      for (int i = i_lo + lane; i <= i_hi && i < L; i += kWave) {
-        const int v = doc[i];
-        if (v >= 0) blo = min(blo, v), bhi = max(bhi, v);
-      }
+      wlo = __builtin_amdgcn_readfirstlane(wave_reduce(wlo, MinIntOp{}));
+      whi = __builtin_amdgcn_readfirstlane(wave_reduce(whi, MaxIntOp{}));
+      if (lane == 0) Key[2 * wave] = wlo, Key[2 * wave + 1] = whi;
+      __syncthreads();
+      lo = wlo;
+      hi = whi;
 #pragma unroll
-      for (int o = 1; o < kWave; o *= 2) {
-        blo = min(blo, __shfl_xor(blo, o, kWave));
-        bhi = max(bhi, __shfl_xor(bhi, o, kWave));
-      }
-      blo = __builtin_amdgcn_readfirstlane(blo);
-      bhi = __builtin_amdgcn_readfirstlane(bhi);
+      for (int w = 0; w < 4; ++w) lo = min(lo, Key[2 * w]), hi = max(hi, Key[2 * w + 1]);
+      lo = __builtin_amdgcn_readfirstlane(lo);
+      hi = __builtin_amdgcn_readfirstlane(hi);
+      __syncthreads();
     }
   }
   // tokens of this wavefront's rows
-  const int w_lo = (r0 + rg * RB * 32) / group, w_hi = min(r0 + (rg + 1) * RB * 32 - 1, R - 1) / group;
+  const int w_lo = (r0 + rg * RB * 32) / group, w_hi = min(r0 + (rg + 1) * RB * 32 - 1, R - 1) / group, block_lo = r0 / group;
 
   // ---- the tiles: first key of each; the tree's own tile is kTreeTile, none left kNoTile
   constexpr int kTreeTile = -1, kNoTile = -2;
   const int tile_end = TREE ? min(L, (split + 1) * chunk) : block_end;
-  uint32_t win_any = 0, win_all = 0;                       // of 16 tiles from win_at on: which hold a document of the rows, nothing but their only one
+  // Documents of 16 tiles from win_at on: tiles that hold one of the workgroup's, nothing but its only one; the same for this wavefront.
+  uint32_t win_any = 0, win_all = 0, win_mine = 0, win_only = 0;
   int win_at = -(16 * KB);
   auto look = [&](int j0) {
     win_at = j0;
-    win_any = win_all = 0;
+    win_any = win_all = win_mine = win_only = 0;
 #pragma unroll 4
     for (int t = 0; t < 16; ++t) {
-      bool any = false, all = true;
+      uint64_t any = 0, all = ~0ull, own = 0, only = ~0ull;
 #pragma unroll
-      for (int u = 0; u < KB / kWave; ++u) {
-        const int j = j0 + t * KB + u * kWave + lane, v = doc[min(j, L - 1)];
-        any |= (j < L) & (v >= blo) & (v <= bhi);
-        all &= (j < L) & (v == blo);
+      for (int u = 0; u < (KB + kWave - 1) / kWave; ++u) {
+        const int k = u * kWave + lane, j = j0 + t * KB + k, v = doc[min(j, L - 1)];
+        const bool in = (j < L) & (k < KB);
+        any |= __ballot(in & (v >= lo) & (v <= hi));
+        all &= __ballot((in & (v == lo)) | (k >= KB));
+        own |= __ballot(in & (v >= wlo) & (v <= whi));
+        only &= __ballot((in & (v == wlo)) | (k >= KB));
       }
-      win_any |= (__any(any) ? 1u : 0u) << t;
-      win_all |= (__all(all) && blo == bhi ? 1u : 0u) << t;
+      win_any |= (any ? 1u : 0u) << t;
+      win_all |= (all == ~0ull && lo == hi ? 1u : 0u) << t;
+      win_mine |= (own ? 1u : 0u) << t;
+      win_only |= (only == ~0ull && wlo == whi ? 1u : 0u) << t;
     }
   };
   auto seek = [&](int j0) -> int {                         // the tile at j0 or the next one that is wanted
@@ -218,48 +249,46 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
     }
     return j0 < tile_end ? j0 : kNoTile;
   };
-  auto after = [&](int j0) -> int { return j0 == kTreeTile ? kNoTile : seek(j0 + KB); };
-  // whether any row of the workgroup leaves out a key of the tile
-  auto whole = [&](int j0, int i_lo) -> bool {
-    if (j0 == kTreeTile || j0 + KB > L) return false;
-    if (TREE) return true;
-    if (a.causal && j0 + KB > i_lo + 1 && j0 + KB > first) return false;
-    return !doc || ((win_all >> ((j0 - win_at) / KB)) & 1);
+  constexpr int kRowsLeaveOut = 1, kMineLeaveOut = 2, kNoneMine = 4;      // some row of the workgroup, some of this wavefront, all of this wavefront
+  auto look_over = [&](int j0) -> int {
+    if (j0 == kNoTile) return 0;
+    if (j0 == kTreeTile || j0 + KB > L) return kRowsLeaveOut | kMineLeaveOut;
+    if (TREE) return 0;
+    int what = 0;
+    if (a.causal && j0 + KB > first) {
+      what |= (j0 + KB > block_lo + 1 ? kRowsLeaveOut : 0) | (j0 + KB > w_lo + 1 ? kMineLeaveOut : 0);
+      if (j0 > w_hi && j0 >= first) what |= kNoneMine;
+    }
+    if (doc) {
+      const int t = (j0 - win_at) / KB;
+      what |= ((win_all >> t) & 1 ? 0 : kRowsLeaveOut) | ((win_only >> t) & 1 ? 0 : kMineLeaveOut) | ((win_mine >> t) & 1 ? 0 : kNoneMine);
+    }
+    return what;
   };
 
-  uint4 kreg[kPer], vreg[kPer];
+  // A lane's place in the loads: its row among those of the load and the piece of it that lands in the lane's 16 bytes (the same one in every load, whose
+  // first rows are a multiple of 16 apart from the wavefront's first ones)
+  const int my_row = wave * Lds::kRowsPerLoad + lane / Lds::kPieces;
+  const int fk = (lane % Lds::kPieces ^ Lds::swz_k(my_row)) * 8, fv = (lane % Lds::kPieces ^ Lds::swz_v(my_row)) * 8;
   int key_reg = 0;
-  const int my_key = tid / (D / 8), my_f = tid % (D / 8) * 8;             // first piece of this thread: the others are 256 / (D / 8) keys apart
-  auto fetch = [&](int j0) {
+  auto issue = [&](int j0, int stage) {
     const bool own_tile = TREE && j0 == kTreeTile;
     const int base = own_tile ? 0 : j0, limit = (own_tile ? a.N : L) - base;
     const long st = own_tile ? a.kv_stride_row : stride;
     const auto rk = rows_from((own_tile ? Kp : Kh) + base * st), rv = rows_from((own_tile ? Vp : Vh) + base * st);
-    const unsigned row = (unsigned)(st * 2), from = my_key * row + my_f * 2;
-#pragma unroll
-    for (int t = 0; t < kPer; ++t) {
-      const bool in = my_key + t * (2048 / D) < limit && my_f < a.d;
-      const unsigned off = in ? from + t * (2048 / D) * row : kDecOob;
-      kreg[t] = rows_load16(rk, off);
-      vreg[t] = rows_load16(rv, off);
-    }
+    const unsigned row = (unsigned)(st * 2), from = my_row * row;
     if (keyed && tid < KB) {
-      const int key = base + tid, there = min(tid, limit - 1) + base;
-      key_reg = TREE ? (own_tile ? node_at : a.pos ? a.pos[head * a.C + there] : key) : doc[there];
+      const int there = base + min(tid, limit - 1);
+      key_reg = TREE ? (own_tile ? node_at : a.pos ? a.pos[head * a.C + there] : there) : doc[there];
       if (!TREE && tid >= limit) key_reg = -1;
     }
-  };
-  auto commit = [&](int stage, bool check, int number) {
-    if (keyed && tid < KB) Key[stage * KB + tid] = key_reg;
-    bool odd = false;
 #pragma unroll
     for (int t = 0; t < kPer; ++t) {
-      const int c = tid + t * 256, key = c / (D / 8), f = c % (D / 8) * 8;
-      lds_store16(Ks + (stage * KB + key) * Lds::kKPitch + f, kreg[t]);
-      lds_store16(Vs + (stage * KB + key) * Lds::kVPitch + f, vreg[t]);
-      if (check) odd |= bf16_odd(vreg[t].x) | bf16_odd(vreg[t].y) | bf16_odd(vreg[t].z) | bf16_odd(vreg[t].w);
+      const bool in = my_row + t * 4 * Lds::kRowsPerLoad < limit;
+      const unsigned at = from + t * 4 * Lds::kRowsPerLoad * row;
+      load_to_lds(rk, Ks + stage * Lds::kTile + (t * 4 + wave) * 1024, (in & (fk < a.d)) ? at + fk * 2 : kDecOob);
+      load_to_lds(rv, Vs + stage * Lds::kTile + (t * 4 + wave) * 1024, (in & (fv < a.d)) ? at + fv * 2 : kDecOob);
     }
-    if (check && odd) Flag[stage] = number;
   };
 
   f32x16_t o_acc[RB][TB];
@@ -280,31 +309,57 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
   const float cap_small = fabsf(to_u) > 1e-4f && fabsf(to_u) < 1e4f ? kTanhSeries / fabsf(to_u) : 0.f;      // powers of others leave float32
   const bool raw = !capped_scores && !biased && sc > 0.f;  // scale and maximum enter the exponent in one fma
 
-  if (tid < kStages) Flag[tid] = 0;
-  int tile = seek(TREE ? split * chunk : 0), number = 1;
-  const int block_lo = r0 / group;
-  bool tile_whole = false;
-  if (tile != kNoTile) {
-    tile_whole = whole(tile, block_lo);
-    fetch(tile);
-    __syncthreads();                                       // Flag is clear
-    commit(0, !tile_whole, number);
+  // ---- NS - 1 tiles are on their way while one is worked on
+  int tiles[NS - 1], what[NS - 1];
+#pragma unroll
+  for (int i = 0; i < NS - 1; ++i) {
+    tiles[i] = i == 0 ? seek(TREE ? split * chunk : 0) : tiles[i - 1] < 0 ? kNoTile : seek(tiles[i - 1] + KB);
+    what[i] = look_over(tiles[i]);
+    if (tiles[i] == kNoTile) continue;
+    issue(tiles[i], i);
+    if (keyed && tid < KB) Key[i * KB + tid] = key_reg;
   }
-  __syncthreads();
-  while (tile != kNoTile) {
-    const int cur = kStages == 2 ? (number - 1) & 1 : 0;
-    const bool was_whole = tile_whole;
-    // masks of this tile are settled before the window of documents moves on
-    const bool mask = TREE ? !was_whole : !whole(tile, w_lo);
-    const int next = after(tile);
-    if (next != kNoTile) {
-      tile_whole = whole(next, block_lo);
-      fetch(next);
+  int cur = 0, number = 1;
+  if (tid == 0) *Flag = 0;
+  while (tiles[0] != kNoTile) {
+    const int tile = tiles[0], seen = what[0];
+    // this tile's loads have landed, and everyone is done with the stage that the next ones go to
+    if (NS > 2 && tiles[NS - 2] != kNoTile) {
+      wait_lgkmcnt0();
+      wait_vmcnt<(NS - 2) * 2 * kPer>();
+    } else {
+      wait_lgkmcnt0();
+      wait_vmcnt<0>();
     }
-    const bool skip = !TREE && a.causal && tile > w_hi && tile >= first;          // no row of this wavefront sees the tile
-    const bool odd_tile = !was_whole && Flag[cur] == number;                      // uniform over the workgroup
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int i = 0; i + 1 < NS - 1; ++i) tiles[i] = tiles[i + 1], what[i] = what[i + 1];
+    const int last = NS > 2 ? tiles[NS - 2] : tile, fresh = cur == 0 ? NS - 1 : cur - 1;
+    const int next = last < 0 ? kNoTile : seek(last + KB);
+    tiles[NS - 2] = next;
+    what[NS - 2] = look_over(next);
+    if (next != kNoTile) issue(next, fresh);
+
+    const bool mask = seen & kMineLeaveOut;
+    bool odd_tile = false;
+    if (seen & kRowsLeaveOut) {                            // uniform over the workgroup
+      bool odd = false;
+#pragma unroll
+      for (int t = 0; t < kPer; ++t) {
+        const u32x4_t v = *(const lds_u32x4_t*)(Vs + cur * Lds::kTile + (t * 4 + wave) * 1024 + lane * 16);
+        odd |= bf16_odd(v.x) | bf16_odd(v.y) | bf16_odd(v.z) | bf16_odd(v.w);
+      }
+      if (odd) *Flag = number;
+      wait_lgkmcnt0();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      odd_tile = *Flag == number;
+    }
+    const bool skip = seen & kNoneMine;                    // no row of this wavefront sees the tile
     if (!skip || odd_tile) {
-      const lds_bf16_t* Kc = Ks + (cur * KB + key0) * Lds::kKPitch;
+      const lds_byte_t* Kc = Ks + cur * Lds::kTile + key0 * Lds::kRow;
+      const lds_byte_t* Vc = Vs + cur * Lds::kTile + key0 * Lds::kRow;
       const lds_int_t* Kk = Key + cur * KB + key0;
       const int base = (tile == kTreeTile ? 0 : tile) + key0 + 4 * half;          // register r of block sb is key base + 32 sb + 8 (r / 4) + r % 4
       f32x16_t s[RB][NSB];
@@ -318,10 +373,12 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
       for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
         for (int sb = 0; sb < NSB; ++sb) {
-          const bf16x8_t kf = *(const lds_bf16x8_t*)(Kc + (sb * 32 + lq) * Lds::kKPitch + kk * 16 + half * 8);
+          // rows 32 apart are permuted alike
+          const bf16x8_t kf = *(const lds_bf16x8_t*)(Kc + (sb * 32 + lq) * Lds::kRow + ((kk * 2 + half) ^ Lds::swz_k(lq)) * 16);
 #pragma unroll
           for (int rb = 0; rb < RB; ++rb) s[rb][sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[rb][kk], s[rb][sb], 0, 0, 0);
         }
+      keep_ahead<NSB * D / 16, 1, RB>();
       bf16x8_t pf[RB][NSB][2];
 #pragma unroll
       for (int rb = 0; rb < RB; ++rb) {
@@ -351,6 +408,7 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
 #pragma unroll
             for (int r = 0; r < 16; ++r) s[rb][sb][r] *= sc;
         }
+        float shift = 0.f;
         if (biased) {
           if (TREE && (a.pos || tile == kTreeTile)) {
 #pragma unroll
@@ -361,6 +419,12 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
 #pragma unroll
                 for (int e = 0; e < 4; ++e) s[rb][sb][4 * r4 + e] = fmaf(-slope[rb], fabsf((float)(mine[rb] - at[e])), s[rb][sb][4 * r4 + e]);
               }
+          } else if (!TREE && a.causal && tile >= first) {  // no key that a row sees lies behind it: -slope (away - c), of which slope away is the same for
+            shift = slope[rb] * (float)(mine[rb] - base);  // the lane's whole tile and joins the maximum
+#pragma unroll
+            for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) s[rb][sb][r] = fmaf(slope[rb], (float)(32 * sb + 8 * (r / 4) + r % 4), s[rb][sb][r]);
           } else {
             const float away = (float)(mine[rb] - base);
 #pragma unroll
@@ -402,10 +466,9 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
         for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
           for (int r = 0; r < 16; ++r) top = fmaxf(top, s[rb][sb][r]);
-        top = across_halves(top, MaxOp{});
-        if (raw) top *= sc;
-        const float mnew = fmaxf(mrun[rb], top);
-        float esc = raw ? sc : 1.0f;                       // exponent = s * esc - mnew
+        top = across_halves(raw ? top * sc : top - shift, MaxOp{});               // the halves' keys are 4 apart, and so are their shifts
+        const float mnew = fmaxf(mrun[rb], top), less = mnew + shift;
+        float esc = raw ? sc : 1.0f;                       // exponent = s * esc - less
         if (raw && __any(fabsf(mnew) > 0x1p29f && mnew != kLowestScore)) {        // the rounded maximum may lie far beside such a score: scale first
 #pragma unroll
           for (int sb = 0; sb < NSB; ++sb)
@@ -423,8 +486,8 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
             uint32_t w[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float p0 = __builtin_amdgcn_exp2f(fmaf(s[rb][sb][8 * st + 2 * e], esc, -mnew));
-              const float p1 = __builtin_amdgcn_exp2f(fmaf(s[rb][sb][8 * st + 2 * e + 1], esc, -mnew));
+              const float p0 = __builtin_amdgcn_exp2f(fmaf(s[rb][sb][8 * st + 2 * e], esc, -less));
+              const float p1 = __builtin_amdgcn_exp2f(fmaf(s[rb][sb][8 * st + 2 * e + 1], esc, -less));
               w[e] = pack_bf16x2(p0, p1);
               sum += p0 + p1;                              // float32 sum of the unrounded weights
             }
@@ -439,13 +502,12 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
         }
       }
 
-      const lds_bf16_t* Vc = Vs + (cur * KB + key0) * Lds::kVPitch;
       if (odd_tile) {
         // which keys hold such a value: a key per lane
         bool odd = false;
         if (lane < KB / KS) {
 #pragma unroll 1
-          for (int f = 0; f < a.d; ++f) odd |= (Vc[lane * Lds::kVPitch + f] & 0x7f80) == 0x7f80;
+          for (int f = 0; f < D; f += 2) odd |= bf16_odd(*(const __attribute__((address_space(3))) uint32_t*)(Vc + lane * Lds::kRow + f * 2));
         }
         const uint64_t odd_keys = __ballot(odd);
 #pragma unroll
@@ -472,25 +534,30 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
           for (uint64_t left = odd_keys; left; left &= left - 1) {
             const int k = __builtin_ctzll(left);
             const bool takes = (under >> k) & 1;
-            const lds_bf16_t* vr = Vc + k * Lds::kVPitch + 4 * half;
+            const lds_byte_t* vr = Vc + k * Lds::kRow + 8 * half;
+            const int swz = Lds::swz_v(k);
 #pragma unroll
             for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
               for (int r = 0; r < 16; ++r) {
-                const uint32_t v = vr[tb * 32 + 8 * (r / 4) + r % 4];
+                const uint32_t v = *(const lds_bf16_t*)(vr + ((tb * 4 + r / 4) ^ swz) * 16 + r % 4 * 2);
                 o_acc[rb][tb][r] += takes & ((v & 0x7f80) == 0x7f80) ? __uint_as_float(v << 16) : 0.f;
               }
           }
         }
-        __syncthreads();
+        wait_lgkmcnt0();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
 #pragma unroll
         for (int t = 0; t < kPer; ++t) {                   // the product runs on the others
-          lds_bf16_t* const v = Vs + (cur * KB + my_key + t * (2048 / D)) * Lds::kVPitch + my_f;
+          lds_bf16_t* const v = (lds_bf16_t*)(Vs + cur * Lds::kTile + (t * 4 + wave) * 1024 + lane * 16);
 #pragma unroll 1
           for (int e = 0; e < 8; ++e)
             if ((v[e] & 0x7f80) == 0x7f80) v[e] = 0;
         }
-        __syncthreads();
+        wait_lgkmcnt0();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
       }
       // O^T += V^T P^T.  In a 16-lane group, lane i points at key row i / 4, features 4 (i % 4) .. + 3 of a 4 x 16 block and receives the
       // 4 keys of feature i; slots 0-3 of step (sb, st) are keys 32 sb + 16 st + 4 half + 0..3, slots 4-7 the same + 8.
@@ -500,21 +567,22 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
         for (int st = 0; st < 2; ++st)
 #pragma unroll
           for (int tb = 0; tb < TB; ++tb) {
-            const lds_bf16_t* vp = Vc + (sb * 32 + st * 16 + 4 * half + l16 / 4) * Lds::kVPitch + tb * 32 + ((lane / 16) % 2) * 16 + (l16 % 4) * 4;
-            const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)vp);
-            const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vp + 8 * Lds::kVPitch));
-            const s16x8_t both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            const int k = sb * 32 + st * 16 + 4 * half + l16 / 4, piece = tb * 4 + lane / 16 % 2 * 2 + l16 % 4 / 2;
+            const lds_byte_t* vp = Vc + k * Lds::kRow + (piece ^ Lds::swz_v(l16 / 4)) * 16 + l16 % 2 * 8;       // rows 4 apart are permuted alike
+            const s16x4_t lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)vp);
+            const s16x4_t hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vp + 8 * Lds::kRow));
+            const s16x8_t both = __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7);
 #pragma unroll
             for (int rb = 0; rb < RB; ++rb)
               o_acc[rb][tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, both), pf[rb][sb][st], o_acc[rb][tb], 0, 0, 0);
           }
+      keep_ahead<NSB * 2 * TB, 2, RB>();
     }
-    if (kStages == 1) __syncthreads();                     // the stage is free
+    if (next != kNoTile && keyed && tid < KB) Key[fresh * KB + tid] = key_reg;
+    cur = cur + 1 == NS ? 0 : cur + 1;
     ++number;
-    if (next != kNoTile) commit(kStages == 2 ? cur ^ 1 : 0, !tile_whole, number);
-    tile = next;
-    __syncthreads();
   }
+  __syncthreads();                                         // the stages are free for the shares
 
   // ---- the result: element r of block tb is feature 32 tb + 8 (r / 4) + 4 half + r % 4
   const bool partial = TREE && parts > 1;
@@ -535,7 +603,7 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
       lds_f32_t* const buf = (lds_f32_t*)dec_smem;
       lds_f32_t* const max_of = buf + 256 * 16 * TB;
       lds_f32_t* const sum_of = max_of + 256;
-      static_assert(256 * 16 * TB * 4 + 2 * 256 * 4 <= Lds::kBytes, "shares fit the stage");
+      static_assert(RB > 1 || 256 * 16 * TB * 4 + 2 * 256 * 4 <= Lds::kBytes, "shares fit the stages");
 #pragma unroll
       for (int u = 0; u < 4 * TB; ++u) *(lds_f32x4_t*)(buf + (u * 256 + tid) * 4) = f32x4v_t{o_acc[rb][u / 4][4 * (u % 4)], o_acc[rb][u / 4][4 * (u % 4) + 1], o_acc[rb][u / 4][4 * (u % 4) + 2], o_acc[rb][u / 4][4 * (u % 4) + 3]};
       max_of[tid] = mtot;
@@ -584,6 +652,11 @@ __global__ __launch_bounds__(256, 2) void decoder_tiles_kernel(DecArgs a, int ro
     }
     if (TREE && a.lse && quad0 == 0 && half == 0) a.lse[(mb * a.N + token[rb]) * a.heads + h] = none ? -INFINITY : (mtot + __builtin_amdgcn_logf(ltot)) * kLn2;
   }
+}
+
+template <int D, int KB, int KS, int RB, int NS, bool TREE>
+__global__ __launch_bounds__(256, D == 64 && RB == 1 ? 3 : 2) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
+  decoder_tiles<D, KB, KS, RB, NS, TREE>(a, (const bf16_t*)a.Q, row_blocks, splits, chunk);
 }
 
 // Sums of the chunks of one row: D / 4 lanes hold its features, 4 each, and SHARE such groups of lanes take every SHARE-th chunk.  Maxima and sums in log2

@@ -101,6 +101,19 @@ template <class Op> __device__ __forceinline__ float wave_reduce(float v, Op&& o
   v = op(v, dpp<kQuadXor2>(v));
   return op(v, dpp<kQuadXor1>(v));
 }
+template <int CTRL> __device__ __forceinline__ int dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, 0xf, 0xf, true); }
+template <class Op> __device__ __forceinline__ int wave_reduce(int v, Op&& op) {
+  const auto h = __builtin_amdgcn_permlane32_swap((unsigned)v, (unsigned)v, false, false);
+  v = op((int)h[0], (int)h[1]);
+  const auto r = __builtin_amdgcn_permlane16_swap((unsigned)v, (unsigned)v, false, false);
+  v = op((int)r[0], (int)r[1]);
+  v = op(v, dpp<kRowRor8>(v));
+  v = op(v, dpp<kRowRor4>(v));
+  v = op(v, dpp<kQuadXor2>(v));
+  return op(v, dpp<kQuadXor1>(v));
+}
+struct MinIntOp { __device__ __forceinline__ int operator()(int a, int b) const { return min(a, b); } };
+struct MaxIntOp { __device__ __forceinline__ int operator()(int a, int b) const { return max(a, b); } };
 struct AddOp { __device__ __forceinline__ float operator()(float a, float b) const { return a + b; } };
 struct MaxOp { __device__ __forceinline__ float operator()(float a, float b) const { return fmaxf(a, b); } };
 __device__ __forceinline__ float wave_sum(float v) { return wave_reduce(v, AddOp{}); }
