@@ -38,6 +38,14 @@ nf_status tree(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   return R <= 16 ? go<T, D, 1, 4, true>(a, splits, chunk, s) : R <= 32 ? go<T, D, 1, 2, true>(a, splits, chunk, s) : go<T, D, 1, 1, true>(a, splits, chunk, s);
 }
 
+// From 12 steps of keys on the four wavefronts of a workgroup share the keys of 16 rows, below that they take 16 rows each: by the length alone, so that a
+// model's bits do not depend on what is merged with it (float32, 12 heads of 64, us, rows each / keys shared: 8 models of 128 tokens 12.4 / 11.3, 32 of 128 24.7 /
+// 33.1, 12 of 300 38.5 / 42.2, 8 of 512 72.7 / 61.7, 2 of 1024 95.7 / 52.6, 8 of 1024 207 / 181; 16 heads of 128, 4 of 256 51.3 / 35.8, 4 of 1024 338 / 251).
+template <typename T, int D>
+nf_status prompt(const DecArgs& a, hipStream_t s) {
+  return a.N >= 12 * 16 * StreamShape<T, D>::NK ? go<T, D, 1, 4, false>(a, 1, 0, s) : go<T, D, 1, 1, false>(a, 1, 0, s);
+}
+
 template <typename T, int D>
 nf_status weigh(const WeighArgs& a, hipStream_t s) {
   constexpr int kKeys = 4 * weigh_keys<T, D>();            // of a workgroup and turn
@@ -53,8 +61,8 @@ nf_status weigh(const WeighArgs& a, hipStream_t s) {
 }  // namespace
 
 nf_status launch_prompt_stream(const DecArgs& a, nf_dtype dt, hipStream_t s) {
-  if (dt == NF_F32) return a.d <= 64 ? go<float, 64, 1, 1, false>(a, 1, 0, s) : a.d <= 128 ? go<float, 128, 1, 1, false>(a, 1, 0, s) : go<float, 256, 1, 1, false>(a, 1, 0, s);
-  return go<bf16_t, 256, 1, 1, false>(a, 1, 0, s);         // smaller heads are decoder_tiles.h's
+  if (dt == NF_F32) return a.d <= 64 ? prompt<float, 64>(a, s) : a.d <= 128 ? prompt<float, 128>(a, s) : prompt<float, 256>(a, s);
+  return prompt<bf16_t, 256>(a, s);                        // smaller heads are decoder_tiles.h's
 }
 
 nf_status launch_tree_stream(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s) {
