@@ -98,7 +98,7 @@ nf_status netfuse_attention_prompt(const void* Q, const void* K, const void* V, 
   a.M = M; a.B = B; a.N = S; a.heads = heads; a.kv = kv_heads; a.d = d; a.causal = causal != 0;
   a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.kv_stride_m = kv_stride_m; a.kv_stride_row = kv_stride_row;
   a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
-  if (pieces_ok(a, dt)) return dt == NF_BF16 && d <= 128 ? launch_prompt_tiles(a, (hipStream_t)stream) : launch_prompt_stream(a, dt, (hipStream_t)stream);
+  if (pieces_ok(a, dt)) return dt == NF_BF16 ? launch_prompt_tiles(a, (hipStream_t)stream) : launch_prompt_stream(a, (hipStream_t)stream);
   return launch_rows<false>(a, dt, (hipStream_t)stream);
 }
 
@@ -140,7 +140,7 @@ nf_status netfuse_attention_tree(const void* Q, const void* K, const void* V, co
   a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
   if (pieces_ok(a, dt)) {
     const int rows = T * (heads / kv_heads), chunk = tree_chunk(rows), splits = (int)(((long long)C + chunk - 1) / chunk);
-    const nf_status st = dt == NF_BF16 && d <= 128 && rows > (d <= 64 ? 32 : 64) ? launch_tree_tiles(a, chunk, splits, (hipStream_t)stream) : launch_tree_stream(a, chunk, splits, dt, (hipStream_t)stream);
+    const nf_status st = dt == NF_BF16 && rows > (d <= 64 || d > 128 ? 32 : 64) ? launch_tree_tiles(a, chunk, splits, (hipStream_t)stream) : launch_tree_stream(a, chunk, splits, dt, (hipStream_t)stream);
     return st != NF_OK || splits == 1 ? st : launch_tree_join(a, chunk, splits, dt, (hipStream_t)stream);
   }
   return launch_rows<true>(a, dt, (hipStream_t)stream);

@@ -15,11 +15,11 @@ inline int tree_chunk(int rows) {
 inline int tree_features(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
 struct WeighArgs;
-// decoder_tiles.h: bfloat16, d <= 128
+// decoder_tiles.h: bfloat16
 nf_status launch_prompt_tiles(const DecArgs& a, hipStream_t s);
 nf_status launch_tree_tiles(const DecArgs& a, int chunk, int splits, hipStream_t s);
-// decoder_stream.h: either type, d <= 256
-nf_status launch_prompt_stream(const DecArgs& a, nf_dtype dt, hipStream_t s);
+// decoder_stream.h: float32 prompts, trees of either type
+nf_status launch_prompt_stream(const DecArgs& a, hipStream_t s);
 nf_status launch_tree_stream(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s);
 nf_status launch_tree_join(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s);
 nf_status launch_weigh_tiles(const WeighArgs& a, nf_dtype dt, hipStream_t s);

@@ -60,9 +60,8 @@ nf_status weigh(const WeighArgs& a, hipStream_t s) {
 
 }  // namespace
 
-nf_status launch_prompt_stream(const DecArgs& a, nf_dtype dt, hipStream_t s) {
-  if (dt == NF_F32) return a.d <= 64 ? prompt<float, 64>(a, s) : a.d <= 128 ? prompt<float, 128>(a, s) : prompt<float, 256>(a, s);
-  return prompt<bf16_t, 256>(a, s);                        // smaller heads are decoder_tiles.h's
+nf_status launch_prompt_stream(const DecArgs& a, hipStream_t s) {
+  return a.d <= 64 ? prompt<float, 64>(a, s) : a.d <= 128 ? prompt<float, 128>(a, s) : prompt<float, 256>(a, s);
 }
 
 nf_status launch_tree_stream(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s) {

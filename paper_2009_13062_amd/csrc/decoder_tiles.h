@@ -33,9 +33,10 @@ template <int D, int KB, int NS> struct DecLds {
   static constexpr int kOffKey = 2 * NS * kTile;           // position or document of each key
   static constexpr int kOffFlag = kOffKey + NS * KB * 4;   // tile whose values are not all finite
   static constexpr int kBytes = kOffFlag + 16;
-  // Piece c of row r lies at c ^ swz(r).  K: 16 lanes that read one piece each of 16 neighbouring rows meet all 16 groups of 4 banks; V: the 4 rows x 64
+  // Piece c of row r lies at c ^ swz(r), the same for rows that a thread's loads are apart.  K: 16 lanes that read one piece each of 16 neighbouring rows meet
+  // all 16 groups of 4 banks (8 of them, twice, for D = 256); V: the 4 rows x 64
   // bytes of 32 lanes of a transposing read tile the 64 banks.
-  __device__ static __forceinline__ int swz_k(int r) { return D == 64 ? (r / 2) % 8 : r % 16; }
+  __device__ static __forceinline__ int swz_k(int r) { return D == 64 ? (r / 2) % 8 : D == 128 ? r % 16 : r % 8; }
   __device__ static __forceinline__ int swz_v(int r) { return D == 64 ? (r / 2) % 2 * 4 : r % 4 * 4; }
 };
 
@@ -266,8 +267,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
     return what;
   };
 
-  // A lane's place in the loads: its row among those of the load and the piece of it that lands in the lane's 16 bytes (the same one in every load, whose
-  // first rows are a multiple of 16 apart from the wavefront's first ones)
+  // A lane's place in the loads: its row among those of the load and the piece of it that lands in the lane's 16 bytes (the same one in every load)
   const int my_row = wave * Lds::kRowsPerLoad + lane / Lds::kPieces;
   const int fk = (lane % Lds::kPieces ^ Lds::swz_k(my_row)) * 8, fv = (lane % Lds::kPieces ^ Lds::swz_v(my_row)) * 8;
   int key_reg = 0;
@@ -655,7 +655,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
 }
 
 template <int D, int KB, int KS, int RB, int NS, bool TREE>
-__global__ __launch_bounds__(256, D == 64 && RB == 1 ? 3 : 2) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
+__global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
   decoder_tiles<D, KB, KS, RB, NS, TREE>(a, (const bf16_t*)a.Q, row_blocks, splits, chunk);
 }
 

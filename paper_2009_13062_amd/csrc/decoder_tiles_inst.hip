@@ -28,13 +28,13 @@ nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
 }  // namespace
 
 nf_status launch_prompt_tiles(const DecArgs& a, hipStream_t s) {
-  return a.d <= 64 ? go<64, 64, 1, 1, 2, false>(a, 1, 0, s) : go<128, 64, 1, 1, 2, false>(a, 1, 0, s);
+  return a.d <= 64 ? go<64, 64, 1, 1, 2, false>(a, 1, 0, s) : a.d <= 128 ? go<128, 64, 1, 1, 2, false>(a, 1, 0, s) : go<256, 64, 1, 1, 2, false>(a, 1, 0, s);
 }
 
 nf_status launch_tree_tiles(const DecArgs& a, int chunk, int splits, hipStream_t s) {
   const int R = a.N * (a.heads / a.kv);
   if (a.d <= 64) return R <= 64 ? go<64, 128, 2, 1, 2, true>(a, splits, chunk, s) : go<64, 64, 1, 1, 2, true>(a, splits, chunk, s);
-  return go<128, 64, 1, 1, 2, true>(a, splits, chunk, s);
+  return a.d <= 128 ? go<128, 64, 1, 1, 2, true>(a, splits, chunk, s) : go<256, 64, 1, 1, 2, true>(a, splits, chunk, s);
 }
 
 }  // namespace nf
