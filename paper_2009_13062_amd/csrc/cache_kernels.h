@@ -53,15 +53,22 @@ __device__ __forceinline__ uint32_t weight_order(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
+// Inclusive sum over a wavefront: within rows of 16 lanes, then each row's last lane into the next row, then lane 31 into the upper half.
+template <int CTRL, int ROWS> __device__ __forceinline__ int add_from(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true); }
+__device__ __forceinline__ int wave_scan(int x) {
+  constexpr int kRowShr = 0x110, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
+  x = add_from<kRowShr + 1, 0xf>(x);
+  x = add_from<kRowShr + 2, 0xf>(x);
+  x = add_from<kRowShr + 4, 0xf>(x);
+  x = add_from<kRowShr + 8, 0xf>(x);
+  x = add_from<kRowBcast15, 0xa>(x);
+  return add_from<kRowBcast31, 0xc>(x);
+}
+
 // Exclusive sum over the NT threads of a workgroup, `total` their sum.  Every thread has to come here; wave_sums must not be in use by another sum.
 template <int NT> __device__ __forceinline__ int block_sum(int v, int* wave_sums, int& total) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  int x = v;
-#pragma unroll
-  for (int o = 1; o < kWave; o *= 2) {
-    const int y = __shfl_up(x, o, kWave);
-    if (lane >= o) x += y;
-  }
+  const int x = wave_scan(v);
   if (lane == kWave - 1) wave_sums[wave] = x;
   __syncthreads();
   int before = 0;
@@ -194,11 +201,11 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
 }
 
 // The same for caches of up to NT E slots, which are read once: a thread holds the weights' order of E slots in a row, turned round through LDS, and
-// E bits for what may leave.  The lists are those of the kernel above.
+// E bits for what may leave.  The lists are those of the kernel above; with MOVE the workgroup moves its rows itself, U at a time, and writes none.
 template <int NT, int E> struct EvictLds {
   static constexpr int kOffGuard = NT * E * 4, kOffHist = kOffGuard + NT * E / 8, kOffSums = kOffHist + 3 * 2048 * 4, kBytes = kOffSums + 7 * 16 * 4;
 };
-template <int NT, int E>
+template <int NT, int E, bool MOVE, typename U>
 __global__ __launch_bounds__(NT) void evict_select_held_kernel(EvictArgs a) {
   using Lds = EvictLds<NT, E>;
   static_assert(E >= 4 && E <= 32 && (E & (E - 1)) == 0, "whole 16-byte pieces, a bit each");
@@ -236,7 +243,7 @@ __global__ __launch_bounds__(NT) void evict_select_held_kernel(EvictArgs a) {
     }
   }
   if (n == 0) {                                            // uniform
-    if (tid == 0) *count = 0;
+    if (!MOVE && tid == 0) *count = 0;
     return;
   }
   __syncthreads();
@@ -293,11 +300,29 @@ __global__ __launch_bounds__(NT) void evict_select_held_kernel(EvictArgs a) {
   for (; hole_bits; hole_bits &= hole_bits - 1) list[hole++] = j0 + __builtin_ctz(hole_bits);
   for (; mover_bits; mover_bits &= mover_bits - 1) list[mover++] = j0 + __builtin_ctz(mover_bits);
   __syncthreads();
-  for (int i = tid; i < pairs; i += NT) {
-    holes[i] = list[i];
-    movers[i] = list[NT * E / 2 + i];
+  if constexpr (MOVE) {
+    U* const Kh = (U*)a.Kc + head * a.C * a.units;
+    U* const Vh = (U*)a.Vc + head * a.C * a.units;
+#pragma unroll 4
+    for (int c = tid; c < pairs * a.units; c += NT) {
+      const int i = c / a.units, u = c - i * a.units;
+      const long to = (long)list[i] * a.units + u, from = (long)list[NT * E / 2 + i] * a.units + u;
+      const U k = Kh[from], v = Vh[from];
+      Kh[to] = k;
+      Vh[to] = v;
+    }
+    for (int i = tid; i < pairs; i += NT) {
+      const int to = list[i], from = list[NT * E / 2 + i];
+      a.weight_out[head * a.C + to] = w[from];
+      if (pos) a.pos_out[head * a.C + to] = pos[from];
+    }
+  } else {
+    for (int i = tid; i < pairs; i += NT) {
+      holes[i] = list[i];
+      movers[i] = list[NT * E / 2 + i];
+    }
+    if (tid == 0) *count = pairs;
   }
-  if (tid == 0) *count = pairs;
 }
 
 // The pairs of the lists: rows of keys and values, position and weight.  Sources lie at or above the budget, targets below it, each once.

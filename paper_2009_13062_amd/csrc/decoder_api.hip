@@ -60,10 +60,10 @@ nf_status launch_rows(const DecArgs& a, nf_dtype dt, hipStream_t s) {
   return launched();
 }
 
-template <int NT, int E>
+template <int NT, int E, bool MOVE = false, typename U = uint32_t>
 nf_status select_held(const EvictArgs& a, long long heads, hipStream_t s) {
   constexpr int kBytes = EvictLds<NT, E>::kBytes;
-  const auto kernel = evict_select_held_kernel<NT, E>;
+  const auto kernel = evict_select_held_kernel<NT, E, MOVE, U>;
   static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
   if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) != hipSuccess) return NF_ELAUNCH;
@@ -234,6 +234,8 @@ nf_status netfuse_cache_evict(void* Kc, void* Vc, const int* pos, const float* w
   const long long blocks = prod({heads, per_head});
   if (heads > kMaxGrid || blocks > kMaxGrid) return NF_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
+  // Small heads: the workgroup that picks the entries moves them too.
+  if (C <= 1024 && wide && (long long)a.most * a.units <= 4096) return select_held<256, 4, true, uint4>(a, heads, s);
   const nf_status st = C <= 1024 ? select_held<256, 4>(a, heads, s) : C <= 4096 ? select_held<256, 16>(a, heads, s) : C <= 8192 ? select_held<1024, 8>(a, heads, s)
                        : C <= 32768 ? select_held<1024, 32>(a, heads, s) : NF_EUNSUPPORTED;
   if (st == NF_ELAUNCH) return st;
