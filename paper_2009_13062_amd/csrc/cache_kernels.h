@@ -15,10 +15,9 @@ struct AppendArgs {
 // consecutive threads take consecutive pieces of a head's row, on both sides.
 template <typename U>
 __global__ __launch_bounds__(256) void cache_append_kernel(AppendArgs a, int rows, int blocks_per_seq) {
-  const long mb = blockIdx.x / blocks_per_seq;
-  const int i0 = (int)(blockIdx.x % blocks_per_seq) * rows;
-  const int b = (int)(mb % a.B);
-  const long m = mb / a.B;
+  const unsigned umb = blockIdx.x / blocks_per_seq;
+  const long mb = umb, m = umb / a.B;
+  const int i0 = (int)(blockIdx.x % blocks_per_seq) * rows, b = (int)(umb % a.B);
   const int cnt = a.count ? clamp_len(a.count[mb], a.n) : a.n, L = clamp_len(a.len[mb], a.C);
   const int end = min(min(i0 + rows, cnt), a.C - L);       // entries past the capacity are not written
   const int per_row = a.kv * a.units;
@@ -116,7 +115,7 @@ __global__ __launch_bounds__(1024) void evict_select_kernel(EvictArgs a) {
   __shared__ int wave_sums[16];
   __shared__ int found[2];
   const int tid = threadIdx.x;
-  const long head = blockIdx.x, mb = head / a.kv;
+  const long head = blockIdx.x, mb = blockIdx.x / a.kv;
   const int L = clamp_len(a.len[mb], a.C);
   const int keep = min(L, a.budget), n = L - keep;
   const long long bound = (long long)(a.start ? a.start[mb] : L) - a.recent;     // guarded from this position on
@@ -216,7 +215,7 @@ __global__ __launch_bounds__(NT) void evict_select_held_kernel(EvictArgs a) {
   int* const wave_sums = (int*)(evict_smem + Lds::kOffSums);
   int* const found = wave_sums + 6 * 16;
   const int tid = threadIdx.x, lane = tid % kWave;
-  const long head = blockIdx.x, mb = head / a.kv;
+  const long head = blockIdx.x, mb = blockIdx.x / a.kv;
   const int L = clamp_len(a.len[mb], a.C), keep = min(L, a.budget), n = L - keep;
   const long long bound = (long long)(a.start ? a.start[mb] : L) - a.recent;     // guarded from this position on
   const float* w = a.weight + head * a.C;

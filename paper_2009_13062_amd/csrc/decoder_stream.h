@@ -67,11 +67,10 @@ __global__ __launch_bounds__(256, D <= 128 && RT == 1 ? 3 : 2) void decoder_stre
   } else {
     rblock = row_blocks - 1 - (int)(id % row_blocks);      // the longest rows of a head first
   }
-  const long head = id / row_blocks;                       // (m, b, g)
-  const int g = (int)(head % a.kv);
-  const long mb = head / a.kv;
-  const int b = (int)(mb % a.B);
-  const long m = mb / a.B;
+  // (m, b, g): divisions in 32 bits, a long one takes a hundred instructions
+  const unsigned uhead = id / row_blocks, umb = uhead / a.kv;
+  const int g = (int)(uhead % a.kv), b = (int)(umb % a.B);
+  const long head = uhead, mb = umb, m = umb / a.B;
   const int group = a.heads / a.kv, R = a.N * group, r0 = rblock * kRows;
   const int L = TREE ? clamp_len(a.len[mb], a.C) : a.len ? clamp_len(a.len[mb], a.N) : a.N;
   const int parts = TREE ? max(1, (L + chunk - 1) / chunk) : 1;

@@ -75,7 +75,7 @@ nf_status launch_tree_join(const DecArgs& a, int chunk, int splits, nf_dtype dt,
   // up to 8 chunks a row is a few loads of one group of lanes, above that a workgroup's
   const bool shared = splits > 8;
   const long long blocks = shared ? rows : (rows * (features / 4) + 255) / 256;
-  if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
+  if (rows > kMaxGrid) return NF_EUNSUPPORTED;
 #define NF_JOIN(T, D, LOG2)                                                                                                              \
   if (shared) nf_launch((decoder_join_kernel<T, D, LOG2, 1024 / D>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk);         \
   else nf_launch((decoder_join_kernel<T, D, LOG2, 1>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk)

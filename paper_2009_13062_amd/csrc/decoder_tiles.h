@@ -106,11 +106,10 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
   } else {
     rblock = row_blocks - 1 - (int)(id % row_blocks);      // the longest rows of a head first
   }
-  const long head = id / row_blocks;                       // (m, b, g)
-  const int g = (int)(head % a.kv);
-  const long mb = head / a.kv;
-  const int b = (int)(mb % a.B);
-  const long m = mb / a.B;
+  // (m, b, g): divisions in 32 bits, a long one takes a hundred instructions
+  const unsigned uhead = id / row_blocks, umb = uhead / a.kv;
+  const int g = (int)(uhead % a.kv), b = (int)(umb % a.B);
+  const long head = uhead, mb = umb, m = umb / a.B;
   const int group = a.heads / a.kv, R = a.N * group, r0 = rblock * kRows;
   const int L = TREE ? clamp_len(a.len[mb], a.C) : a.len ? clamp_len(a.len[mb], a.N) : a.N;
   const int parts = TREE ? max(1, (L + chunk - 1) / chunk) : 1;           // chunks that this cache fills
@@ -219,6 +218,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
     win_any = win_all = win_mine = win_only = 0;
 #pragma unroll 4
     for (int t = 0; t < 16; ++t) {
+      if (j0 + t * KB >= tile_end) break;                  // uniform
       uint64_t any = 0, all = ~0ull, own = 0, only = ~0ull;
 #pragma unroll
       for (int u = 0; u < (KB + kWave - 1) / kWave; ++u) {
@@ -667,10 +667,11 @@ __global__ __launch_bounds__(256) void decoder_join_kernel(DecArgs a, int splits
   static_assert(SHARE == 1 || SHARE == kGroups, "a group per row, or all of them on one");
   const int lane = threadIdx.x % kLanes, grp = threadIdx.x / kLanes;
   const int group = a.heads / a.kv, R = a.N * group;
-  const long row = (long)blockIdx.x * kRows + (SHARE == 1 ? grp : 0);
-  if (row >= (long)a.M * a.B * a.kv * R) return;
-  const long head = row / R, mb = head / a.kv;
-  const int r = (int)(row % R), i = r / group, h = (int)(head % a.kv) * group + r % group;
+  const unsigned urow = blockIdx.x * (unsigned)kRows + (SHARE == 1 ? grp : 0);  // fewer than 2^31 rows
+  if (urow >= (unsigned)(a.M * a.B * a.kv) * R) return;
+  const unsigned uhead = urow / R, umb = uhead / a.kv;
+  const long row = urow, mb = umb;
+  const int r = (int)(urow % R), i = r / group, h = (int)(uhead % a.kv) * group + r % group;
   const int parts = (clamp_len(a.len[mb], a.C) + chunk - 1) / chunk;
   if (parts <= 1) return;                                  // written already; uniform where groups share a row
   const float* o = a.ws + row * splits * D + lane * 4;

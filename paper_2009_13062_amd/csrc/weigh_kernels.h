@@ -36,12 +36,11 @@ __global__ __launch_bounds__(256) void weigh_tiles_kernel(WeighArgs a, int block
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int g4 = lane / 16, l16 = lane % 16;
-  const long head = blockIdx.x / blocks_per_head;          // (m, b, g)
+  const unsigned uhead = blockIdx.x / blocks_per_head, umb = uhead / a.kv;      // (m, b, g)
   const int first = ((int)(blockIdx.x % blocks_per_head) * 4 * turns + wave) * kKeys;
   if (first >= a.C) return;                                // uniform per wavefront; no barrier below
-  const long mb = head / a.kv;
-  const int g = (int)(head % a.kv), b = (int)(mb % a.B), group = a.heads / a.kv;
-  const long m = mb / a.B;
+  const long head = uhead, mb = umb, m = umb / a.B;
+  const int g = (int)(uhead % a.kv), b = (int)(umb % a.B), group = a.heads / a.kv;
   const int L = clamp_len(a.len[mb], a.C), cnt = a.count ? clamp_len(a.count[mb], a.n) : a.n;
   const int held = min(L + cnt, a.C), rows = cnt * group;
   const float unit = kBf ? kLog2e : 1.f;
