@@ -18,8 +18,8 @@
  *     environment variable.
  *   - `stream` is a hipStream_t passed as void* (NULL = the default stream).  A call validates
  *     its arguments on the host BEFORE touching HIP, enqueues its kernels and returns; it
- *     never synchronises.  Kernels use no atomics and no hidden workspace: results are
- *     deterministic and the calls can be captured into a HIP graph.
+ *     never synchronises.  Kernels use no atomics in device memory and no hidden workspace (two decoder
+ *     calls take one from the caller): results are deterministic and the calls can be captured into a HIP graph.
  *   - Tensors are dense row-major (last index fastest) unless a stride is given.
  *   - `dt` is the STORAGE type of activations and weight tensors (float or bfloat16 bit
  *     patterns).  Arithmetic is always fp32 (fp32 accumulation; products of float32 matrices may be
@@ -197,13 +197,17 @@ nf_status netfuse_attention_relpos(const void* Q, const void* K, const void* V, 
  *   - Cache: Kc and Vc [M][B][kv_heads][C][d] dense, C the capacity.  len[M][B]: entries that each sequence holds, in slots 0 ... len-1,
  *     the same number for every head.  pos[M][B][kv_heads][C] int: position of each entry, or NULL: its slot.  weight[...] float: attention
  *     weight that each entry has collected.  What lies in other slots is neither read nor written.
- *   - start[M][B] int: position of the first new token of each sequence, or NULL: len.
+ *     C is at most 2^30.
+ *   - start[M][B] int: position of the first new token of each sequence, or NULL: len.  Positions are 0 ... 2^30.
  *   - Scores: s_ij = f(scale * q_i . k_j) - slope[m][head] * |position_i - position_j|,  f(x) = cap * tanh(x / cap), or x for cap = 0.
  *     slope: float[M][heads], finite, or NULL.  cap: 0, or 1e-30 ... 1e30.
  *   - What a row does not see has no part in it whatever it holds, infinities and NaN too.  A row that sees nothing gives 0.
  *   - Integer operands are DEVICE arrays that the kernels bound: a length, count or number of nodes below 0 counts as 0, above its range as the
  *     largest.  No call changes len or start: after an append the caller adds the counts, after an eviction it takes min(len, budget).
- *   - NF_EUNSUPPORTED for d > 256.
+ *   - NF_EUNSUPPORTED for d > 256.  The kernels on the matrix pipe need d, strides and pointers in multiples of 16 bytes and 64 rows of K and V within
+ *     2 GB; everything else takes slower general ones.
+ *   - Sums, maxima and scores are float32; with bfloat16 storage the attention weights are rounded to bfloat16 for the product with V, as the result is.
+ *   - A sequence's bits depend neither on the models and sequences that are merged with it nor on C.
  */
 
 /*

@@ -30,6 +30,8 @@ bool rows_ok(int M, long long rows, long long width, long stride_m, long stride_
   return M == 1 || stride_m >= (rows - 1) * stride_row + width;
 }
 
+constexpr int kMostEntries = 1 << 30;                      // slot numbers and what is added to them stay in an int
+
 bool heads_ok(int heads, int kv_heads, int d) { return heads > 0 && kv_heads > 0 && d > 0 && heads % kv_heads == 0; }
 
 // What the kernels on the matrix pipe take: rows in 16-byte pieces, row numbers in an int.
@@ -103,7 +105,7 @@ nf_status netfuse_attention_prompt(const void* Q, const void* K, const void* V, 
 }
 
 long long netfuse_attention_tree_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt) {
-  if (M <= 0 || B <= 0 || T <= 0 || T > 64 || C <= 0 || !heads_ok(heads, kv_heads, d) || d > 256 || !is_dtype(dt)) return -1;
+  if (M <= 0 || B <= 0 || T <= 0 || T > 64 || C <= 0 || C > kMostEntries || !heads_ok(heads, kv_heads, d) || d > 256 || !is_dtype(dt)) return -1;
   if (!pieces_sizes(T, heads, kv_heads, d, dt)) return 0;
   const int chunk = tree_chunk(T * (heads / kv_heads)), splits = (int)(((long long)C + chunk - 1) / chunk);
   if (splits == 1) return 0;                               // no cache is shared out
@@ -117,7 +119,7 @@ nf_status netfuse_attention_tree(const void* Q, const void* K, const void* V, co
                                  int heads, int kv_heads, int d, long q_stride_m, long q_stride_row, long kv_stride_m,
                                  long kv_stride_row, float scale, float cap, nf_dtype dt, void* stream) {
   if (!Q || !K || !V || !Kc || !Vc || !len || !O) return NF_EINVAL;
-  if (M <= 0 || B <= 0 || T <= 0 || C <= 0 || !heads_ok(heads, kv_heads, d)) return NF_EINVAL;
+  if (M <= 0 || B <= 0 || T <= 0 || C <= 0 || C > kMostEntries || !heads_ok(heads, kv_heads, d)) return NF_EINVAL;
   if (!is_dtype(dt) || !score_ok(scale, cap)) return NF_EINVAL;
   if (prod({B, T}) > INT_MAX / 2 || prod({M, B, T, heads, d}) >= kMaxElems || prod({M, B, kv_heads, C, d}) >= kMaxElems) return NF_EINVAL;
   if (!rows_ok(M, (long long)B * T, (long long)heads * d, q_stride_m, q_stride_row) ||
@@ -150,7 +152,7 @@ nf_status netfuse_cache_append(const void* K, const void* V, const int* index, c
                                void* Kc, void* Vc, int* pos, float* weight, int M, int B, int T, int n, int C, int kv_heads, int d,
                                long kv_stride_m, long kv_stride_row, nf_dtype dt, void* stream) {
   if (!K || !V || !Kc || !Vc || !len) return NF_EINVAL;
-  if (M <= 0 || B <= 0 || T <= 0 || n <= 0 || C <= 0 || kv_heads <= 0 || d <= 0 || !is_dtype(dt)) return NF_EINVAL;
+  if (M <= 0 || B <= 0 || T <= 0 || n <= 0 || C <= 0 || C > kMostEntries || kv_heads <= 0 || d <= 0 || !is_dtype(dt)) return NF_EINVAL;
   if (!index && n != T) return NF_EINVAL;
   if (prod({B, T}) > INT_MAX / 2 || prod({B, n}) > INT_MAX / 2 || prod({M, B, kv_heads, C, d}) >= kMaxElems) return NF_EINVAL;
   if (!rows_ok(M, (long long)B * T, (long long)kv_heads * d, kv_stride_m, kv_stride_row)) return NF_EINVAL;
@@ -182,7 +184,7 @@ nf_status netfuse_cache_weigh(const void* Q, const float* lse, const int* index,
                               int B, int T, int n, int C, int heads, int kv_heads, int d, long q_stride_m, long q_stride_row,
                               float scale, float cap, nf_dtype dt, void* stream) {
   if (!Q || !lse || !Kc || !len || !weight || !weight_out) return NF_EINVAL;
-  if (M <= 0 || B <= 0 || T <= 0 || n <= 0 || C <= 0 || !heads_ok(heads, kv_heads, d) || !is_dtype(dt) || !score_ok(scale, cap)) return NF_EINVAL;
+  if (M <= 0 || B <= 0 || T <= 0 || n <= 0 || C <= 0 || C > kMostEntries || !heads_ok(heads, kv_heads, d) || !is_dtype(dt) || !score_ok(scale, cap)) return NF_EINVAL;
   if (!index && n != T) return NF_EINVAL;
   if (prod({B, T}) > INT_MAX / 2 || prod({B, n}) > INT_MAX / 2 || prod({M, B, T, heads}) >= kMaxElems || prod({M, B, kv_heads, C, d}) >= kMaxElems)
     return NF_EINVAL;
@@ -206,7 +208,7 @@ nf_status netfuse_cache_weigh(const void* Q, const float* lse, const int* index,
 }
 
 long long netfuse_cache_evict_workspace(int M, int B, int C, int kv_heads, int budget) {
-  if (M <= 0 || B <= 0 || C <= 0 || kv_heads <= 0 || budget <= 0 || budget > C) return -1;
+  if (M <= 0 || B <= 0 || C <= 0 || C > kMostEntries || kv_heads <= 0 || budget <= 0 || budget > C) return -1;
   const long long bytes = prod({M, B, kv_heads, 4, 1 + 2LL * std::min(budget, C - budget)});
   return bytes >= kMaxElems ? -1 : bytes;
 }
@@ -215,7 +217,7 @@ nf_status netfuse_cache_evict(void* Kc, void* Vc, const int* pos, const float* w
                               float* weight_out, void* workspace, long long workspace_bytes, int M, int B, int C, int kv_heads,
                               int d, int budget, int recent, nf_dtype dt, void* stream) {
   if (!Kc || !Vc || !weight || !len || !weight_out || !workspace) return NF_EINVAL;
-  if (M <= 0 || B <= 0 || C <= 0 || kv_heads <= 0 || d <= 0 || budget <= 0 || budget > C || recent < 0 || !is_dtype(dt)) return NF_EINVAL;
+  if (M <= 0 || B <= 0 || C <= 0 || C > kMostEntries || kv_heads <= 0 || d <= 0 || budget <= 0 || budget > C || recent < 0 || !is_dtype(dt)) return NF_EINVAL;
   if ((pos == nullptr) != (pos_out == nullptr) || (recent > 0 && !pos)) return NF_EINVAL;
   if (prod({M, B, kv_heads, C, d}) >= kMaxElems) return NF_EINVAL;
   const size_t esz = dt == NF_F32 ? 4 : 2;

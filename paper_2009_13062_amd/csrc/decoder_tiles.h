@@ -676,15 +676,17 @@ __global__ __launch_bounds__(256) void decoder_join_kernel(DecArgs a, int splits
   if (parts <= 1) return;                                  // written already; uniform where groups share a row
   const float* o = a.ws + row * splits * D + lane * 4;
   const float2* ml = reinterpret_cast<const float2*>(a.ws + (long)a.M * a.B * a.kv * R * splits * D) + row * splits;
-  const int first = SHARE == 1 ? 0 : grp;
+  // Up to 8 chunks one group takes them all, in this form too: the order of the sums follows from the length, not from the capacity.
+  const bool split_up = SHARE > 1 && parts > 8;
+  const int first = SHARE == 1 ? 0 : split_up ? grp : grp == 0 ? 0 : parts, step = split_up ? SHARE : 1;
   f32x4_t acc = f32x4_t{0.f, 0.f, 0.f, 0.f};
   float top = kLowestScore, sum = 0.f;
-  for (int k0 = first; k0 < parts; k0 += 8 * SHARE) {      // 8 loads of each kind at a time
+  for (int k0 = first; k0 < parts; k0 += 8 * step) {       // 8 loads of each kind at a time
     float2 p[8];
     f32x4_t v[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const int k = min(k0 + u * SHARE, parts - 1);
+      const int k = min(k0 + u * step, parts - 1);
       p[u] = ml[k];
       v[u] = *reinterpret_cast<const f32x4_t*>(o + (long)k * D);
     }
@@ -698,7 +700,7 @@ __global__ __launch_bounds__(256) void decoder_join_kernel(DecArgs a, int splits
     for (int e = 0; e < 4; ++e) acc[e] *= old;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const float c = k0 + u * SHARE < parts ? (LOG2 ? __builtin_amdgcn_exp2f(p[u].x - top) : expf(p[u].x - top)) : 0.f;
+      const float c = k0 + u * step < parts ? (LOG2 ? __builtin_amdgcn_exp2f(p[u].x - top) : expf(p[u].x - top)) : 0.f;
       sum = fmaf(p[u].y, c, sum);
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[u][e], c, acc[e]);

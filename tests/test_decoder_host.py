@@ -41,13 +41,13 @@ def test_tree_refuses(nf):
     call = caller(nf.lib.netfuse_attention_tree, names, ok)
     for bad in (dict(Q=None), dict(K=None), dict(V=None), dict(Kc=None), dict(Vc=None), dict(len=None), dict(O=None), dict(M=0), dict(B=0), dict(T=0), dict(C=0), dict(heads=3), dict(kv=0), dict(d=-1),
                 dict(qr=255), dict(kr=1), dict(qm=1), dict(km=1), dict(scale=float("nan")), dict(cap=-2.0), dict(dt=5), dict(Q=P + 1), dict(Kc=P + 1), dict(Vc=P + 1), dict(pos=P + 1), dict(len=P + 1),
-                dict(start=P + 1), dict(parent=P + 2), dict(nodes=P + 1), dict(slope=P + 1), dict(lse=P + 2), dict(ws=P + 8), dict(M=BIG, B=BIG, kv=BIG, heads=BIG, C=BIG)):
+                dict(start=P + 1), dict(parent=P + 2), dict(nodes=P + 1), dict(slope=P + 1), dict(lse=P + 2), dict(ws=P + 8), dict(M=BIG, B=BIG, kv=BIG, heads=BIG, C=BIG), dict(C=(1 << 30) + 1)):
         assert call(**bad) == EINVAL, bad
     assert call(T=65, qm=65 * 256, km=65 * 128) == EUNSUPPORTED
     assert call(d=257, qr=2048, qm=2048 * 8, kr=1024, km=1024 * 8) == EUNSUPPORTED
     size = nf.lib.netfuse_attention_tree_workspace
     for bad in ((0, 1, 8, 100, 4, 2, 64, 1), (2, 0, 8, 100, 4, 2, 64, 1), (2, 1, 0, 100, 4, 2, 64, 1), (2, 1, 65, 100, 4, 2, 64, 1), (2, 1, 8, 0, 4, 2, 64, 1), (2, 1, 8, 100, 3, 2, 64, 1),
-                (2, 1, 8, 100, 4, 2, 257, 1), (2, 1, 8, 100, 4, 2, 64, 9)):
+                (2, 1, 8, 100, 4, 2, 257, 1), (2, 1, 8, 100, 4, 2, 64, 9), (1, 1, 1, (1 << 30) + 1, 1, 1, 8, 1)):
         assert size(*bad) == -1, bad
     for dt in (0, 1):
         need = size(1, 1, 1, 1 << 20, 8, 1, 128, dt)
@@ -61,7 +61,7 @@ def test_cache_calls_refuse(nf):
     names = "K V index count len start Kc Vc pos weight M B T n C kv d km kr dt stream".split()
     call = caller(nf.lib.netfuse_cache_append, names, dict(K=P, V=P, index=P, count=P, len=P, start=P, Kc=P, Vc=P, pos=P, weight=P, M=2, B=1, T=8, n=3, C=100, kv=2, d=64, km=8 * 128, kr=128, dt=1, stream=None))
     for bad in (dict(K=None), dict(V=None), dict(Kc=None), dict(Vc=None), dict(len=None), dict(M=0), dict(B=0), dict(T=0), dict(n=0), dict(C=0), dict(kv=0), dict(d=0), dict(index=None), dict(kr=127), dict(km=5),
-                dict(dt=-1), dict(K=P + 1), dict(Kc=P + 1), dict(index=P + 1), dict(count=P + 2), dict(pos=P + 1), dict(weight=P + 2), dict(start=P + 1), dict(len=P + 1), dict(B=BIG, n=BIG), dict(B=BIG, T=BIG)):
+                dict(dt=-1), dict(K=P + 1), dict(Kc=P + 1), dict(index=P + 1), dict(count=P + 2), dict(pos=P + 1), dict(weight=P + 2), dict(start=P + 1), dict(len=P + 1), dict(B=BIG, n=BIG), dict(B=BIG, T=BIG), dict(C=(1 << 30) + 1)):
         assert call(**bad) == EINVAL, bad
     assert call(d=257, kr=1024, km=8 * 1024) == EUNSUPPORTED
 
@@ -69,18 +69,18 @@ def test_cache_calls_refuse(nf):
     call = caller(nf.lib.netfuse_cache_weigh, names, dict(Q=P, lse=P, index=P, count=P, Kc=P, pos=P, len=P, start=P, slope=P, weight=P, out=P, M=2, B=1, T=8, n=3, C=100, heads=4, kv=2, d=64, qm=8 * 256, qr=256,
                                                           scale=0.125, cap=0.0, dt=1, stream=None))
     for bad in (dict(Q=None), dict(lse=None), dict(Kc=None), dict(len=None), dict(weight=None), dict(out=None), dict(M=0), dict(T=0), dict(n=-1), dict(C=0), dict(heads=5), dict(index=None), dict(qr=9), dict(qm=9),
-                dict(scale=float("inf")), dict(cap=-1.0), dict(dt=3), dict(Q=P + 1), dict(lse=P + 1), dict(weight=P + 1), dict(out=P + 2), dict(slope=P + 1), dict(pos=P + 1)):
+                dict(scale=float("inf")), dict(cap=-1.0), dict(dt=3), dict(Q=P + 1), dict(lse=P + 1), dict(weight=P + 1), dict(out=P + 2), dict(slope=P + 1), dict(pos=P + 1), dict(C=(1 << 30) + 1)):
         assert call(**bad) == EINVAL, bad
     assert call(d=257, qr=2048, qm=8 * 2048) == EUNSUPPORTED
 
     names = "Kc Vc pos weight len start pos_out weight_out ws wsb M B C kv d budget recent dt stream".split()
     call = caller(nf.lib.netfuse_cache_evict, names, dict(Kc=P, Vc=P, pos=P, weight=P, len=P, start=P, pos_out=P, weight_out=P, ws=P, wsb=1 << 40, M=2, B=1, C=100, kv=2, d=64, budget=60, recent=4, dt=1, stream=None))
     for bad in (dict(Kc=None), dict(Vc=None), dict(weight=None), dict(len=None), dict(weight_out=None), dict(ws=None), dict(wsb=16), dict(pos=None), dict(pos_out=None), dict(pos=None, pos_out=None), dict(M=0),
-                dict(C=0), dict(kv=0), dict(d=0), dict(budget=0), dict(budget=101), dict(recent=-1), dict(dt=2), dict(Kc=P + 1), dict(weight=P + 1), dict(ws=P + 4), dict(weight_out=P + 1)):
+                dict(C=0), dict(kv=0), dict(d=0), dict(budget=0), dict(budget=101), dict(recent=-1), dict(dt=2), dict(Kc=P + 1), dict(weight=P + 1), dict(ws=P + 4), dict(weight_out=P + 1), dict(C=(1 << 30) + 1)):
         assert call(**bad) == EINVAL, bad
     assert call(d=257) == EUNSUPPORTED
     size = nf.lib.netfuse_cache_evict_workspace
-    for bad in ((0, 1, 100, 2, 60), (2, 0, 100, 2, 60), (2, 1, 0, 2, 60), (2, 1, 100, 0, 60), (2, 1, 100, 2, 0), (2, 1, 100, 2, 101), (BIG, BIG, BIG, BIG, 2 ** 30)):
+    for bad in ((0, 1, 100, 2, 60), (2, 0, 100, 2, 60), (2, 1, 0, 2, 60), (2, 1, 100, 0, 60), (2, 1, 100, 2, 0), (2, 1, 100, 2, 101), (1, 1, (1 << 30) + 1, 1, 5), (BIG, BIG, BIG, BIG, 2 ** 30)):
         assert size(*bad) == -1, bad
     assert size(2, 1, 100, 2, 100) >= 4
 

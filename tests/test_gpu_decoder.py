@@ -112,7 +112,7 @@ def test_prompt_masks(nf, dtype, S, mask):
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
-@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64), (BF, 20)], ids=str)
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (BF, 192), (F32, 64), (F32, 128), (F32, 256), (BF, 20)], ids=str)
 def test_prompt_what_is_not_seen_has_no_part(nf, dtype, d, bad):
     """Later tokens, other documents, padding and rows past the length hold NaN or infinities: the other rows' bits stay."""
     g = gen(3)
@@ -177,6 +177,19 @@ def test_prompt_layouts_change_no_bit(nf, dtype, d):
         return wide[:, :, 1:-2]
     ref, tol = plain.prompt(Q, K, V, B, S, heads, kv)
     near(nf.attention_prompt(at_odd(Q), at_odd(K), at_odd(V), B, S, heads, kv), ref, tol)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64), (F32, 128), (F32, 200)], ids=str)
+def test_prompt_infinite_values_add_up(nf, dtype, d):
+    """One infinity under a weight gives that infinity, two of opposite signs NaN, and neither reaches the rows before it."""
+    g = gen(15)
+    S = 420
+    Q, K, V = (x.contiguous() for x in rows(g, 1, S, 1, 1, d, dtype))
+    ok = nf.attention_prompt(Q, K, V, 1, S, 1)
+    V[0, 300, 3], V[0, 350, 3], V[0, 333, 0] = float("inf"), -float("inf"), -float("inf")
+    got = nf.attention_prompt(Q, K, V, 1, S, 1).cpu()[0].float()
+    assert torch.equal(got[:300], ok.cpu()[0, :300].float()) and torch.equal(got[:, 4:], ok.cpu()[0, :, 4:].float())
+    assert (got[300:350, 3] == float("inf")).all() and got[350:, 3].isnan().all() and (got[333:, 0] == -float("inf")).all()
 
 
 def test_prompt_far_rows(nf):
@@ -276,6 +289,28 @@ def test_tree_long_cache(nf, dtype, C, T):
     """Caches long enough to be shared out, sequences of very different lengths."""
     check_tree(nf, gen(10), dtype, 1, 3, T, C, 4, 1, 64, [[C, 130, 0]], slope=True, start=[[C + 5, 4000, 0]])
     check_tree(nf, gen(11), dtype, 1, 1, T, C, 2, 2, 128, [[C - 1]])
+
+
+@pytest.mark.parametrize("T", [1, 6, 13, 26])
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (F32, 64), (BF, 256), (BF, 20)], ids=str)
+def test_tree_bits_are_a_sequences_own(nf, dtype, d, T):
+    """Models and sequences merged or alone, and caches of another capacity: the same bits, also where a cache is shared out."""
+    g = gen(14)
+    M, B, heads, kv, C = 2, 2, 4, 1, 2500
+    Q, K, V = rows(g, M, B * T, heads, kv, d, dtype)
+    Kc, Vc = cache(g, M, B, kv, C, d, dtype)
+    length, parent, slope = ints([[2500, 700], [1, 1300]]), random_parents(g, M, B, T), slopes(g, M, heads) * 0.01
+    want = nf.attention_tree(Q, K, V, Kc, Vc, length, parent=parent, slope=slope)
+    wide = [torch.full((M, B, kv, 5000, d), float("nan"), dtype=dtype, device="cuda") for _ in range(2)]
+    for w, x in zip(wide, (Kc, Vc)):
+        w[:, :, :, :C] = x
+    assert torch.equal(nf.attention_tree(Q, K, V, *wide, length, parent=parent, slope=slope), want)
+    for m in range(M):
+        for b in range(B):
+            r = slice(b * T, b * T + T)
+            one = nf.attention_tree(Q[m:m + 1, r].contiguous(), K[m:m + 1, r].contiguous(), V[m:m + 1, r].contiguous(), Kc[m:m + 1, b:b + 1].contiguous(), Vc[m:m + 1, b:b + 1].contiguous(),
+                                    length[m:m + 1, b:b + 1].contiguous(), parent=parent[m:m + 1, b:b + 1].contiguous(), slope=slope[m:m + 1])
+            assert torch.equal(one, want[m:m + 1, r])
 
 
 @pytest.mark.parametrize("bad", [float("nan"), float("inf")])
