@@ -47,7 +47,7 @@ template <typename T> __device__ __forceinline__ f32x4_t slice_product(const uin
 }
 
 template <typename T, int D, int RT, int KS, bool TREE>
-__global__ __launch_bounds__(256, D <= 128 && RT == 1 ? 3 : 2) void decoder_stream_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
+__global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 ? 3 : 2) void decoder_stream_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
   using Sh = StreamShape<T, D>;
   constexpr bool kBf = Sh::kBf;
   constexpr int NK = Sh::NK, NB = Sh::NB, VF = Sh::VF, VC = Sh::VC, SL = Sh::kSlices, kStep = 16 * NK, RG = 4 / KS;

@@ -1,8 +1,8 @@
 // Merged decoders, bfloat16 attention on the matrix pipe: head sizes that are multiples of 8, up to D features.
 //
 // The rows of one key head are its tokens times its query heads, row r = token r / group, so keys and values are read once for the
-// whole group.  A workgroup is 4 wavefronts: RG groups of 32 RB rows times KS shares of the keys (RG KS = 4); keys pass KB at a time through LDS, the
-// next tile's loads being in flight in registers meanwhile.  Scores are computed transposed, S^T = K Q^T, so the 32 x 32
+// whole group.  A workgroup is 4 wavefronts: RG groups of 32 rows times KS shares of 64 keys (RG KS = 4); the keys pass a tile of 64 KS at a time through
+// two stages in LDS, loaded past the registers, the next tile on its way while one is worked on.  Scores are computed transposed, S^T = K Q^T, so the 32 x 32
 // accumulator of a lane holds 16 keys of ONE row (lane % 32): the softmax statistics are per-lane scalars, the two lane halves hold
 // the same row, and the weights are already in the register order of the B operand of O^T = V^T P^T, the keys of a 16-key step being
 // permuted alike on the V^T side, which comes from the transposing LDS read.  Scores, maximum and sum are float32 in log2 units;
@@ -26,12 +26,12 @@ typedef int int4v_t __attribute__((ext_vector_type(4)));
 // 16 bytes per lane from `off` of the resource to the lane's place in 1 KB of LDS
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, lds_u8_t* to, unsigned off) { __builtin_amdgcn_raw_ptr_buffer_load_lds(r, to, 16, (int)off, 0, 0, 0); }
 
-template <int D, int KB, int NS> struct DecLds {
+template <int D, int KB> struct DecLds {
   static constexpr int kRow = D * 2, kTile = KB * kRow;    // bytes of a row, of the keys or values of a stage
   static constexpr int kPieces = D / 8, kRowsPerLoad = 1024 / kRow;
-  static constexpr int kOffV = NS * kTile;
-  static constexpr int kOffKey = 2 * NS * kTile;           // position or document of each key
-  static constexpr int kOffFlag = kOffKey + NS * KB * 4;   // tile whose values are not all finite
+  static constexpr int kOffV = 2 * kTile;
+  static constexpr int kOffKey = 4 * kTile;                // position or document of each key
+  static constexpr int kOffFlag = kOffKey + 2 * KB * 4;    // tile whose values are not all finite
   static constexpr int kBytes = kOffFlag + 16;
   // Piece c of row r lies at c ^ swz(r), the same for rows that a thread's loads are apart.  K: 16 lanes that read one piece each of 16 neighbouring rows meet
   // all 16 groups of 4 banks (8 of them, twice, for D = 256); V: the 4 rows x 64
@@ -63,28 +63,28 @@ __device__ __forceinline__ float tanh_either(float u) {
 // Either half of a dword an infinity or NaN of bfloat16
 __device__ __forceinline__ bool bf16_odd(uint32_t x) { return ((x & 0x7f80u) == 0x7f80u) | ((x & 0x7f800000u) == 0x7f800000u); }
 
-// Order of the N operands of a product that come from LDS, READS reads and MF matrix instructions each: four operands are asked for ahead of the
+// Order of the N operands of a product that come from LDS, READS reads and one matrix instruction each: four operands are asked for ahead of the
 // instruction that takes them.  (Left to itself the compiler asks for one and waits for it.)
-template <int N, int READS, int MF> __device__ __forceinline__ void keep_ahead() {
+template <int N, int READS> __device__ __forceinline__ void keep_ahead() {
   constexpr int kAhead = N < 4 ? N : 4;
   __builtin_amdgcn_sched_group_barrier(0x100, kAhead * READS, 0);
 #pragma unroll
   for (int i = 0; i < N - kAhead; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x8, MF, 0);
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
     __builtin_amdgcn_sched_group_barrier(0x100, READS, 0);
   }
-  __builtin_amdgcn_sched_group_barrier(0x8, kAhead * MF, 0);
+  __builtin_amdgcn_sched_group_barrier(0x8, kAhead, 0);
 }
 
 // `Q` is a.Q once more: a pointer that is declared not to alias is what keeps the compiler from waiting for every load into LDS before a transposing read.
-template <int D, int KB, int KS, int RB, int NS, bool TREE>
+template <int D, int KS, bool TREE>
 __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __restrict__ Q, int row_blocks, int splits, int chunk) {
-  constexpr int RG = 4 / KS, TB = D / 32;
-  constexpr int kRows = RG * RB * 32;                      // per workgroup
-  constexpr int NSB = KB / KS / 32;                        // 32-key blocks of a tile per wavefront
-  using Lds = DecLds<D, KB, NS>;
+  constexpr int KB = 64 * KS, RG = 4 / KS, TB = D / 32;
+  constexpr int kRows = RG * 32;                           // per workgroup
+  constexpr int NSB = 2;                                   // 32-key blocks of a tile per wavefront
+  using Lds = DecLds<D, KB>;
   constexpr int kPer = Lds::kTile / 1024 / 4;              // loads per wavefront, tensor and tile
-  static_assert(Lds::kTile % 4096 == 0 && NSB >= 1 && NS >= 2, "whole loads, whole blocks");
+  static_assert(Lds::kTile % 4096 == 0, "whole loads");
   extern __shared__ __align__(16) unsigned char dec_smem[];
   typedef lds_u8_t lds_byte_t;
   typedef __attribute__((address_space(3))) int lds_int_t;
@@ -126,23 +126,22 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
   const long stride = TREE ? a.d : a.kv_stride_row;
 
   // ---- this lane's rows: the B operand of S^T = K Q^T, 8 consecutive features per 16-step
-  int token[RB], end[RB], mine[RB], docr[RB];
-  uint64_t path[RB];
-  float slope[RB];
-  bf16x8_t qf[RB][D / 16];
-#pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int r = r0 + (rg * RB + rb) * 32 + lq;
+  int token, end, mine, docr;
+  uint64_t path;
+  float slope;
+  bf16x8_t qf[D / 16];
+  {
+    const int r = r0 + rg * 32 + lq;
     const int i = min(r, R - 1) / group, h = g * group + (min(r, R - 1) - i * group);
-    token[rb] = i;
+    token = i;
     const bf16_t* q = Q + m * a.q_stride_m + ((long)b * a.N + i) * a.q_stride_row + (long)h * a.d;
 #pragma unroll
     for (int kk = 0; kk < D / 16; ++kk) {
       uint4 v = make_uint4(0, 0, 0, 0);
       if (r < R && kk * 16 + half * 8 < a.d) v = *reinterpret_cast<const uint4*>(q + kk * 16 + half * 8);
-      qf[rb][kk] = __builtin_bit_cast(bf16x8_t, v);
+      qf[kk] = __builtin_bit_cast(bf16x8_t, v);
     }
-    slope[rb] = a.slope ? a.slope[m * a.heads + h] * kLog2e : 0.f;
+    slope = a.slope ? a.slope[m * a.heads + h] * kLog2e : 0.f;
   }
 
   int node_at = 0;                                         // position of node `lane`
@@ -166,28 +165,22 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
     }
     const int begin = a.start ? a.start[mb] : L;
     node_at = begin + __popcll(all) - 1;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const uint32_t x = __shfl((uint32_t)all, token[rb], kWave), y = __shfl((uint32_t)(all >> 32), token[rb], kWave);
-      path[rb] = ((uint64_t)y << 32) | x;
-      mine[rb] = begin + __popcll(path[rb]) - 1;
-      end[rb] = L;
-      docr[rb] = 0;
-    }
+    const uint32_t x = __shfl((uint32_t)all, token, kWave), y = __shfl((uint32_t)(all >> 32), token, kWave);
+    path = ((uint64_t)y << 32) | x;
+    mine = begin + __popcll(path) - 1;
+    end = L;
+    docr = 0;
   } else {
     wlo = 0x7fffffff;
     whi = -1;
-#pragma unroll
-    for (int rb = 0; rb < RB; ++rb) {
-      const int i = token[rb];
-      path[rb] = 0;
-      mine[rb] = i;
-      docr[rb] = doc ? doc[i] : 0;
-      const bool valid = i < L && docr[rb] >= 0;
-      end[rb] = !valid ? 0 : a.causal ? max(i + 1, first) : L;
-      wlo = min(wlo, valid ? docr[rb] : 0x7fffffff);
-      whi = max(whi, valid ? docr[rb] : -1);
-    }
+    const int i = token;
+    path = 0;
+    mine = i;
+    docr = doc ? doc[i] : 0;
+    const bool valid = i < L && docr >= 0;
+    end = !valid ? 0 : a.causal ? max(i + 1, first) : L;
+    wlo = min(wlo, valid ? docr : 0x7fffffff);
+    whi = max(whi, valid ? docr : -1);
     const int i_lo = r0 / group, i_hi = min(r0 + kRows, R) - 1;
     block_end = i_lo >= L ? 0 : a.causal ? min(max(i_hi / group + 1, first), L) : L;
     if (doc) {
@@ -205,7 +198,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
     }
   }
   // tokens of this wavefront's rows
-  const int w_lo = (r0 + rg * RB * 32) / group, w_hi = min(r0 + (rg + 1) * RB * 32 - 1, R - 1) / group, block_lo = r0 / group;
+  const int w_lo = (r0 + rg * 32) / group, w_hi = min(r0 + (rg + 1) * 32 - 1, R - 1) / group, block_lo = r0 / group;
 
   // ---- the tiles: first key of each; the tree's own tile is kTreeTile, none left kNoTile
   constexpr int kTreeTile = -1, kNoTile = -2;
@@ -291,17 +284,14 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
     }
   };
 
-  f32x16_t o_acc[RB][TB];
-  float mrun[RB], lrun[RB];
+  f32x16_t o_acc[TB];
+  float mrun, lrun;
+  mrun = kLowestScore;
+  lrun = 0.f;                                        // this half's partial sum
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    mrun[rb] = kLowestScore;
-    lrun[rb] = 0.f;                                        // this half's partial sum
+  for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
-    for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) o_acc[rb][tb][r] = 0.f;
-  }
+    for (int r = 0; r < 16; ++r) o_acc[tb][r] = 0.f;
   const bool capped_scores = a.cap != 0.f, biased = a.slope != nullptr;
   const float sc = a.scale * kLog2e;
   const float to_u = a.scale * a.inv_cap, back = a.cap * kLog2e, u2 = to_u * to_u;
@@ -309,36 +299,22 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
   const float cap_small = fabsf(to_u) > 1e-4f && fabsf(to_u) < 1e4f ? kTanhSeries / fabsf(to_u) : 0.f;      // powers of others leave float32
   const bool raw = !capped_scores && !biased && sc > 0.f;  // scale and maximum enter the exponent in one fma
 
-  // ---- NS - 1 tiles are on their way while one is worked on
-  int tiles[NS - 1], what[NS - 1];
-#pragma unroll
-  for (int i = 0; i < NS - 1; ++i) {
-    tiles[i] = i == 0 ? seek(TREE ? split * chunk : 0) : tiles[i - 1] < 0 ? kNoTile : seek(tiles[i - 1] + KB);
-    what[i] = look_over(tiles[i]);
-    if (tiles[i] == kNoTile) continue;
-    issue(tiles[i], i);
-    if (keyed && tid < KB) Key[i * KB + tid] = key_reg;
+  // ---- one tile is on its way while one is worked on
+  int tile = seek(TREE ? split * chunk : 0), seen = look_over(tile);
+  if (tile != kNoTile) {
+    issue(tile, 0);
+    if (keyed && tid < KB) Key[tid] = key_reg;
   }
   int cur = 0, number = 1;
   if (tid == 0) *Flag = 0;
-  while (tiles[0] != kNoTile) {
-    const int tile = tiles[0], seen = what[0];
+  while (tile != kNoTile) {
     // this tile's loads have landed, and everyone is done with the stage that the next ones go to
-    if (NS > 2 && tiles[NS - 2] != kNoTile) {
-      wait_lgkmcnt0();
-      wait_vmcnt<(NS - 2) * 2 * kPer>();
-    } else {
-      wait_lgkmcnt0();
-      wait_vmcnt<0>();
-    }
+    wait_lgkmcnt0();
+    wait_vmcnt<0>();
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-#pragma unroll
-    for (int i = 0; i + 1 < NS - 1; ++i) tiles[i] = tiles[i + 1], what[i] = what[i + 1];
-    const int last = NS > 2 ? tiles[NS - 2] : tile, fresh = cur == 0 ? NS - 1 : cur - 1;
-    const int next = last < 0 ? kNoTile : seek(last + KB);
-    tiles[NS - 2] = next;
-    what[NS - 2] = look_over(next);
+    const int next = tile < 0 ? kNoTile : seek(tile + KB), fresh = 1 - cur;
+    const int next_seen = look_over(next);
     if (next != kNoTile) issue(next, fresh);
 
     const bool mask = seen & kMineLeaveOut;
@@ -362,144 +338,138 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
       const lds_byte_t* Vc = Vs + cur * Lds::kTile + key0 * Lds::kRow;
       const lds_int_t* Kk = Key + cur * KB + key0;
       const int base = (tile == kTreeTile ? 0 : tile) + key0 + 4 * half;          // register r of block sb is key base + 32 sb + 8 (r / 4) + r % 4
-      f32x16_t s[RB][NSB];
+      f32x16_t s[NSB];
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb)
+      for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-        for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[rb][sb][r] = 0.f;
+        for (int r = 0; r < 16; ++r) s[sb][r] = 0.f;
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
         for (int sb = 0; sb < NSB; ++sb) {
           // rows 32 apart are permuted alike
           const bf16x8_t kf = *(const lds_bf16x8_t*)(Kc + (sb * 32 + lq) * Lds::kRow + ((kk * 2 + half) ^ Lds::swz_k(lq)) * 16);
-#pragma unroll
-          for (int rb = 0; rb < RB; ++rb) s[rb][sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[rb][kk], s[rb][sb], 0, 0, 0);
+          s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], s[sb], 0, 0, 0);
         }
-      keep_ahead<NSB * D / 16, 1, RB>();
-      bf16x8_t pf[RB][NSB][2];
+      keep_ahead<NSB * D / 16, 1>();
+      bf16x8_t pf[NSB][2];
+      if (capped_scores) {                               // uniform
+        float top = 0.f;
 #pragma unroll
-      for (int rb = 0; rb < RB; ++rb) {
-        if (capped_scores) {                               // uniform
-          float top = 0.f;
+        for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(s[sb][r]));
+        if (__all(top < cap_small)) {                    // as a rule: the series in the unscaled score, its last term below 2^-21
 #pragma unroll
           for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(s[rb][sb][r]));
-          if (__all(top < cap_small)) {                    // as a rule: the series in the unscaled score, its last term below 2^-21
-#pragma unroll
-            for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const float w = s[rb][sb][r] * s[rb][sb][r];
-                s[rb][sb][r] *= fmaf(fmaf(fmaf(w, cap3, cap2), w, cap1), w, sc);
-              }
-          } else {
-#pragma unroll
-            for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) s[rb][sb][r] = tanh_either(s[rb][sb][r] * to_u) * back;
-          }
-        } else if (!raw) {
+            for (int r = 0; r < 16; ++r) {
+              const float w = s[sb][r] * s[sb][r];
+              s[sb][r] *= fmaf(fmaf(fmaf(w, cap3, cap2), w, cap1), w, sc);
+            }
+        } else {
 #pragma unroll
           for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[rb][sb][r] *= sc;
+            for (int r = 0; r < 16; ++r) s[sb][r] = tanh_either(s[sb][r] * to_u) * back;
         }
-        float shift = 0.f;
-        if (biased) {
-          if (TREE && (a.pos || tile == kTreeTile)) {
+      } else if (!raw) {
+#pragma unroll
+        for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s[sb][r] *= sc;
+      }
+      float shift = 0.f;
+      if (biased) {
+        if (TREE && (a.pos || tile == kTreeTile)) {
+#pragma unroll
+          for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+              const int4v_t at = *(const lds_int4_t*)(Kk + sb * 32 + 8 * r4 + 4 * half);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[sb][4 * r4 + e] = fmaf(-slope, fabsf((float)(mine - at[e])), s[sb][4 * r4 + e]);
+            }
+        } else if (!TREE && a.causal && tile >= first) {  // no key that a row sees lies behind it: -slope (away - c), of which slope away is the same for
+          shift = slope * (float)(mine - base);  // the lane's whole tile and joins the maximum
+#pragma unroll
+          for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[sb][r] = fmaf(slope, (float)(32 * sb + 8 * (r / 4) + r % 4), s[sb][r]);
+        } else {
+          const float away = (float)(mine - base);
+#pragma unroll
+          for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[sb][r] = fmaf(-slope, fabsf(away - (float)(32 * sb + 8 * (r / 4) + r % 4)), s[sb][r]);
+        }
+      }
+      if (mask) {                                        // weight 0 whatever the score
+        if (TREE && tile == kTreeTile) {
+          const uint64_t bits = path >> (key0 + 4 * half);
+#pragma unroll
+          for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int c = 32 * sb + 8 * (r / 4) + r % 4;
+              s[sb][r] = key0 + 4 * half + c < 64 && ((bits >> c) & 1) ? s[sb][r] : -INFINITY;
+            }
+        } else {
+          const int left = end - base;
+#pragma unroll
+          for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) s[sb][r] = 32 * sb + 8 * (r / 4) + r % 4 < left ? s[sb][r] : -INFINITY;
+          if (!TREE && doc) {
 #pragma unroll
             for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
               for (int r4 = 0; r4 < 4; ++r4) {
-                const int4v_t at = *(const lds_int4_t*)(Kk + sb * 32 + 8 * r4 + 4 * half);
+                const int4v_t of = *(const lds_int4_t*)(Kk + sb * 32 + 8 * r4 + 4 * half);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) s[rb][sb][4 * r4 + e] = fmaf(-slope[rb], fabsf((float)(mine[rb] - at[e])), s[rb][sb][4 * r4 + e]);
+                for (int e = 0; e < 4; ++e) s[sb][4 * r4 + e] = of[e] == docr ? s[sb][4 * r4 + e] : -INFINITY;
               }
-          } else if (!TREE && a.causal && tile >= first) {  // no key that a row sees lies behind it: -slope (away - c), of which slope away is the same for
-            shift = slope[rb] * (float)(mine[rb] - base);  // the lane's whole tile and joins the maximum
-#pragma unroll
-            for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) s[rb][sb][r] = fmaf(slope[rb], (float)(32 * sb + 8 * (r / 4) + r % 4), s[rb][sb][r]);
-          } else {
-            const float away = (float)(mine[rb] - base);
-#pragma unroll
-            for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) s[rb][sb][r] = fmaf(-slope[rb], fabsf(away - (float)(32 * sb + 8 * (r / 4) + r % 4)), s[rb][sb][r]);
           }
         }
-        if (mask) {                                        // weight 0 whatever the score
-          if (TREE && tile == kTreeTile) {
-            const uint64_t bits = path[rb] >> (key0 + 4 * half);
+      }
+      float top = -INFINITY;
 #pragma unroll
-            for (int sb = 0; sb < NSB; ++sb)
+      for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const int c = 32 * sb + 8 * (r / 4) + r % 4;
-                s[rb][sb][r] = key0 + 4 * half + c < 64 && ((bits >> c) & 1) ? s[rb][sb][r] : -INFINITY;
-              }
-          } else {
-            const int left = end[rb] - base;
-#pragma unroll
-            for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) s[rb][sb][r] = 32 * sb + 8 * (r / 4) + r % 4 < left ? s[rb][sb][r] : -INFINITY;
-            if (!TREE && doc) {
-#pragma unroll
-              for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-                for (int r4 = 0; r4 < 4; ++r4) {
-                  const int4v_t of = *(const lds_int4_t*)(Kk + sb * 32 + 8 * r4 + 4 * half);
-#pragma unroll
-                  for (int e = 0; e < 4; ++e) s[rb][sb][4 * r4 + e] = of[e] == docr[rb] ? s[rb][sb][4 * r4 + e] : -INFINITY;
-                }
-            }
-          }
-        }
-        float top = -INFINITY;
+        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[sb][r]);
+      top = across_halves(raw ? top * sc : top - shift, MaxOp{});               // the halves' keys are 4 apart, and so are their shifts
+      const float mnew = fmaxf(mrun, top), less = mnew + shift;
+      float esc = raw ? sc : 1.0f;                       // exponent = s * esc - less
+      if (raw && __any(fabsf(mnew) > 0x1p29f && mnew != kLowestScore)) {        // the rounded maximum may lie far beside such a score: scale first
 #pragma unroll
         for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) top = fmaxf(top, s[rb][sb][r]);
-        top = across_halves(raw ? top * sc : top - shift, MaxOp{});               // the halves' keys are 4 apart, and so are their shifts
-        const float mnew = fmaxf(mrun[rb], top), less = mnew + shift;
-        float esc = raw ? sc : 1.0f;                       // exponent = s * esc - less
-        if (raw && __any(fabsf(mnew) > 0x1p29f && mnew != kLowestScore)) {        // the rounded maximum may lie far beside such a score: scale first
+          for (int r = 0; r < 16; ++r) s[sb][r] *= sc;
+        esc = 1.0f;
+      }
+      const float corr = __builtin_amdgcn_exp2f(mrun - mnew);
+      mrun = mnew;
+      float sum = 0.f;
 #pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
+      for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[rb][sb][r] *= sc;
-          esc = 1.0f;
-        }
-        const float corr = __builtin_amdgcn_exp2f(mrun[rb] - mnew);
-        mrun[rb] = mnew;
-        float sum = 0.f;
+        for (int st = 0; st < 2; ++st) {
+          uint32_t w[4];
 #pragma unroll
-        for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-          for (int st = 0; st < 2; ++st) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const float p0 = __builtin_amdgcn_exp2f(fmaf(s[rb][sb][8 * st + 2 * e], esc, -less));
-              const float p1 = __builtin_amdgcn_exp2f(fmaf(s[rb][sb][8 * st + 2 * e + 1], esc, -less));
-              w[e] = pack_bf16x2(p0, p1);
-              sum += p0 + p1;                              // float32 sum of the unrounded weights
-            }
-            pf[rb][sb][st] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+          for (int e = 0; e < 4; ++e) {
+            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[sb][8 * st + 2 * e], esc, -less));
+            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[sb][8 * st + 2 * e + 1], esc, -less));
+            w[e] = pack_bf16x2(p0, p1);
+            sum += p0 + p1;                              // float32 sum of the unrounded weights
           }
-        lrun[rb] = lrun[rb] * corr + sum;
-        if (__any(corr != 1.0f)) {                         // after the first tiles the maximum of a row seldom moves
-#pragma unroll
-          for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o_acc[rb][tb][r] *= corr;
+          pf[sb][st] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
         }
+      lrun = lrun * corr + sum;
+      if (__any(corr != 1.0f)) {                         // after the first tiles the maximum of a row seldom moves
+#pragma unroll
+        for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o_acc[tb][r] *= corr;
       }
 
       if (odd_tile) {
@@ -510,40 +480,37 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
           for (int f = 0; f < D; f += 2) odd |= bf16_odd(*(const __attribute__((address_space(3))) uint32_t*)(Vc + lane * Lds::kRow + f * 2));
         }
         const uint64_t odd_keys = __ballot(odd);
+        uint32_t lo = 0, hi = 0;                         // keys under a weight that is not 0: this half's, then both
 #pragma unroll
-        for (int rb = 0; rb < RB; ++rb) {
-          uint32_t lo = 0, hi = 0;                         // keys under a weight that is not 0: this half's, then both
+        for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
+          for (int st = 0; st < 2; ++st) {
+            const uint4 w = __builtin_bit_cast(uint4, pf[sb][st]);
+            const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-            for (int st = 0; st < 2; ++st) {
-              const uint4 w = __builtin_bit_cast(uint4, pf[rb][sb][st]);
-              const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-              for (int e = 0; e < 8; ++e) {
-                const uint32_t bit = (ws[e / 2] >> (e % 2 * 16) & 0x7fffu) != 0 ? 1u << (16 * st + 8 * (e / 4) + e % 4) : 0u;
-                if (sb == 0) lo |= bit; else hi |= bit;
-              }
+            for (int e = 0; e < 8; ++e) {
+              const uint32_t bit = (ws[e / 2] >> (e % 2 * 16) & 0x7fffu) != 0 ? 1u << (16 * st + 8 * (e / 4) + e % 4) : 0u;
+              if (sb == 0) lo |= bit; else hi |= bit;
             }
-          lo <<= 4 * half;
-          hi <<= 4 * half;
-          lo |= __shfl_xor(lo, 32, kWave);
-          hi |= __shfl_xor(hi, 32, kWave);
-          const uint64_t under = (uint64_t)hi << 32 | lo;
-#pragma unroll 1
-          for (uint64_t left = odd_keys; left; left &= left - 1) {
-            const int k = __builtin_ctzll(left);
-            const bool takes = (under >> k) & 1;
-            const lds_byte_t* vr = Vc + k * Lds::kRow + 8 * half;
-            const int swz = Lds::swz_v(k);
-#pragma unroll
-            for (int tb = 0; tb < TB; ++tb)
-#pragma unroll
-              for (int r = 0; r < 16; ++r) {
-                const uint32_t v = *(const lds_bf16_t*)(vr + ((tb * 4 + r / 4) ^ swz) * 16 + r % 4 * 2);
-                o_acc[rb][tb][r] += takes & ((v & 0x7f80) == 0x7f80) ? __uint_as_float(v << 16) : 0.f;
-              }
           }
+        lo <<= 4 * half;
+        hi <<= 4 * half;
+        lo |= __shfl_xor(lo, 32, kWave);
+        hi |= __shfl_xor(hi, 32, kWave);
+        const uint64_t under = (uint64_t)hi << 32 | lo;
+#pragma unroll 1
+        for (uint64_t left = odd_keys; left; left &= left - 1) {
+          const int k = __builtin_ctzll(left);
+          const bool takes = (under >> k) & 1;
+          const lds_byte_t* vr = Vc + k * Lds::kRow + 8 * half;
+          const int swz = Lds::swz_v(k);
+#pragma unroll
+          for (int tb = 0; tb < TB; ++tb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const uint32_t v = *(const lds_bf16_t*)(vr + ((tb * 4 + r / 4) ^ swz) * 16 + r % 4 * 2);
+              o_acc[tb][r] += takes & ((v & 0x7f80) == 0x7f80) ? __uint_as_float(v << 16) : 0.f;
+            }
         }
         wait_lgkmcnt0();
         __builtin_amdgcn_s_barrier();
@@ -572,91 +539,88 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
             const s16x4_t lo4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)vp);
             const s16x4_t hi4 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t*)(vp + 8 * Lds::kRow));
             const s16x8_t both = __builtin_shufflevector(lo4, hi4, 0, 1, 2, 3, 4, 5, 6, 7);
-#pragma unroll
-            for (int rb = 0; rb < RB; ++rb)
-              o_acc[rb][tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, both), pf[rb][sb][st], o_acc[rb][tb], 0, 0, 0);
+            o_acc[tb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, both), pf[sb][st], o_acc[tb], 0, 0, 0);
           }
-      keep_ahead<NSB * 2 * TB, 2, RB>();
+      keep_ahead<NSB * 2 * TB, 2>();
     }
     if (next != kNoTile && keyed && tid < KB) Key[fresh * KB + tid] = key_reg;
-    cur = cur + 1 == NS ? 0 : cur + 1;
+    cur = fresh;
     ++number;
+    tile = next;
+    seen = next_seen;
   }
   __syncthreads();                                         // the stages are free for the shares
 
   // ---- the result: element r of block tb is feature 32 tb + 8 (r / 4) + 4 half + r % 4
   const bool partial = TREE && parts > 1;
   float* const ml = a.ws + (long)a.M * a.B * a.kv * R * splits * D;
+  const int r = r0 + rg * 32 + lq;
+  float ltot = across_halves(lrun, AddOp{}), mtot = mrun;
+  constexpr int kQuads = 4 * TB / KS;                    // pieces of 4 features that a lane finishes
+  const int quad0 = wave / RG * kQuads;
+  f32x4_t out[kQuads];
+  if constexpr (KS == 1) {
 #pragma unroll
-  for (int rb = 0; rb < RB; ++rb) {
-    const int r = r0 + (rg * RB + rb) * 32 + lq;
-    float ltot = across_halves(lrun[rb], AddOp{}), mtot = mrun[rb];
-    constexpr int kQuads = 4 * TB / KS;                    // pieces of 4 features that a lane finishes
-    const int quad0 = wave / RG * kQuads;
-    f32x4_t out[kQuads];
-    if constexpr (KS == 1) {
+    for (int u = 0; u < kQuads; ++u)
 #pragma unroll
-      for (int u = 0; u < kQuads; ++u)
+      for (int e = 0; e < 4; ++e) out[u][e] = o_acc[u / 4][4 * (u % 4) + e];
+  } else {
+    lds_f32_t* const buf = (lds_f32_t*)dec_smem;
+    lds_f32_t* const max_of = buf + 256 * 16 * TB;
+    lds_f32_t* const sum_of = max_of + 256;
+    static_assert(256 * 16 * TB * 4 + 2 * 256 * 4 <= Lds::kBytes, "shares fit the stages");
 #pragma unroll
-        for (int e = 0; e < 4; ++e) out[u][e] = o_acc[rb][u / 4][4 * (u % 4) + e];
-    } else {
-      lds_f32_t* const buf = (lds_f32_t*)dec_smem;
-      lds_f32_t* const max_of = buf + 256 * 16 * TB;
-      lds_f32_t* const sum_of = max_of + 256;
-      static_assert(RB > 1 || 256 * 16 * TB * 4 + 2 * 256 * 4 <= Lds::kBytes, "shares fit the stages");
+    for (int u = 0; u < 4 * TB; ++u) *(lds_f32x4_t*)(buf + (u * 256 + tid) * 4) = f32x4v_t{o_acc[u / 4][4 * (u % 4)], o_acc[u / 4][4 * (u % 4) + 1], o_acc[u / 4][4 * (u % 4) + 2], o_acc[u / 4][4 * (u % 4) + 3]};
+    max_of[tid] = mtot;
+    sum_of[tid] = ltot;
+    __syncthreads();
+    const int lane0 = tid % (RG * kWave);                // this lane in share 0
+    mtot = kLowestScore;
 #pragma unroll
-      for (int u = 0; u < 4 * TB; ++u) *(lds_f32x4_t*)(buf + (u * 256 + tid) * 4) = f32x4v_t{o_acc[rb][u / 4][4 * (u % 4)], o_acc[rb][u / 4][4 * (u % 4) + 1], o_acc[rb][u / 4][4 * (u % 4) + 2], o_acc[rb][u / 4][4 * (u % 4) + 3]};
-      max_of[tid] = mtot;
-      sum_of[tid] = ltot;
-      __syncthreads();
-      const int lane0 = tid % (RG * kWave);                // this lane in share 0
-      mtot = kLowestScore;
+    for (int k = 0; k < KS; ++k) mtot = fmaxf(mtot, max_of[lane0 + k * RG * kWave]);
+    ltot = 0.f;
 #pragma unroll
-      for (int k = 0; k < KS; ++k) mtot = fmaxf(mtot, max_of[lane0 + k * RG * kWave]);
-      ltot = 0.f;
+    for (int u = 0; u < kQuads; ++u) out[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int u = 0; u < kQuads; ++u) out[u] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        const int from = lane0 + k * RG * kWave;
-        const float c = __builtin_amdgcn_exp2f(max_of[from] - mtot);
-        ltot = fmaf(sum_of[from], c, ltot);
-#pragma unroll
-        for (int u = 0; u < kQuads; ++u) {
-          const f32x4v_t v = *(const lds_f32x4_t*)(buf + ((quad0 + u) * 256 + from) * 4);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) out[u][e] = fmaf(v[e], c, out[u][e]);
-        }
-      }
-    }
-    if (r >= R) continue;
-    const bool valid = TREE ? token[rb] < there : end[rb] > 0;
-    const int h = g * group + (r - token[rb] * group);
-    if (partial) {
-      const long at = (head * R + r) * splits + split;
+    for (int k = 0; k < KS; ++k) {
+      const int from = lane0 + k * RG * kWave;
+      const float c = __builtin_amdgcn_exp2f(max_of[from] - mtot);
+      ltot = fmaf(sum_of[from], c, ltot);
 #pragma unroll
       for (int u = 0; u < kQuads; ++u) {
-        const int f = 8 * (quad0 + u) + 4 * half;
-        *reinterpret_cast<f32x4_t*>(a.ws + at * D + f) = out[u];
+        const f32x4v_t v = *(const lds_f32x4_t*)(buf + ((quad0 + u) * 256 + from) * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) out[u][e] = fmaf(v[e], c, out[u][e]);
       }
-      if (quad0 == 0 && half == 0) *reinterpret_cast<float2*>(ml + 2 * at) = make_float2(mtot, ltot);
-      continue;
     }
-    const float inv = valid && ltot != 0.f ? 1.0f / ltot : 0.f;
-    const bool none = !valid || ltot == 0.f;
-    bf16_t* Op = (bf16_t*)a.O + (mb * a.N + token[rb]) * ((long)a.heads * a.d) + (long)h * a.d;
+  }
+  if (r >= R) return;
+  const bool valid = TREE ? token < there : end > 0;
+  const int h = g * group + (r - token * group);
+  if (partial) {
+    const long at = (head * R + r) * splits + split;
 #pragma unroll
     for (int u = 0; u < kQuads; ++u) {
       const int f = 8 * (quad0 + u) + 4 * half;
-      if (f < a.d) *reinterpret_cast<uint2*>(Op + f) = none ? make_uint2(0, 0) : make_uint2(pack_bf16x2(out[u][0] * inv, out[u][1] * inv), pack_bf16x2(out[u][2] * inv, out[u][3] * inv));
+      *reinterpret_cast<f32x4_t*>(a.ws + at * D + f) = out[u];
     }
-    if (TREE && a.lse && quad0 == 0 && half == 0) a.lse[(mb * a.N + token[rb]) * a.heads + h] = none ? -INFINITY : (mtot + __builtin_amdgcn_logf(ltot)) * kLn2;
+    if (quad0 == 0 && half == 0) *reinterpret_cast<float2*>(ml + 2 * at) = make_float2(mtot, ltot);
+    return;
   }
+  const float inv = valid && ltot != 0.f ? 1.0f / ltot : 0.f;
+  const bool none = !valid || ltot == 0.f;
+  bf16_t* Op = (bf16_t*)a.O + (mb * a.N + token) * ((long)a.heads * a.d) + (long)h * a.d;
+#pragma unroll
+  for (int u = 0; u < kQuads; ++u) {
+    const int f = 8 * (quad0 + u) + 4 * half;
+    if (f < a.d) *reinterpret_cast<uint2*>(Op + f) = none ? make_uint2(0, 0) : make_uint2(pack_bf16x2(out[u][0] * inv, out[u][1] * inv), pack_bf16x2(out[u][2] * inv, out[u][3] * inv));
+  }
+  if (TREE && a.lse && quad0 == 0 && half == 0) a.lse[(mb * a.N + token) * a.heads + h] = none ? -INFINITY : (mtot + __builtin_amdgcn_logf(ltot)) * kLn2;
 }
 
-template <int D, int KB, int KS, int RB, int NS, bool TREE>
+template <int D, int KS, bool TREE>
 __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
-  decoder_tiles<D, KB, KS, RB, NS, TREE>(a, (const bf16_t*)a.Q, row_blocks, splits, chunk);
+  decoder_tiles<D, KS, TREE>(a, (const bf16_t*)a.Q, row_blocks, splits, chunk);
 }
 
 // Sums of the chunks of one row: D / 4 lanes hold its features, 4 each, and SHARE such groups of lanes take every SHARE-th chunk.  Maxima and sums in log2

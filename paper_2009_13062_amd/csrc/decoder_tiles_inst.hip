@@ -9,13 +9,13 @@
 namespace nf {
 namespace {
 
-template <int D, int KB, int KS, int RB, int NS, bool TREE>
+template <int D, int KS, bool TREE>
 nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
-  constexpr int kRows = 4 / KS * RB * 32, kBytes = DecLds<D, KB, NS>::kBytes;
+  constexpr int kRows = 4 / KS * 32, kBytes = DecLds<D, 64 * KS>::kBytes;
   const long long R = (long long)a.N * (a.heads / a.kv), row_blocks = (R + kRows - 1) / kRows;
   const long long total = prod({a.M, a.B, a.kv, row_blocks, splits});
   if (total > kMaxGrid) return NF_EUNSUPPORTED;
-  const auto kernel = decoder_tiles_kernel<D, KB, KS, RB, NS, TREE>;
+  const auto kernel = decoder_tiles_kernel<D, KS, TREE>;
   static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
   if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) != hipSuccess) return NF_ELAUNCH;
@@ -28,13 +28,13 @@ nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
 }  // namespace
 
 nf_status launch_prompt_tiles(const DecArgs& a, hipStream_t s) {
-  return a.d <= 64 ? go<64, 64, 1, 1, 2, false>(a, 1, 0, s) : a.d <= 128 ? go<128, 64, 1, 1, 2, false>(a, 1, 0, s) : go<256, 64, 1, 1, 2, false>(a, 1, 0, s);
+  return a.d <= 64 ? go<64, 1, false>(a, 1, 0, s) : a.d <= 128 ? go<128, 1, false>(a, 1, 0, s) : go<256, 1, false>(a, 1, 0, s);
 }
 
 nf_status launch_tree_tiles(const DecArgs& a, int chunk, int splits, hipStream_t s) {
   const int R = a.N * (a.heads / a.kv);
-  if (a.d <= 64) return R <= 64 ? go<64, 128, 2, 1, 2, true>(a, splits, chunk, s) : go<64, 64, 1, 1, 2, true>(a, splits, chunk, s);
-  return a.d <= 128 ? go<128, 64, 1, 1, 2, true>(a, splits, chunk, s) : go<256, 64, 1, 1, 2, true>(a, splits, chunk, s);
+  if (a.d <= 64) return R <= 64 ? go<64, 2, true>(a, splits, chunk, s) : go<64, 1, true>(a, splits, chunk, s);
+  return a.d <= 128 ? go<128, 1, true>(a, splits, chunk, s) : go<256, 1, true>(a, splits, chunk, s);
 }
 
 }  // namespace nf
