@@ -107,7 +107,7 @@ nf_status netfuse_attention_prompt(const void* Q, const void* K, const void* V, 
 long long netfuse_attention_tree_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt) {
   if (M <= 0 || B <= 0 || T <= 0 || T > 64 || C <= 0 || C > kMostEntries || !heads_ok(heads, kv_heads, d) || d > 256 || !is_dtype(dt)) return -1;
   if (!pieces_sizes(T, heads, kv_heads, d, dt)) return 0;
-  const int chunk = tree_chunk(T * (heads / kv_heads)), splits = (int)(((long long)C + chunk - 1) / chunk);
+  const int chunk = tree_chunk(T * (heads / kv_heads), dt), splits = (int)(((long long)C + chunk - 1) / chunk);
   if (splits == 1) return 0;                               // no cache is shared out
   const long long bytes = prod({M, B, heads, T, splits, 4LL * (tree_features(d) + 2)});      // a row's sums, its maximum and its total per chunk
   return bytes >= kMaxElems ? -1 : bytes;
@@ -141,8 +141,11 @@ nf_status netfuse_attention_tree(const void* Q, const void* K, const void* V, co
   a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.kv_stride_m = kv_stride_m; a.kv_stride_row = kv_stride_row;
   a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
   if (pieces_ok(a, dt)) {
-    const int rows = T * (heads / kv_heads), chunk = tree_chunk(rows), splits = (int)(((long long)C + chunk - 1) / chunk);
-    const nf_status st = dt == NF_BF16 && rows > (d <= 64 || d > 128 ? 32 : 64) ? launch_tree_tiles(a, chunk, splits, (hipStream_t)stream) : launch_tree_stream(a, chunk, splits, dt, (hipStream_t)stream);
+    const int rows = T * (heads / kv_heads), chunk = tree_chunk(rows, dt), splits = (int)(((long long)C + chunk - 1) / chunk);
+    // Many rows of bfloat16 take their keys through LDS, few ones straight into registers (16 caches of 4096 entries, groups of 4, us, registers / LDS: 8 key heads of 128 features, 20 rows
+    // 53 / 66, 36 66 / 56, 64 67 / 58; 8 of 64, 20 rows 41 / 37; 4 of 256, 20 rows 68 / 85, 36 76 / 78; 32 caches of 700, 8 key heads of 128, 18 rows 25 / 29, 64 features 20.6 / 18.3).
+    const bool tiles = dt == NF_BF16 && rows > (d <= 64 ? 16 : 32);
+    const nf_status st = tiles ? launch_tree_tiles(a, chunk, splits, (hipStream_t)stream) : launch_tree_stream(a, chunk, splits, dt, (hipStream_t)stream);
     return st != NF_OK || splits == 1 ? st : launch_tree_join(a, chunk, splits, dt, (hipStream_t)stream);
   }
   return launch_rows<true>(a, dt, (hipStream_t)stream);

@@ -32,17 +32,18 @@ nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
 template <typename T, int D>
 nf_status tree(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   const int R = a.N * (a.heads / a.kv);
+  constexpr bool kBf = sizeof(T) == 2;                     // of more than 32 rows (16 up to 64 features): decoder_tiles.h
   if (R <= 16) return go<T, D, 1, 4, true>(a, splits, chunk, s);
   if constexpr (D == 128) {
     // 32 rows per wavefront: its keys and values serve twice the rows, and their loads are what bounds it (4 models of 4 caches of 4096 entries, 8 key heads of 128,
-    // groups of 4, us, 16 rows / 32: bfloat16 5 tokens 73.6 / 55.6, 16 113 / 76; float32 5 140 / 112, 12 187 / 176, 26 353 / 375; 8 heads of 64 31.3 / 33.7)
+    // groups of 4, us, 16 rows / 32: bfloat16 5 tokens 73.6 / 55.6; float32 5 140 / 112, 12 187 / 176, 26 353 / 375; 8 heads of 64 31.3 / 33.7, of 256 spill)
     if (R <= 32) return go<T, D, 2, 4, true>(a, splits, chunk, s);
-    if (R <= 64) return go<T, D, 2, 2, true>(a, splits, chunk, s);
-  } else {
+    if constexpr (!kBf) if (R <= 64) return go<T, D, 2, 2, true>(a, splits, chunk, s);
+  } else if constexpr (D == 256 || !kBf) {
     if (R <= 32) return go<T, D, 1, 2, true>(a, splits, chunk, s);
   }
-  if constexpr (sizeof(T) == 4) return go<T, D, 1, 1, true>(a, splits, chunk, s);
-  return NF_EUNSUPPORTED;                                  // bfloat16 of more rows: decoder_tiles.h
+  if constexpr (kBf) return NF_EUNSUPPORTED;
+  else return go<T, D, 1, 1, true>(a, splits, chunk, s);
 }
 
 // From 12 steps of keys on the four wavefronts of a workgroup share the keys of 16 rows, below that they take 16 rows each: by the length alone, so that a
