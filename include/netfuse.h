@@ -200,7 +200,7 @@ nf_status netfuse_attention_relpos(const void* Q, const void* K, const void* V, 
  *     C is at most 2^30.
  *   - start[M][B] int: position of the first new token of each sequence, or NULL: len.  Positions are 0 ... 2^30.
  *   - Scores: s_ij = f(scale * q_i . k_j) - slope[m][head] * |position_i - position_j|,  f(x) = cap * tanh(x / cap), or x for cap = 0.
- *     slope: float[M][heads], finite, or NULL.  cap: 0, or 1e-30 ... 1e30.
+ *     slope: float[M][heads], -1e20 ... 1e20, or NULL.  cap: 0, or 1e-30 ... 1e30.
  *   - What a row does not see has no part in it whatever it holds, infinities and NaN too.  A row that sees nothing gives 0.
  *   - Integer operands are DEVICE arrays that the kernels bound: a length, count or number of nodes below 0 counts as 0, above its range as the
  *     largest.  No call changes len or start: after an append the caller adds the counts, after an eviction it takes min(len, budget).

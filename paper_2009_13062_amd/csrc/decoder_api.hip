@@ -239,7 +239,10 @@ nf_status netfuse_cache_evict(void* Kc, void* Vc, const int* pos, const float* w
   const long long blocks = prod({heads, per_head});
   if (heads > kMaxGrid || blocks > kMaxGrid) return NF_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
-  // Small heads: the workgroup that picks the entries moves them too.
+  // Small heads: the workgroup that picks the entries moves them too, as long as a head's rows are a few loads per thread (192 heads of 1024 entries cut to 896: 13.6 us by two
+  // kernels, 12.8 by one).  Up to 32768 entries a head's weights stay in registers, of as few threads and as few to a thread as hold them (us, whole evictions: 128 heads of
+  // 32768 147, by the kernel that reads them again for each digit 192; 128 / 768 heads of 6000, 8 or 32 to a thread 59 / 103 and 70 / 145; of 4096, 256 or 1024 threads
+  // 53 / 73 and 48 / 76, of 2048 33 / 41 and 30 / 45).
   if (C <= 1024 && wide && (long long)a.most * a.units <= 4096) return select_held<256, 4, true, uint4>(a, heads, s);
   const nf_status st = C <= 1024 ? select_held<256, 4>(a, heads, s) : C <= 4096 ? select_held<256, 16>(a, heads, s) : C <= 8192 ? select_held<1024, 8>(a, heads, s)
                        : C <= 32768 ? select_held<1024, 32>(a, heads, s) : NF_EUNSUPPORTED;

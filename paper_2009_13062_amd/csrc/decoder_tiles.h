@@ -10,11 +10,17 @@
 //
 // Which keys a row sees is an upper end per row (causal, prefix, lengths), the documents of a tile (staged with its keys) or, for the tree's
 // own tile, a bit per node.  Tiles that every row of a wavefront sees in full are not masked, tiles that none sees are left out.  In a masked
-// tile, values that are infinite or NaN are found as they are staged, and that tile's second product is then summed by each lane over
-// the keys that have a weight (0 times NaN would reach the rows that do not see them).
+// tile, values that are infinite or NaN are looked for in the stage; each row adds those of the keys that have a weight in it, and the second product then runs on
+// the others (0 times NaN would reach the rows that do not see them).
 //
 // A cache is shared out among workgroups in chunks of a length that depends on the number of rows alone: a sequence's bits depend neither on
 // what is merged with it nor on the capacity.  Where a sequence fills more than one chunk, partial sums go to the workspace and a second kernel joins them.
+//
+// Long prompts are bound by vector arithmetic: per score one fma and a quarter-rate exponential, half a maximum, a sum and half a rounding, with a bias one fma
+// more, under a cap five.  (2 models of 8191 tokens, 32 heads over 8 of 128 features, biased: 1.21 ms, 907 TFLOP/s where a library product reaches 1165 to 1197; of the cycles the
+// vector units are busy 68 %, the matrix units 41 %.)  So scores stay as they come from the product until the exponent, and the branches below keep whole paths apart.  64 keys of
+// 32 rows per step: two workgroups (three of up to 64 features) share a compute unit's LDS and registers, one's exponentials beside the other's products.
+// Trees are bound by the cache's bytes below some 64 rows, then as prompts are (26 tokens over 32 caches of up to 4096 entries: 120 us and 14 to join).
 #pragma once
 #include "decoder.h"
 #include "gemm_dma.h"
@@ -54,7 +60,7 @@ __device__ __forceinline__ float tanh_exp(float u) {
   const float e = __builtin_amdgcn_exp2f(fabsf(u) * (2.f * kLog2e));      // infinite for large u: 1
   return copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), u);
 }
-constexpr float kTanhSeries = 0.25f;
+constexpr float kTanhSeries = 0.25f, kTanhShort = 0.14f;   // 62/2835 u^8 and 17/315 u^6 are below 2^-21 there
 __device__ __forceinline__ float tanh_either(float u) {
   const float t = tanh_series(u), e = tanh_exp(u);
   return fabsf(u) < kTanhSeries ? t : e;
@@ -76,9 +82,15 @@ template <int N, int READS> __device__ __forceinline__ void keep_ahead() {
   __builtin_amdgcn_sched_group_barrier(0x8, kAhead, 0);
 }
 
+// Scores: as they come from the product, scale and maximum entering the exponent in one fma, or any (capped, odd scales); each without and with a bias by distance.
+constexpr int kRawScore = 0, kRawBiased = 1, kAnyScore = 2, kAnyBiased = 3;
+constexpr std::true_type kShift;
+constexpr std::false_type kNoShift;
+
 // `Q` is a.Q once more: a pointer that is declared not to alias is what keeps the compiler from waiting for every load into LDS before a transposing read.
-template <int D, int KS, bool TREE>
+template <int D, int KS, bool TREE, int FORM>
 __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __restrict__ Q, int row_blocks, int splits, int chunk) {
+  constexpr bool kRaw = FORM == kRawScore || FORM == kRawBiased, kBiased = FORM == kRawBiased || FORM == kAnyBiased;
   constexpr int KB = 64 * KS, RG = 4 / KS, TB = D / 32;
   constexpr int kRows = RG * 32;                           // per workgroup
   constexpr int NSB = 2;                                   // 32-key blocks of a tile per wavefront
@@ -117,7 +129,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
   const int there = TREE && a.nodes ? clamp_len(a.nodes[mb], a.N) : a.N;
   const int first = !TREE && a.prefix ? clamp_len(a.prefix[mb], L) : 0;   // keys below it are seen by every row
   const int* doc = !TREE && a.doc ? a.doc + mb * a.N : nullptr;
-  const bool keyed = TREE ? a.slope != nullptr : doc != nullptr;          // a value per key is staged
+  const bool keyed = TREE ? kBiased : doc != nullptr;          // a value per key is staged
 
   const bf16_t* Kp = (const bf16_t*)a.K + m * a.kv_stride_m + (long)b * a.N * a.kv_stride_row + (long)g * a.d;
   const bf16_t* Vp = (const bf16_t*)a.V + m * a.kv_stride_m + (long)b * a.N * a.kv_stride_row + (long)g * a.d;
@@ -141,7 +153,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
       if (r < R && kk * 16 + half * 8 < a.d) v = *reinterpret_cast<const uint4*>(q + kk * 16 + half * 8);
       qf[kk] = __builtin_bit_cast(bf16x8_t, v);
     }
-    slope = a.slope ? a.slope[m * a.heads + h] * kLog2e : 0.f;
+    slope = kBiased ? a.slope[m * a.heads + h] * kLog2e : 0.f;
   }
 
   int node_at = 0;                                         // position of node `lane`
@@ -292,12 +304,12 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
   for (int tb = 0; tb < TB; ++tb)
 #pragma unroll
     for (int r = 0; r < 16; ++r) o_acc[tb][r] = 0.f;
-  const bool capped_scores = a.cap != 0.f, biased = a.slope != nullptr;
-  const float sc = a.scale * kLog2e;
+  const float sc = a.scale * kLog2e, slope_raw = slope / sc;
+  // series of the capped score: used within these bounds, not at all for caps and scales whose powers leave float32 (nor without a cap: 0)
   const float to_u = a.scale * a.inv_cap, back = a.cap * kLog2e, u2 = to_u * to_u;
   const float cap1 = sc * u2 * -0.3333333333333333f, cap2 = sc * u2 * u2 * 0.13333333333333333f, cap3 = sc * u2 * u2 * u2 * -0.05396825396825397f;
-  const float cap_small = fabsf(to_u) > 1e-4f && fabsf(to_u) < 1e4f ? kTanhSeries / fabsf(to_u) : 0.f;      // powers of others leave float32
-  const bool raw = !capped_scores && !biased && sc > 0.f;  // scale and maximum enter the exponent in one fma
+  const bool series = fabsf(to_u) > 1e-4f && fabsf(to_u) < 1e4f;
+  const float cap_short = series ? kTanhShort / fabsf(to_u) : 0.f, cap_small = series ? kTanhSeries / fabsf(to_u) : 0.f;
 
   // ---- one tile is on its way while one is worked on
   int tile = seek(TREE ? split * chunk : 0), seen = look_over(tile);
@@ -352,119 +364,164 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
           s[sb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, qf[kk], s[sb], 0, 0, 0);
         }
       keep_ahead<NSB * D / 16, 1>();
+      float x[NSB][16];                                    // single values: a branch changes them in place
+#pragma unroll
+      for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[sb][r] = s[sb][r];
       bf16x8_t pf[NSB][2];
-      if (capped_scores) {                               // uniform
-        float top = 0.f;
-#pragma unroll
-        for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) top = fmaxf(top, fabsf(s[sb][r]));
-        if (__all(top < cap_small)) {                    // as a rule: the series in the unscaled score, its last term below 2^-21
-#pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const float w = s[sb][r] * s[sb][r];
-              s[sb][r] *= fmaf(fmaf(fmaf(w, cap3, cap2), w, cap1), w, sc);
-            }
-        } else {
-#pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[sb][r] = tanh_either(s[sb][r] * to_u) * back;
-        }
-      } else if (!raw) {
-#pragma unroll
-        for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[sb][r] *= sc;
-      }
-      float shift = 0.f;
-      if (biased) {
-        if (TREE && (a.pos || tile == kTreeTile)) {
-#pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-              const int4v_t at = *(const lds_int4_t*)(Kk + sb * 32 + 8 * r4 + 4 * half);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) s[sb][4 * r4 + e] = fmaf(-slope, fabsf((float)(mine - at[e])), s[sb][4 * r4 + e]);
-            }
-        } else if (!TREE && a.causal && tile >= first) {  // no key that a row sees lies behind it: -slope (away - c), of which slope away is the same for
-          shift = slope * (float)(mine - base);  // the lane's whole tile and joins the maximum
-#pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[sb][r] = fmaf(slope, (float)(32 * sb + 8 * (r / 4) + r % 4), s[sb][r]);
-        } else {
-          const float away = (float)(mine - base);
-#pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[sb][r] = fmaf(-slope, fabsf(away - (float)(32 * sb + 8 * (r / 4) + r % 4)), s[sb][r]);
-        }
-      }
-      if (mask) {                                        // weight 0 whatever the score
-        if (TREE && tile == kTreeTile) {
-          const uint64_t bits = path >> (key0 + 4 * half);
-#pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int c = 32 * sb + 8 * (r / 4) + r % 4;
-              s[sb][r] = key0 + 4 * half + c < 64 && ((bits >> c) & 1) ? s[sb][r] : -INFINITY;
-            }
-        } else {
-          const int left = end - base;
-#pragma unroll
-          for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[sb][r] = 32 * sb + 8 * (r / 4) + r % 4 < left ? s[sb][r] : -INFINITY;
-          if (!TREE && doc) {
+      // Scores x * esc - shift (log2 units, shift the same for a lane's whole tile) to weights.  It stands in each path below that tiles often take: where such paths
+      // meet before it, the compiler copies all 32 scores of a lane, 32 of 250 vector instructions (long prompt 1290 -> 1212 us, drafted trees 129 -> 123).
+      float corr;
+      auto weigh = [&](auto shifted, float shift, float esc) __attribute__((always_inline)) {
+        if (mask) {                                        // weight 0 whatever the score
+          if (TREE && tile == kTreeTile) {
+            const uint64_t bits = path >> (key0 + 4 * half);
 #pragma unroll
             for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-              for (int r4 = 0; r4 < 4; ++r4) {
-                const int4v_t of = *(const lds_int4_t*)(Kk + sb * 32 + 8 * r4 + 4 * half);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[sb][4 * r4 + e] = of[e] == docr ? s[sb][4 * r4 + e] : -INFINITY;
+              for (int r = 0; r < 16; ++r) {
+                const int c = 32 * sb + 8 * (r / 4) + r % 4;
+                x[sb][r] = key0 + 4 * half + c < 64 && ((bits >> c) & 1) ? x[sb][r] : -INFINITY;
               }
+          } else {
+            const int left = end - base;
+#pragma unroll
+            for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) x[sb][r] = 32 * sb + 8 * (r / 4) + r % 4 < left ? x[sb][r] : -INFINITY;
+            if (!TREE && doc) {
+#pragma unroll
+              for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+                for (int r4 = 0; r4 < 4; ++r4) {
+                  const int4v_t of = *(const lds_int4_t*)(Kk + sb * 32 + 8 * r4 + 4 * half);
+#pragma unroll
+                  for (int e = 0; e < 4; ++e) x[sb][4 * r4 + e] = of[e] == docr ? x[sb][4 * r4 + e] : -INFINITY;
+                  __builtin_amdgcn_sched_barrier(0);       // 32 documents at a time would take registers from the tile
+                }
+            }
           }
         }
-      }
-      float top = -INFINITY;
-#pragma unroll
-      for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) top = fmaxf(top, s[sb][r]);
-      top = across_halves(raw ? top * sc : top - shift, MaxOp{});               // the halves' keys are 4 apart, and so are their shifts
-      const float mnew = fmaxf(mrun, top), less = mnew + shift;
-      float esc = raw ? sc : 1.0f;                       // exponent = s * esc - less
-      if (raw && __any(fabsf(mnew) > 0x1p29f && mnew != kLowestScore)) {        // the rounded maximum may lie far beside such a score: scale first
+        float top = -INFINITY;
 #pragma unroll
         for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) s[sb][r] *= sc;
-        esc = 1.0f;
-      }
-      const float corr = __builtin_amdgcn_exp2f(mrun - mnew);
-      mrun = mnew;
-      float sum = 0.f;
+          for (int r = 0; r < 16; ++r) top = fmaxf(top, x[sb][r]);
+        top *= esc;
+        const float mnew = fmaxf(mrun, across_halves(shifted ? top - shift : top, MaxOp{}));     // the halves' keys are 4 apart, and so are their shifts
+        const float less = shifted ? fmaxf(mnew + shift, top) : mnew;          // not below the lane's own maximum, however its sum with a large shift was rounded
+        if (kRaw && __any(fabsf(less) > 0x1p29f && mnew != kLowestScore)) {     // the rounded maximum may lie far beside such a score: scale first
 #pragma unroll
-      for (int sb = 0; sb < NSB; ++sb)
+          for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-        for (int st = 0; st < 2; ++st) {
-          uint32_t w[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float p0 = __builtin_amdgcn_exp2f(fmaf(s[sb][8 * st + 2 * e], esc, -less));
-            const float p1 = __builtin_amdgcn_exp2f(fmaf(s[sb][8 * st + 2 * e + 1], esc, -less));
-            w[e] = pack_bf16x2(p0, p1);
-            sum += p0 + p1;                              // float32 sum of the unrounded weights
-          }
-          pf[sb][st] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+            for (int r = 0; r < 16; ++r) x[sb][r] *= esc;
+          esc = 1.0f;
         }
-      lrun = lrun * corr + sum;
+        corr = __builtin_amdgcn_exp2f(mrun - mnew);
+        mrun = mnew;
+        float sum = 0.f;
+#pragma unroll
+        for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+          for (int st = 0; st < 2; ++st) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float p0 = __builtin_amdgcn_exp2f(fmaf(x[sb][8 * st + 2 * e], esc, -less));
+              const float p1 = __builtin_amdgcn_exp2f(fmaf(x[sb][8 * st + 2 * e + 1], esc, -less));
+              w[e] = pack_bf16x2(p0, p1);
+              sum += p0 + p1;                              // float32 sum of the unrounded weights
+            }
+            pf[sb][st] = __builtin_bit_cast(bf16x8_t, make_uint4(w[0], w[1], w[2], w[3]));
+          }
+        lrun = lrun * corr + sum;
+      };
+      auto bias_table = [&](float by) __attribute__((always_inline)) {           // positions of the tile's keys
+#pragma unroll
+        for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+          for (int r4 = 0; r4 < 4; ++r4) {
+            const int4v_t at = *(const lds_int4_t*)(Kk + sb * 32 + 8 * r4 + 4 * half);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[sb][4 * r4 + e] = fmaf(-by, fabsf((float)(mine - at[e])), x[sb][4 * r4 + e]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+      };
+      auto bias_behind = [&](float by) __attribute__((always_inline)) {          // no key that a row sees lies behind it: -by (away - c), of which by * away is the shift
+#pragma unroll
+        for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x[sb][r] = fmaf(by, (float)(32 * sb + 8 * (r / 4) + r % 4), x[sb][r]);
+      };
+      const float away = (float)(mine - base);
+      auto bias_away = [&](float by) __attribute__((always_inline)) {
+#pragma unroll
+        for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) x[sb][r] = fmaf(-by, fabsf(away - (float)(32 * sb + 8 * (r / 4) + r % 4)), x[sb][r]);
+      };
+      const bool by_table = TREE && (a.pos || tile == kTreeTile), behind = !TREE && a.causal && tile >= first;
+      if constexpr (FORM == kRawScore) {
+        weigh(kNoShift, 0.f, sc);
+      } else if constexpr (FORM == kRawBiased) {
+        if (by_table) {
+          bias_table(slope_raw);
+          weigh(kNoShift, 0.f, sc);
+        } else if (behind) {
+          bias_behind(slope_raw);
+          weigh(kShift, slope * away, sc);
+        } else {
+          bias_away(slope_raw);
+          weigh(kNoShift, 0.f, sc);
+        }
+      } else {
+        constexpr bool kOneWay = TREE && D == 64;          // two copies would spill there
+        float most = 0.f;
+#pragma unroll
+        for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(x[sb][r]));
+        if (!kBiased && __all(most < cap_short)) {         // as a rule: the series in the unscaled score, what it leaves out below 2^-21 of it
+#pragma unroll
+          for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float w = x[sb][r] * x[sb][r];
+              x[sb][r] *= fmaf(fmaf(w, cap2, cap1), w, sc);
+            }
+          if (!kOneWay) weigh(kNoShift, 0.f, 1.0f);
+        } else {
+          if (__all(most < cap_small)) {                   // one term more
+#pragma unroll
+            for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                const float w = x[sb][r] * x[sb][r];
+                x[sb][r] *= fmaf(fmaf(fmaf(w, cap3, cap2), w, cap1), w, sc);
+              }
+          } else if (a.cap != 0.f) {
+#pragma unroll
+            for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) {
+                x[sb][r] = tanh_either(x[sb][r] * to_u) * back;
+                if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);             // 32 of them at a time would take registers from the tile
+              }
+          } else {
+#pragma unroll
+            for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+              for (int r = 0; r < 16; ++r) x[sb][r] *= sc;
+          }
+          if (kBiased) {
+            if (by_table) bias_table(slope);
+            else bias_away(slope);
+          }
+          if (!kOneWay) weigh(kNoShift, 0.f, 1.0f);
+        }
+        if (kOneWay) weigh(kNoShift, 0.f, 1.0f);
+      }
       if (__any(corr != 1.0f)) {                         // after the first tiles the maximum of a row seldom moves
 #pragma unroll
         for (int tb = 0; tb < TB; ++tb)
@@ -473,11 +530,14 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
       }
 
       if (odd_tile) {
+        int at = lane;                                     // the compiler shall not keep this block's addresses in registers all along
+        asm volatile("" : "+v"(at));
+        const int up = at / 32;
         // which keys hold such a value: a key per lane
         bool odd = false;
-        if (lane < KB / KS) {
+        if (at < KB / KS) {
 #pragma unroll 1
-          for (int f = 0; f < D; f += 2) odd |= bf16_odd(*(const __attribute__((address_space(3))) uint32_t*)(Vc + lane * Lds::kRow + f * 2));
+          for (int f = 0; f < D; f += 2) odd |= bf16_odd(*(const __attribute__((address_space(3))) uint32_t*)(Vc + at * Lds::kRow + f * 2));
         }
         const uint64_t odd_keys = __ballot(odd);
         uint32_t lo = 0, hi = 0;                         // keys under a weight that is not 0: this half's, then both
@@ -493,8 +553,8 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
               if (sb == 0) lo |= bit; else hi |= bit;
             }
           }
-        lo <<= 4 * half;
-        hi <<= 4 * half;
+        lo <<= 4 * up;
+        hi <<= 4 * up;
         lo |= __shfl_xor(lo, 32, kWave);
         hi |= __shfl_xor(hi, 32, kWave);
         const uint64_t under = (uint64_t)hi << 32 | lo;
@@ -502,7 +562,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
         for (uint64_t left = odd_keys; left; left &= left - 1) {
           const int k = __builtin_ctzll(left);
           const bool takes = (under >> k) & 1;
-          const lds_byte_t* vr = Vc + k * Lds::kRow + 8 * half;
+          const lds_byte_t* vr = Vc + k * Lds::kRow + 8 * up;
           const int swz = Lds::swz_v(k);
 #pragma unroll
           for (int tb = 0; tb < TB; ++tb)
@@ -510,6 +570,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
             for (int r = 0; r < 16; ++r) {
               const uint32_t v = *(const lds_bf16_t*)(vr + ((tb * 4 + r / 4) ^ swz) * 16 + r % 4 * 2);
               o_acc[tb][r] += takes & ((v & 0x7f80) == 0x7f80) ? __uint_as_float(v << 16) : 0.f;
+              if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);     // more of them at a time would take registers from every tile
             }
         }
         wait_lgkmcnt0();
@@ -517,7 +578,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
         asm volatile("" ::: "memory");
 #pragma unroll
         for (int t = 0; t < kPer; ++t) {                   // the product runs on the others
-          lds_bf16_t* const v = (lds_bf16_t*)(Vs + cur * Lds::kTile + (t * 4 + wave) * 1024 + lane * 16);
+          lds_bf16_t* const v = (lds_bf16_t*)(Vs + cur * Lds::kTile + (t * 4 + wave) * 1024 + at * 16);
 #pragma unroll 1
           for (int e = 0; e < 8; ++e)
             if ((v[e] & 0x7f80) == 0x7f80) v[e] = 0;
@@ -618,9 +679,9 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
   if (TREE && a.lse && quad0 == 0 && half == 0) a.lse[(mb * a.N + token) * a.heads + h] = none ? -INFINITY : (mtot + __builtin_amdgcn_logf(ltot)) * kLn2;
 }
 
-template <int D, int KS, bool TREE>
+template <int D, int KS, bool TREE, int FORM>
 __global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
-  decoder_tiles<D, KS, TREE>(a, (const bf16_t*)a.Q, row_blocks, splits, chunk);
+  decoder_tiles<D, KS, TREE, FORM>(a, (const bf16_t*)a.Q, row_blocks, splits, chunk);
 }
 
 // Sums of the chunks of one row: D / 4 lanes hold its features, 4 each, and SHARE such groups of lanes take every SHARE-th chunk.  Maxima and sums in log2

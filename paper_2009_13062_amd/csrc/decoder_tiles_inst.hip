@@ -9,13 +9,13 @@
 namespace nf {
 namespace {
 
-template <int D, int KS, bool TREE>
-nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
+template <int D, int KS, bool TREE, int FORM>
+nf_status go_form(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   constexpr int kRows = 4 / KS * 32, kBytes = DecLds<D, 64 * KS>::kBytes;
   const long long R = (long long)a.N * (a.heads / a.kv), row_blocks = (R + kRows - 1) / kRows;
   const long long total = prod({a.M, a.B, a.kv, row_blocks, splits});
   if (total > kMaxGrid) return NF_EUNSUPPORTED;
-  const auto kernel = decoder_tiles_kernel<D, KS, TREE>;
+  const auto kernel = decoder_tiles_kernel<D, KS, TREE, FORM>;
   static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
   if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) != hipSuccess) return NF_ELAUNCH;
@@ -23,6 +23,13 @@ nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   }
   nf_launch(kernel, dim3((unsigned)total), dim3(256), kBytes, s, a, (int)row_blocks, splits, chunk);
   return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH;
+}
+
+template <int D, int KS, bool TREE>
+nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
+  const bool raw = a.cap == 0.f && a.scale >= 1e-12f && a.scale <= 1e12f;          // a scale that the bias can be divided by
+  if (a.slope) return raw ? go_form<D, KS, TREE, kRawBiased>(a, splits, chunk, s) : go_form<D, KS, TREE, kAnyBiased>(a, splits, chunk, s);
+  return raw ? go_form<D, KS, TREE, kRawScore>(a, splits, chunk, s) : go_form<D, KS, TREE, kAnyScore>(a, splits, chunk, s);
 }
 
 }  // namespace

@@ -192,6 +192,17 @@ def test_prompt_infinite_values_add_up(nf, dtype, d):
     assert (got[300:350, 3] == float("inf")).all() and got[350:, 3].isnan().all() and (got[333:, 0] == -float("inf")).all()
 
 
+@pytest.mark.parametrize("dtype", (BF, F32))
+@pytest.mark.parametrize("causal", (True, False))
+@pytest.mark.parametrize("slope, cap", ((1e6, 0.0), (1e12, 0.0), (1e6, 30.0)))
+def test_prompt_steep_slopes(nf, dtype, causal, slope, cap):
+    """Every other key weighs nothing: a row gives its own value.  (The weight may be rounded, and the result.)"""
+    Q, K, V = rows(gen(9), 1, 2000, 2, 1, 64, dtype)
+    got = nf.attention_prompt(Q, K, V, 1, 2000, 2, 1, causal=causal, cap=cap, slope=torch.full((1, 2), slope, device="cuda"))
+    want = V.cpu().double().repeat(1, 1, 2)
+    near(got, want, want.abs() * (2 * 2.0 ** -8 if dtype == BF else 4 * 2.0 ** -24), "O")
+
+
 def test_prompt_far_rows(nf):
     """Rows more than 2^31 elements and 2^32 bytes into a buffer."""
     M, S, heads, d = 2, 100, 1, 64
