@@ -203,6 +203,29 @@ def test_prompt_steep_slopes(nf, dtype, causal, slope, cap):
     near(got, want, want.abs() * (2 * 2.0 ** -8 if dtype == BF else 4 * 2.0 ** -24), "O")
 
 
+FORMS = {"plain": dict(), "biased": dict(slope=True), "capped": dict(cap=5.0), "capped and biased": dict(cap=5.0, slope=True), "negative scale": dict(scale=-0.1), "negative scale, biased": dict(scale=-0.1, slope=True)}
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (BF, 256), (F32, 64), (F32, 128), (F32, 256)], ids=str)
+def test_prompt_forms_of_scores(nf, dtype, d, form):
+    """Every form of the scores, over documents, with infinities in rows past the length and in keys that some rows see."""
+    g, kw = gen(d), dict(FORMS[form])
+    M, B, S, heads, kv = 2, 2, 140, 4, 2
+    if kw.pop("slope", False):
+        kw["slope"] = slopes(g, M, heads)
+    kw.update(length=ints([[S, 99], [130, S]]), doc=ints((torch.arange(S) // 50).expand(M, B, S)))
+    Q, K, V = (x.contiguous() for x in rows(g, M, B * S, heads, kv, d, dtype))
+    want, tol = plain.prompt(Q, K, V, B, S, heads, kv, **kw)
+    near(nf.attention_prompt(Q, K, V, B, S, heads, kv, **kw), want, tol)
+    V[0, S + 99:], K[0, S + 99:], V[1, 60, :d] = math.nan, math.inf, math.inf
+    got = nf.attention_prompt(Q, K, V, B, S, heads, kv, **kw).cpu()
+    sees = torch.zeros(want.shape, dtype=torch.bool)
+    sees[1, 60:100, :heads // kv * d] = True                  # its own document's later rows, under the heads of the first key head
+    assert (got[sees] == math.inf).all()
+    near(torch.where(sees, 0.0, got.double()), torch.where(sees, 0.0, want), tol)
+
+
 def test_prompt_far_rows(nf):
     """Rows more than 2^31 elements and 2^32 bytes into a buffer."""
     M, S, heads, d = 2, 100, 1, 64
@@ -282,6 +305,15 @@ def test_tree_heads(nf, dtype, T, heads, kv):
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 def test_tree_head_sizes(nf, dtype, d):
     check_tree(nf, gen(d), dtype, 1, 2, 4, 140, 4, 2, d, [[140, 77]], cap=3.0)
+
+
+@pytest.mark.parametrize("T", [3, 6, 13, 20])
+@pytest.mark.parametrize("form", [f for f in FORMS if "scale" not in f])
+@pytest.mark.parametrize("dtype,d", [(BF, 64), (BF, 128), (BF, 256), (F32, 64), (F32, 128), (F32, 256)], ids=str)
+def test_tree_forms_of_scores(nf, dtype, d, form, T):
+    """Every form of the scores with rows of every kernel (12, 24, 52 and 80 to a key head)."""
+    kw = dict(FORMS[form])
+    check_tree(nf, gen(T), dtype, 1, 2, T, 1300, 8, 2, d, [[1300, 70]], **kw)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
@@ -454,6 +486,11 @@ def test_evict(nf, dtype, d, C, budget):
     nf.cache_evict(a, b, None, w, length, budget)             # without positions
     want = plain.evict(Kc, Vc, None, weight, length, budget)
     assert torch.equal(a.cpu(), want[0]) and torch.equal(b.cpu(), want[1]) and torch.equal(w.cpu(), want[3])
+
+
+@pytest.mark.parametrize("C,budget", [(3000, 1000), (20000, 3000), (32769, 32000), (40001, 17)])
+def test_evict_long(nf, C, budget):
+    test_evict(nf, BF, 8, C, budget)
 
 
 def test_evict_odd_weights(nf):
