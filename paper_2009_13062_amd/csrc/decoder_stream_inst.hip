@@ -58,11 +58,14 @@ template <typename T, int D>
 nf_status weigh(const WeighArgs& a, hipStream_t s) {
   constexpr int kKeys = 4 * weigh_keys<T, D>();            // of a workgroup and turn
   const long long heads = prod({a.M, a.B, a.kv}), pieces = ((long long)a.C + kKeys - 1) / kKeys;
-  const int turns = (int)std::max<long long>(1, std::min<long long>(8, prod({heads, pieces}) / 2048));     // as many as leave 8 workgroups per compute unit (one token over 32 caches of 8192 entries, 8 heads of 128, us: 1 turn 118, 2 102, 4 96, 8 95; 32 in a quarter of the workgroups 119)
+  // as many turns as leave 16 workgroups per compute unit (one token over 32 caches of 8192 entries, 8 heads of 128: 4 turns 78 us, 8 81; before four wavefronts fit a SIMD
+  // 1 turn 118, 2 102, 4 96, 8 95, 32 in a quarter of the workgroups 119)
+  const int turns = (int)std::max<long long>(1, std::min<long long>(8, prod({heads, pieces}) / 4096));
   const int per_head = (int)((pieces + turns - 1) / turns);
   const long long blocks = prod({heads, per_head});
   if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
-  nf_launch((weigh_tiles_kernel<T, D>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head, turns);
+  if ((long long)a.n * (a.heads / a.kv) > 16) nf_launch((weigh_tiles_kernel<T, D, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head, turns);
+  else nf_launch((weigh_tiles_kernel<T, D, false>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head, turns);
   return launched();
 }
 
