@@ -715,6 +715,15 @@ __global__ __launch_bounds__(256) void decoder_join_kernel(DecArgs a, int splits
       p[u] = ml[k];
       v[u] = *reinterpret_cast<const f32x4_t*>(o + (long)k * D);
     }
+    // a chunk that is not there is left out by a select, its sums too: these may be infinite, and 0 times them NaN
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const bool there = k0 + u * step < parts;
+      p[u].x = there ? p[u].x : kLowestScore;
+      p[u].y = there ? p[u].y : 0.f;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[u][e] = there ? v[u][e] : 0.f;
+    }
     float most = top;
 #pragma unroll
     for (int u = 0; u < 8; ++u) most = fmaxf(most, p[u].x);
@@ -725,7 +734,7 @@ __global__ __launch_bounds__(256) void decoder_join_kernel(DecArgs a, int splits
     for (int e = 0; e < 4; ++e) acc[e] *= old;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
-      const float c = k0 + u * step < parts ? (LOG2 ? __builtin_amdgcn_exp2f(p[u].x - top) : expf(p[u].x - top)) : 0.f;
+      const float c = LOG2 ? __builtin_amdgcn_exp2f(p[u].x - top) : expf(p[u].x - top);
       sum = fmaf(p[u].y, c, sum);
 #pragma unroll
       for (int e = 0; e < 4; ++e) acc[e] = fmaf(v[u][e], c, acc[e]);
