@@ -411,12 +411,14 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
         top *= esc;
         const float mnew = fmaxf(mrun, across_halves(shifted ? top - shift : top, MaxOp{}));     // the halves' keys are 4 apart, and so are their shifts
         const float less = shifted ? fmaxf(mnew + shift, top) : mnew;          // not below the lane's own maximum, however its sum with a large shift was rounded
-        if (kRaw && __any(fabsf(less) > 0x1p29f && mnew != kLowestScore)) {     // the rounded maximum may lie far beside such a score: scale first
+        const bool large = fabsf(less) > 0x1p29f && mnew != kLowestScore;       // the rounded maximum may lie far beside such a score: scale first
+        if (kRaw && __any(large)) {
+          const float by = large ? esc : 1.0f;             // by the row's own maximum: the others' scores keep their bits
 #pragma unroll
           for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[sb][r] *= esc;
-          esc = 1.0f;
+            for (int r = 0; r < 16; ++r) x[sb][r] *= by;
+          esc = large ? 1.0f : esc;
         }
         corr = __builtin_amdgcn_exp2f(mrun - mnew);
         mrun = mnew;
