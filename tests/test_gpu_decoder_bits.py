@@ -5,7 +5,7 @@ import torch
 
 pytestmark = pytest.mark.gpu
 BF, F32 = torch.bfloat16, torch.float32
-FORMS = {"plain": (0.0, False), "biased": (0.0, True)}
+FORMS = {"plain": (0.0, False), "biased": (0.0, True), "cap 5": (5.0, False), "cap 50": (50.0, False), "cap 5 biased": (5.0, True), "cap 50 biased": (50.0, True)}
 TYPES = [(BF, 64), (BF, 128), (BF, 256), (BF, 20), (F32, 64), (F32, 128)]
 
 
@@ -73,7 +73,7 @@ def test_tree_rows_keep_their_bits(nf, dtype, d, T, form, factor):
     assert not different(lse.cpu()[0][keep], ok_lse[keep])
 
 
-@pytest.mark.parametrize("cap", [0.0])
+@pytest.mark.parametrize("cap", [0.0, 5.0, 50.0])
 @pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
 def test_a_row_alone_has_the_bits_that_it_has_among_others(nf, dtype, cap):
     """Cached tokens and prompts, where neighbours of a tile hold scores of every size: each model alone against all of them."""
