@@ -324,18 +324,19 @@ __global__ __launch_bounds__(NT) void evict_select_held_kernel(EvictArgs a) {
   }
 }
 
-// The pairs of the lists: rows of keys and values, position and weight.  Sources lie at or above the budget, targets below it, each once.
+// The pairs of the lists: rows of keys and values, position and weight.  Sources lie at or above the budget, targets below it, each once.  Lists are bounded where they
+// are read: a workspace that another call writes at the same time gives wrong entries, no address outside the cache.
 template <typename U>
 __global__ __launch_bounds__(256) void evict_move_kernel(EvictArgs a, int rows, int blocks_per_head) {
   const long head = blockIdx.x / blocks_per_head;
   const int* count = a.ws + head * (1 + 2 * (long)a.most);
   const int* holes = count + 1;
   const int* movers = holes + a.most;
-  const int i0 = (int)(blockIdx.x % blocks_per_head) * rows, end = min(i0 + rows, *count);
+  const int i0 = (int)(blockIdx.x % blocks_per_head) * rows, end = min(i0 + rows, clamp_len(*count, a.most));
   U* Kh = (U*)a.Kc + head * a.C * a.units;
   U* Vh = (U*)a.Vc + head * a.C * a.units;
   for (int i = i0 + (int)threadIdx.x / a.units, u = (int)threadIdx.x % a.units; i < end;) {
-    const long to = holes[i], from = movers[i];
+    const long to = clamp_len(holes[i], a.C - 1), from = clamp_len(movers[i], a.C - 1);
     Kh[to * a.units + u] = Kh[from * a.units + u];
     Vh[to * a.units + u] = Vh[from * a.units + u];
     if (u == 0) {

@@ -3,7 +3,8 @@
 Argument marshalling only, as in the package's ``__init__``, which exports these functions.  Rows (Q, K, V) are [M, B*N, heads*d]
 tensors whose last dimension is contiguous: dense, or column blocks of one packed projection (``qkv[..., :heads*d]``).  Caches,
 lengths and every other operand are contiguous; integers are int32, slopes, weights and lse float32.  All operands live on the
-current device.
+current device.  With ``stream=`` a call runs there and takes its own memory there: that stream has to be behind whatever writes the
+operands, and operands are to be kept, and results not read elsewhere, until it has passed the call.
 """
 from __future__ import annotations
 
@@ -72,12 +73,21 @@ def _cache_shape(Kc, Vc, dtype):
     return tuple(Kc.shape), _dense(Kc, "Kc", Kc.shape, dtype), _dense(Vc, "Vc", Kc.shape, dtype)
 
 
-def _kept_until(stream, *tensors) -> None:
-    """Memory that a call on a given stream allocated is not handed out again before that stream has passed the call."""
+def _own(stream, shape, dtype, device):
+    """Memory of a call's own: from the pool of the stream that the call runs on.  A block of the current stream's pool may still be in use by work
+    that is queued there, which nothing would hold the given stream back from."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _output(stream, shape, dtype, device):
+    """The same for a result, which the caller goes on to use on the current stream: freed, it is not handed out again before that stream has passed."""
+    t = _own(stream, shape, dtype, device)
     if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
+        t.record_stream(torch.cuda.current_stream())
+    return t
 
 
 def attention_prompt(Q, K, V, B, S, heads, kv_heads=None, causal=True, scale=None, cap=0.0, slope=None, length=None, prefix=None, doc=None, out=None, stream=None):
@@ -98,12 +108,10 @@ def attention_prompt(Q, K, V, B, S, heads, kv_heads=None, causal=True, scale=Non
     k, v, km, kr = _key_value_rows(K, V, M, B * S, kv_heads * d, Q.dtype)
     small = (_dense(slope, "slope", (M, heads), torch.float32), _dense(length, "length", (M, B), torch.int32), _dense(prefix, "prefix", (M, B), torch.int32),
              _dense(doc, "doc", (M, B, S), torch.int32))
-    O = torch.empty((M, B * S, heads * d), dtype=Q.dtype, device=Q.device) if out is None else out
+    O = _output(stream, (M, B * S, heads * d), Q.dtype, Q.device) if out is None else out
     nf._check("netfuse_attention_prompt", nf.lib.netfuse_attention_prompt(
         q, k, v, *small, _dense(O, "out", (M, B * S, heads * d), Q.dtype), M, B, S, heads, kv_heads, d, qm, qr, km, kr, int(bool(causal)),
         float(d ** -0.5 if scale is None else scale), float(cap), dt, nf._stream(stream)))
-    if out is None:
-        _kept_until(stream, O)
     return O
 
 
@@ -115,10 +123,10 @@ def attention_tree_workspace(M, B, T, C, heads, kv_heads, d, dtype=torch.bfloat1
     return n
 
 
-def _workspace(workspace, need, device):
+def _workspace(workspace, need, device, stream):
     """The caller's workspace, or one of this call; its address and size."""
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device) if need else None
+        workspace = _own(stream, need, torch.uint8, device) if need else None
     else:
         _on_current(workspace)
         if not workspace.is_contiguous():
@@ -150,13 +158,12 @@ def attention_tree(Q, K, V, Kc, Vc, length, start=None, parent=None, nodes=None,
     small = (_dense(pos, "pos", (M, B, kv_heads, C), torch.int32), _dense(length, "length", (M, B), torch.int32), _dense(start, "start", (M, B), torch.int32),
              _dense(parent, "parent", (M, B, T), torch.int32), _dense(nodes, "nodes", (M, B), torch.int32), _dense(slope, "slope", (M, heads), torch.float32))
     z = _dense(lse, "lse", (M, B * T, heads), torch.float32)
-    O = torch.empty((M, B * T, heads * d), dtype=Q.dtype, device=Q.device) if out is None else out
+    O = _output(stream, (M, B * T, heads * d), Q.dtype, Q.device) if out is None else out
     o = _dense(O, "out", (M, B * T, heads * d), Q.dtype)
     need = max(0, nf.lib.netfuse_attention_tree_workspace(M, B, T, C, heads, kv_heads, d, dt))
-    ws, ws_ptr, ws_bytes = _workspace(workspace, need, Q.device)
+    ws, ws_ptr, ws_bytes = _workspace(workspace, need, Q.device, stream)
     nf._check("netfuse_attention_tree", nf.lib.netfuse_attention_tree(
         q, k, v, kc, vc, *small, o, z, ws_ptr, ws_bytes, M, B, T, C, heads, kv_heads, d, qm, qr, km, kr, float(d ** -0.5 if scale is None else scale), float(cap), dt, nf._stream(stream)))
-    _kept_until(stream, O if out is None else None, ws if workspace is None else None)
     return O
 
 
@@ -199,15 +206,13 @@ def cache_weigh(Q, lse, Kc, weight, length, start=None, index=None, count=None, 
     if lse is None or weight is None or length is None:
         raise ValueError("lse, weight and length are required")
     q, qm, qr = _rows(Q, "Q", M, B * T, heads * d, Q.dtype)
-    W = torch.empty_like(weight) if out is None else out
+    small = (_dense(lse, "lse", (M, B * T, heads), torch.float32), _dense(index, "index", (M, B, n), torch.int32), _dense(count, "count", (M, B), torch.int32),
+             _dense(Kc, "Kc", Kc.shape, Q.dtype), _dense(pos, "pos", (M, B, kv_heads, C), torch.int32), _dense(length, "length", (M, B), torch.int32),
+             _dense(start, "start", (M, B), torch.int32), _dense(slope, "slope", (M, heads), torch.float32), _dense(weight, "weight", (M, B, kv_heads, C), torch.float32))
+    W = _output(stream, (M, B, kv_heads, C), torch.float32, Q.device) if out is None else out
     nf._check("netfuse_cache_weigh", nf.lib.netfuse_cache_weigh(
-        q, _dense(lse, "lse", (M, B * T, heads), torch.float32), _dense(index, "index", (M, B, n), torch.int32), _dense(count, "count", (M, B), torch.int32),
-        _dense(Kc, "Kc", Kc.shape, Q.dtype), _dense(pos, "pos", (M, B, kv_heads, C), torch.int32), _dense(length, "length", (M, B), torch.int32),
-        _dense(start, "start", (M, B), torch.int32), _dense(slope, "slope", (M, heads), torch.float32), _dense(weight, "weight", (M, B, kv_heads, C), torch.float32),
-        _dense(W, "out", (M, B, kv_heads, C), torch.float32), M, B, T, n, C, heads, kv_heads, d, qm, qr, float(d ** -0.5 if scale is None else scale), float(cap),
+        q, *small, _dense(W, "out", (M, B, kv_heads, C), torch.float32), M, B, T, n, C, heads, kv_heads, d, qm, qr, float(d ** -0.5 if scale is None else scale), float(cap),
         nf._dt(Q), nf._stream(stream)))
-    if out is None:
-        _kept_until(stream, W)
     return W
 
 
@@ -235,8 +240,7 @@ def cache_evict(Kc, Vc, pos, weight, length, budget, start=None, recent=0, pos_o
     small = (_dense(pos, "pos", shape, torch.int32), _dense(weight, "weight", shape, torch.float32), _dense(length, "length", (M, B), torch.int32),
              _dense(start, "start", (M, B), torch.int32), _dense(pos_out, "pos_out", shape, torch.int32), _dense(weight_out, "weight_out", shape, torch.float32))
     need = max(0, nf.lib.netfuse_cache_evict_workspace(M, B, C, kv_heads, budget))
-    ws, ws_ptr, ws_bytes = _workspace(workspace, max(need, 4), Kc.device)
+    ws, ws_ptr, ws_bytes = _workspace(workspace, max(need, 4), Kc.device, stream)
     nf._check("netfuse_cache_evict", nf.lib.netfuse_cache_evict(
         kc, vc, *small, ws_ptr, ws_bytes, M, B, C, kv_heads, d, int(budget), int(recent), nf._dt(Kc), nf._stream(stream)))
-    _kept_until(stream, ws if workspace is None else None)
     return pos_out, weight_out
