@@ -51,7 +51,7 @@ bool pieces_ok(const DecArgs& a, nf_dtype dt) {
 template <bool TREE>
 nf_status launch_rows(const DecArgs& a, nf_dtype dt, hipStream_t s) {
   const long long blocks = (prod({a.M, a.B, a.heads, a.N}) + 3) / 4;
-  if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
+  if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
 #define NF_ROWS(T, DPL) nf_launch((decoder_rows_kernel<T, DPL, TREE>), dim3((unsigned)blocks), dim3(256), 0, s, a)
   if (dt == NF_F32) {
     if (a.d <= 64) NF_ROWS(float, 1); else if (a.d <= 128) NF_ROWS(float, 2); else NF_ROWS(float, 4);
@@ -142,6 +142,7 @@ nf_status netfuse_attention_tree(const void* Q, const void* K, const void* V, co
   a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
   if (pieces_ok(a, dt)) {
     const int rows = T * (heads / kv_heads), chunk = tree_chunk(rows, dt), splits = (int)(((long long)C + chunk - 1) / chunk);
+    if (splits > 1 && !grid_fits(tree_join_blocks(a, splits), 256)) return NF_EUNSUPPORTED;      // before the first of the two is enqueued
     // Many rows of bfloat16 take their keys through LDS, few ones straight into registers (16 caches of 4096 entries, groups of 4, us, registers / LDS: 8 key heads of 128 features, 20 rows
     // 53 / 66, 36 66 / 56, 64 67 / 58; 8 of 64, 20 rows 41 / 37; 4 of 256, 20 rows 68 / 85, 36 76 / 78; 32 caches of 700, 8 key heads of 128, 18 rows 25 / 29, 64 features 20.6 / 18.3).
     const bool tiles = dt == NF_BF16 && rows > (d <= 64 ? 16 : 32);
@@ -174,7 +175,7 @@ nf_status netfuse_cache_append(const void* K, const void* V, const int* index, c
   const int rows = (int)std::max<long long>(1, std::min<long long>(n, 1024 / per_row));       // about 4 pieces per thread and tensor
   const int per_seq = (n + rows - 1) / rows;
   const long long blocks = prod({M, B, per_seq});
-  if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
+  if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
 #define NF_APPEND(U) nf_launch((cache_append_kernel<U>), dim3((unsigned)blocks), dim3(256), 0, s, a, rows, per_seq)
   if (wide) NF_APPEND(uint4); else if (esz == 4) NF_APPEND(uint32_t); else NF_APPEND(uint16_t);
@@ -203,7 +204,7 @@ nf_status netfuse_cache_weigh(const void* Q, const float* lse, const int* index,
     return launch_weigh_tiles(a, dt, (hipStream_t)stream);
   const int per_head = (int)((C + 255LL) / 256);
   const long long blocks = prod({M, B, kv_heads, per_head});
-  if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
+  if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   if (dt == NF_F32) nf_launch((weigh_rows_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head);
   else nf_launch((weigh_rows_kernel<bf16_t>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head);
@@ -237,17 +238,24 @@ nf_status netfuse_cache_evict(void* Kc, void* Vc, const int* pos, const float* w
   const int rows = std::max(1, 256 / a.units);                             // a piece of each tensor per thread
   const int per_head = std::max(1, (a.most + rows - 1) / rows);
   const long long blocks = prod({heads, per_head});
-  if (heads > kMaxGrid || blocks > kMaxGrid) return NF_EUNSUPPORTED;
+  const bool moves = C <= 1024 && wide && (long long)a.most * a.units <= 4096;
+  if (!grid_fits(heads, C <= 4096 ? 256 : 1024) || (!moves && !grid_fits(blocks, 256))) return NF_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   // Small heads: the workgroup that picks the entries moves them too, as long as a head's rows are a few loads per thread (192 heads of 1024 entries cut to 896: 13.6 us by two
   // kernels, 12.8 by one).  Up to 32768 entries a head's weights stay in registers, of as few threads and as few to a thread as hold them (us, whole evictions: 128 heads of
   // 32768 147, by the kernel that reads them again for each digit 192; 128 / 768 heads of 6000, 8 or 32 to a thread 59 / 103 and 70 / 145; of 4096, 256 or 1024 threads
   // 53 / 73 and 48 / 76, of 2048 33 / 41 and 30 / 45).
-  if (C <= 1024 && wide && (long long)a.most * a.units <= 4096) return select_held<256, 4, true, uint4>(a, heads, s);
-  const nf_status st = C <= 1024 ? select_held<256, 4>(a, heads, s) : C <= 4096 ? select_held<256, 16>(a, heads, s) : C <= 8192 ? select_held<1024, 8>(a, heads, s)
-                       : C <= 32768 ? select_held<1024, 32>(a, heads, s) : NF_EUNSUPPORTED;
-  if (st == NF_ELAUNCH) return st;
-  if (st == NF_EUNSUPPORTED) nf_launch(evict_select_kernel, dim3((unsigned)heads), dim3(1024), 0, s, a);
+  if (moves) return select_held<256, 4, true, uint4>(a, heads, s);
+  nf_status st;
+  if (C <= 1024) st = select_held<256, 4>(a, heads, s);
+  else if (C <= 4096) st = select_held<256, 16>(a, heads, s);
+  else if (C <= 8192) st = select_held<1024, 8>(a, heads, s);
+  else if (C <= 32768) st = select_held<1024, 32>(a, heads, s);
+  else {
+    nf_launch(evict_select_kernel, dim3((unsigned)heads), dim3(1024), 0, s, a);
+    st = launched();
+  }
+  if (st != NF_OK) return st;                              // without its lists nothing moves
   if (a.most > 0) {
 #define NF_MOVE(U) nf_launch((evict_move_kernel<U>), dim3((unsigned)blocks), dim3(256), 0, s, a, rows, per_head)
     if (wide) NF_MOVE(uint4); else if (esz == 4) NF_MOVE(uint32_t); else NF_MOVE(uint16_t);

@@ -20,6 +20,7 @@ nf_status launch_tree_tiles(const DecArgs& a, int chunk, int splits, hipStream_t
 // decoder_stream.h: float32 prompts, trees of either type
 nf_status launch_prompt_stream(const DecArgs& a, hipStream_t s);
 nf_status launch_tree_stream(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s);
+long long tree_join_blocks(const DecArgs& a, int splits);       // workgroups of 256
 nf_status launch_tree_join(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s);
 nf_status launch_weigh_tiles(const WeighArgs& a, nf_dtype dt, hipStream_t s);
 

@@ -18,7 +18,7 @@ nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   constexpr int kRows = 4 / KS * RT * 16, kBytes = stream_lds_bytes(RT, KS, D / 16);
   const long long R = (long long)a.N * (a.heads / a.kv), row_blocks = (R + kRows - 1) / kRows;
   const long long total = prod({a.M, a.B, a.kv, row_blocks, splits});
-  if (total > kMaxGrid) return NF_EUNSUPPORTED;
+  if (!grid_fits(total, 256)) return NF_EUNSUPPORTED;
   const auto kernel = decoder_stream_kernel<T, D, RT, KS, TREE>;
   static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
   if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {
@@ -63,7 +63,7 @@ nf_status weigh(const WeighArgs& a, hipStream_t s) {
   const int turns = (int)std::max<long long>(1, std::min<long long>(8, prod({heads, pieces}) / 4096));
   const int per_head = (int)((pieces + turns - 1) / turns);
   const long long blocks = prod({heads, per_head});
-  if (blocks > kMaxGrid) return NF_EUNSUPPORTED;
+  if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
   if ((long long)a.n * (a.heads / a.kv) > 16) nf_launch((weigh_tiles_kernel<T, D, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head, turns);
   else nf_launch((weigh_tiles_kernel<T, D, false>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head, turns);
   return launched();
@@ -80,13 +80,16 @@ nf_status launch_tree_stream(const DecArgs& a, int chunk, int splits, nf_dtype d
   return a.d <= 64 ? tree<bf16_t, 64>(a, splits, chunk, s) : a.d <= 128 ? tree<bf16_t, 128>(a, splits, chunk, s) : tree<bf16_t, 256>(a, splits, chunk, s);
 }
 
-nf_status launch_tree_join(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s) {
+// Up to 8 chunks a row's are loads of one group of lanes at a time; above that the groups of a workgroup share them (two caches of 196 chunks, whole call 142 us, by one group 162).
+long long tree_join_blocks(const DecArgs& a, int splits) {
   const long long rows = prod({a.M, a.B, a.heads, a.N});
+  return splits > 8 ? rows : (prod({rows, tree_features(a.d) / 4}) + 255) / 256;
+}
+
+nf_status launch_tree_join(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s) {
   const int features = tree_features(a.d);
-  // Up to 8 chunks a row's are loads of one group of lanes at a time; above that the groups of a workgroup share them (two caches of 196 chunks, whole call 142 us, by one group 162).
   const bool shared = splits > 8;
-  const long long blocks = shared ? rows : (rows * (features / 4) + 255) / 256;
-  if (rows > kMaxGrid) return NF_EUNSUPPORTED;
+  const long long blocks = tree_join_blocks(a, splits);
 #define NF_JOIN(T, D, LOG2)                                                                                                              \
   if (shared) nf_launch((decoder_join_kernel<T, D, LOG2, 1024 / D>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk);         \
   else nf_launch((decoder_join_kernel<T, D, LOG2, 1>), dim3((unsigned)blocks), dim3(256), 0, s, a, splits, chunk)

@@ -14,7 +14,7 @@ nf_status go_form(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   constexpr int kRows = 4 / KS * 32, kBytes = DecLds<D, 64 * KS>::kBytes;
   const long long R = (long long)a.N * (a.heads / a.kv), row_blocks = (R + kRows - 1) / kRows;
   const long long total = prod({a.M, a.B, a.kv, row_blocks, splits});
-  if (total > kMaxGrid) return NF_EUNSUPPORTED;
+  if (!grid_fits(total, 256)) return NF_EUNSUPPORTED;
   const auto kernel = decoder_tiles_kernel<D, KS, TREE, FORM>;
   static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
   if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {

@@ -24,5 +24,7 @@ inline long long prod(std::initializer_list<long long> v) {
 }
 constexpr long long kMaxElems = (1LL << 62);     // element counts must stay below this
 constexpr long long kMaxGrid = 0x7fffffffLL;
+// HIP counts the threads of a grid in 32 bits: whether it takes so many workgroups of so many threads
+inline bool grid_fits(long long blocks, int threads) { return blocks <= 0xffffffffLL / threads; }
 
 }  // namespace nf
