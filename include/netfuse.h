@@ -205,7 +205,7 @@ nf_status netfuse_attention_relpos(const void* Q, const void* K, const void* V, 
  *   - Integer operands are DEVICE arrays that the kernels bound: a length, count or number of nodes below 0 counts as 0, above its range as the
  *     largest.  No call changes len or start: after an append the caller adds the counts, after an eviction it takes min(len, budget).
  *   - NF_EUNSUPPORTED for d > 256, and for sizes that would take 2^32 threads or more in one launch.  The kernels on the matrix pipe need d, strides and pointers in multiples of 16 bytes and 64 rows of K and V within
- *     2 GB; everything else takes slower general ones.
+ *     2 GB, and with bfloat16 and a cap |scale| / cap within 1e-37 ... 1e38; everything else takes slower general ones.
  *   - Sums, maxima and scores are float32; with bfloat16 storage the attention weights are rounded to bfloat16 for the product with V, as the result is.
  *   - A sequence's bits depend neither on the models and sequences that are merged with it nor on C.
  */

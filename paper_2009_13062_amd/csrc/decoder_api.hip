@@ -42,9 +42,15 @@ bool pieces_strides(long stride_m, long stride_row, nf_dtype dt) {
   const int n = dt == NF_F32 ? 4 : 8;
   return stride_m % n == 0 && stride_row % n == 0;
 }
+// The bfloat16 kernels on the matrix pipe take scale / cap in one factor, which has to be a normal number.  (Two factors there cost 4 % of the weights of a capped token;
+// the general kernels have them.)
+bool ratio_ok(float scale, float cap, nf_dtype dt) {
+  const double r = cap != 0.f ? fabs((double)scale) / cap : 0.0;
+  return dt == NF_F32 || r == 0.0 || (r > 1e-37 && r < 1e38);
+}
 bool pieces_ok(const DecArgs& a, nf_dtype dt) {
   // 64 rows of keys within 31 bits of bytes: a tile's offsets
-  return a.kv_stride_row < (1L << 31) / 64 / (dt == NF_F32 ? 4 : 2) && pieces_sizes(a.N, a.heads, a.kv, a.d, dt) && pieces_strides(a.q_stride_m, a.q_stride_row, dt) && pieces_strides(a.kv_stride_m, a.kv_stride_row, dt) &&
+  return ratio_ok(a.scale, a.cap, dt) && a.kv_stride_row < (1L << 31) / 64 / (dt == NF_F32 ? 4 : 2) && pieces_sizes(a.N, a.heads, a.kv, a.d, dt) && pieces_strides(a.q_stride_m, a.q_stride_row, dt) && pieces_strides(a.kv_stride_m, a.kv_stride_row, dt) &&
          aligned(a.Q, 16) && aligned(a.K, 16) && aligned(a.V, 16) && aligned(a.Kc, 16) && aligned(a.Vc, 16) && aligned(a.O, 16);
 }
 
@@ -200,7 +206,7 @@ nf_status netfuse_cache_weigh(const void* Q, const float* lse, const int* index,
   if (d > 256) return NF_EUNSUPPORTED;
   WeighArgs a = {Q, lse, index, count, Kc, pos, len, start, slope, weight, weight_out, M, B, T, n, C, heads, kv_heads, d,
                  q_stride_m, q_stride_row, scale, cap, cap != 0.f ? 1.f / cap : 0.f};
-  if (pieces_sizes(n, heads, kv_heads, d, dt) && pieces_strides(q_stride_m, q_stride_row, dt) && aligned(Q, 16) && aligned(Kc, 16))
+  if (ratio_ok(scale, cap, dt) && pieces_sizes(n, heads, kv_heads, d, dt) && pieces_strides(q_stride_m, q_stride_row, dt) && aligned(Q, 16) && aligned(Kc, 16))
     return launch_weigh_tiles(a, dt, (hipStream_t)stream);
   const int per_head = (int)((C + 255LL) / 256);
   const long long blocks = prod({M, B, kv_heads, per_head});
