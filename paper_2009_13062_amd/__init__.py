@@ -138,7 +138,7 @@ try:
                  _address(lib.netfuse_attention), _address(lib.netfuse_attention_relpos), _address(lib.netfuse_conv2d))
     _native.bind_decoder(*[_address(getattr(lib, "netfuse_" + f)) for f in (
         "attention_prompt", "attention_tree", "attention_tree_workspace", "cache_append", "cache_weigh", "cache_evict", "cache_evict_workspace")])
-except (ImportError, AttributeError):                        # not built, for another torch or Python, or from older sources
+except ImportError:                                          # not built, or for another torch or Python; one from older sources is an error
     _native = None
 if _raw_stream is None or _device is None:
     _native = None
