@@ -60,11 +60,16 @@ __device__ __forceinline__ float tanh_exp(float u) {
   const float e = __builtin_amdgcn_exp2f(fabsf(u) * (2.f * kLog2e));      // infinite for large u: 1
   return copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), u);
 }
-constexpr float kTanhSeries = 0.25f;                       // 62/2835 u^8 is below 2^-21 there
+// Of 1 - t / 3 + 2 t^2 / 15 - 17 t^3 / 315 + 62 t^4 / 2835, t = u^2, what is left out is below 2^-21 up to kTanhSeries; and up to kTanhShort, t0 its square, with t0 for one t of
+// the fourth term: 17 / 315 t^2 (t0 - t) at most.
+constexpr float kTanhSeries = 0.25f, kTanhShort = 0.1975f;
 __device__ __forceinline__ float tanh_either(float u) {
   const float t = tanh_series(u), e = tanh_exp(u);
   return fabsf(u) < kTanhSeries ? t : e;
 }
+
+// A value that is the same in every lane, in a scalar register: the coefficients of the cap would take 8 vector registers that the tiles need (64 features: 9 spilled, 1 with this)
+__device__ __forceinline__ float uniform(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
 
 // Either half of a dword an infinity or NaN of bfloat16
 __device__ __forceinline__ bool bf16_odd(uint32_t x) { return ((x & 0x7f80u) == 0x7f80u) | ((x & 0x7f800000u) == 0x7f800000u); }
@@ -305,11 +310,12 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
 #pragma unroll
     for (int r = 0; r < 16; ++r) o_acc[tb][r] = 0.f;
   const float sc = a.scale * kLog2e, slope_raw = slope / sc;
-  // series of the capped score: used within this bound, not at all for caps and scales whose powers leave float32 (nor without a cap: 0)
-  const float to_u = a.scale * a.inv_cap, back = a.cap * kLog2e, u2 = to_u * to_u;
-  const float cap1 = sc * u2 * -0.3333333333333333f, cap2 = sc * u2 * u2 * 0.13333333333333333f, cap3 = sc * u2 * u2 * u2 * -0.05396825396825397f;
+  // series of the capped score: used within these bounds, not at all for caps and scales whose powers leave float32 (nor without a cap: 0)
+  const float to_u = uniform(a.scale * a.inv_cap), back = uniform(a.cap * kLog2e), u2 = to_u * to_u;
+  const float cap1 = uniform(sc * u2 * -0.3333333333333333f), cap2 = uniform(sc * u2 * u2 * 0.13333333333333333f), cap3 = uniform(sc * u2 * u2 * u2 * -0.05396825396825397f);
   const bool series = fabsf(to_u) > 1e-4f && fabsf(to_u) < 1e4f;
-  const float cap_small = series ? kTanhSeries / fabsf(to_u) : 0.f;
+  const float cap_short = uniform(series ? kTanhShort / fabsf(to_u) : 0.f), cap_small = uniform(series ? kTanhSeries / fabsf(to_u) : 0.f);
+  const float w_short = uniform(cap_short * cap_short), cap23 = uniform(fmaf(w_short, cap3, cap2));
 
   // ---- one tile is on its way while one is worked on
   int tile = seek(TREE ? split * chunk : 0), seen = look_over(tile);
@@ -480,8 +486,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
       } else {
         constexpr bool kOneWay = TREE && D == 64;          // two copies would spill there
         // A score's form follows from that score alone: the series in the unscaled score below cap_small, the exponential above.  `most`, over all that the tile
-        // holds, seen or not, only tells which of them there are.  (A series of one term less below 0.14 cap, chosen score by score: 2 models of 8191 tokens, cap 50,
-        // 1337 -> 1303 us, but packed documents, whose tiles mix both, 48.0 -> 50.2 and cap 5 1820 -> 1918.)
+        // holds, seen or not, only tells which of them there are.
         float most = 0.f;
 #pragma unroll
         for (int sb = 0; sb < NSB; ++sb)
@@ -489,16 +494,19 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
           for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(x[sb][r]));
         auto by_series = [&](float v) __attribute__((always_inline)) {
           const float w = v * v;
-          return v * fmaf(fmaf(fmaf(w, cap3, cap2), w, cap1), w, sc);
+          return v * fmaf(fmaf(fmaf(kBiased ? w : fmaxf(w, w_short), cap3, cap2), w, cap1), w, sc);
         };
-        if (!kBiased && __all(most < cap_small)) {         // as a rule
+        if (!kBiased && __all(most < cap_short)) {         // as a rule: by_series, whose innermost term is cap23 for all of them
 #pragma unroll
           for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) x[sb][r] = by_series(x[sb][r]);
+            for (int r = 0; r < 16; ++r) {
+              const float w = x[sb][r] * x[sb][r];
+              x[sb][r] *= fmaf(fmaf(cap23, w, cap1), w, sc);
+            }
           if (!kOneWay) weigh(kNoShift, 0.f, 1.0f);
         } else {
-          if (kBiased && __all(most < cap_small)) {
+          if (__all(most < cap_small)) {
 #pragma unroll
             for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll

@@ -24,7 +24,7 @@ def different(a, b):
     return (a != b).view(a.shape[0], -1).any(1).nonzero().flatten().tolist()
 
 
-@pytest.mark.parametrize("factor", [6.0, 40.0, 1e10])
+@pytest.mark.parametrize("factor", [1.6, 6.0, 40.0, 1e10])
 @pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("dtype,d", TYPES, ids=str)
 def test_prompt_rows_keep_their_bits(nf, dtype, d, form, factor):
@@ -46,7 +46,7 @@ def test_prompt_rows_keep_their_bits(nf, dtype, d, form, factor):
     assert not different(got[same.view(-1)], ok[same.view(-1)])
 
 
-@pytest.mark.parametrize("factor", [6.0, 40.0, 1e10])
+@pytest.mark.parametrize("factor", [1.6, 6.0, 40.0, 1e10])
 @pytest.mark.parametrize("form", FORMS)
 @pytest.mark.parametrize("T", [6, 20])
 @pytest.mark.parametrize("dtype,d", TYPES, ids=str)
