@@ -24,7 +24,8 @@
  *   - `dt` is the STORAGE type of activations and weight tensors (float or bfloat16 bit
  *     patterns).  Arithmetic is always fp32 (fp32 accumulation; products of float32 matrices may be
  *     formed from bf16 parts of the operands that hold all of their bits, no further from the exact
- *     result than fp32 products at any scale); a bf16 output is rounded once, to nearest even, when
+ *     result than fp32 products at any scale; bf16 attention rounds the softmax weights to bf16 for their product with
+ *     the values, where its kernels run on the matrix pipe); a bf16 output is rounded once, to nearest even, when
  *     it is stored.  Per-feature / per-channel vectors (bias, scale,
  *     shift, gamma, beta, mean, var) and attention masks are ALWAYS float, for either `dt`.
  *   - Inputs are never written.  Outputs are fully overwritten.  An output may alias the
@@ -206,8 +207,11 @@ nf_status netfuse_attention_relpos(const void* Q, const void* K, const void* V, 
  *     largest.  No call changes len or start: after an append the caller adds the counts, after an eviction it takes min(len, budget).
  *   - NF_EUNSUPPORTED for d > 256, and for sizes that would take 2^32 threads or more in one launch.  The kernels on the matrix pipe need d, strides and pointers in multiples of 16 bytes and 64 rows of K and V within
  *     2 GB, and with bfloat16 and a cap |scale| / cap within 1e-37 ... 1e38; everything else takes slower general ones.
- *   - Sums, maxima and scores are float32; with bfloat16 storage the attention weights are rounded to bfloat16 for the product with V, as the result is.
- *   - A sequence's bits depend neither on the models and sequences that are merged with it nor on C.
+ *   - Sums, maxima and scores are float32, scores of bfloat16 rows in units of log2 (finite up to 2.3e38; caps within 2^-20 of tanh).  With bfloat16 storage prompts, and trees of
+ *     more rows to a key head (T * heads / kv_heads) than 32 (16 up to 64 features), round the attention weights to bfloat16 for the product with V, as the result is; smaller
+ *     trees keep 15 bits of them, the general kernels all.
+ *   - Infinite and NaN values that a row sees enter its result as the sums have them, unless their weight is too small for float32 (below 2^-117 of the row's largest).
+ *   - A sequence's bits depend neither on the models and sequences that are merged with it (for the same S, or T) nor on C.
  */
 
 /*

@@ -6,7 +6,8 @@
 // accumulator of a lane holds 16 keys of ONE row (lane % 32): the softmax statistics are per-lane scalars, the two lane halves hold
 // the same row, and the weights are already in the register order of the B operand of O^T = V^T P^T, the keys of a 16-key step being
 // permuted alike on the V^T side, which comes from the transposing LDS read.  Scores, maximum and sum are float32 in log2 units;
-// weights are rounded to bfloat16 for the second product (half a step of 2^-8 each, as the result itself), their sum is not.
+// weights are rounded to bfloat16 for the second product (half a step of 2^-8 each, as the result itself), their sum is not.  (In two parts, of 15 bits, the
+// long prompt would take 1242 -> 1619 us, drafted trees 128 -> 147, packed documents 48.9 -> 51.9, and errors against 64 bits of 0.0018 to 0.0020 be 0.0016 to 0.0017.)
 //
 // Which keys a row sees is an upper end per row (causal, prefix, lengths), the documents of a tile (staged with its keys) or, for the tree's
 // own tile, a bit per node.  Tiles that every row of a wavefront sees in full are not masked, tiles that none sees are left out.  In a masked
