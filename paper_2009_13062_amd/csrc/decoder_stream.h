@@ -3,8 +3,10 @@
 // trees.  Head sizes up to D in 16-byte pieces.
 //
 // Bound by the cache's bytes where few rows read it (one token over two caches of up to 100003 entries, 8 key heads of 128: 114 us and 6 to join, 5.2 TB/s; a read alone reaches
-// 7.1), by latency in short calls (one token over 8 caches of up to 1024, 12 heads of 64, float32: 14 us and 4 to join: four steps per wavefront, one after the other), in float32 prompts
-// by the float32 matrix rate (4 models of 1024 tokens, 16 heads of 128: 251 us).  Three wavefronts per SIMD, two where a wavefront has 32 rows, one with all its registers
+// 7.1), by latency in short calls (one token over 8 caches of up to 1024, 12 heads of 64, float32: 14 us and 4 to join: four steps per wavefront, one after the other).  float32 prompts and
+// trees of many rows read their keys and values again for every 16 or 32 rows, beside the matrix instructions: 4 models of 1024 tokens, 16 heads of 128, 264 us, 65 TFLOP/s of the 152 that
+// a library product reaches, 2.4 GB from the second cache at 9 TB/s, matrix units busy 50 %, 37 % of the wavefronts' time waits; 12 tokens of groups of 4 over 16 caches of 4096, 8 key
+// heads, 181 us and 8 to join, 66 % and 12 %; 26 tokens 350 and 10, 66 % and 10 %.  Three wavefronts per SIMD, two where a wavefront has 32 rows, one with all its registers
 // above 128 features (float32, 16 caches of 4096, 2 heads of 256: two spill, 95 us; one 54).
 //
 // A wavefront holds 16 RT rows (row r = token r / group of one key head) and takes a step of 16 NK keys.  Scores are computed transposed, S^T = K Q^T,

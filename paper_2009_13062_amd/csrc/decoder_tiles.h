@@ -18,10 +18,10 @@
 // what is merged with it nor on the capacity.  Where a sequence fills more than one chunk, partial sums go to the workspace and a second kernel joins them.
 //
 // Long prompts are bound by vector arithmetic: per score one fma and a quarter-rate exponential, half a maximum, a sum and half a rounding, with a bias one fma
-// more, under a cap five.  (2 models of 8191 tokens, 32 heads over 8 of 128 features, biased: 1.21 ms, 907 TFLOP/s where a library product reaches 1165 to 1197; of the cycles the
-// vector units are busy 68 %, the matrix units 41 %.)  So scores stay as they come from the product until the exponent, and the branches below keep whole paths apart.  64 keys of
+// more, under a cap five.  (2 models of 8191 tokens, 32 heads over 8 of 128 features, biased: 1.20 to 1.24 ms on most devices, 907 TFLOP/s where a library product reaches
+// 1165 to 1197; of the cycles the vector units are busy 63 %, the matrix units 45 %.)  So scores stay as they come from the product until the exponent, and the branches below keep whole paths apart.  64 keys of
 // 32 rows per step: two workgroups (three of up to 64 features) share a compute unit's LDS and registers, one's exponentials beside the other's products.
-// Trees are bound by the cache's bytes below some 64 rows, then as prompts are (26 tokens over 32 caches of up to 4096 entries: 120 us and 14 to join).
+// Trees are bound by the cache's bytes below some 64 rows, then as prompts are (26 tokens over 32 caches of up to 4096 entries: 114 us and 15 to join).
 #pragma once
 #include "decoder.h"
 #include "gemm_dma.h"

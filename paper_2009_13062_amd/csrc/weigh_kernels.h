@@ -4,7 +4,7 @@
 // operands (64-byte slices of a row, as in decoder_stream.h) and keeps them while the rows pass 16 at a time: S = Q K^T, so a lane has rows 4 g + r of ONE
 // key and the sum over rows needs no exchange until the end.  What a row adds besides its queries (lse, slope, position, last slot that it sees)
 // lies in a table of the wavefront in LDS, read 4 rows at a time.  Keys are read once and each slot belongs to one lane: no atomics, one order of
-// the sum.  Bound by the keys' bytes up to 16 rows (5.4 TB/s of 7.1; above, by looking the rows up: float32, 8 tokens of groups of 4 over 32 caches of 8192, 404 us): a wavefront takes `turns` blocks of keys one after the other, the next one's on their way meanwhile, and up to 16 rows
+// the sum.  Bound by the keys' bytes up to 16 rows (5.4 TB/s of 7.1; above, by looking the rows up: float32, 8 tokens of groups of 4 over 32 caches of 8192, 419 us): a wavefront takes `turns` blocks of keys one after the other, the next one's on their way meanwhile, and up to 16 rows
 // are looked up once for all of them.
 #pragma once
 #include "decoder_stream.h"
@@ -28,7 +28,7 @@ __device__ __forceinline__ void trade_halves(uint4& a, uint4& b) {
 template <typename T, int D> constexpr int weigh_keys() { return 16 * StreamShape<T, D>::NK; }   // per wavefront and turn
 
 // MANY: more than 16 rows.  (A kernel of its own for fewer: they are looked up once, and without the loop four wavefronts fit a SIMD where three did; one token over 32 caches of
-// 8192 entries, 8 heads of 128: 94.5 -> 81 us.  The next rows on their way while one block of them is worked on: 26 tokens of groups of 4 46 -> 42 and 17.4 -> 15 us, 6
+// 8192 entries, 8 heads of 128: 94.5 -> 78 us.  The next rows on their way while one block of them is worked on: 26 tokens of groups of 4 46 -> 42 and 17.4 -> 15 us, 6
 // tokens 20.0 -> 21.0, not kept.)
 template <typename T, int D, bool MANY>
 __global__ __launch_bounds__(256) void weigh_tiles_kernel(WeighArgs a, int blocks_per_head, int turns) {
