@@ -1,0 +1,560 @@
+"""The operators of a merged decoder's step that surround its attention, as they are measured: queries and keys normed and rotated, rows quantised into a
+cache of 4 bits and read back, attention of drafted tokens over that cache, and the log probabilities of the tokens at the end.
+
+All of them act on M models of B sequences each, rows [M, B*S, heads*d] as of the other decoder operators.
+
+  rotate     y = x / sqrt(mean(x^2) + eps) * gamma over the features of a head; then pair i of the first `rot` features turns by position * freq[i], the
+             position being that of the pair's axis (one, or time, height and width)
+  append     32 neighbouring features share a scale 2^e, the smallest e (of -125 ... 125) with |x| <= 7 * 2^e for all of them; an element is the nearest of
+             +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^e (halfway: the one with the even code); what was appended is then read back
+  read       element = value of its code * 2^e
+  tree       s_ij = f(scale q_i . k_j) - slope_h |pos_i - pos_j|,  f(x) = cap tanh(x / cap), or x where cap is 0; softmax over the cache's entries, a node's
+             ancestors and itself
+  logprobs   x_j = f(scale logit_j) over the tokens of the model's vocabulary: x_t - log sum exp(x) of given tokens, - sum p log p, and the k largest logits,
+             the lowest token first among equals"""
+import math
+
+import torch
+
+own = False
+
+BF, F32 = "bfloat16", "float32"
+
+
+# ---------------------------------------------------------------------------------------------------------------------------- cases
+def listed():
+    """Two cases or more of each operator; heads and features as in the cases of the other decoder operators."""
+    return [
+        # one token for each of 8 merged models, in float32, no norms: what latency allows
+        dict(name="rotate_token_f32", op="rotate", M=8, B=1, S=1, heads=12, kv=12, d=64, rot=64, axes=1, norm=False, inter=False, dtype=F32, ragged=False, start=5000),
+        # prompts with images among the text, queries and keys normed, positions in time, height and width
+        dict(name="rotate_prompt", op="rotate", M=4, B=4, S=2039, heads=32, kv=8, d=128, rot=128, axes=3, norm=True, inter=False, dtype=BF, ragged=True, start=0),
+        # the accepted path of a draft goes into the cache
+        dict(name="append_path_f32", op="append", M=8, B=4, T=26, n=6, C=2048, kv=8, d=64, dtype=F32, ragged=True, start=5000),
+        # whole prompts go into the cache
+        dict(name="append_prompt", op="append", M=8, B=4, T=2039, n=0, C=4096, kv=8, d=128, dtype=BF, ragged=True, start=0),
+        # the entries of short caches in float32, for an operator that takes them dense
+        dict(name="read_short_f32", op="read", M=8, B=1, C=1024, kv=12, d=64, dtype=F32, ragged=True),
+        # long caches read back whole
+        dict(name="read_long", op="read", M=4, B=4, C=16384, kv=8, d=128, dtype=BF, ragged=True),
+        # one token for each of 8 models over a short cache, in float32: what latency allows
+        dict(name="tree_token_f32", op="tree", M=8, B=1, T=1, C=1024, heads=12, kv=12, d=64, dtype=F32, cap=0.0, slopes=True, ragged=True, start=0, lse=True),
+        # trees of 26 drafted tokens, capped scores, caches that have been evicted from
+        dict(name="tree_draft", op="tree", M=4, B=8, T=26, C=4096, heads=32, kv=8, d=128, dtype=BF, cap=50.0, slopes=False, ragged=True, start=9000, lse=True),
+        # one token over long caches of two sequences: the keys have to be shared out
+        dict(name="tree_long", op="tree", M=1, B=2, T=1, C=100003, heads=32, kv=8, d=128, dtype=BF, cap=0.0, slopes=True, ragged=True, start=0, lse=False),
+        # the next token of 8 models, five alternatives each: what latency allows
+        dict(name="logprobs_token", op="logprobs", M=8, B=1, T=1, V=32000, n=1, k=5, dtype=BF, cap=0.0, scale=1.25, vocab=False, ragged=False),
+        # trees of 26 drafted tokens: the log probabilities of a node's children and its best alternatives, capped logits, vocabularies of different sizes
+        dict(name="logprobs_draft", op="logprobs", M=4, B=8, T=26, V=131071, n=4, k=8, dtype=BF, cap=30.0, scale=1.0, vocab=True, ragged=True),
+        # whole prompts scored token by token, in float32
+        dict(name="logprobs_prompt_f32", op="logprobs", M=4, B=1, T=1021, V=50001, n=1, k=20, dtype=F32, cap=0.0, scale=1.0, vocab=False, ragged=False),
+    ]
+
+
+def _log(rng, low, high):
+    return int(round(math.exp(rng.uniform(math.log(low), math.log(high)))))
+
+
+def draw(rng):
+    """A case between the listed ones: its operator, then sizes over the logarithm of their range, made smaller until it costs no more than the largest listed one."""
+    op = rng.choice(("rotate", "append", "read", "tree", "logprobs"))
+    c = dict(op=op, M=rng.choice((1, 2, 3, 4, 8, 16, 32)), B=rng.choice((1, 1, 2, 3, 4, 8)), dtype=rng.choice((F32, BF, BF)), ragged=rng.random() < 0.6)
+    kv, group = rng.choice((1, 2, 3, 4, 8, 12)), rng.choice((1, 1, 2, 4, 8))
+    if op != "logprobs":
+        c.update(kv=kv, d=rng.choice((32, 64, 64, 80, 128, 128)))
+    if op in ("rotate", "tree"):
+        c["heads"] = kv * group
+    if op == "rotate":
+        c.update(S=_log(rng, 1, 8191), rot=rng.choice((c["d"], c["d"], c["d"] // 2)), axes=rng.choice((1, 1, 3)), norm=rng.random() < 0.6, inter=rng.random() < 0.3, start=rng.choice((0, 0, 7000, 1000003)))
+    if op in ("append", "tree"):
+        c["start"] = rng.choice((0, 0, 7000))
+    if op in ("append", "read", "tree"):
+        c["C"] = _log(rng, 64, 100003)
+    if op == "append":
+        c["T"] = _log(rng, 1, c["C"])
+        c["n"] = rng.choice((0, rng.randint(1, c["T"])))
+    if op == "tree":
+        c.update(T=_log(rng, 1, 64), cap=rng.choice((0.0, 0.0, 15.0, 30.0, 50.0)), slopes=rng.random() < 0.5, lse=rng.random() < 0.5)
+    if op == "logprobs":
+        c.update(T=_log(rng, 1, 1021), V=_log(rng, 1000, 200000), n=rng.choice((0, 1, 1, 4)), k=rng.choice((0, 1, 5, 20)), cap=rng.choice((0.0, 0.0, 30.0)), scale=rng.choice((1.0, 1.0, 1.25, 0.7)),
+                 vocab=rng.random() < 0.4)
+    top = max((work(x) for x in listed() if x["op"] == op), key=lambda w: w["bytes"] + w["flops"] / 50)
+    while work(c)["bytes"] > top["bytes"] or work(c)["flops"] > top["flops"] or _elements(c) > 1 << 29:
+        big = max((k for k in ("M", "B", "kv") if c.get(k, 1) > 1), key=lambda k: c[k], default=None)
+        if big is None:
+            for k in ("S", "C", "T", "n"):
+                if c.get(k, 0) > 1:
+                    c[k] = max(1, c[k] // 2)
+        elif big == "kv":
+            c["kv"] //= 2
+            c.update({"heads": c["kv"] * group} if "heads" in c else {})
+        else:
+            c[big] = c[big] // 2
+    return c
+
+
+def _elements(c):
+    """Of the largest tensor of the case: rows, logits, cache or, for the plain form of a tree, a quarter of the scores."""
+    rows = c["M"] * c["B"]
+    if c["op"] == "rotate":
+        return rows * c["S"] * (c["heads"] + c["kv"]) * c["d"]
+    if c["op"] == "logprobs":
+        return rows * c["T"] * c["V"]
+    return rows * max(c["kv"] * c["C"] * c["d"], c.get("T", 1) * c.get("heads", 0) * c["C"] // 4)
+
+
+# -------------------------------------------------------------------------------------------------- lengths, from the case alone
+def _lengths(c, full, least=1):
+    """Valid tokens of each of the M B sequences: all of them, or between a half and all."""
+    k = torch.arange(c["M"] * c["B"])
+    off = (k * 37 + 11) % 64 * (full // 2) // 64 if c["ragged"] else k * 0
+    return (full - off).clamp(min=least).view(c["M"], c["B"]).to(torch.int32)
+
+
+def _cached(c):
+    """Entries of each cache before the step: room is left for what is appended."""
+    return _lengths(c, max(c["C"] - ((c["n"] or c["T"]) if c["op"] == "append" else 0), 0), 0)
+
+
+def _vocabulary(c):
+    """Tokens that each model knows: all of the columns, or some fewer."""
+    return (c["V"] - torch.arange(c["M"]) * 37 % 64 * (c["V"] // 8) // 64 * int(c["vocab"])).to(torch.int32)
+
+
+def _sections(c):
+    """Pairs of each axis: all of them, or a quarter for time and the rest for height and width."""
+    pairs = c["rot"] // 2
+    return [pairs] if c["axes"] == 1 else [pairs // 4, (pairs - pairs // 4 + 1) // 2, (pairs - pairs // 4) // 2]
+
+
+def _groups(c):
+    """Groups of 32 features of a head, and scales that a row of the cache has room for: an even number."""
+    G = -(-c["d"] // 32)
+    return G, G + G % 2
+
+
+def work(case):
+    """Bytes: inputs and outputs that belong to a valid token, once; a row of the cache is half a byte per feature and one per group of 32."""
+    c, e = case, 4 if case["dtype"] == F32 else 2
+    rows = c["M"] * c["B"]
+    if c["op"] == "rotate":
+        n = float(_lengths(c, c["S"]).sum())
+        row = (c["heads"] + c["kv"]) * c["d"]
+        return {"bytes": n * (row * 2 * e + (4 * c["axes"] if c["axes"] > 1 else 0)) + 4.0 * (2 * rows + c["rot"] // 2 + (2 * c["M"] * c["d"] if c["norm"] else 0)),
+                "flops": n * (c["heads"] + c["kv"]) * (3.0 * c["rot"] + (4.0 * c["d"] if c["norm"] else 0))}
+    if c["op"] == "logprobs":
+        n = float((_lengths(c, c["T"]).sum(1) * _vocabulary(c)).sum())
+        return {"bytes": n * e + rows * c["T"] * (8.0 * c["n"] + 4 + 8.0 * c["k"]), "flops": 4.0 * n}
+    held = 2 * (c["d"] / 2 + c["d"] / 32)  # of a key and its value
+    if c["op"] == "append":
+        n = float(_lengths(c, c["n"] or c["T"]).sum()) * c["kv"]
+        return {"bytes": n * (4 * c["d"] * e + held + 8) + 12.0 * rows, "flops": 0.0}
+    L = _cached(c).double().view(-1)
+    if c["op"] == "read":
+        return {"bytes": float(L.sum()) * c["kv"] * (held + 2 * c["d"] * e) + 4.0 * rows, "flops": 0.0}
+    t = _lengths(c, c["T"]).double().view(-1)
+    cache = float(L.sum()) * c["kv"] * (held + (4 if c["slopes"] and c["start"] else 0))
+    own_rows = float(t.sum()) * (c["heads"] + 2 * c["kv"]) * c["d"] * e + rows * c["T"] * c["heads"] * (c["d"] * e + (4 if c["lse"] else 0))
+    return {"bytes": cache + own_rows + 4.0 * rows * (c["T"] + 3), "flops": 4.0 * float((t * (L + (t + 1) / 2)).sum()) * c["heads"] * c["d"]}
+
+
+# --------------------------------------------------------------------------------------------------------------------------- inputs
+def prepare(case, seed):
+    c = case
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    dt = torch.float32 if c["dtype"] == F32 else torch.bfloat16
+    M, B = c["M"], c["B"]
+    s = dict(c, seed=seed, dt=dt)
+    randn = lambda *n: torch.randn(n, generator=g, device="cuda", dtype=torch.float32)  # noqa: E731
+    rand = lambda *n: torch.rand(n, generator=g, device="cuda")  # noqa: E731
+    dev = lambda t: t.to("cuda").contiguous()  # noqa: E731
+    if c["op"] == "logprobs":
+        T, V, n, k = c["T"], c["V"], c["n"], c["k"]
+        logits = randn(M, B * T, V).mul_(2.5)
+        best = (rand(M, B * T, max(n, 1)) * V).long()  # some tokens stand out, as they do where a model knows what follows
+        logits.scatter_add_(2, best, 6 + 6 * rand(*best.shape))
+        wide = logits.to(dt)
+        vocab = _vocabulary(c)
+        token = torch.where(rand(M, B * T, n) < 0.5, best[:, :, :n], (rand(M, B * T, n) * V).long()) if n else None
+        s.update(logits=wide, token=torch.minimum(token, dev(vocab).view(M, 1, 1) - 1).to(torch.int32) if n else None, size=dev(vocab) if c["vocab"] else None,
+                 nodes=dev(_lengths(c, T)) if c["ragged"] else None)
+        f32, i32 = dict(dtype=torch.float32, device="cuda"), dict(dtype=torch.int32, device="cuda")
+        s["out"] = (torch.empty((M, B * T, n), **f32) if n else None, torch.empty((M, B * T), **f32), torch.empty((M, B * T, k), **i32) if k else None, torch.empty((M, B * T, k), **f32) if k else None)
+        return s
+    kv, d = c["kv"], c["d"]
+    if c["op"] in ("rotate", "tree"):  # one projection gives the three, side by side
+        N, H = B * c.get("S", c.get("T", 0)), c["heads"]
+        qkv = randn(M, N, (H + 2 * kv) * d)
+        qkv[:, :, :H * d] *= 1.5
+        qkv = qkv.to(dt)
+        s.update(qkv=qkv, Q=qkv[:, :, :H * d], K=qkv[:, :, H * d:(H + kv) * d], V=qkv[:, :, (H + kv) * d:])
+    if c["op"] == "rotate":
+        S, pairs = c["S"], c["rot"] // 2
+        s["freq"] = (10000.0 ** (-torch.arange(pairs, device="cuda", dtype=torch.float64) / max(1, pairs))).float()
+        s["gamma_q"], s["gamma_k"] = (1 + 0.2 * randn(M, d), 1 + 0.2 * randn(M, d)) if c["norm"] else (None, None)
+        s["length"] = dev(_lengths(c, S)) if c["ragged"] else None
+        begin = c["start"] + torch.arange(M * B).view(M, B) * 3
+        s["begin"] = dev(begin.to(torch.int32))
+        s["sections"], s["pos"] = _sections(c), None
+        if c["axes"] > 1:  # text, then the patches of an image of equal sides
+            at, text = torch.arange(S), S // 4
+            side = max(1, int((S - text) ** 0.5))
+            patch = (at - text).clamp(min=0)
+            grid = torch.stack((torch.where(at < text, at, text), torch.where(at < text, at, text + patch // side), torch.where(at < text, at, text + patch % side)), -1)
+            s["pos"] = dev((begin[:, :, None, None] + grid).to(torch.int32))
+        s["out_q"], s["out_k"] = torch.zeros((M, B * S, c["heads"] * d), dtype=dt, device="cuda"), torch.zeros((M, B * S, kv * d), dtype=dt, device="cuda")
+        return s
+    L = _cached(c)
+    s["length"] = dev(L)
+    s["begin"] = dev(L + c["start"]) if c.get("start") else None
+    held = lambda: _quantised(randn(M, B, kv, c["C"], d))  # noqa: E731
+    (s["Kc"], s["Ks"]), (s["Vc"], s["Vs"]) = held(), held()
+    s["pos"] = None
+    if c.get("start") or c["op"] == "append":  # evicted caches are in no order: any positions below the next one's
+        order = rand(M, B, kv, c["C"]).argsort(-1)
+        s["pos"] = (order * (1 + c["start"] // c["C"])).to(torch.int32)
+    if c["op"] == "tree":
+        s["scale"] = d ** -0.5
+        s["slope"] = None
+        if c["slopes"]:  # the usual powers of two between 2^-1 and 2^-8 over the heads, another factor for each model
+            s["slope"] = (2.0 ** -(1 + 7 * torch.arange(c["heads"], device="cuda") / max(1, c["heads"] - 1)) * (1 + 0.1 * rand(M, 1))).float().contiguous()
+        host = torch.Generator().manual_seed(seed)
+        parent = (torch.rand((M, B, c["T"]), generator=host) * torch.arange(c["T"])).floor().to(torch.int32)  # one root, children of earlier nodes
+        parent[:, :, 0] = -1
+        s.update(parent=dev(parent), nodes=dev(_lengths(c, c["T"])) if c["ragged"] and c["T"] > 1 else None, out=torch.empty((M, B * c["T"], c["heads"] * d), dtype=dt, device="cuda"))
+        s["lse_out"] = torch.empty((M, B * c["T"], c["heads"]), dtype=torch.float32, device="cuda") if c["lse"] else None
+    if c["op"] == "append":
+        n = c["n"] or c["T"]
+        pick = rand(M, B, c["T"]).argsort(-1)[:, :, :n].sort(-1).values
+        s["index"] = pick.to(torch.int32).contiguous() if c["n"] else None
+        s["count"] = dev(_lengths(c, n))
+        kvs = randn(M, B * c["T"], 2 * kv * d).to(dt)
+        s.update(K=kvs[:, :, :kv * d], V=kvs[:, :, kv * d:], weight=randn(M, B, kv, c["C"]).square())
+    if c["op"] in ("append", "read"):
+        n = (c["n"] or c["T"]) if c["op"] == "append" else c["C"]
+        s["n_read"] = n
+        s["out_k"], s["out_v"] = torch.empty((M, B, kv, n, d), dtype=dt, device="cuda"), torch.empty((M, B, kv, n, d), dtype=dt, device="cuda")
+    return s
+
+
+# ------------------------------------------------------------------------------------------------------------------------------ run
+def run(state):
+    s = state
+    if own:
+        import paper_2009_13062_amd as nf
+        if s["op"] == "rotate":
+            q, k = nf.rotate_heads(s["Q"], s["K"], s["B"], s["S"], s["heads"], s["kv"], freq=s["freq"], gamma_q=s["gamma_q"], gamma_k=s["gamma_k"], pos=s["pos"], start=s["begin"], length=s["length"],
+                                   sections=s["sections"], interleaved=s["inter"], out_q=s["out_q"], out_k=s["out_k"])
+            return {"Q": q, "K": k}
+        if s["op"] == "append":
+            nf.cache_append_fp4(s["K"], s["V"], s["Kc"], s["Ks"], s["Vc"], s["Vs"], s["pos"], s["weight"], s["length"], start=s["begin"], index=s["index"], count=s["count"])
+            k, v = nf.cache_read_fp4(s["Kc"], s["Ks"], s["Vc"], s["Vs"], s["d"], n=s["n_read"], first=s["length"], count=s["count"], out_k=s["out_k"], out_v=s["out_v"])
+            return {"K": k, "V": v, "pos": s["pos"], "weight": s["weight"]}
+        if s["op"] == "read":
+            k, v = nf.cache_read_fp4(s["Kc"], s["Ks"], s["Vc"], s["Vs"], s["d"], count=s["length"], out_k=s["out_k"], out_v=s["out_v"])
+            return {"K": k, "V": v}
+        if s["op"] == "tree":
+            O = nf.attention_tree_fp4(s["Q"], s["K"], s["V"], s["Kc"], s["Ks"], s["Vc"], s["Vs"], s["length"], start=s["begin"], parent=s["parent"], nodes=s["nodes"], pos=s["pos"], slope=s["slope"],
+                                      scale=s["scale"], cap=s["cap"], out=s["out"], lse=s["lse_out"])
+            return {"O": O, "lse": s["lse_out"]}
+        logp, entropy, top, top_logp = nf.token_logprobs(s["logits"], s["token"], k=s["k"], vocab=s["size"], nodes=s["nodes"], scale=s["scale"], cap=s["cap"], out=s["out"])
+        return {"logp": logp, "entropy": entropy, "top": top, "top_logp": top_logp}
+    return {"rotate": _plain_rotate, "append": _plain_append, "read": _plain_read, "tree": _plain_tree, "logprobs": _plain_logprobs}[s["op"]](s)
+
+
+def _normed_rotated(x, s, gamma, out):
+    """Rows of one of the two: [M, B S, heads d], normed and rotated into `out` where they are valid."""
+    M, B, S, d, rot = s["M"], s["B"], s["S"], s["d"], s["rot"]
+    y = x.float().view(M, B, S, -1, d)
+    if gamma is not None:
+        y = y * torch.rsqrt(y.square().mean(-1, keepdim=True) + 1e-6) * gamma.view(M, 1, 1, 1, d)
+    at = torch.arange(S, device="cuda")
+    pos = s["pos"] if s["pos"] is not None else (s["begin"][..., None] + at)[..., None]
+    axis = torch.repeat_interleave(torch.arange(len(s["sections"]), device="cuda"), torch.tensor(s["sections"], device="cuda"))
+    angle = (pos[..., axis].double() * s["freq"].double())[:, :, :, None]  # [M, B, S, 1, pairs]
+    cos, sin = angle.cos().float(), angle.sin().float()
+    turned, rest = y[..., :rot], y[..., rot:]
+    if s["inter"]:
+        a, b = turned[..., 0::2], turned[..., 1::2]
+        turned = torch.stack((a * cos - b * sin, a * sin + b * cos), -1).flatten(-2)
+    else:
+        a, b = turned[..., :rot // 2], turned[..., rot // 2:]
+        turned = torch.cat((a * cos - b * sin, a * sin + b * cos), -1)
+    y = torch.cat((turned, rest), -1).reshape(M, B * S, -1).to(s["dt"])
+    if s["length"] is None:
+        return out.copy_(y)
+    valid = (at < s["length"][..., None]).view(M, B * S, 1)
+    return out.copy_(torch.where(valid, y, out))
+
+
+def _plain_rotate(s):
+    return {"Q": _normed_rotated(s["Q"], s, s["gamma_q"], s["out_q"]), "K": _normed_rotated(s["K"], s, s["gamma_k"], s["out_k"])}
+
+
+def _power(e):
+    """2^e in 32 bits, exactly, for -126 <= e <= 127."""
+    return ((e + 127) << 23).to(torch.int32).view(torch.float32)
+
+
+def _quantised(x):
+    """Rows [..., d] in 32 bits -> codes [..., 16 G] two to a byte, the lower feature in the lower half, and scales [..., G or G + 1], e + 127."""
+    d = x.shape[-1]
+    G = -(-d // 32)
+    x = torch.nn.functional.pad(x, (0, 32 * G - d)).unflatten(-1, (G, 32))
+    part, e = torch.frexp(x.abs().amax(-1))
+    e = (e.int() - 3 + (part > 0.875).int()).masked_fill(part == 0, -125).clamp(-125, 125)
+    x = x * _power(-e)[..., None]
+    a = x.abs()
+    code = (a > 0.25).byte() + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5) + torch.signbit(x) * 8
+    code = code.flatten(-2)
+    return code[..., 0::2] | code[..., 1::2] << 4, torch.nn.functional.pad((e + 127).byte(), (0, G % 2))
+
+
+def _values(code, scale, d):
+    """The values that rows of the cache stand for, in 32 bits."""
+    of = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, -0.0, -0.5, -1, -1.5, -2, -3, -4, -6], device=code.device)
+    G = -(-d // 32)
+    x = of[torch.stack((code & 15, code >> 4), -1).flatten(-2).int()].unflatten(-1, (G, 32))
+    return (x * _power(scale[..., :G].int() - 127)[..., None]).flatten(-2)[..., :d]
+
+
+def _plain_append(s):
+    M, B, T, C, kv, d, n = s["M"], s["B"], s["T"], s["C"], s["kv"], s["d"], s["n_read"]
+    pick = s["index"].long() if s["index"] is not None else torch.arange(n, device="cuda").expand(M, B, n)
+    which = torch.arange(C, device="cuda") - s["length"][..., None]                                      # which of the new rows a slot holds
+    new = ((which >= 0) & (which < s["count"][..., None]))[:, :, None]                                   # [M, B, 1, C]
+    at = which.clamp(0, n - 1)[:, :, None, :, None]
+    slot = (s["length"][..., None] + torch.arange(n, device="cuda")).clamp(max=C - 1)[:, :, None, :, None].long()
+    there = (torch.arange(n, device="cuda") < s["count"][..., None])[:, :, None, :, None]
+    back = {}
+    for name, codes, scales in (("K", "Kc", "Ks"), ("V", "Vc", "Vs")):
+        rows = torch.gather(s[name].float().reshape(M, B, T, kv, d).transpose(2, 3), 3, pick[:, :, None, :, None].expand(M, B, kv, n, d))
+        for cache, fresh in zip((s[codes], s[scales]), _quantised(rows)):
+            cache.copy_(torch.where(new[..., None], torch.gather(fresh, 3, at.expand(M, B, kv, C, fresh.shape[-1])), cache))
+        read = [torch.gather(x, 3, slot.expand(M, B, kv, n, x.shape[-1])) for x in (s[codes], s[scales])]
+        back[name] = _values(*read, d).masked_fill(~there, 0.0).to(s["dt"])
+    begin = s["begin"] if s["begin"] is not None else s["length"]
+    s["pos"].copy_(torch.where(new, (begin[..., None] + which)[:, :, None].to(torch.int32), s["pos"]))
+    s["weight"].masked_fill_(new, 0.0)
+    return {"K": back["K"], "V": back["V"], "pos": s["pos"], "weight": s["weight"]}
+
+
+def _plain_read(s):
+    held = (torch.arange(s["C"], device="cuda") < s["length"][..., None])[:, :, None, :, None]
+    return {name: _values(s[codes], s[scales], s["d"]).masked_fill(~held, 0.0).to(s["dt"]) for name, codes, scales in (("K", "Kc", "Ks"), ("V", "Vc", "Vs"))}
+
+
+def _capped(x, cap):
+    return x.div_(cap).tanh_().mul_(cap) if cap else x
+
+
+def _by_head(x, M, B, S, kv, d):
+    """[M, B S, heads d] -> [M, B, kv, group, S, d] in 32 bits."""
+    return x.float().view(M, B, S, kv, -1, d).permute(0, 1, 3, 4, 2, 5)
+
+
+def _ancestors(parent):
+    """[M, B, T] parents -> which node sees which [M, B, T, T] (itself and its ancestors), and depths, by squaring the relation."""
+    T = parent.shape[-1]
+    at = torch.arange(T, device=parent.device)
+    see = (parent[..., None] == at).float() + torch.eye(T, device=parent.device)
+    for _ in range(T.bit_length()):  # a path of 2^k steps after k of them
+        see = (torch.matmul(see, see) > 0).float()
+    return see > 0, see.sum(-1).to(torch.int32) - 1
+
+
+def _plain_tree(s):
+    M, B, T, C, kv, d = s["M"], s["B"], s["T"], s["C"], s["kv"], s["d"]
+    G = s["heads"] // kv
+    q = _by_head(s["Q"], M, B, T, kv, d).reshape(M, B, kv, G * T, d)
+    k = torch.cat((_values(s["Kc"], s["Ks"], d), _by_head(s["K"], M, B, T, kv, d).reshape(M, B, kv, T, d)), 3)
+    v = torch.cat((_values(s["Vc"], s["Vs"], d), _by_head(s["V"], M, B, T, kv, d).reshape(M, B, kv, T, d)), 3)
+    sc = _capped(torch.matmul(q, k.transpose(-1, -2).contiguous()).mul_(s["scale"]), s["cap"]).view(M, B, kv, G, T, C + T)
+    see, depth = _ancestors(s["parent"])
+    slot, node = torch.arange(C, device="cuda"), torch.arange(T, device="cuda")
+    valid = node < (s["nodes"] if s["nodes"] is not None else torch.full_like(s["length"], T))[..., None]
+    seen = torch.cat(((slot < s["length"][..., None])[:, :, None].expand(M, B, T, C), see & valid[:, :, None]), 3) & valid[..., None]
+    if s["slope"] is not None:
+        mine = (s["begin"] if s["begin"] is not None else s["length"])[..., None] + depth  # [M, B, T]
+        cached = s["pos"] if s["pos"] is not None else slot.to(torch.int32).expand(M, B, kv, C)
+        theirs = torch.cat((cached, mine[:, :, None].expand(M, B, kv, T)), 3)
+        sc.addcmul_(s["slope"].view(M, 1, kv, G, 1, 1), (mine[:, :, None, None, :, None] - theirs[:, :, :, None, None]).abs().float(), value=-1.0)
+    sc.masked_fill_(~seen[:, :, None, None], -math.inf)
+    top = sc.amax(-1, keepdim=True)
+    top.masked_fill_(top == -math.inf, 0.0)
+    p = sc.sub_(top).exp_()
+    total = p.sum(-1, keepdim=True)
+    o = torch.matmul(p.view(M, B, kv, G * T, C + T), v).view(M, B, kv, G, T, d) / total.masked_fill(total == 0, 1.0)
+    lse = (top + total.log()).squeeze(-1)
+    o = o.permute(0, 1, 4, 2, 3, 5).reshape(M, B * T, s["heads"] * d).to(s["dt"])
+    return {"O": o, "lse": lse.permute(0, 1, 4, 2, 3).reshape(M, B * T, s["heads"]) if s["lse"] else None}
+
+
+def _plain_logprobs(s):
+    M, B, T, V, n, k = s["M"], s["B"], s["T"], s["V"], s["n"], s["k"]
+    known = torch.arange(V, device="cuda") < (s["size"].view(M, 1, 1) if s["size"] is not None else V)
+    if s["nodes"] is not None:
+        known = known & (torch.arange(T, device="cuda") < s["nodes"][..., None]).view(M, B * T, 1)
+    x = _capped(s["logits"].float() * s["scale"], s["cap"]).masked_fill_(~known, -math.inf)
+    top = x.amax(-1, keepdim=True)
+    x -= top.masked_fill(top == -math.inf, 0.0)
+    p = x.exp()
+    total = p.sum(-1, keepdim=True)
+    empty = total == 0
+    x -= total.log().masked_fill_(empty, 0.0)  # log probabilities
+    logp = torch.gather(x, 2, s["token"].long()) if n else None
+    p /= total.masked_fill(empty, 1.0)
+    entropy = -(p * x.masked_fill(p == 0, 0.0)).sum(-1)
+    del p
+    best = best_logp = None
+    if k:  # the logits' bits in the order of their values, then the lower token: one key each, no two alike
+        bits = s["logits"].float().masked_fill(~known, -math.inf).add_(0.0).view(torch.int32)
+        bits = torch.where(bits < 0, bits ^ 0x7FFFFFFF, bits).long().mul_(1 << 32).add_(V - 1 - torch.arange(V, device="cuda"))
+        best = V - 1 - (torch.topk(bits, k, -1).values & 0xFFFFFFFF)
+        best_logp = torch.gather(x, 2, best)
+        best = best.masked_fill(best_logp == -math.inf, -1).to(torch.int32)
+    return {"logp": logp, "entropy": entropy, "top": best, "top_logp": best_logp}
+
+
+# ---------------------------------------------------------------------------------------------------------------------------- exact
+def exact(case, seed):
+    """The definitions in 64 bits: element by element for what is rotated and quantised, one sequence and head, or one block of rows, at a time for the others."""
+    s = prepare(case, seed)
+    return {"rotate": _exact_rotate, "append": _exact_append, "read": _exact_read, "tree": _exact_tree, "logprobs": _exact_logprobs}[case["op"]](s)
+
+
+def _exact_rotate(s):
+    M, B, S, d, rot = s["M"], s["B"], s["S"], s["d"], s["rot"]
+    out = {}
+    for name, gamma in (("Q", s["gamma_q"]), ("K", s["gamma_k"])):
+        heads = s["heads"] if name == "Q" else s["kv"]
+        y = torch.zeros((M, B, S, heads, d), dtype=torch.float64, device="cuda")
+        for m in range(M):
+            for b in range(B):
+                t = int(s["length"][m, b]) if s["length"] is not None else S
+                x = s[name][m].reshape(B, S, heads, d)[b, :t].double()
+                if gamma is not None:
+                    x = x / (x.pow(2).sum(-1, keepdim=True) / d + 1e-6).sqrt() * gamma[m].double()
+                z = x.clone()
+                first = 0
+                for axis, pairs in enumerate(s["sections"]):
+                    at = torch.arange(first, first + pairs, device="cuda")
+                    first += pairs
+                    where = s["pos"][m, b, :t, axis].double() if s["pos"] is not None else int(s["begin"][m, b]) + torch.arange(t, device="cuda").double()
+                    angle = (where[:, None] * s["freq"][at].double())[:, None]
+                    i, j = (2 * at, 2 * at + 1) if s["inter"] else (at, at + rot // 2)
+                    z[..., i] = x[..., i] * torch.cos(angle) - x[..., j] * torch.sin(angle)
+                    z[..., j] = x[..., j] * torch.cos(angle) + x[..., i] * torch.sin(angle)
+                y[m, b, :t] = z
+        out[name] = y.view(M, B * S, heads * d)
+    return out
+
+
+def _exact_held(x):
+    """What rows [..., d] in 64 bits become in the cache: the nearest of 15 values, a group of 32 at a time."""
+    d = x.shape[-1]
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device=x.device)
+    out = torch.empty_like(x)
+    for f in range(0, d, 32):
+        part = x[..., f:f + 32]
+        e = torch.ceil(torch.log2(part.abs().amax(-1, keepdim=True) / 7)).clamp(-125, 125)
+        low = torch.exp2(e - 1)
+        e = torch.where(part.abs().amax(-1, keepdim=True) <= 7 * low, e - 1, e).clamp(-125, 125)  # log2 is rounded: one step either way
+        e = torch.where(part.abs().amax(-1, keepdim=True) > 7 * torch.exp2(e), e + 1, e).clamp(-125, 125)
+        part = part * torch.exp2(-e)
+        near = torch.stack([(part.abs() - v).abs() for v in grid], -1)
+        near[..., 1::2] += 1e-14  # halfway: the even code
+        out[..., f:f + 32] = grid[near.argmin(-1)] * torch.sign(part) * torch.exp2(e)
+    return out
+
+
+def _exact_append(s):
+    M, B, T, kv, d = s["M"], s["B"], s["T"], s["kv"], s["d"]
+    out = {"K": torch.zeros_like(s["out_k"], dtype=torch.float64), "V": torch.zeros_like(s["out_v"], dtype=torch.float64), "pos": s["pos"], "weight": s["weight"].double()}
+    for m in range(M):
+        for b in range(B):
+            t, length = int(s["count"][m, b]), int(s["length"][m, b])
+            take = s["index"][m, b, :t].long() if s["index"] is not None else torch.arange(t, device="cuda")
+            for name in ("K", "V"):
+                out[name][m, b, :, :t] = _exact_held(s[name][m].reshape(B, T, kv, d)[b, take].double().transpose(0, 1))
+            out["pos"][m, b, :, length:length + t] = (int(s["begin"][m, b]) if s["begin"] is not None else length) + torch.arange(t, device="cuda", dtype=torch.int32)
+            out["weight"][m, b, :, length:length + t] = 0.0
+    return out
+
+
+def _exact_values(code, scale, d):
+    """Rows of the cache in 64 bits, from the fields of a code: a sign, two bits of exponent, one of fraction."""
+    code = torch.stack((code % 16, code // 16), -1).flatten(-2)[..., :d].long()
+    power, part = code // 2 % 4, code % 2
+    x = torch.where(power == 0, part * 0.5, (1 + part * 0.5) * torch.exp2((power - 1).double())) * (1 - 2 * (code // 8))
+    return x * torch.exp2(scale.double() - 127).repeat_interleave(32, -1)[..., :d]
+
+
+def _exact_read(s):
+    out = {}
+    for name, codes, scales in (("K", "Kc", "Ks"), ("V", "Vc", "Vs")):
+        out[name] = torch.zeros((s["M"], s["B"], s["kv"], s["C"], s["d"]), dtype=torch.float64, device="cuda")
+        for m in range(s["M"]):
+            for b in range(s["B"]):
+                t = int(s["length"][m, b])
+                out[name][m, b, :, :t] = _exact_values(s[codes][m, b, :, :t], s[scales][m, b, :, :t], s["d"])
+    return out
+
+
+def _exact_tree(s):
+    M, B, N, kv, d = s["M"], s["B"], s["T"], s["kv"], s["d"]
+    G = s["heads"] // kv
+    slope = s["slope"].double().cpu() if s["slope"] is not None else torch.zeros((M, s["heads"]), dtype=torch.float64)
+    out = torch.zeros((M, B, N, s["heads"], d), dtype=torch.float64, device="cuda")
+    lse = torch.full((M, B, N, s["heads"]), -math.inf, dtype=torch.float64, device="cuda")
+    rows = lambda x, m, b, h, t: x[m].view(B, N, -1)[b, :t, h * d:(h + 1) * d].double()  # noqa: E731
+    for m in range(M):
+        for b in range(B):
+            length = int(s["length"][m, b])
+            begin = int(s["begin"][m, b]) if s["begin"] is not None else length
+            t = int(s["nodes"][m, b]) if s["nodes"] is not None else N
+            par, see, depth = s["parent"][m, b].tolist(), torch.zeros((t, t), dtype=torch.bool), [0] * t
+            for a in range(t):
+                if par[a] >= 0:
+                    see[a], depth[a] = see[par[a]], depth[par[a]] + 1
+                see[a, a] = True
+            q_at = begin + torch.tensor(depth, device="cuda")
+            ok = torch.cat((torch.ones((t, length), dtype=torch.bool), see), 1).cuda()
+            for h in range(kv):
+                k = torch.cat((_exact_values(s["Kc"][m, b, h, :length], s["Ks"][m, b, h, :length], d), rows(s["K"], m, b, h, t)))
+                v = torch.cat((_exact_values(s["Vc"][m, b, h, :length], s["Vs"][m, b, h, :length], d), rows(s["V"], m, b, h, t)))
+                k_at = torch.cat((s["pos"][m, b, h, :length].long() if s["pos"] is not None else torch.arange(length, device="cuda"), q_at))
+                far = (q_at[:, None] - k_at[None]).abs().double()
+                for x in range(h * G, h * G + G):
+                    sc = torch.mm(rows(s["Q"], m, b, x, t), k.t()) * s["scale"]
+                    if s["cap"]:
+                        sc = s["cap"] * torch.tanh(sc / s["cap"])
+                    sc = (sc - float(slope[m, x]) * far).masked_fill(~ok, -math.inf)
+                    lse[m, b, :t, x] = torch.logsumexp(sc, 1)
+                    out[m, b, :t, x] = torch.mm(torch.softmax(sc, 1).nan_to_num(0.0), v)
+    return {"O": out.view(M, B * N, s["heads"] * d), "lse": lse.view(M, B * N, -1) if s["lse"] else None}
+
+
+def _exact_logprobs(s):
+    M, B, T, V, n, k = s["M"], s["B"], s["T"], s["V"], s["n"], s["k"]
+    N = B * T
+    none = torch.full((M, N, max(n, k, 1)), -math.inf, dtype=torch.float64, device="cuda")
+    logp, entropy, best_logp = none[..., :n].clone(), torch.zeros((M, N), dtype=torch.float64, device="cuda"), none[..., :k].clone()
+    best = torch.full((M, N, k), -1, dtype=torch.int32, device="cuda")
+    for m in range(M):
+        size = int(s["size"][m]) if s["size"] is not None else V
+        valid = torch.cat([b * T + torch.arange(int(s["nodes"][m, b]) if s["nodes"] is not None else T) for b in range(B)]).cuda()
+        for at in valid.split(max(1, (1 << 26) // V)):
+            raw = s["logits"][m, at, :size].double()
+            x = raw * s["scale"]
+            x = s["cap"] * torch.tanh(x / s["cap"]) if s["cap"] else x
+            x = x - torch.logsumexp(x, 1, keepdim=True)
+            entropy[m, at] = -(torch.exp(x) * x).sum(1)
+            if n:
+                logp[m, at] = x.gather(1, s["token"][m, at].long())
+            if k:
+                most = min(k, size)
+                order = raw.sort(dim=1, descending=True, stable=True).indices[:, :most]
+                best[m, at, :most], best_logp[m, at, :most] = order.to(torch.int32), x.gather(1, order)
+    return {"logp": logp if n else None, "entropy": entropy, "top": best if k else None, "top_logp": best_logp if k else None}
