@@ -306,7 +306,7 @@ def _quantised(x):
     e = (e.int() - 3 + (part > 0.875).int()).masked_fill(part == 0, -125).clamp(-125, 125)
     x = x * _power(-e)[..., None]
     a = x.abs()
-    code = (a > 0.25).byte() + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5) + torch.signbit(x) * 8
+    code = (a > 0.25).byte() + (a >= 0.75) + (a > 1.25) + (a >= 1.75) + (a > 2.5) + (a >= 3.5) + (a > 5) + torch.signbit(x).byte() * 8
     code = code.flatten(-2)
     return code[..., 0::2] | code[..., 1::2] << 4, torch.nn.functional.pad((e + 127).byte(), (0, G % 2))
 
