@@ -278,6 +278,74 @@ nf_status netfuse_cache_evict(void* Kc, void* Vc, const int* pos, const float* w
                               int d, int budget, int recent, nf_dtype dt, void* stream);
 
 /*
+ * A decoder's step around its attention (the common notes above hold): heads normed and rotated before it, a cache of 4 bits per element that it can read instead,
+ * log probabilities after it.
+ */
+
+/*
+ * Queries and keys normed head by head and rotated by position, in one pass:  y = x / sqrt(mean(x^2) + eps) * gamma  over the d features of a head (gamma_q, gamma_k:
+ * float[M][d]; NULL: y = x), then pair i of the first `rot` features turns by the angle position * freq[i]:
+ *   (y_a, y_b) -> (y_a cos - y_b sin, y_a sin + y_b cos),   a, b = i, i + rot/2, or with interleaved != 0  2 i, 2 i + 1;   the other d - rot features stay y.
+ *   rot: even, 0 ... d.   freq: float[rot/2] (NULL with rot = 0).   Angles are formed in 64 bits (off by 2^-51 of themselves), cosines and sines are within 2^-21.
+ *   axes: 1 ... 4 positions per token (time, height, width).  sections: HOST array of `axes` numbers of pairs that add up to rot/2, the first pairs being axis 0's; NULL with one axis.
+ *   pos: int[M][B][S][axes], or NULL with one axis: start[m][b] + s (start: int[M][B], or NULL: 0).   Any position of 32 bits.
+ *   len: int[M][B] or NULL: rows at and past it are left as they are in Qo and Ko.
+ *   Qo, Ko: rows with strides of their own; Qo may be Q and Ko may be K with the same strides (turned in place), nothing else may overlap.
+ *   K and Ko may be NULL, with kv_heads = 0.   heads need not be a multiple of kv_heads here.
+ */
+nf_status netfuse_rotate_heads(const void* Q, const void* K, const float* gamma_q, const float* gamma_k, const float* freq, const int* pos,
+                               const int* start, const int* len, const int* sections, void* Qo, void* Ko, int M, int B, int S, int heads,
+                               int kv_heads, int d, int rot, int axes, long q_stride_m, long q_stride_row, long k_stride_m,
+                               long k_stride_row, long qo_stride_m, long qo_stride_row, long ko_stride_m, long ko_stride_row, float eps,
+                               int interleaved, nf_dtype dt, void* stream);
+
+/*
+ * A cache of 4 bits per element.  32 neighbouring features share a scale 2^e; an element is one of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^e, the code of the value's place in that
+ * list and 8 for the sign.  With G = ceil(d / 32):
+ *   Kc, Vc: bytes [M][B][kv_heads][C][16 G], feature 2 i in the lower half of byte i, features past d as 0.
+ *   Ks, Vs: bytes [M][B][kv_heads][C][G, or G + 1 where G is odd], byte e + 127 of each group (the byte behind an odd number of them is 0).   All four 16-byte aligned.
+ * Appending takes the smallest e of -125 ... 125 with |x| <= 7 * 2^e in the whole group and rounds to the nearest code, halfway to the even one (magnitudes past 7 * 2^125 to
+ * 6 * 2^125); a group that holds an infinity or NaN gets the byte 255 and reads as NaN.  Readers take any byte 0 ... 254 as 2^(byte - 127).
+ * Rows of codes and rows of scales are rows like any others to netfuse_cache_evict (as bfloat16 of half as many elements: a head's codes, then, from the same
+ * pos and weight into the same pos_out and weight_out, its scales), and netfuse_cache_weigh takes the keys that netfuse_cache_read_fp4 gives.
+ *
+ * netfuse_cache_append_fp4: as netfuse_cache_append.   NF_EUNSUPPORTED for d > 256, here and below.
+ * netfuse_cache_read_fp4: K, V [M][B][kv_heads][n][d] dense of either type, entry i < count[m][b] being slot first[m][b] + i of the cache; entries at and past count, and those
+ *   whose slot is not one of the C, are written as 0.   first, count: int[M][B] or NULL (0; all n).   Vc, Vs and V may be NULL together.
+ */
+nf_status netfuse_cache_append_fp4(const void* K, const void* V, const int* index, const int* count, const int* len, const int* start, void* Kc,
+                                   void* Ks, void* Vc, void* Vs, int* pos, float* weight, int M, int B, int T, int n, int C, int kv_heads,
+                                   int d, long kv_stride_m, long kv_stride_row, nf_dtype dt, void* stream);
+nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc, const void* Vs, const int* first, const int* count, void* K, void* V,
+                                 int M, int B, int n, int C, int kv_heads, int d, nf_dtype dt, void* stream);
+
+/*
+ * netfuse_attention_tree over a cache of 4 bits; the new tokens' own K and V are of type dt.  Cached elements enter the products exactly.
+ */
+long long netfuse_attention_tree_fp4_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt);
+nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V, const void* Kc, const void* Ks, const void* Vc, const void* Vs,
+                                     const int* pos, const int* len, const int* start, const int* parent, const int* nodes, const float* slope,
+                                     void* O, float* lse, void* workspace, long long workspace_bytes, int M, int B, int T, int C, int heads,
+                                     int kv_heads, int d, long q_stride_m, long q_stride_row, long kv_stride_m, long kv_stride_row,
+                                     float scale, float cap, nf_dtype dt, void* stream);
+
+/*
+ * Log probabilities of tokens.  Row (b, t) of model m has the logits ptr[m*stride_m + (b*T + t)*stride_row + j], j < V, of which the first vocab[m] are that model's tokens
+ * (vocab: int[M] or NULL: all V); what lies behind them is not read.  With x_j = f(scale * logit_j), scale > 0 (one over a temperature), f and cap as for scores:
+ *   logp[m][b*T + t][i] = x_j - log sum exp(x) for j = token[m][b*T + t][i], i < n (-infinity for a number that is not one of the row's tokens);   n = 0: token and logp NULL
+ *   entropy[m][b*T + t] = - sum p_j log p_j
+ *   top, top_logp [m][b*T + t][k]: the k <= 32 tokens of the largest logits, the lower one first among equals, and their log probabilities;   k = 0: both NULL
+ * A logit of -infinity has probability 0 under a cap too and is no alternative; where a row has fewer than k alternatives the rest are -1 with -infinity.  A row without
+ * any token (and the rows of nodes that are not there: nodes int[M][B] or NULL) has logp -infinity, entropy 0 and no alternatives.  NaN, and +infinity without a cap, make
+ * every log probability that is not -infinity and the entropy of their row NaN; the order of the alternatives stands, without the NaN ones.
+ * Results are float.  NF_EUNSUPPORTED for k > 32.   workspace: as for netfuse_attention_tree, of netfuse_token_logprobs_workspace(...) bytes (never 0).
+ */
+long long netfuse_token_logprobs_workspace(int M, int B, int T, int V, int k);
+nf_status netfuse_token_logprobs(const void* logits, const int* token, const int* vocab, const int* nodes, float* logp, float* entropy, int* top,
+                                 float* top_logp, void* workspace, long long workspace_bytes, int M, int B, int T, int V, int n, int k,
+                                 long stride_m, long stride_row, float scale, float cap, nf_dtype dt, void* stream);
+
+/*
  * Non-trainable operators merge by concatenation (Section 3.1, "Non-trainable operations"), so
  * these act per channel of the channel-merged tensor; Ctot = M*C.
  * Max pooling: x[B][Ctot][H][W] -> y[B][Ctot][Ho][Wo], window k x k, Ho = (H + 2 pad - k)/stride + 1;

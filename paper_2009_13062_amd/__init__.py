@@ -31,7 +31,9 @@ EXPORTS = ("netfuse_linear", "netfuse_conv2d", "netfuse_layernorm", "netfuse_bat
            "netfuse_time_next_launch", "netfuse_linear_packed_supported", "netfuse_linear_ragged",
            "netfuse_attention_relpos", "netfuse_probe_mfma", "netfuse_probe_hbm_read", "netfuse_attention_prompt",
            "netfuse_attention_tree_workspace", "netfuse_attention_tree", "netfuse_cache_append", "netfuse_cache_weigh",
-           "netfuse_cache_evict_workspace", "netfuse_cache_evict", "netfuse_strerror")
+           "netfuse_cache_evict_workspace", "netfuse_cache_evict", "netfuse_rotate_heads", "netfuse_cache_append_fp4", "netfuse_cache_read_fp4",
+           "netfuse_attention_tree_fp4_workspace", "netfuse_attention_tree_fp4", "netfuse_token_logprobs_workspace", "netfuse_token_logprobs",
+           "netfuse_strerror")
 
 
 class NetFuseError(RuntimeError):
@@ -72,6 +74,13 @@ def _load() -> ctypes.CDLL:
     lib.netfuse_cache_weigh.argtypes = [vp, fp] + [vp] * 6 + [fp] * 3 + [i] * 8 + [l, l, f, f, i, vp]
     lib.netfuse_cache_evict_workspace.argtypes = [i] * 5
     lib.netfuse_cache_evict.argtypes = [vp] * 3 + [fp] + [vp] * 3 + [fp, vp, ll] + [i] * 7 + [i, vp]
+    lib.netfuse_rotate_heads.argtypes = [vp, vp, fp, fp, fp] + [vp] * 3 + [ctypes.POINTER(ctypes.c_int), vp, vp] + [i] * 8 + [l] * 8 + [f, i, i, vp]
+    lib.netfuse_cache_append_fp4.argtypes = [vp] * 11 + [fp] + [i] * 7 + [l, l, i, vp]
+    lib.netfuse_cache_read_fp4.argtypes = [vp] * 8 + [i] * 7 + [vp]
+    lib.netfuse_attention_tree_fp4_workspace.argtypes = [i] * 8
+    lib.netfuse_attention_tree_fp4.argtypes = [vp] * 12 + [fp, vp, fp, vp, ll] + [i] * 7 + [l] * 4 + [f, f, i, vp]
+    lib.netfuse_token_logprobs_workspace.argtypes = [i] * 5
+    lib.netfuse_token_logprobs.argtypes = [vp] * 4 + [fp, fp, vp, fp, vp, ll] + [i] * 6 + [l, l, f, f, i, vp]
     for name in EXPORTS[:-1]:
         getattr(lib, name).restype = ll if name.endswith("_workspace") else ctypes.c_int
     lib.netfuse_strerror.argtypes = [ctypes.c_int]
@@ -138,6 +147,8 @@ try:
                  _address(lib.netfuse_attention), _address(lib.netfuse_attention_relpos), _address(lib.netfuse_conv2d))
     _native.bind_decoder(*[_address(getattr(lib, "netfuse_" + f)) for f in (
         "attention_prompt", "attention_tree", "attention_tree_workspace", "cache_append", "cache_weigh", "cache_evict", "cache_evict_workspace")])
+    _native.bind_step(*[_address(getattr(lib, "netfuse_" + f)) for f in (
+        "rotate_heads", "cache_append_fp4", "cache_read_fp4", "attention_tree_fp4", "attention_tree_fp4_workspace", "token_logprobs", "token_logprobs_workspace")])
 except ImportError:                                          # not built, or for another torch or Python; one from older sources is an error
     _native = None
 if _raw_stream is None or _device is None:
@@ -394,3 +405,5 @@ def merge_transpose(src, M, to_channel, out=None, stream=None):
 
 from .decoder import (attention_prompt, attention_tree, attention_tree_workspace, cache_append, cache_evict,  # noqa: E402,F401
                       cache_evict_workspace, cache_weigh)
+from .step import (attention_tree_fp4, attention_tree_fp4_workspace, cache_append_fp4, cache_fp4, cache_read_fp4, rotate_heads,  # noqa: E402,F401
+                   token_logprobs, token_logprobs_workspace)

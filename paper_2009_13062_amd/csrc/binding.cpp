@@ -28,6 +28,13 @@ decltype(&netfuse_cache_append) f_append;
 decltype(&netfuse_cache_weigh) f_weigh;
 decltype(&netfuse_cache_evict) f_evict;
 decltype(&netfuse_cache_evict_workspace) f_evict_workspace;
+decltype(&netfuse_rotate_heads) f_rotate;
+decltype(&netfuse_cache_append_fp4) f_append_fp4;
+decltype(&netfuse_cache_read_fp4) f_read_fp4;
+decltype(&netfuse_attention_tree_fp4) f_tree_fp4;
+decltype(&netfuse_attention_tree_fp4_workspace) f_tree_fp4_workspace;
+decltype(&netfuse_token_logprobs) f_logprobs;
+decltype(&netfuse_token_logprobs_workspace) f_logprobs_workspace;
 PyObject* g_error;                           // callable (entry point, status) that raises
 
 const c10::DispatchKeySet kWrapped({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::FuncTorchGradWrapper,
@@ -487,6 +494,289 @@ PyObject* cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ---- a decoder's step around its attention: step.py, as above
+
+// The caller's workspace, if any: its address, and its size in place of `bytes`.
+bool workspace(PyObject* o, int device, void** p, long long* bytes) {
+  *p = nullptr;
+  if (o == Py_None) return true;
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& w = THPVariable_Unpack(o);
+  if (!w.defined() || !w.is_cuda() || w.layout() != at::kStrided || w.key_set().has_any(kWrapped) || !w.has_storage() || !w.is_contiguous() || w.device().index() != device) return false;
+  *p = w.data_ptr();
+  *bytes = w.numel() * (long long)w.element_size();
+  return true;
+}
+struct CacheFp4 {
+  int M, B, kv, C, d;
+  void *Kc, *Ks, *Vc, *Vs;
+};
+// Codes and scales of keys and, where `o` has them, of values, for heads of c->d features
+bool cache_fp4(PyObject* const* o, int device, bool values, CacheFp4* c) {
+  const at::Tensor* t = strided(o[0], at::kByte, device);
+  if (!t || t->dim() != 5 || !size(t->size(0), &c->M) || !size(t->size(1), &c->B) || !size(t->size(2), &c->kv) || !size(t->size(3), &c->C) || t->numel() == 0) return false;
+  const int64_t G = (c->d + 31) / 32, codes = 16 * G, scales = G + G % 2;
+  return dense(o[0], at::kByte, {c->M, c->B, c->kv, c->C, codes}, device, true, &c->Kc) && dense(o[1], at::kByte, {c->M, c->B, c->kv, c->C, scales}, device, true, &c->Ks) &&
+         dense(o[2], at::kByte, {c->M, c->B, c->kv, c->C, codes}, device, values, &c->Vc) && dense(o[3], at::kByte, {c->M, c->B, c->kv, c->C, scales}, device, values, &c->Vs);
+}
+// Features of a head: of rows of kv heads, kv the third size of the codes
+bool head_size(const at::Tensor* rows, PyObject* codes, int device, int* d) {
+  const at::Tensor* t = strided(codes, at::kByte, device);
+  return rows && rows->dim() == 3 && t && t->dim() == 5 && t->size(2) > 0 && rows->size(2) > 0 && rows->size(2) % t->size(2) == 0 && size(rows->size(2) / t->size(2), d);
+}
+
+// Q, K, B, S, heads, kv_heads, freq, gamma_q, gamma_k, pos, start, length, sections, interleaved, eps, out_q, out_k, device, stream
+PyObject* rotate_heads(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, B, S, heads, kv, M, d, pairs = 0, axes = 1, parts[4];
+    float eps;
+    void *gq, *gk, *freq, *pos, *start, *len, *s;
+    if (n != 19 || !types(a[0], a[17], &st, &device)) return not_taken();
+    const at::Tensor *Q = strided(a[0], st, device), *K = a[1] == Py_None ? nullptr : strided(a[1], st, device);
+    if (!Q || (a[1] != Py_None && !K) || Q->dim() != 3 || !whole(a[2], &B) || !whole(a[3], &S) || !whole(a[4], &heads) || B <= 0 || S <= 0 || heads <= 0 || !size(Q->size(0), &M) || M <= 0 ||
+        Q->size(2) % heads || !size(Q->size(2) / heads, &d) || d <= 0 || !PyBool_Check(a[13]) || !number(a[14], &eps) || !stream_of(a[18], &s))
+      return not_taken();
+    kv = heads;
+    if (a[5] != Py_None && !whole(a[5], &kv)) return not_taken();
+    if (!K) kv = 0;
+    if (K && kv <= 0) return not_taken();
+    if (a[6] != Py_None) {
+      const at::Tensor* f = strided(a[6], at::kFloat, device);
+      if (!f || f->dim() != 1 || !size(f->size(0), &pairs) || pairs > (1 << 20)) return not_taken();
+    }
+    if (a[12] != Py_None) {
+      if (!PyList_CheckExact(a[12])) return not_taken();
+      const Py_ssize_t count = PyList_GET_SIZE(a[12]);
+      if (count < 1 || count > 4) return not_taken();
+      axes = (int)count;
+      for (int x = 0; x < axes; ++x)
+        if (!whole(PyList_GET_ITEM(a[12], x), &parts[x])) return not_taken();
+    }
+    const int64_t N = (int64_t)B * S;
+    if (a[9] == Py_None) {
+      if (axes > 1) return not_taken();
+      pos = nullptr;
+    } else if (!dense(a[9], at::kInt, {M, B, S, axes}, device, true, &pos) && (axes > 1 || !dense(a[9], at::kInt, {M, B, S}, device, true, &pos))) {
+      return not_taken();
+    }
+    Rows q, k = {nullptr, 0, 0}, qo, ko = {nullptr, 0, 0};
+    if (!rows(Q, M, N, (int64_t)heads * d, &q) || (K && !rows(K, M, N, (int64_t)kv * d, &k)) || !dense(a[6], at::kFloat, {pairs}, device, false, &freq) ||
+        !dense(a[7], at::kFloat, {M, d}, device, false, &gq) || !dense(a[8], at::kFloat, {M, d}, device, false, &gk) || !dense(a[10], at::kInt, {M, B}, device, false, &start) ||
+        !dense(a[11], at::kInt, {M, B}, device, false, &len))
+      return not_taken();
+    // new results where no row of them is left out; with lengths step.py clears them
+    at::Tensor new_q, new_k;
+    const at::Tensor *Qo = nullptr, *Ko = nullptr;
+    if (a[15] != Py_None ? !(Qo = strided(a[15], st, device)) : len != nullptr) return not_taken();
+    if (K ? (a[16] != Py_None ? !(Ko = strided(a[16], st, device)) : len != nullptr) : a[16] != Py_None) return not_taken();
+    if ((Qo && !rows(Qo, M, N, (int64_t)heads * d, &qo)) || (Ko && !rows(Ko, M, N, (int64_t)kv * d, &ko))) return not_taken();
+    const int interleaved = a[13] == Py_True;
+    const nf_dtype dt = type_of(*Q);
+    nf_status done_as;
+    {
+      Unlocked unlocked;
+      if (!Qo) {
+        new_q = at::empty({M, N, (int64_t)heads * d}, Q->options());
+        qo = {new_q.data_ptr(), (long)(N * heads * d), (long)heads * d};
+      }
+      if (K && !Ko) {
+        new_k = at::empty({M, N, (int64_t)kv * d}, Q->options());
+        ko = {new_k.data_ptr(), (long)(N * kv * d), (long)kv * d};
+      }
+      done_as = f_rotate(q.p, k.p, (const float*)gq, (const float*)gk, (const float*)freq, (const int*)pos, (const int*)start, (const int*)len, a[12] != Py_None ? parts : nullptr, (void*)qo.p,
+                         (void*)ko.p, M, B, S, heads, kv, d, 2 * pairs, axes, q.model, q.row, k.model, k.row, qo.model, qo.row, ko.model, ko.row, eps, interleaved, dt, s);
+    }
+    PyObject* first = done("netfuse_rotate_heads", done_as, a[15], new_q);
+    if (!first) return nullptr;
+    PyObject* second = a[16];
+    if (K && !Ko) second = THPVariable_Wrap(std::move(new_k));
+    else Py_INCREF(second);
+    PyObject* both = second ? PyTuple_Pack(2, first, second) : nullptr;
+    Py_DECREF(first);
+    Py_XDECREF(second);
+    return both;
+  });
+}
+
+// K, V, Kc, Ks, Vc, Vs, pos, weight, length, start, index, count, device, stream
+PyObject* cache_append_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, T, m;
+    void *pos, *weight, *len, *start, *index, *count, *s;
+    CacheFp4 c;
+    if (n != 14 || !types(a[0], a[12], &st, &device) || !stream_of(a[13], &s)) return not_taken();
+    const at::Tensor *K = strided(a[0], st, device), *V = strided(a[1], st, device);
+    if (!head_size(K, a[2], device, &c.d) || !cache_fp4(a + 2, device, true, &c) || !batch(K, {c.M, c.B, c.kv, c.C, c.d, nullptr}, &T)) return not_taken();
+    m = T;
+    if (a[10] != Py_None) {
+      const at::Tensor* i = strided(a[10], at::kInt, device);
+      if (!i || i->dim() != 3 || !size(i->size(2), &m)) return not_taken();
+    }
+    Rows k, v;
+    const int64_t N = (int64_t)c.B * T, W = (int64_t)c.kv * c.d;
+    const at::DimVector shape({c.M, c.B, c.kv, c.C});
+    if (!rows(K, c.M, N, W, &k) || !rows(V, c.M, N, W, &v) || k.model != v.model || k.row != v.row || !dense(a[6], at::kInt, shape, device, false, &pos) ||
+        !dense(a[7], at::kFloat, shape, device, false, &weight) || !dense(a[8], at::kInt, {c.M, c.B}, device, true, &len) || !dense(a[9], at::kInt, {c.M, c.B}, device, false, &start) ||
+        !dense(a[10], at::kInt, {c.M, c.B, m}, device, false, &index) || !dense(a[11], at::kInt, {c.M, c.B}, device, false, &count))
+      return not_taken();
+    const nf_dtype dt = type_of(*K);
+    return made("netfuse_cache_append_fp4", [=] {
+      return f_append_fp4(k.p, v.p, (const int*)index, (const int*)count, (const int*)len, (const int*)start, c.Kc, c.Ks, c.Vc, c.Vs, (int*)pos, (float*)weight, c.M, c.B, T, m, c.C, c.kv, c.d, k.model,
+                          k.row, dt, s);
+    });
+  });
+}
+
+// Kc, Ks, Vc, Vs, d, n, first, count, out_k, out_v, device, stream (new results are step.py's)
+PyObject* cache_read_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, m;
+    void *first, *count, *k, *v, *s;
+    CacheFp4 c;
+    if (n != 12 || !types(a[8], a[10], &st, &device) || !stream_of(a[11], &s) || !whole(a[4], &c.d) || c.d <= 0 || c.d > 256) return not_taken();
+    const bool values = a[9] != Py_None;
+    if (!cache_fp4(a, device, values, &c) || (c.Vc != nullptr) != values || (c.Vs != nullptr) != values) return not_taken();
+    m = c.C;
+    if (a[5] != Py_None && (!whole(a[5], &m) || m <= 0)) return not_taken();
+    const at::DimVector shape({c.M, c.B, c.kv, m, c.d});
+    if (!dense(a[6], at::kInt, {c.M, c.B}, device, false, &first) || !dense(a[7], at::kInt, {c.M, c.B}, device, false, &count) || !dense(a[8], st, shape, device, true, &k) ||
+        !dense(a[9], st, shape, device, false, &v))
+      return not_taken();
+    const nf_dtype dt = st == at::kFloat ? NF_F32 : NF_BF16;
+    return made("netfuse_cache_read_fp4",
+                [=] { return f_read_fp4(c.Kc, c.Ks, c.Vc, c.Vs, (const int*)first, (const int*)count, k, v, c.M, c.B, m, c.C, c.kv, c.d, dt, s); });
+  });
+}
+
+// Q, K, V, Kc, Ks, Vc, Vs, length, start, parent, nodes, pos, slope, scale, cap, out, lse, workspace, device, stream
+PyObject* attention_tree_fp4(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, T, heads;
+    float scale, cap;
+    void *len, *start, *parent, *nodes, *pos, *slope, *given, *lse, *ws, *s;
+    CacheFp4 c;
+    if (n != 20 || !types(a[0], a[18], &st, &device)) return not_taken();
+    const at::Tensor *Q = strided(a[0], st, device), *K = strided(a[1], st, device), *V = strided(a[2], st, device);
+    if (!head_size(K, a[3], device, &c.d) || !cache_fp4(a + 3, device, true, &c) || !batch(Q, {c.M, c.B, c.kv, c.C, c.d, nullptr}, &T) || Q->size(2) % c.d || !size(Q->size(2) / c.d, &heads) ||
+        !scale_of(a[13], c.d, &scale) || !number(a[14], &cap) || !stream_of(a[19], &s))
+      return not_taken();
+    Rows q, k, v;
+    const int64_t N = (int64_t)c.B * T, W = (int64_t)heads * c.d;
+    if (!rows(Q, c.M, N, W, &q) || !rows(K, c.M, N, (int64_t)c.kv * c.d, &k) || !rows(V, c.M, N, (int64_t)c.kv * c.d, &v) || k.model != v.model || k.row != v.row ||
+        !dense(a[7], at::kInt, {c.M, c.B}, device, true, &len) || !dense(a[8], at::kInt, {c.M, c.B}, device, false, &start) || !dense(a[9], at::kInt, {c.M, c.B, T}, device, false, &parent) ||
+        !dense(a[10], at::kInt, {c.M, c.B}, device, false, &nodes) || !dense(a[11], at::kInt, {c.M, c.B, c.kv, c.C}, device, false, &pos) ||
+        !dense(a[12], at::kFloat, {c.M, heads}, device, false, &slope) || !dense(a[15], st, {c.M, N, W}, device, false, &given) ||
+        !dense(a[16], at::kFloat, {c.M, N, heads}, device, false, &lse))
+      return not_taken();
+    const nf_dtype dt = type_of(*Q);
+    long long bytes = f_tree_fp4_workspace(c.M, c.B, T, c.C, heads, c.kv, c.d, dt);
+    if (bytes < 0 || !workspace(a[17], device, &ws, &bytes)) return not_taken();
+    at::Tensor room;
+    const bool mine = a[17] == Py_None && bytes > 0;
+    return produce("netfuse_attention_tree_fp4", a[15], {c.M, N, W}, Q->options(), [&](void* y) {
+      if (mine) {
+        room = at::empty({bytes}, Q->options().dtype(at::kByte));
+        ws = room.data_ptr();
+      }
+      return f_tree_fp4(q.p, k.p, v.p, c.Kc, c.Ks, c.Vc, c.Vs, (const int*)pos, (const int*)len, (const int*)start, (const int*)parent, (const int*)nodes, (const float*)slope, y, (float*)lse, ws, bytes,
+                        c.M, c.B, T, c.C, heads, c.kv, c.d, q.model, q.row, k.model, k.row, scale, cap, dt, s);
+    });
+  });
+}
+
+// logits, token, k, vocab, nodes, scale, cap, out, workspace, device, stream: the tuple given, or a new one
+PyObject* token_logprobs(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded([&]() -> PyObject* {
+    at::ScalarType st;
+    int device, M, N, V, k, B = 1, m = 0;
+    float scale, cap;
+    void *token, *vocab, *nodes, *ws, *s, *to[4] = {nullptr, nullptr, nullptr, nullptr};
+    if (n != 11 || !types(a[0], a[9], &st, &device) || !whole(a[2], &k) || k < 0 || k > 32 || !number(a[5], &scale) || !number(a[6], &cap) || !stream_of(a[10], &s)) return not_taken();
+    const at::Tensor* X = strided(a[0], st, device);
+    if (!X || X->dim() != 3 || !size(X->size(0), &M) || !size(X->size(1), &N) || !size(X->size(2), &V) || M <= 0 || N <= 0 || V <= 0) return not_taken();
+    Rows x;
+    if (!rows(X, M, N, V, &x)) return not_taken();
+    if (a[4] != Py_None) {
+      const at::Tensor* t = strided(a[4], at::kInt, device);
+      if (!t || t->dim() != 2 || !size(t->size(1), &B) || B <= 0 || N % B) return not_taken();
+    }
+    if (a[1] != Py_None) {
+      const at::Tensor* t = strided(a[1], at::kInt, device);
+      if (!t || t->dim() != 3 || !size(t->size(2), &m) || m <= 0) return not_taken();
+    }
+    if (!dense(a[1], at::kInt, {M, N, m}, device, false, &token) || !dense(a[3], at::kInt, {M}, device, false, &vocab) || !dense(a[4], at::kInt, {M, B}, device, false, &nodes)) return not_taken();
+    const at::DimVector shape[4] = {{M, N, m}, {M, N}, {M, N, k}, {M, N, k}};
+    const at::ScalarType type[4] = {at::kFloat, at::kFloat, at::kInt, at::kFloat};
+    const bool wanted[4] = {m > 0, true, k > 0, k > 0};
+    const bool given = a[7] != Py_None;
+    if (given) {
+      if (!PyTuple_CheckExact(a[7]) || PyTuple_GET_SIZE(a[7]) != 4) return not_taken();
+      for (int i = 0; i < 4; ++i)
+        if (!dense(PyTuple_GET_ITEM(a[7], i), type[i], shape[i], device, wanted[i], &to[i])) return not_taken();
+    }
+    long long bytes = f_logprobs_workspace(M, B, N / B, V, k);
+    if (bytes < 0 || !workspace(a[8], device, &ws, &bytes)) return not_taken();
+    const nf_dtype dt = type_of(*X);
+    at::Tensor room, made[4];
+    nf_status done_as;
+    {
+      Unlocked unlocked;
+      if (a[8] == Py_None) {
+        room = at::empty({bytes}, X->options().dtype(at::kByte));
+        ws = room.data_ptr();
+      }
+      for (int i = 0; i < 4 && !given; ++i)
+        if (wanted[i]) {
+          made[i] = at::empty(shape[i], X->options().dtype(type[i]));
+          to[i] = made[i].data_ptr();
+        }
+      done_as = f_logprobs(x.p, (const int*)token, (const int*)vocab, (const int*)nodes, (float*)to[0], (float*)to[1], (int*)to[2], (float*)to[3], ws, bytes, M, B, N / B, V, m, k, x.model, x.row, scale,
+                           cap, dt, s);
+    }
+    at::Tensor none;
+    PyObject* ok = done("netfuse_token_logprobs", done_as, given ? a[7] : Py_True, none);
+    if (!ok || given) return ok;
+    Py_DECREF(ok);
+    PyObject* all = PyTuple_New(4);
+    for (int i = 0; all && i < 4; ++i) {
+      PyObject* t = Py_None;
+      if (wanted[i]) t = THPVariable_Wrap(std::move(made[i]));
+      else Py_INCREF(t);
+      if (!t) {
+        Py_DECREF(all);
+        return nullptr;
+      }
+      PyTuple_SET_ITEM(all, i, t);
+    }
+    return all;
+  });
+}
+
+// bind_step: the addresses of rotate_heads, cache_append_fp4, cache_read_fp4, attention_tree_fp4 and its workspace, token_logprobs and its workspace
+PyObject* bind_step(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 7) {
+    PyErr_SetString(PyExc_TypeError, "bind_step takes seven addresses");
+    return nullptr;
+  }
+  void* p[7];
+  for (int i = 0; i < 7; ++i) {
+    p[i] = PyLong_AsVoidPtr(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  f_rotate = (decltype(f_rotate))p[0];
+  f_append_fp4 = (decltype(f_append_fp4))p[1];
+  f_read_fp4 = (decltype(f_read_fp4))p[2];
+  f_tree_fp4 = (decltype(f_tree_fp4))p[3];
+  f_tree_fp4_workspace = (decltype(f_tree_fp4_workspace))p[4];
+  f_logprobs = (decltype(f_logprobs))p[5];
+  f_logprobs_workspace = (decltype(f_logprobs_workspace))p[6];
+  Py_RETURN_NONE;
+}
+
 // bind_decoder: the addresses of prompt, tree and its workspace, append, weigh, evict and its workspace
 PyObject* bind_decoder(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 7) {
@@ -532,7 +822,8 @@ PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(bind), FAST(linear), FAST(linear_packed), FAST(layernorm), FAST(attention_packed), FAST(attention_relpos_packed),
-                         FAST(conv2d), FAST(bind_decoder), FAST(attention_prompt), FAST(attention_tree), FAST(cache_append), FAST(cache_weigh), FAST(cache_evict), {nullptr, nullptr, 0, nullptr}};
+                         FAST(conv2d), FAST(bind_decoder), FAST(attention_prompt), FAST(attention_tree), FAST(cache_append), FAST(cache_weigh), FAST(cache_evict), FAST(bind_step),
+                         FAST(rotate_heads), FAST(cache_append_fp4), FAST(cache_read_fp4), FAST(attention_tree_fp4), FAST(token_logprobs), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

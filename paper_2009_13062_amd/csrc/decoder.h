@@ -21,6 +21,7 @@ struct DecArgs {
   int M, B, N, C, heads, kv, d, causal;
   long q_stride_m, q_stride_row, kv_stride_m, kv_stride_row;
   float scale, cap, inv_cap;                            // inv_cap = 1 / cap, 0 without a cap
+  const uint8_t* Ks; const uint8_t* Vs;                 // scales of a cache of 4 bits, null for others
 };
 
 struct WeighArgs {

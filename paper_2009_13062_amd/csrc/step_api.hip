@@ -1,0 +1,233 @@
+// C ABI of what surrounds the decoders' attention: heads normed and rotated, the cache of 4 bits and the attention over it, log probabilities of tokens.  Argument validation
+// on the host before any HIP call, kernel selection by sizes, type and alignment.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include <algorithm>
+
+#include "cache_fp4_kernels.h"
+#include "decoder.h"
+#include "decoder_fp4_generic.h"
+#include "decoder_host.h"
+#include "logprob_kernels.h"
+#include "nf_host.h"
+#include "nf_launch.h"
+#include "rotate_kernels.h"
+
+using namespace nf;
+
+namespace {
+
+inline nf_status launched() { return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH; }
+inline bool whole_pieces(long stride_m, long stride_row, size_t esz) { return stride_m * (long)esz % 16 == 0 && stride_row * (long)esz % 16 == 0; }
+
+template <typename T>
+nf_status launch_rotate(const RotateArgs& a, bool pieces, hipStream_t s) {
+  const long long tokens = prod({a.M, a.B, a.S});
+  if (!pieces) {
+    const long long blocks = (prod({tokens, a.heads + (long long)a.kv}) + 3) / 4;
+    if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
+    nf_launch((rotate_rows_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+    return launched();
+  }
+  constexpr int P = Piece<T>::kN;
+  const int units = (a.d + 2 * P - 1) / (2 * P);
+  int lph = 1;
+  while (lph < units) lph *= 2;
+  const int at_once = kWave / lph, steps = (a.heads + at_once - 1) / at_once + (a.kv + at_once - 1) / at_once;
+  const int parts = 1, per_wave = steps;
+  const long long blocks = (prod({tokens, parts}) + 3) / 4;
+  if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
+#define NF_ROTATE(LPH) nf_launch((rotate_pieces_kernel<T, LPH>), dim3((unsigned)blocks), dim3(256), 0, s, a, parts, per_wave)
+  switch (lph) {
+    case 1: NF_ROTATE(1); break;
+    case 2: NF_ROTATE(2); break;
+    case 4: NF_ROTATE(4); break;
+    case 8: NF_ROTATE(8); break;
+    case 16: NF_ROTATE(16); break;
+    default: NF_ROTATE(32); break;
+  }
+#undef NF_ROTATE
+  return launched();
+}
+
+nf_status launch_fp4_rows(const DecArgs& a, nf_dtype dt, hipStream_t s) {
+  const long long blocks = (prod({a.M, a.B, a.heads, a.N}) + 3) / 4;
+  if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
+#define NF_ROWS(T, DPL) nf_launch((decoder_fp4_rows_kernel<T, DPL>), dim3((unsigned)blocks), dim3(256), 0, s, a)
+  if (dt == NF_F32) {
+    if (a.d <= 64) NF_ROWS(float, 1); else if (a.d <= 128) NF_ROWS(float, 2); else NF_ROWS(float, 4);
+  } else {
+    if (a.d <= 64) NF_ROWS(bf16_t, 1); else if (a.d <= 128) NF_ROWS(bf16_t, 2); else NF_ROWS(bf16_t, 4);
+  }
+#undef NF_ROWS
+  return launched();
+}
+
+int logprob_chunks(int V) { return (int)(((long long)V + LogprobShape::kChunk - 1) / LogprobShape::kChunk); }
+
+}  // namespace
+
+extern "C" {
+
+nf_status netfuse_rotate_heads(const void* Q, const void* K, const float* gamma_q, const float* gamma_k, const float* freq, const int* pos,
+                               const int* start, const int* len, const int* sections, void* Qo, void* Ko, int M, int B, int S, int heads,
+                               int kv_heads, int d, int rot, int axes, long q_stride_m, long q_stride_row, long k_stride_m,
+                               long k_stride_row, long qo_stride_m, long qo_stride_row, long ko_stride_m, long ko_stride_row, float eps,
+                               int interleaved, nf_dtype dt, void* stream) {
+  if (!Q || !Qo || (K == nullptr) != (Ko == nullptr) || (K == nullptr) != (kv_heads == 0)) return NF_EINVAL;
+  if (M <= 0 || B <= 0 || S <= 0 || heads <= 0 || kv_heads < 0 || d <= 0 || !is_dtype(dt)) return NF_EINVAL;
+  if (rot < 0 || rot > d || rot % 2 || (rot > 0 && !freq) || axes < 1 || axes > 4 || (axes > 1 && (!sections || !pos))) return NF_EINVAL;
+  if (!std::isfinite(eps) || eps < 0.f) return NF_EINVAL;
+  if (prod({B, S}) > INT_MAX / 2 || prod({M, B, S, heads, d}) >= kMaxElems || (long long)heads + kv_heads > INT_MAX) return NF_EINVAL;
+  const long long N = (long long)B * S;
+  if (!rows_ok(M, N, (long long)heads * d, q_stride_m, q_stride_row) || !rows_ok(M, N, (long long)heads * d, qo_stride_m, qo_stride_row)) return NF_EINVAL;
+  if (K && (!rows_ok(M, N, (long long)kv_heads * d, k_stride_m, k_stride_row) || !rows_ok(M, N, (long long)kv_heads * d, ko_stride_m, ko_stride_row))) return NF_EINVAL;
+  const size_t esz = dt == NF_F32 ? 4 : 2;
+  if (!aligned(Q, esz) || !aligned(K, esz) || !aligned(Qo, esz) || !aligned(Ko, esz) || !aligned(gamma_q, 4) || !aligned(gamma_k, 4) || !aligned(freq, 4) ||
+      !aligned(pos, 4) || !aligned(start, 4) || !aligned(len, 4))
+    return NF_EINVAL;
+  if ((Q == Qo && (q_stride_m != qo_stride_m || q_stride_row != qo_stride_row)) || (K && K == Ko && (k_stride_m != ko_stride_m || k_stride_row != ko_stride_row))) return NF_EINVAL;
+  RotateArgs a = {};
+  a.Q = Q; a.K = K; a.gamma_q = gamma_q; a.gamma_k = gamma_k; a.freq = freq; a.pos = pos; a.start = start; a.len = len; a.Qo = Qo; a.Ko = Ko;
+  a.M = M; a.B = B; a.S = S; a.heads = heads; a.kv = kv_heads; a.d = d; a.rot = rot; a.axes = axes; a.interleaved = interleaved != 0;
+  long long pairs = 0;
+  for (int x = 0; x < 3; ++x) a.axis_end[x] = INT_MAX;
+  for (int x = 0; x < axes && sections; ++x) {
+    if (sections[x] < 0) return NF_EINVAL;
+    pairs += sections[x];
+    if (x + 1 < axes) a.axis_end[x] = (int)std::min<long long>(pairs, INT_MAX);
+  }
+  if (sections && pairs != rot / 2) return NF_EINVAL;
+  if (d > 256) return NF_EUNSUPPORTED;
+  a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.k_stride_m = k_stride_m; a.k_stride_row = k_stride_row;
+  a.qo_stride_m = qo_stride_m; a.qo_stride_row = qo_stride_row; a.ko_stride_m = ko_stride_m; a.ko_stride_row = ko_stride_row;
+  a.eps = eps;
+  const int P = 16 / (int)esz;
+  const bool pieces = d % P == 0 && rot % (2 * P) == 0 && whole_pieces(q_stride_m, q_stride_row, esz) && whole_pieces(qo_stride_m, qo_stride_row, esz) &&
+                      (!K || (whole_pieces(k_stride_m, k_stride_row, esz) && whole_pieces(ko_stride_m, ko_stride_row, esz))) && aligned(Q, 16) && aligned(K, 16) && aligned(Qo, 16) &&
+                      aligned(Ko, 16);
+  return dt == NF_F32 ? launch_rotate<float>(a, pieces, (hipStream_t)stream) : launch_rotate<bf16_t>(a, pieces, (hipStream_t)stream);
+}
+
+nf_status netfuse_cache_append_fp4(const void* K, const void* V, const int* index, const int* count, const int* len, const int* start, void* Kc,
+                                   void* Ks, void* Vc, void* Vs, int* pos, float* weight, int M, int B, int T, int n, int C, int kv_heads,
+                                   int d, long kv_stride_m, long kv_stride_row, nf_dtype dt, void* stream) {
+  if (!K || !V || !Kc || !Ks || !Vc || !Vs || !len) return NF_EINVAL;
+  if (M <= 0 || B <= 0 || T <= 0 || n <= 0 || C <= 0 || C > kMostEntries || kv_heads <= 0 || d <= 0 || !is_dtype(dt)) return NF_EINVAL;
+  if (!index && n != T) return NF_EINVAL;
+  if (prod({B, T}) > INT_MAX / 2 || prod({B, n}) > INT_MAX / 2 || prod({M, B, kv_heads, C, d}) >= kMaxElems) return NF_EINVAL;
+  if (!rows_ok(M, (long long)B * T, (long long)kv_heads * d, kv_stride_m, kv_stride_row)) return NF_EINVAL;
+  const size_t esz = dt == NF_F32 ? 4 : 2;
+  if (!aligned(K, esz) || !aligned(V, esz) || !aligned(Kc, 16) || !aligned(Ks, 16) || !aligned(Vc, 16) || !aligned(Vs, 16) || !aligned(index, 4) || !aligned(count, 4) ||
+      !aligned(len, 4) || !aligned(start, 4) || !aligned(pos, 4) || !aligned(weight, 4))
+    return NF_EINVAL;
+  if (d > 256) return NF_EUNSUPPORTED;
+  const long long per_row = 4LL * kv_heads * fp4_groups(d);
+  if (per_row > INT_MAX / 2) return NF_EUNSUPPORTED;
+  const AppendFp4Args a = {K, V, index, count, len, start, (uint8_t*)Kc, (uint8_t*)Ks, (uint8_t*)Vc, (uint8_t*)Vs, pos, weight, M, B, T, n, C, kv_heads, d, kv_stride_m, kv_stride_row};
+  const int rows = (int)std::max<long long>(1, std::min<long long>(n, 512 / per_row));
+  const int per_seq = (n + rows - 1) / rows;
+  const long long blocks = prod({M, B, per_seq});
+  if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
+  const bool wide = d * esz % 16 == 0 && whole_pieces(kv_stride_m, kv_stride_row, esz) && aligned(K, 16) && aligned(V, 16);
+  hipStream_t s = (hipStream_t)stream;
+#define NF_APPEND(T, WIDE) nf_launch((cache_append_fp4_kernel<T, WIDE>), dim3((unsigned)blocks), dim3(256), 0, s, a, rows, per_seq)
+  if (dt == NF_F32) { if (wide) NF_APPEND(float, true); else NF_APPEND(float, false); }
+  else { if (wide) NF_APPEND(bf16_t, true); else NF_APPEND(bf16_t, false); }
+#undef NF_APPEND
+  return launched();
+}
+
+nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc, const void* Vs, const int* first, const int* count, void* K, void* V,
+                                 int M, int B, int n, int C, int kv_heads, int d, nf_dtype dt, void* stream) {
+  if (!Kc || !Ks || !K || (Vc == nullptr) != (V == nullptr) || (Vs == nullptr) != (V == nullptr)) return NF_EINVAL;
+  if (M <= 0 || B <= 0 || n <= 0 || C <= 0 || C > kMostEntries || n > kMostEntries || kv_heads <= 0 || d <= 0 || !is_dtype(dt)) return NF_EINVAL;
+  if (prod({M, B, kv_heads, C, d}) >= kMaxElems || prod({M, B, kv_heads, n, d}) >= kMaxElems) return NF_EINVAL;
+  const size_t esz = dt == NF_F32 ? 4 : 2;
+  if (!aligned(Kc, 16) || !aligned(Ks, 16) || !aligned(Vc, 16) || !aligned(Vs, 16) || !aligned(K, esz) || !aligned(V, esz) || !aligned(first, 4) || !aligned(count, 4)) return NF_EINVAL;
+  if (d > 256) return NF_EUNSUPPORTED;
+  const ReadFp4Args a = {(const uint8_t*)Kc, (const uint8_t*)Ks, (const uint8_t*)Vc, (const uint8_t*)Vs, first, count, K, V, M, B, n, C, kv_heads, d};
+  const int units = (d + 7) / 8, rows = std::max(1, std::min(n, 1024 / units)), per_head = (n + rows - 1) / rows;
+  const long long blocks = prod({M, B, kv_heads, per_head});
+  if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
+  const bool wide = d * esz % 16 == 0 && aligned(K, 16) && aligned(V, 16);
+  hipStream_t s = (hipStream_t)stream;
+#define NF_READ(T, WIDE) nf_launch((cache_read_fp4_kernel<T, WIDE, 4>), dim3((unsigned)blocks), dim3(256), 0, s, a, rows, per_head)
+  if (dt == NF_F32) { if (wide) NF_READ(float, true); else NF_READ(float, false); }
+  else { if (wide) NF_READ(bf16_t, true); else NF_READ(bf16_t, false); }
+#undef NF_READ
+  return launched();
+}
+
+long long netfuse_attention_tree_fp4_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt) {
+  if (M <= 0 || B <= 0 || T <= 0 || T > 64 || C <= 0 || C > kMostEntries || !heads_ok(heads, kv_heads, d) || d > 256 || !is_dtype(dt)) return -1;
+  return 0;
+}
+
+nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V, const void* Kc, const void* Ks, const void* Vc, const void* Vs,
+                                     const int* pos, const int* len, const int* start, const int* parent, const int* nodes, const float* slope,
+                                     void* O, float* lse, void* workspace, long long workspace_bytes, int M, int B, int T, int C, int heads,
+                                     int kv_heads, int d, long q_stride_m, long q_stride_row, long kv_stride_m, long kv_stride_row,
+                                     float scale, float cap, nf_dtype dt, void* stream) {
+  if (!Q || !K || !V || !Kc || !Ks || !Vc || !Vs || !len || !O) return NF_EINVAL;
+  if (M <= 0 || B <= 0 || T <= 0 || C <= 0 || C > kMostEntries || !heads_ok(heads, kv_heads, d)) return NF_EINVAL;
+  if (!is_dtype(dt) || !score_ok(scale, cap)) return NF_EINVAL;
+  if (prod({B, T}) > INT_MAX / 2 || prod({M, B, T, heads, d}) >= kMaxElems || prod({M, B, kv_heads, C, d}) >= kMaxElems) return NF_EINVAL;
+  if (!rows_ok(M, (long long)B * T, (long long)heads * d, q_stride_m, q_stride_row) ||
+      !rows_ok(M, (long long)B * T, (long long)kv_heads * d, kv_stride_m, kv_stride_row))
+    return NF_EINVAL;
+  const size_t esz = dt == NF_F32 ? 4 : 2;
+  if (!aligned(Q, esz) || !aligned(K, esz) || !aligned(V, esz) || !aligned(Kc, 16) || !aligned(Ks, 16) || !aligned(Vc, 16) || !aligned(Vs, 16) || !aligned(O, esz) ||
+      !aligned(pos, 4) || !aligned(len, 4) || !aligned(start, 4) || !aligned(parent, 4) || !aligned(nodes, 4) || !aligned(slope, 4) || !aligned(lse, 4) || !aligned(workspace, 16))
+    return NF_EINVAL;
+  if (T > 64 || d > 256) return NF_EUNSUPPORTED;
+  const long long need = netfuse_attention_tree_fp4_workspace(M, B, T, C, heads, kv_heads, d, dt);
+  if (need < 0) return NF_EUNSUPPORTED;
+  if (need > 0 && (!workspace || workspace_bytes < need)) return NF_EINVAL;
+  DecArgs a = {};
+  a.Q = Q; a.K = K; a.V = V; a.Kc = Kc; a.Vc = Vc; a.Ks = (const uint8_t*)Ks; a.Vs = (const uint8_t*)Vs; a.slope = slope; a.len = len; a.start = start; a.parent = parent;
+  a.nodes = nodes; a.pos = pos; a.O = O; a.lse = lse; a.ws = (float*)workspace;
+  a.M = M; a.B = B; a.N = T; a.C = C; a.heads = heads; a.kv = kv_heads; a.d = d;
+  a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.kv_stride_m = kv_stride_m; a.kv_stride_row = kv_stride_row;
+  a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
+  return launch_fp4_rows(a, dt, (hipStream_t)stream);
+}
+
+long long netfuse_token_logprobs_workspace(int M, int B, int T, int V, int k) {
+  if (M <= 0 || B <= 0 || T <= 0 || V <= 0 || V > kMostEntries || k < 0 || k > kMostAlternatives) return -1;
+  const long long bytes = prod({M, B, T, logprob_chunks(V), 4LL * logprob_words(k)});
+  return bytes >= kMaxElems ? -1 : bytes;
+}
+
+nf_status netfuse_token_logprobs(const void* logits, const int* token, const int* vocab, const int* nodes, float* logp, float* entropy, int* top,
+                                 float* top_logp, void* workspace, long long workspace_bytes, int M, int B, int T, int V, int n, int k,
+                                 long stride_m, long stride_row, float scale, float cap, nf_dtype dt, void* stream) {
+  if (!logits || !entropy || !workspace) return NF_EINVAL;
+  if (M <= 0 || B <= 0 || T <= 0 || V <= 0 || V > kMostEntries || n < 0 || k < 0 || !is_dtype(dt)) return NF_EINVAL;
+  if ((n > 0 && (!token || !logp)) || (k > 0 && (!top || !top_logp))) return NF_EINVAL;
+  if (!score_ok(scale, cap) || scale <= 0.f) return NF_EINVAL;
+  if (prod({B, T}) > INT_MAX / 2 || prod({M, B, T, V}) >= kMaxElems || prod({M, B, T, n}) >= kMaxElems || prod({M, B, T}) > INT_MAX) return NF_EINVAL;
+  if (!rows_ok(M, (long long)B * T, V, stride_m, stride_row)) return NF_EINVAL;
+  const size_t esz = dt == NF_F32 ? 4 : 2;
+  if (!aligned(logits, esz) || !aligned(token, 4) || !aligned(vocab, 4) || !aligned(nodes, 4) || !aligned(logp, 4) || !aligned(entropy, 4) || !aligned(top, 4) ||
+      !aligned(top_logp, 4) || !aligned(workspace, 16))
+    return NF_EINVAL;
+  if (k > kMostAlternatives) return NF_EUNSUPPORTED;
+  const long long need = netfuse_token_logprobs_workspace(M, B, T, V, k);
+  if (need < 0 || workspace_bytes < need) return NF_EINVAL;
+  const LogprobArgs a = {logits, token, vocab, nodes, logp, entropy, top, top_logp, (float*)workspace, M, B, T, V, n, k, logprob_chunks(V),
+                         stride_m, stride_row, scale, cap, cap != 0.f ? 1.f / cap : 0.f};
+  const long long rows = prod({M, B, T}), blocks = (prod({rows, a.chunks}) + 3) / 4;
+  if (!grid_fits(blocks, 256) || !grid_fits(rows, 64)) return NF_EUNSUPPORTED;          // before the first of the two is enqueued
+  hipStream_t s = (hipStream_t)stream;
+  if (dt == NF_F32) nf_launch((logprob_chunks_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+  else nf_launch((logprob_chunks_kernel<bf16_t>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+  const nf_status st = launched();
+  if (st != NF_OK) return st;
+  if (dt == NF_F32) nf_launch((logprob_join_kernel<float>), dim3((unsigned)rows), dim3(64), 0, s, a);
+  else nf_launch((logprob_join_kernel<bf16_t>), dim3((unsigned)rows), dim3(64), 0, s, a);
+  return launched();
+}
+
+}  // extern "C"
