@@ -1,0 +1,48 @@
+// Attention of drafted trees over a cache of 4 bits on the matrix pipe: instances and launches of decoder_stream.h.
+#include <atomic>
+
+#include "decoder_launch.h"
+#include "decoder_stream.h"
+#include "nf_host.h"
+#include "nf_launch.h"
+
+namespace nf {
+namespace {
+
+template <typename T, int D, int RT, int KS, bool EXACT>
+nf_status go_rows(const DecArgs& a, int splits, int chunk, hipStream_t s) {
+  constexpr int kRows = 4 / KS * RT * 16, kBytes = stream_lds_bytes(RT, KS, D / 16);
+  const long long R = (long long)a.N * (a.heads / a.kv), row_blocks = (R + kRows - 1) / kRows;
+  const long long total = prod({a.M, a.B, a.kv, row_blocks, splits});
+  if (!grid_fits(total, 256)) return NF_EUNSUPPORTED;
+  const auto kernel = decoder_stream_kernel<T, D, RT, KS, true, true, EXACT>;
+  static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
+  if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {
+    if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) != hipSuccess) return NF_ELAUNCH;
+    opted_in.store(true, std::memory_order_release);
+  }
+  nf_launch(kernel, dim3((unsigned)total), dim3(256), kBytes, s, a, (int)row_blocks, splits, chunk);
+  return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH;
+}
+
+template <typename T, int D, int RT, int KS>
+nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
+  return a.d == D ? go_rows<T, D, RT, KS, true>(a, splits, chunk, s) : go_rows<T, D, RT, KS, false>(a, splits, chunk, s);
+}
+
+template <typename T, int D>
+nf_status tree(const DecArgs& a, int splits, int chunk, hipStream_t s) {
+  const int R = a.N * (a.heads / a.kv);
+  if (R <= 16) return go<T, D, 1, 4>(a, splits, chunk, s);
+  if (R <= 32) return go<T, D, 1, 2>(a, splits, chunk, s);
+  return go<T, D, 1, 1>(a, splits, chunk, s);
+}
+
+}  // namespace
+
+nf_status launch_tree_fp4_stream(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s) {
+  if (dt == NF_F32) return a.d <= 64 ? tree<float, 64>(a, splits, chunk, s) : a.d <= 128 ? tree<float, 128>(a, splits, chunk, s) : tree<float, 256>(a, splits, chunk, s);
+  return a.d <= 64 ? tree<bf16_t, 64>(a, splits, chunk, s) : a.d <= 128 ? tree<bf16_t, 128>(a, splits, chunk, s) : tree<bf16_t, 256>(a, splits, chunk, s);
+}
+
+}  // namespace nf

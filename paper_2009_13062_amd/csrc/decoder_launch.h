@@ -13,6 +13,10 @@ namespace nf {
 inline int tree_chunk(int rows, nf_dtype dt) { return rows > (dt == NF_F32 ? 64 : 32) ? 1024 : 512; }
 inline int tree_features(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
+// Of a cache of 4 bits
+inline int tree_fp4_chunk(int rows, nf_dtype dt) { return tree_chunk(rows, dt); }
+nf_status launch_tree_fp4_stream(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s);
+
 struct WeighArgs;
 // decoder_tiles.h: bfloat16
 nf_status launch_prompt_tiles(const DecArgs& a, hipStream_t s);

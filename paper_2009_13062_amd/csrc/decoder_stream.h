@@ -23,6 +23,7 @@
 #pragma once
 #include "decoder.h"
 #include "decoder_tiles.h"
+#include "fp4.h"
 
 namespace nf {
 
@@ -42,6 +43,36 @@ constexpr int stream_lds_bytes(int RT, int KS, int NB) { return KS > 1 ? (256 * 
 
 template <int W> struct Words { uint32_t w[W]; };
 
+// Eight float32 values in bfloat16 parts, a pair to a dword: two that hold 15 bits -- the upper 8, of a value a little smaller, and the rest, rounded; neither is 0
+// where the value is not, so an infinity on the other side of the product stays that infinity -- and three that hold all 24.  What is not finite is the first part's alone.
+__device__ __forceinline__ void split2(const float (&v)[8], uint32_t (&w)[3][4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t x = __float_as_uint(v[2 * e] * 0x1.ffp-1f), y = __float_as_uint(v[2 * e + 1] * 0x1.ffp-1f);
+    w[0][e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    w[1][e] = pack_bf16x2(v[2 * e] - __uint_as_float(x & 0xffff0000u), v[2 * e + 1] - __uint_as_float(y & 0xffff0000u));
+  }
+}
+__device__ __forceinline__ void split3(const float (&v)[8], uint32_t (&w)[3][4]) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float a[2], b[2], c[2];
+#pragma unroll
+    for (int z = 0; z < 2; ++z) {
+      const float x = v[2 * e + z];
+      a[z] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+      const float rest = fabsf(x) < INFINITY ? x - a[z] : 0.f;
+      b[z] = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
+      c[z] = rest - b[z];
+    }
+    // a NaN whose payload lies in the lower half is an infinity in the upper one: kept by the conversion's rounding instead
+    w[0][e] = fabsf(v[2 * e]) < INFINITY && fabsf(v[2 * e + 1]) < INFINITY ? __builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), 0x07060302u)
+                                                                         : pack_bf16x2(v[2 * e] != v[2 * e] ? v[2 * e] : a[0], v[2 * e + 1] != v[2 * e + 1] ? v[2 * e + 1] : a[1]);
+    w[1][e] = __builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), 0x07060302u);
+    w[2][e] = __builtin_amdgcn_perm(__float_as_uint(c[1]), __float_as_uint(c[0]), 0x07060302u);
+  }
+}
+
 // a . b^T over a 64-byte slice, accumulated: 16 rows of a (lane % 16) by 16 rows of b
 template <typename T> __device__ __forceinline__ f32x4_t slice_product(const uint4& a, const uint4& b, f32x4_t c) {
   if constexpr (sizeof(T) == 2) {
@@ -54,9 +85,18 @@ template <typename T> __device__ __forceinline__ f32x4_t slice_product(const uin
   }
 }
 
-template <typename T, int D, int RT, int KS, bool TREE>
-__global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 ? 3 : 2) void decoder_stream_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
+// Of a cache of 4 bits: 16-key blocks of a step, dwords of codes of a lane and key, parts that queries and weights are taken in (float32: 8 bits in each of three)
+template <typename T, int D> struct Fp4Shape {
+  static constexpr int NK = D > 128 ? 2 : 4, kStep = 16 * NK, kWords = D / 32, kScales = D > 128 ? 2 : 1;
+  static constexpr int kQueryParts = sizeof(T) == 2 ? 1 : 3, kWeightParts = sizeof(T) == 2 ? 2 : 3;
+};
+
+// FP4: the cache is one of 4 bits (TREE); EXACT: of D features, so that rows lie a known number of bytes apart and a step's loads differ in their immediate offsets.
+template <typename T, int D, int RT, int KS, bool TREE, bool FP4 = false, bool EXACT = false>
+__global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void decoder_stream_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
+  static_assert(TREE || !FP4, "prompts have no cache");
   using Sh = StreamShape<T, D>;
+  using Q4 = Fp4Shape<T, D>;
   constexpr bool kBf = Sh::kBf;
   constexpr int NK = Sh::NK, NB = Sh::NB, VF = Sh::VF, VC = Sh::VC, SL = Sh::kSlices, kStep = 16 * NK, RG = 4 / KS;
   constexpr int kRows = RG * RT * 16;                      // per workgroup
@@ -103,7 +143,8 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 ? 3 : 2) void decoder_st
 
   // ---- the steps of this wavefront: of its chunk of the cache, then of the tree; every KS-th is its own
   const int key_start = TREE ? split * chunk : 0;
-  const int cached_steps = key_end > key_start ? (key_end - key_start + kStep - 1) / kStep : 0;
+  constexpr int kCachedStep = FP4 ? Q4::kStep : kStep;
+  const int cached_steps = key_end > key_start ? (key_end - key_start + kCachedStep - 1) / kCachedStep : 0;
   const int steps = cached_steps + (TREE && split == parts - 1 ? (a.N + kStep - 1) / kStep : 0);
   constexpr int kPerBallot = kStep < kWave ? kWave / kStep : 1, kWindow = 8 * kPerBallot;
   uint32_t win_any = 0, win_all = 0;                       // of kWindow steps from win_at on: which hold a document of the rows, nothing but their only one
@@ -140,9 +181,11 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 ? 3 : 2) void decoder_st
     return !doc || ((win_all >> (st - win_at)) & 1);
   };
 
+  // The feature that a lane's piece of slice sl begins with.  A lane of a cache of 4 bits takes D / 4 neighbouring features, whose codes are one load.
+  auto feature = [&](int sl) { return FP4 ? g4 * (D / 4) + sl * Sh::kPiece : sl * Sh::kSliceF + g4 * Sh::kPiece; };
   uint4 kreg[NK][SL];
   Words<Sh::kVWords> vreg[NK * 4][VC];
-  int key_reg = 0;                                         // position or document of key `lane` of the step
+  int key_reg = 0, key_first = 0;                          // position or document of key `lane` of the step
   auto load_keys = [&](int st) {
     const bool own_step = TREE && st >= cached_steps;
     const int base = own_step ? (st - cached_steps) * kStep : key_start + st * kStep, limit = (own_step ? a.N : L) - base;
@@ -151,9 +194,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 ? 3 : 2) void decoder_st
     const unsigned row = (unsigned)(rows * (long)sizeof(T));
 #pragma unroll
     for (int k = 0; k < NK; ++k) {
-      const unsigned from = 16 * k + l16 < limit ? (16 * k + l16) * row + g4 * 16 : kDecOob;
+      const unsigned from = 16 * k + l16 < limit ? (16 * k + l16) * row + g4 * (FP4 ? SL * 16 : 16) : kDecOob;
 #pragma unroll
-      for (int sl = 0; sl < SL; ++sl) kreg[k][sl] = rows_load16(rk, sl * Sh::kSliceF + g4 * Sh::kPiece < a.d ? from + sl * 64 : kDecOob);
+      for (int sl = 0; sl < SL; ++sl) kreg[k][sl] = rows_load16(rk, feature(sl) < a.d ? from + sl * (FP4 ? 16 : 64) : kDecOob);
     }
     if (keyed) {
       const int there = base + min(lane, limit - 1);
@@ -186,7 +229,72 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 ? 3 : 2) void decoder_st
 
   int st = share;
   const bool early = TREE || !doc;                         // the first keys are on their way before anything else is looked up
-  if (early && st < steps) load_keys(st);
+
+  // ---- a cache of 4 bits: codes and scales of a step as they are held.  A resource ends with the chunk's last entry, so what lies behind it comes back as 0.
+  uint32_t kcode[Q4::NK][Q4::kWords], kscale[Q4::NK][Q4::kScales], vcode[Q4::NK * 4][VC], vscale[Q4::NK * 4][VC];
+  const int code_row = EXACT ? fp4_code_bytes(D) : fp4_code_bytes(a.d), scale_row = EXACT ? fp4_scale_bytes(D) : fp4_scale_bytes(a.d);
+  int fp4_lane = lane;                                     // made new in every step: offsets that stay the same would be kept in a register each
+  auto fp4_rows = [&](const void* p, int base, int row) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)p + (head * a.C + base) * row), 0, (key_end - base) * row, 0x00020000);
+  };
+  auto load_fp4_keys = [&](int st4) {
+    const int base = key_start + st4 * Q4::kStep;
+    const auto rk = fp4_rows(a.Kc, base, code_row), rs = fp4_rows(a.Ks, base, scale_row);
+    const int k0 = fp4_lane % 16, part = fp4_lane / 16 * (D / 8), grp = fp4_lane / 16 * (D / 4) / kFp4Group;
+    const int from = k0 * code_row + part, scale_from = k0 * scale_row + grp;
+#pragma unroll
+    for (int k = 0; k < Q4::NK; ++k) {
+#pragma unroll
+      for (int w = 0; w < Q4::kWords; w += 4) {
+        const int off = EXACT || part + w * 4 < code_row ? from + 16 * k * code_row + w * 4 : (int)kDecOob;
+        if constexpr (Q4::kWords == 2) {
+          const dec_u32x2_t v = __builtin_amdgcn_raw_buffer_load_b64(rk, off, 0, 0);
+          kcode[k][0] = v.x;
+          kcode[k][1] = v.y;
+        } else {
+          const uint4 v = rows_load16(rk, off);
+          kcode[k][w] = v.x; kcode[k][w + 1] = v.y; kcode[k][w + 2] = v.z; kcode[k][w + 3] = v.w;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < Q4::kScales; ++x)
+        kscale[k][x] = __builtin_amdgcn_raw_buffer_load_b8(rs, EXACT || grp + x < scale_row ? scale_from + 16 * k * scale_row + x : (int)kDecOob, 0, 0);
+    }
+    if (biased && a.pos) key_reg = a.pos[head * a.C + base + min(lane, key_end - base - 1)];
+  };
+  // A key's scales come whole where a row of them is 2 bytes (up to 64 features) or 4 (up to 128).
+  const int value_group = l16 * VF / kFp4Group;
+  auto load_fp4_values = [&](int st4) {
+    const int base = key_start + st4 * Q4::kStep;
+    const auto rv = fp4_rows(a.Vc, base, code_row), rs = fp4_rows(a.Vs, base, scale_row);
+    const int k0 = fp4_lane / 16 * 4, byte = fp4_lane % 16 * VF / 2, grp = fp4_lane % 16 * VF / kFp4Group;
+    const int from = k0 * code_row + byte, scale_from = k0 * scale_row + (D > 128 ? grp : 0);
+#pragma unroll
+    for (int e = 0; e < Q4::NK * 4; ++e) {
+      const int key = e / 4 * 16 + e % 4;
+#pragma unroll
+      for (int c = 0; c < VC; ++c) {
+        const int off = EXACT || byte + c * 8 * VF < code_row ? from + key * code_row + c * 8 * VF : (int)kDecOob, soff = scale_from + key * scale_row;
+        if constexpr (VF == 4) vcode[e][c] = __builtin_amdgcn_raw_buffer_load_b16(rv, off, 0, kOnce);
+        else vcode[e][c] = __builtin_amdgcn_raw_buffer_load_b32(rv, off, 0, kOnce);
+        if constexpr (D == 64) vscale[e][c] = __builtin_amdgcn_raw_buffer_load_b16(rs, soff, 0, 0);
+        else if constexpr (D == 128) vscale[e][c] = __builtin_amdgcn_raw_buffer_load_b32(rs, soff, 0, 0);
+        else vscale[e][c] = __builtin_amdgcn_raw_buffer_load_b8(rs, EXACT || c * VF / 2 + grp < scale_row ? soff + c * VF / 2 : (int)kDecOob, 0, 0);
+      }
+    }
+  };
+  int st4 = share;
+  if constexpr (FP4) {                                     // the tree's own steps come first
+    if (st4 < cached_steps) {
+      load_fp4_keys(st4);
+      load_fp4_values(st4);
+    }
+    st = cached_steps + share;
+    key_first = key_reg;
+    if (st < steps) load_keys(st);
+  } else {
+    if (early && st < steps) load_keys(st);
+  }
 
   // ---- this lane's rows
   int token[RT], end[RT], mine[RT], docr[RT];
@@ -201,7 +309,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 ? 3 : 2) void decoder_st
     const T* q = (const T*)a.Q + m * a.q_stride_m + ((long)b * a.N + i) * a.q_stride_row + (long)h * a.d;
 #pragma unroll
     for (int sl = 0; sl < SL; ++sl) {
-      const int f = sl * Sh::kSliceF + g4 * Sh::kPiece;
+      const int f = feature(sl);
       qf[rt][sl] = make_uint4(0, 0, 0, 0);
       if (r < R && f < a.d) qf[rt][sl] = *reinterpret_cast<const uint4*>(q + f);
     }
@@ -449,6 +557,150 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 ? 3 : 2) void decoder_st
             o_acc[rt][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(vreg[e][i / VF].w[i % VF]), s[rt][e / 4][e % 4], o_acc[rt][i], 0, 0, 0);
     }
     st = next;
+  }
+
+  if constexpr (FP4) {
+    constexpr int NK4 = Q4::NK, QP = Q4::kQueryParts, WP = Q4::kWeightParts, SL4 = D / 32;
+    // float32 queries in three bfloat16 parts of 8 bits each, which hold all of them (an infinity or NaN in the first)
+    bf16x8_t qp[QP][RT][SL4];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int sl = 0; sl < SL4; ++sl) {
+        if constexpr (kBf) {
+          qp[0][rt][sl] = __builtin_bit_cast(bf16x8_t, qf[rt][sl]);
+        } else {
+          const uint4 x = qf[rt][2 * sl], y = qf[rt][2 * sl + 1];
+          float v[8] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w), __uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)};
+          uint32_t w[3][4];
+          split3(v, w);
+#pragma unroll
+          for (int p = 0; p < 3; ++p) qp[p][rt][sl] = __builtin_bit_cast(bf16x8_t, make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]));
+        }
+      }
+    key_reg = key_first;
+    while (st4 < cached_steps) {
+      const int base = key_start + st4 * Q4::kStep, limit = key_end - base, key_now = key_reg;
+      asm volatile("" : "+v"(fp4_lane));
+      f32x4_t s[RT][NK4];
+#pragma unroll
+      for (int k = 0; k < NK4; ++k) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) s[rt][k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        float scale[Q4::kScales];
+#pragma unroll
+        for (int x = 0; x < Q4::kScales; ++x) scale[x] = fp4_scale_value(kscale[k][x]);
+#pragma unroll
+        for (int sl = 0; sl < SL4; ++sl) {
+          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, fp4_values_bf16(kcode[k][sl], scale[Q4::kScales == 2 ? sl / 4 : 0]));
+#pragma unroll
+          for (int p = QP - 1; p >= 0; --p)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s[rt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qp[p][rt][sl], s[rt][k], 0, 0, 0);
+        }
+      }
+      const int next = st4 + KS;
+      if (next < cached_steps) load_fp4_keys(next);
+
+      // element r of block k: key base + 16 k + 4 g4 + r of row l16
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+        for (int k = 0; k < NK4; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            float x = s[rt][k][r];
+            if (capped_scores) {
+              if constexpr (kBf) x = tanh_either(x * (a.scale * a.inv_cap)) * (a.cap * kLog2e);
+              else x = a.cap * tanhf(x * a.scale * a.inv_cap);
+            } else {
+              x *= sc;
+            }
+            s[rt][k][r] = x;
+          }
+        if (biased) {
+#pragma unroll
+          for (int k = 0; k < NK4; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+              const int at = a.pos ? __shfl(key_now, 16 * k + 4 * g4 + r, kWave) : base + 16 * k + 4 * g4 + r;
+              s[rt][k][r] = fmaf(-slope[rt], fabsf((float)(mine[rt] - at)), s[rt][k][r]);
+            }
+        }
+        if (limit < Q4::kStep) {                           // every row sees every entry that is there
+#pragma unroll
+          for (int k = 0; k < NK4; ++k)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) s[rt][k][r] = 16 * k + 4 * g4 + r < limit ? s[rt][k][r] : -INFINITY;
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int k = 0; k < NK4; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[rt][k][r]);
+        top = across_halves(across_rows(top, MaxOp{}), MaxOp{});
+        const float mnew = fmaxf(mrun[rt], top);
+        const float corr = kBf ? __builtin_amdgcn_exp2f(mrun[rt] - mnew) : expf(mrun[rt] - mnew);
+        mrun[rt] = mnew;
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < NK4; ++k)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            s[rt][k][r] = kBf ? __builtin_amdgcn_exp2f(s[rt][k][r] - mnew) : expf(s[rt][k][r] - mnew);
+            sum += s[rt][k][r];
+          }
+        lrun[rt] = fmaf(lrun[rt], corr, sum);
+        if (__any(corr != 1.0f)) {
+#pragma unroll
+          for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) o_acc[rt][i][r] *= corr;
+        }
+      }
+
+#pragma unroll
+      for (int k = 0; k < NK4; k += 2) {
+        bf16x8_t wp[WP][RT];                               // weights of the lane's 8 keys in parts of 8 bits
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          float v[8];
+          uint32_t w[3][4];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[e] = s[rt][k + e / 4][e % 4];
+          if constexpr (kBf) split2(v, w); else split3(v, w);
+#pragma unroll
+          for (int p = 0; p < WP; ++p) wp[p][rt] = __builtin_bit_cast(bf16x8_t, make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]));
+        }
+        Words<VF / 2> vw[8][VC];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int c = 0; c < VC; ++c) {
+            const uint32_t code = vcode[4 * k + e][c], held = vscale[4 * k + e][c];
+            const float scale = fp4_scale_value(D > 128 ? held : held >> (8 * value_group + c * VF * 4) & 0xff);
+            vw[e][c].w[0] = fp4_pair_bf16<0>(code, scale);
+            vw[e][c].w[1] = fp4_pair_bf16<1>(code, scale);
+            if constexpr (VF == 8) {
+              vw[e][c].w[2] = fp4_pair_bf16<2>(code, scale);
+              vw[e][c].w[3] = fp4_pair_bf16<3>(code, scale);
+            }
+          }
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          uint32_t x[4];
+#pragma unroll
+          for (int e = 0; e < 8; e += 2) x[e / 2] = __builtin_amdgcn_perm(vw[e + 1][i / VF].w[i % VF / 2], vw[e][i / VF].w[i % VF / 2], i % 2 ? 0x07060302u : 0x05040100u);
+          const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
+#pragma unroll
+          for (int p = WP - 1; p >= 0; --p)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) o_acc[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, wp[p][rt], o_acc[rt][i], 0, 0, 0);
+        }
+      }
+      if (next < cached_steps) load_fp4_values(next);
+      st4 = next;
+    }
   }
 
   // ---- the result: for each of its elements r a lane has the NB features of row l16; share k of KS finishes elements 4 / KS k ..
