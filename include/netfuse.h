@@ -331,7 +331,7 @@ nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V
 
 /*
  * Log probabilities of tokens.  Row (b, t) of model m has the logits ptr[m*stride_m + (b*T + t)*stride_row + j], j < V, of which the first vocab[m] are that model's tokens
- * (vocab: int[M] or NULL: all V); what lies behind them is not read.  With x_j = f(scale * logit_j), scale > 0 (one over a temperature), f and cap as for scores:
+ * (vocab: int[M] or NULL: all V); what lies behind them is not read.  With x_j = f(scale * logit_j), scale (one over a temperature) 1e-30 ... 1e30, f and cap as for scores:
  *   logp[m][b*T + t][i] = x_j - log sum exp(x) for j = token[m][b*T + t][i], i < n (-infinity for a number that is not one of the row's tokens);   n = 0: token and logp NULL
  *   entropy[m][b*T + t] = - sum p_j log p_j
  *   top, top_logp [m][b*T + t][k]: the k <= 32 tokens of the largest logits, the lower one first among equals, and their log probabilities;   k = 0: both NULL

@@ -30,17 +30,24 @@ __device__ __forceinline__ uint32_t logit_order(float v) {
 }
 __device__ __forceinline__ float logit_of(uint32_t order) { return order == 0u ? -INFINITY : __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order); }
 
-__device__ __forceinline__ float logit_value(float v, const LogprobArgs& a) {
-  v *= a.scale;
-  return a.cap != 0.f ? a.cap * tanhf(v * a.inv_cap) : v;
-}
+// x of a logit under a cap, in units of log2 (tanh within 2^-20)
+__device__ __forceinline__ float capped_logit(float v, const LogprobArgs& a) { return tanh_either(v * (a.scale * a.inv_cap)) * (a.cap * kLog2e); }
+// x - x(top), in units of log2.  Without a cap the difference comes first: the types' lowest values, which stand for masks, do not leave float32.
+struct FromTop {
+  float top, most;
+  __device__ __forceinline__ FromTop(float t, const LogprobArgs& a) : top(t), most(a.cap != 0.f ? capped_logit(t, a) : 0.f) {}
+  __device__ __forceinline__ float operator()(float v, const LogprobArgs& a) const { return a.cap != 0.f ? capped_logit(v, a) - most : (v - top) * (a.scale * kLog2e); }
+  __device__ __forceinline__ float natural(float v, const LogprobArgs& a) const { return a.cap != 0.f ? (capped_logit(v, a) - most) * kLn2 : (v - top) * a.scale; }
+};
 
-struct LogprobShape { static constexpr int kChunk = 4096, kPer = kChunk / kWave; };    // logits of a wavefront, of a lane
+constexpr int kLogprobList = 64;                           // candidates of a wavefront
+constexpr int logprob_chunk(size_t bytes) { return bytes == 2 ? 4096 : 2048; }   // logits of a wavefront, by the size of one
 
-// What a chunk leaves in the workspace: its largest logit, the two sums at it (of 1 and of x - top), then k pairs (order, token), the most likely first.
+// What a chunk leaves in the workspace: its largest logit and the two sums at it (of 1 and of x - top, that in units of log2), then k pairs (order, token), the most likely first.
 constexpr int logprob_words(int k) { return 4 + 2 * k; }
 
-// The better of two alternatives over the wavefront: the larger order, then the lower token.
+// An alternative as one number: the larger order wins, then the lower token.
+__device__ __forceinline__ uint64_t alternative(uint32_t order, int token) { return (uint64_t)order << 32 | (uint32_t)~token; }
 __device__ __forceinline__ uint64_t wave_best(uint64_t v) {
 #pragma unroll
   for (int o = 1; o < kWave; o *= 2) {
@@ -50,117 +57,298 @@ __device__ __forceinline__ uint64_t wave_best(uint64_t v) {
   }
   return v;
 }
-__device__ __forceinline__ uint64_t alternative(uint32_t order, int token) { return (uint64_t)order << 32 | (uint32_t)~token; }
 
-template <typename T>
-__global__ __launch_bounds__(256) void logprob_chunks_kernel(LogprobArgs a) {
-  constexpr int E = LogprobShape::kPer, P = 16 / (int)sizeof(T), N = E / P;      // logits per lane, per 16 bytes, loads
+// An order that at least k lanes' own best ones reach, and few others of a wavefront's do: the k-th largest of the 64, its upper 16 bits found one by one with ballots.
+__device__ __forceinline__ uint32_t few_above(uint32_t best, int k) {
+  uint32_t found = 0;
+#pragma unroll
+  for (int bit = 15; bit >= 0; --bit) {
+    const uint32_t trial = found | 1u << bit;
+    if (__popcll(__ballot(best >> 16 >= trial)) >= k) found = trial;             // uniform
+  }
+  return max(found << 16, 0x00800000u);                    // the order of the lowest finite number: -infinity and NaN are no candidates
+}
+// A lane's candidates go into the list, which holds kList; `count` goes on past that.
+template <class What> __device__ __forceinline__ void list_if(bool in, uint64_t* list, int& count, What&& what) {
+  const uint64_t who = __ballot(in);
+  if (who == 0) return;                                    // uniform
+  const int at = count + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+  if (in && at < kLogprobList) list[at] = what();
+  count += __popcll(who);
+}
+// The list's place r for r < k: lane i ranks candidate i among all.  put(r, alternative), 0 where there are fewer.
+template <class Put> __device__ __forceinline__ void rank_list(const uint64_t* list, int count, int k, Put&& put) {
   const int lane = threadIdx.x % kWave;
-  const long wid = (long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const long row = wid / a.chunks;
-  if (row >= (long)a.M * a.B * a.T) return;                // uniform per wavefront, as the next ones
-  const int chunk = (int)(wid % a.chunks), t = (int)(row % a.T);
-  const long mb = row / a.T, m = mb / a.B;
+  __builtin_amdgcn_wave_barrier();
+  const uint64_t mine = lane < count ? list[lane] : 0;
+  int rank = 0;
+  for (int i = 0; i < count; ++i) rank += list[i] > mine;
+  if (lane < count && rank < k) put(rank, mine);
+  if (lane >= count && lane < k) put(lane, (uint64_t)0);
+  __builtin_amdgcn_wave_barrier();
+}
+
+template <typename T> struct Logits;                       // 16 bytes of them
+template <> struct Logits<float> {
+  static constexpr int kN = 4;
+  using Bits = uint32_t;
+  __device__ static __forceinline__ float at(const uint4& w, int e) { return __uint_as_float(e == 0 ? w.x : e == 1 ? w.y : e == 2 ? w.z : w.w); }
+  static constexpr uint32_t kNone = 0xff800000u;           // -infinity
+};
+template <> struct Logits<bf16_t> {
+  static constexpr int kN = 8;
+  using Bits = uint16_t;
+  __device__ static __forceinline__ float at(const uint4& w, int e) {
+    const uint32_t x = e < 2 ? w.x : e < 4 ? w.y : e < 6 ? w.z : w.w;
+    return __uint_as_float(e % 2 ? x & 0xffff0000u : x << 16);
+  }
+  static constexpr uint32_t kNone = 0xff80ff80u;
+};
+
+// tanh(u) / u on u^2: minimax fits of the relative error, 2^-23 in float32, up to kTanhNear and kTanhWide
+constexpr float kTanhNear = 0.35f, kTanhWide = 0.8f;
+
+template <typename T, bool CAP>
+__global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
+  using L = Logits<T>;
+  constexpr int kChunk = logprob_chunk(sizeof(T)), P = L::kN, N = kChunk / kWave / P;
+  __shared__ uint64_t lists[4][kLogprobList];
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const unsigned wid = blockIdx.x * 4 + wave, row = wid / a.chunks;              // fewer than 2^26 and 2^31
+  if (row >= (unsigned)(a.M * a.B) * (unsigned)a.T) return;                      // uniform per wavefront, as the next ones
+  const int chunk = (int)(wid - row * a.chunks);
+  const unsigned mb = row / a.T, m = mb / a.B;
+  const int t = (int)(row - mb * a.T);
   const int V = a.vocab ? clamp_len(a.vocab[m], a.V) : a.V;
-  const int base = chunk * LogprobShape::kChunk, left = V - base;
+  const int base = chunk * kChunk, left = V - base;
   if (left <= 0 || (a.nodes && t >= a.nodes[mb])) return;
-  const T* p = (const T*)a.logits + m * a.stride_m + (row - m * a.B * a.T) * a.stride_row + base;
-  float v[E];
+  const T* p = (const T*)a.logits + m * a.stride_m + (long)(row - m * a.B * a.T) * a.stride_row + base;
+  // 16 bytes of each lane, -infinity where the row has ended; whether a piece is whole for all of them is the same for all of them
+  auto piece = [&](int i) -> uint4 {
+    const int j = (i * kWave + lane) * P;
+    if ((i + 1) * kWave * P <= left) return load_at<uint4>(p + j);
+    uint32_t x[4] = {L::kNone, L::kNone, L::kNone, L::kNone};
+    if (i * kWave * P < left) {
+      uint32_t v[P];
+#pragma unroll
+      for (int e = 0; e < P; ++e) v[e] = __builtin_bit_cast(typename L::Bits, p[min(j + e, left - 1)]);
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+        v[e] = j + e < left ? v[e] : L::kNone >> (32 - 8 * sizeof(T));
+        if constexpr (P == 4) x[e] = v[e];
+        else x[e / 2] = e % 2 ? x[e / 2] | v[e] << 16 : v[e];
+      }
+    }
+    return make_uint4(x[0], x[1], x[2], x[3]);
+  };
+  uint4 w[N];
+  if (left >= kChunk) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = load_at<uint4>(p + (i * kWave + lane) * P);
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = piece(i);
+  }
+  // The logits stay as they came: each pass opens them again.  (Left to itself the compiler keeps what it made of them in the pass before, all 64 of it.)
+  auto as_they_came = [&]() __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(w[i].x), "+v"(w[i].y), "+v"(w[i].z), "+v"(w[i].w));
+  };
+  float piece_top[N], mine = -INFINITY, low = INFINITY;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const int j = (i * kWave + lane) * P;
+    piece_top[i] = L::at(w[i], 0);
 #pragma unroll
-    for (int e = 0; e < P; ++e) v[i * P + e] = j + e < left ? load_f32(p + j + e) : -INFINITY;
+    for (int e = 1; e < P; ++e) piece_top[i] = fmaxf(piece_top[i], L::at(w[i], e));
+    mine = fmaxf(mine, piece_top[i]);
+    if (CAP) {
+#pragma unroll
+      for (int e = 0; e < P; ++e) low = fminf(low, L::at(w[i], e));
+    }
+    __builtin_amdgcn_sched_barrier(0);
   }
-  float top = -INFINITY;
-#pragma unroll
-  for (int e = 0; e < E; ++e) top = fmaxf(top, v[e]);
-  top = wave_max(top);
-  const float most = logit_value(top, a);
+  const float top = wave_max(mine);
+  as_they_came();
+  const FromTop from_top(top, a);
   float sum = 0.f, first = 0.f;
+  bool plain = !CAP;                                       // each x from one polynomial of its logit
+  const float x1 = a.scale * kLog2e;
+  auto add = [&](float x) __attribute__((always_inline)) {
+    const float e = __builtin_amdgcn_exp2f(x);
+    sum += e;
+    first = fmaf(e, x, first);
+  };
+  if constexpr (!CAP) {
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    const int j = (e / P * kWave + lane) * P + e % P;
-    const float x = logit_value(v[e], a) - most, w = j < left && v[e] != -INFINITY ? expf(x) : 0.f;
-    sum += w;
-    first += w != 0.f ? x * w : 0.f;
+    for (int i = 0; i < N; ++i) {
+#pragma unroll
+      for (int e = 0; e < P; ++e) add((L::at(w[i], e) - top) * x1);
+      __builtin_amdgcn_sched_barrier(0);                   // one piece's numbers at a time: more would take registers from other wavefronts
+    }
+  } else {
+    const float u1 = a.scale * a.inv_cap, reach = fmaxf(fabsf(top), fabsf(wave_max(-low))) * u1, u2 = u1 * u1;
+    const bool sane = u1 > 1e-4f && u1 < 1e4f;                     // powers of the factor that float32 holds
+    const float most = from_top.most;
+    if (sane && reach <= kTanhNear) {
+      plain = true;
+      const float c0 = x1 * 0.9999999403953552f, c1 = x1 * u2 * -0.33332422375679016f, c2 = x1 * u2 * u2 * 0.13295799493789673f, c3 = x1 * u2 * u2 * u2 * -0.04895823076367378f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+          const float v = L::at(w[i], e), q = v * v;
+          add(fmaf(v, fmaf(fmaf(fmaf(c3, q, c2), q, c1), q, c0), -most));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    } else if (sane && reach <= kTanhWide) {
+      plain = true;
+      const float c0 = x1 * 0.9999999403953552f, c1 = x1 * u2 * -0.3333267569541931f, c2 = x1 * u2 * u2 * 0.13321048021316528f, c3 = x1 * u2 * u2 * u2 * -0.05311431363224983f,
+                  c4 = x1 * u2 * u2 * u2 * u2 * 0.01909330114722252f, c5 = x1 * u2 * u2 * u2 * u2 * u2 * -0.004355299286544323f;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+          const float v = L::at(w[i], e), q = v * v;
+          add(fmaf(v, fmaf(fmaf(fmaf(fmaf(fmaf(c5, q, c4), q, c3), q, c2), q, c1), q, c0), -most));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  if (!plain || __any(first != first)) {                   // logits of -infinity (0 times it), NaN, or under a cap large ones: with more care
+    sum = first = 0.f;
+    as_they_came();
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+#pragma unroll
+      for (int e = 0; e < P; ++e) {
+        const float y = L::at(w[i], e), x = CAP ? capped_logit(y, a) - from_top.most : (y - top) * x1, f = y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x);
+        sum += f;
+        first += f != 0.f ? x * f : 0.f;
+        if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);                       // more of them at a time would take registers from every chunk
+      }
   }
   sum = wave_sum(sum);
   first = wave_sum(first);
-  float* out = a.ws + (row * a.chunks + chunk) * logprob_words(a.k);
+  float* const out = a.ws + ((long)row * a.chunks + chunk) * logprob_words(a.k);
   if (lane == 0) *reinterpret_cast<float2*>(out) = make_float2(top, sum), out[2] = first;
+  if (a.k == 0) return;
+
+  auto put = [&](int r, uint64_t x) { *reinterpret_cast<uint2*>(out + 4 + 2 * r) = make_uint2((uint32_t)(x >> 32), ~(uint32_t)x); };
+  const float border = logit_of(few_above(logit_order(mine), a.k));
+  int count = 0;
+  as_they_came();
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (!__any(piece_top[i] >= border)) continue;          // uniform
+#pragma unroll
+    for (int e = 0; e < P; ++e) {
+      const float v = L::at(w[i], e);
+      list_if(v >= border, lists[wave], count, [&] { return alternative(logit_order(v), base + (i * kWave + lane) * P + e); });
+    }
+  }
+  if (count <= kLogprobList) {
+    rank_list(lists[wave], count, a.k, put);
+    return;
+  }
+  // many alike: the best one that is left, k times
   uint64_t last = ~0ull;
+#pragma unroll 1
   for (int r = 0; r < a.k; ++r) {
     uint64_t best = 0;
+#pragma unroll 1
+    for (int i = 0; i < N; ++i) {
+      const uint4 v = piece(i);                            // again from memory: numbered registers would have to be there for it
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int j = base + (e / P * kWave + lane) * P + e % P;
-      const uint64_t x = alternative(logit_order(v[e]), j);
-      best = x < last && x > best ? x : best;
+      for (int e = 0; e < P; ++e) {
+        const uint64_t x = alternative(logit_order(L::at(v, e)), base + (i * kWave + lane) * P + e);
+        best = x < last && x > best ? x : best;
+      }
     }
     last = wave_best(best);
-    if (lane == 0) *reinterpret_cast<uint2*>(out + 4 + 2 * r) = make_uint2((uint32_t)(last >> 32), ~(uint32_t)last);
+    if (lane == 0) put(r, last);
   }
 }
 
 // A row's chunks: one wavefront.
 template <typename T>
 __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
+  constexpr int kChunk = logprob_chunk(sizeof(T));
+  __shared__ uint64_t list[kLogprobList];
   const int lane = threadIdx.x;
-  const long row = blockIdx.x;
-  const int t = (int)(row % a.T);
-  const long mb = row / a.T, m = mb / a.B;
+  const unsigned row = blockIdx.x, mb = row / a.T, m = mb / a.B;
+  const int t = (int)(row - mb * a.T);
   const int V = a.nodes && t >= a.nodes[mb] ? 0 : a.vocab ? clamp_len(a.vocab[m], a.V) : a.V;
-  const int chunks = (V + LogprobShape::kChunk - 1) / LogprobShape::kChunk, words = logprob_words(a.k);
-  const float* ws = a.ws + row * a.chunks * words;
+  const int chunks = (V + kChunk - 1) / kChunk, words = logprob_words(a.k);
+  const float* const ws = a.ws + (long)row * a.chunks * words;
+  const T* const p = (const T*)a.logits + m * a.stride_m + (long)(row - m * a.B * a.T) * a.stride_row;
+  // what the first lanes need, all on its way at once
+  const int token0 = lane < a.n ? a.token[(long)row * a.n + lane] : -1;
+  const bool known0 = token0 >= 0 && token0 < V;
+  const float logit0 = known0 ? load_f32(p + token0) : -INFINITY;
   float top = -INFINITY;
   for (int c = lane; c < chunks; c += kWave) top = fmaxf(top, ws[(long)c * words]);
   top = wave_max(top);
-  const float most = logit_value(top, a);
+  const FromTop from_top(top, a);
   float sum = 0.f, first = 0.f;
   for (int c = lane; c < chunks; c += kWave) {
-    const float* w = ws + (long)c * words;
-    const float x = logit_value(w[0], a) - most, f = w[0] != -INFINITY ? expf(x) : 0.f;
-    if (w[1] != 0.f) {                                     // a chunk of -infinity alone adds nothing
-      sum = fmaf(w[1], f, sum);
-      first += f != 0.f ? f * fmaf(x, w[1], w[2]) : 0.f;
+    const float2 w = *reinterpret_cast<const float2*>(ws + (long)c * words);
+    const float z = ws[(long)c * words + 2], x = from_top(w.x, a), f = __builtin_amdgcn_exp2f(x);
+    if (w.y != 0.f) {                                      // a chunk of -infinity alone adds nothing
+      sum = fmaf(w.y, f, sum);
+      first += f != 0.f ? f * fmaf(x, w.y, z) : 0.f;
     }
   }
   sum = wave_sum(sum);
   first = wave_sum(first);
   const bool none = sum == 0.f;
-  const float log_sum = none ? 0.f : logf(sum);
-  if (lane == 0) a.entropy[row] = none ? 0.f : log_sum - first / sum;
-  const T* p = (const T*)a.logits + m * a.stride_m + (row - m * a.B * a.T) * a.stride_row;
-  for (int i = lane; i < a.n; i += kWave) {
-    const int j = a.token[row * a.n + i];
-    float x = -INFINITY;
-    if (!none && j >= 0 && j < V) {
-      const float v = load_f32(p + j);
-      x = v == -INFINITY ? v : logit_value(v, a) - most - log_sum;
-    }
-    a.logp[row * a.n + i] = x;
+  const float log_sum = none ? 0.f : __builtin_amdgcn_logf(sum);
+  if (lane == 0) a.entropy[row] = none ? 0.f : (log_sum - first / sum) * kLn2;
+  auto logp_of = [&](float v) { return none || v == -INFINITY ? -INFINITY : from_top.natural(v, a) - log_sum * kLn2; };
+  if (lane < a.n) a.logp[(long)row * a.n + lane] = logp_of(logit0);
+  for (int i = lane + kWave; i < a.n; i += kWave) {
+    const int j = a.token[(long)row * a.n + i];
+    a.logp[(long)row * a.n + i] = logp_of(j >= 0 && j < V ? load_f32(p + j) : -INFINITY);
   }
   if (a.k == 0) return;
-  // the best of the chunks' first ones, k times: lane c % 64 keeps how far chunk c is used up (at most 32 of 2^31 / 4096 chunks: read again each time)
+
+  // The same choice among the chunks' alternatives, candidate i being number i % k of chunk i / k.
+  const int all = chunks * a.k;
+  auto candidate = [&](int i) -> uint64_t {
+    const int c = i / a.k;
+    const uint2 w = *reinterpret_cast<const uint2*>(ws + (long)c * words + 4 + 2 * (i - c * a.k));
+    return alternative(w.x, (int)w.y);
+  };
+  auto put = [&](int r, uint64_t x) {
+    const uint32_t order = (uint32_t)(x >> 32);
+    a.top[(long)row * a.k + r] = order ? (int)~(uint32_t)x : -1;
+    a.top_logp[(long)row * a.k + r] = order ? logp_of(logit_of(order)) : -INFINITY;
+  };
+  uint64_t mine = 0;
+  for (int i = lane; i < all; i += kWave) {
+    const uint64_t x = candidate(i);
+    mine = x > mine ? x : mine;
+  }
+  const uint32_t border = few_above((uint32_t)(mine >> 32), a.k);
+  int count = 0;
+  for (int i0 = 0; i0 < all; i0 += kWave) {
+    const uint64_t x = i0 + lane < all ? candidate(i0 + lane) : 0;
+    list_if((uint32_t)(x >> 32) >= border, list, count, [&] { return x; });
+  }
+  if (count <= kLogprobList) {
+    rank_list(list, count, a.k, put);
+    return;
+  }
   uint64_t last = ~0ull;
   for (int r = 0; r < a.k; ++r) {
     uint64_t best = 0;
-    for (int c = lane; c < chunks; c += kWave)
-      for (int i = 0; i < a.k; ++i) {
-        const uint2 w = *reinterpret_cast<const uint2*>(ws + (long)c * words + 4 + 2 * i);
-        const uint64_t x = (uint64_t)w.x << 32 | ~w.y;
-        if (x < last) {
-          best = x > best ? x : best;
-          break;
-        }
-      }
-    last = wave_best(best);
-    const uint32_t order = (uint32_t)(last >> 32);
-    if (lane == 0) {
-      a.top[row * a.k + r] = order ? (int)~(uint32_t)last : -1;
-      a.top_logp[row * a.k + r] = order && !none ? logit_value(logit_of(order), a) - most - log_sum : -INFINITY;
+    for (int i = lane; i < all; i += kWave) {
+      const uint64_t x = candidate(i);
+      best = x < last && x > best ? x : best;
     }
+    last = wave_best(best);
+    if (lane == 0) put(r, last);
   }
 }
 

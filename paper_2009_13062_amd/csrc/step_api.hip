@@ -65,7 +65,7 @@ nf_status launch_fp4_rows(const DecArgs& a, nf_dtype dt, hipStream_t s) {
   return launched();
 }
 
-int logprob_chunks(int V) { return (int)(((long long)V + LogprobShape::kChunk - 1) / LogprobShape::kChunk); }
+int logprob_chunks(int V, nf_dtype dt) { return (int)(((long long)V + logprob_chunk(dt == NF_F32 ? 4 : 2) - 1) / logprob_chunk(dt == NF_F32 ? 4 : 2)); }
 
 }  // namespace
 
@@ -207,7 +207,7 @@ nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V
 
 long long netfuse_token_logprobs_workspace(int M, int B, int T, int V, int k) {
   if (M <= 0 || B <= 0 || T <= 0 || V <= 0 || V > kMostEntries || k < 0 || k > kMostAlternatives) return -1;
-  const long long bytes = prod({M, B, T, logprob_chunks(V), 4LL * logprob_words(k)});
+  const long long bytes = prod({M, B, T, logprob_chunks(V, NF_F32), 4LL * logprob_words(k)});
   return bytes >= kMaxElems ? -1 : bytes;
 }
 
@@ -217,7 +217,7 @@ nf_status netfuse_token_logprobs(const void* logits, const int* token, const int
   if (!logits || !entropy || !workspace) return NF_EINVAL;
   if (M <= 0 || B <= 0 || T <= 0 || V <= 0 || V > kMostEntries || n < 0 || k < 0 || !is_dtype(dt)) return NF_EINVAL;
   if ((n > 0 && (!token || !logp)) || (k > 0 && (!top || !top_logp))) return NF_EINVAL;
-  if (!score_ok(scale, cap) || scale <= 0.f) return NF_EINVAL;
+  if (!score_ok(scale, cap) || scale < 1e-30f || scale > 1e30f) return NF_EINVAL;
   if (prod({B, T}) > INT_MAX / 2 || prod({M, B, T, V}) >= kMaxElems || prod({M, B, T, n}) >= kMaxElems || prod({M, B, T}) > INT_MAX) return NF_EINVAL;
   if (!rows_ok(M, (long long)B * T, V, stride_m, stride_row)) return NF_EINVAL;
   const size_t esz = dt == NF_F32 ? 4 : 2;
@@ -227,13 +227,15 @@ nf_status netfuse_token_logprobs(const void* logits, const int* token, const int
   if (k > kMostAlternatives) return NF_EUNSUPPORTED;
   const long long need = netfuse_token_logprobs_workspace(M, B, T, V, k);
   if (need < 0 || workspace_bytes < need) return NF_EINVAL;
-  const LogprobArgs a = {logits, token, vocab, nodes, logp, entropy, top, top_logp, (float*)workspace, M, B, T, V, n, k, logprob_chunks(V),
+  const LogprobArgs a = {logits, token, vocab, nodes, logp, entropy, top, top_logp, (float*)workspace, M, B, T, V, n, k, logprob_chunks(V, dt),
                          stride_m, stride_row, scale, cap, cap != 0.f ? 1.f / cap : 0.f};
   const long long rows = prod({M, B, T}), blocks = (prod({rows, a.chunks}) + 3) / 4;
   if (!grid_fits(blocks, 256) || !grid_fits(rows, 64)) return NF_EUNSUPPORTED;          // before the first of the two is enqueued
   hipStream_t s = (hipStream_t)stream;
-  if (dt == NF_F32) nf_launch((logprob_chunks_kernel<float>), dim3((unsigned)blocks), dim3(256), 0, s, a);
-  else nf_launch((logprob_chunks_kernel<bf16_t>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+#define NF_CHUNKS(T, CAP) nf_launch((logprob_chunks_kernel<T, CAP>), dim3((unsigned)blocks), dim3(256), 0, s, a)
+  if (dt == NF_F32) { if (cap != 0.f) NF_CHUNKS(float, true); else NF_CHUNKS(float, false); }
+  else { if (cap != 0.f) NF_CHUNKS(bf16_t, true); else NF_CHUNKS(bf16_t, false); }
+#undef NF_CHUNKS
   const nf_status st = launched();
   if (st != NF_OK) return st;
   if (dt == NF_F32) nf_launch((logprob_join_kernel<float>), dim3((unsigned)rows), dim3(64), 0, s, a);
