@@ -13,8 +13,10 @@ namespace nf {
 inline int tree_chunk(int rows, nf_dtype dt) { return rows > (dt == NF_F32 ? 64 : 32) ? 1024 : 512; }
 inline int tree_features(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// Of a cache of 4 bits
-inline int tree_fp4_chunk(int rows, nf_dtype dt) { return tree_chunk(rows, dt); }
+// Of a cache of 4 bits, whose chunks are shorter in bytes (us, 512 / 1024 / 2048 keys, 8 key heads of 128, bfloat16: one token of groups of 4 over two caches of up to 100003 57 / 49 / 47,
+// 32 of 4096 37 / 32 / 31, one of 8192 11.5 / 14 / 22; 5 tokens over 16 of 4096 36 / 32 / 40; 26 over 32 of 4096 141 / 120 / 112; 9 over 16 of 4096 55 / 48 / 71)
+constexpr int kTreeFp4Chunk = 1024;
+nf_status launch_tree_fp4_tiles(const DecArgs& a, int chunk, int splits, hipStream_t s);        // bfloat16
 nf_status launch_tree_fp4_stream(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s);
 
 struct WeighArgs;

@@ -43,33 +43,36 @@ constexpr int stream_lds_bytes(int RT, int KS, int NB) { return KS > 1 ? (256 * 
 
 template <int W> struct Words { uint32_t w[W]; };
 
-// Eight float32 values in bfloat16 parts, a pair to a dword: two that hold 15 bits -- the upper 8, of a value a little smaller, and the rest, rounded; neither is 0
-// where the value is not, so an infinity on the other side of the product stays that infinity -- and three that hold all 24.  What is not finite is the first part's alone.
-__device__ __forceinline__ void split2(const float (&v)[8], uint32_t (&w)[3][4]) {
+// Eight float32 values in bfloat16 parts of 8 bits each, a pair to a dword: N = 2 of them, which hold 15 bits (the last part is rounded), or 3, which hold all.
+template <int N> __device__ __forceinline__ void to_parts(const float (&v)[8], uint32_t (&w)[N][4]) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const uint32_t x = __float_as_uint(v[2 * e] * 0x1.ffp-1f), y = __float_as_uint(v[2 * e + 1] * 0x1.ffp-1f);
-    w[0][e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-    w[1][e] = pack_bf16x2(v[2 * e] - __uint_as_float(x & 0xffff0000u), v[2 * e + 1] - __uint_as_float(y & 0xffff0000u));
+    float x = v[2 * e], y = v[2 * e + 1];
+#pragma unroll
+    for (int p = 0; p < N - 1; ++p) {
+      w[p][e] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
+      x -= __uint_as_float(__float_as_uint(x) & 0xffff0000u);
+      y -= __uint_as_float(__float_as_uint(y) & 0xffff0000u);
+    }
+    w[N - 1][e] = N == 2 ? pack_bf16x2(x, y) : __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
   }
 }
-__device__ __forceinline__ void split3(const float (&v)[8], uint32_t (&w)[3][4]) {
+// The same of any value in three: an infinity or NaN is the first part's alone.
+__device__ __forceinline__ void to_parts_any(const float (&v)[8], uint32_t (&w)[3][4]) {
+  float finite[8];
+  bool odd = false;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    float a[2], b[2], c[2];
+  for (int e = 0; e < 8; ++e) {
+    finite[e] = fabsf(v[e]) < INFINITY ? v[e] : 0.f;
+    odd |= !(fabsf(v[e]) < INFINITY);
+  }
+  to_parts<3>(finite, w);
+  if (odd) {
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const float x = v[2 * e + z];
-      a[z] = __uint_as_float(__float_as_uint(x) & 0xffff0000u);
-      const float rest = fabsf(x) < INFINITY ? x - a[z] : 0.f;
-      b[z] = __uint_as_float(__float_as_uint(rest) & 0xffff0000u);
-      c[z] = rest - b[z];
+    for (int e = 0; e < 4; ++e) {
+      if (!(fabsf(v[2 * e]) < INFINITY)) w[0][e] = (w[0][e] & 0xffff0000u) | f32_to_bf16(v[2 * e]);
+      if (!(fabsf(v[2 * e + 1]) < INFINITY)) w[0][e] = (w[0][e] & 0xffffu) | (uint32_t)f32_to_bf16(v[2 * e + 1]) << 16;
     }
-    // a NaN whose payload lies in the lower half is an infinity in the upper one: kept by the conversion's rounding instead
-    w[0][e] = fabsf(v[2 * e]) < INFINITY && fabsf(v[2 * e + 1]) < INFINITY ? __builtin_amdgcn_perm(__float_as_uint(a[1]), __float_as_uint(a[0]), 0x07060302u)
-                                                                         : pack_bf16x2(v[2 * e] != v[2 * e] ? v[2 * e] : a[0], v[2 * e + 1] != v[2 * e + 1] ? v[2 * e + 1] : a[1]);
-    w[1][e] = __builtin_amdgcn_perm(__float_as_uint(b[1]), __float_as_uint(b[0]), 0x07060302u);
-    w[2][e] = __builtin_amdgcn_perm(__float_as_uint(c[1]), __float_as_uint(c[0]), 0x07060302u);
   }
 }
 
@@ -263,7 +266,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
     if (biased && a.pos) key_reg = a.pos[head * a.C + base + min(lane, key_end - base - 1)];
   };
   // A key's scales come whole where a row of them is 2 bytes (up to 64 features) or 4 (up to 128).
-  const int value_group = l16 * VF / kFp4Group;
+  uint32_t value_turn[VC];                                 // turns the byte of the lane's group up to bit 23
+#pragma unroll
+  for (int c = 0; c < VC; ++c) value_turn[c] = (8 * (c * VF / 2 + l16 * VF / kFp4Group) + 9) % 32;
   auto load_fp4_values = [&](int st4) {
     const int base = key_start + st4 * Q4::kStep;
     const auto rv = fp4_rows(a.Vc, base, code_row), rs = fp4_rows(a.Vs, base, scale_row);
@@ -289,7 +294,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
       load_fp4_keys(st4);
       load_fp4_values(st4);
     }
-    st = cached_steps + share;
+    st = cached_steps + (KS - 1 - share);                  // by the wavefronts that have the fewest of the others
     key_first = key_reg;
     if (st < steps) load_keys(st);
   } else {
@@ -573,7 +578,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
           const uint4 x = qf[rt][2 * sl], y = qf[rt][2 * sl + 1];
           float v[8] = {__uint_as_float(x.x), __uint_as_float(x.y), __uint_as_float(x.z), __uint_as_float(x.w), __uint_as_float(y.x), __uint_as_float(y.y), __uint_as_float(y.z), __uint_as_float(y.w)};
           uint32_t w[3][4];
-          split3(v, w);
+          to_parts_any(v, w);
 #pragma unroll
           for (int p = 0; p < 3; ++p) qp[p][rt][sl] = __builtin_bit_cast(bf16x8_t, make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]));
         }
@@ -584,49 +589,49 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
       asm volatile("" : "+v"(fp4_lane));
       f32x4_t s[RT][NK4];
 #pragma unroll
-      for (int k = 0; k < NK4; ++k) {
+      for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) s[rt][k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        float scale[Q4::kScales];
+        for (int k = 0; k < NK4; ++k) s[rt][k] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      // block after block within a slice, so that a product does not wait for the one before it
 #pragma unroll
-        for (int x = 0; x < Q4::kScales; ++x) scale[x] = fp4_scale_value(kscale[k][x]);
+      for (int sl = 0; sl < SL4; ++sl) {
+        bf16x8_t kf[NK4];
 #pragma unroll
-        for (int sl = 0; sl < SL4; ++sl) {
-          const bf16x8_t kf = __builtin_bit_cast(bf16x8_t, fp4_values_bf16(kcode[k][sl], scale[Q4::kScales == 2 ? sl / 4 : 0]));
+        for (int k = 0; k < NK4; ++k) kf[k] = __builtin_bit_cast(bf16x8_t, fp4_values_bf16(kcode[k][sl], fp4_scale_value(kscale[k][Q4::kScales == 2 ? sl / 4 : 0])));
 #pragma unroll
-          for (int p = QP - 1; p >= 0; --p)
+        for (int p = QP - 1; p >= 0; --p)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) s[rt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qp[p][rt][sl], s[rt][k], 0, 0, 0);
-        }
+          for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int k = 0; k < NK4; ++k) s[rt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k], qp[p][rt][sl], s[rt][k], 0, 0, 0);
       }
       const int next = st4 + KS;
       if (next < cached_steps) load_fp4_keys(next);
 
-      // element r of block k: key base + 16 k + 4 g4 + r of row l16
+      // element r of block k: key base + 16 k + 4 g4 + r of row l16.  Each question is asked once, not for each score.
+      auto every = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-        for (int k = 0; k < NK4; ++k)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            float x = s[rt][k][r];
-            if (capped_scores) {
-              if constexpr (kBf) x = tanh_either(x * (a.scale * a.inv_cap)) * (a.cap * kLog2e);
-              else x = a.cap * tanhf(x * a.scale * a.inv_cap);
-            } else {
-              x *= sc;
-            }
-            s[rt][k][r] = x;
-          }
-        if (biased) {
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
           for (int k = 0; k < NK4; ++k)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-              const int at = a.pos ? __shfl(key_now, 16 * k + 4 * g4 + r, kWave) : base + 16 * k + 4 * g4 + r;
-              s[rt][k][r] = fmaf(-slope[rt], fabsf((float)(mine[rt] - at)), s[rt][k][r]);
-            }
-        }
+            for (int r = 0; r < 4; ++r) s[rt][k][r] = f(s[rt][k][r], rt, 16 * k + 4 * g4 + r);
+      };
+      if (capped_scores) {
+        if constexpr (kBf) every([&](float x, int, int) { return tanh_either(x * (a.scale * a.inv_cap)) * (a.cap * kLog2e); });
+        else every([&](float x, int, int) { return a.cap * tanhf(x * a.scale * a.inv_cap); });
+      } else {
+        every([&](float x, int, int) { return x * sc; });
+      }
+      if (biased) {
+        float away[RT];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) away[rt] = (float)(mine[rt] - base - 4 * g4);
+        if (a.pos) every([&](float x, int rt, int key) { return fmaf(-slope[rt], fabsf((float)(mine[rt] - __shfl(key_now, key, kWave))), x); });
+        else every([&](float x, int rt, int key) { return fmaf(-slope[rt], fabsf(away[rt] - (float)(key - 4 * g4)), x); });
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
         if (limit < Q4::kStep) {                           // every row sees every entry that is there
 #pragma unroll
           for (int k = 0; k < NK4; ++k)
@@ -665,10 +670,10 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
           float v[8];
-          uint32_t w[3][4];
+          uint32_t w[WP][4];
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] = s[rt][k + e / 4][e % 4];
-          if constexpr (kBf) split2(v, w); else split3(v, w);
+          to_parts<WP>(v, w);                                 // no cached value is infinite, so a part may be 0
 #pragma unroll
           for (int p = 0; p < WP; ++p) wp[p][rt] = __builtin_bit_cast(bf16x8_t, make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]));
         }
@@ -677,8 +682,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
         for (int e = 0; e < 8; ++e)
 #pragma unroll
           for (int c = 0; c < VC; ++c) {
-            const uint32_t code = vcode[4 * k + e][c], held = vscale[4 * k + e][c];
-            const float scale = fp4_scale_value(D > 128 ? held : held >> (8 * value_group + c * VF * 4) & 0xff);
+            const uint32_t code = vcode[4 * k + e][c], row = vscale[4 * k + e][c];
+            // the byte to the place of an exponent: its neighbours are then sign and fraction, which the conversions do not look at
+            const float scale = D > 128 ? fp4_scale_value(row) : __uint_as_float(__builtin_amdgcn_alignbit(row, row, value_turn[c]));
             vw[e][c].w[0] = fp4_pair_bf16<0>(code, scale);
             vw[e][c].w[1] = fp4_pair_bf16<1>(code, scale);
             if constexpr (VF == 8) {
@@ -687,15 +693,22 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
             }
           }
 #pragma unroll
-        for (int i = 0; i < NB; ++i) {
-          uint32_t x[4];
+        for (int i0 = 0; i0 < NB; i0 += 4) {
+          bf16x8_t vf[4];
 #pragma unroll
-          for (int e = 0; e < 8; e += 2) x[e / 2] = __builtin_amdgcn_perm(vw[e + 1][i / VF].w[i % VF / 2], vw[e][i / VF].w[i % VF / 2], i % 2 ? 0x07060302u : 0x05040100u);
-          const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
+          for (int i = 0; i < 4; ++i) {
+            uint32_t x[4];
+#pragma unroll
+            for (int e = 0; e < 8; e += 2)
+              x[e / 2] = __builtin_amdgcn_perm(vw[e + 1][(i0 + i) / VF].w[(i0 + i) % VF / 2], vw[e][(i0 + i) / VF].w[(i0 + i) % VF / 2], i % 2 ? 0x07060302u : 0x05040100u);
+            vf[i] = __builtin_bit_cast(bf16x8_t, make_uint4(x[0], x[1], x[2], x[3]));
+          }
 #pragma unroll
           for (int p = WP - 1; p >= 0; --p)
 #pragma unroll
-            for (int rt = 0; rt < RT; ++rt) o_acc[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, wp[p][rt], o_acc[rt][i], 0, 0, 0);
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o_acc[rt][i0 + i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[i], wp[p][rt], o_acc[rt][i0 + i], 0, 0, 0);
         }
       }
       if (next < cached_steps) load_fp4_values(next);

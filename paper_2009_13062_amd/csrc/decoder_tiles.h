@@ -24,6 +24,7 @@
 // Trees are bound by the cache's bytes below some 64 rows, then as prompts are (26 tokens over 32 caches of up to 4096 entries: 114 us and 15 to join).
 #pragma once
 #include "decoder.h"
+#include "fp4.h"
 #include "gemm_dma.h"
 
 namespace nf {
@@ -94,7 +95,9 @@ constexpr std::true_type kShift;
 constexpr std::false_type kNoShift;
 
 // `Q` is a.Q once more: a pointer that is declared not to alias is what keeps the compiler from waiting for every load into LDS before a transposing read.
-template <int D, int KS, bool TREE, int FORM>
+// FP4: the cache is one of 4 bits (TREE): a thread loads a few neighbouring features of a key and of its value as they are held, and opens them into the stage, bfloat16 then, once
+// the tile before has been worked on.
+template <int D, int KS, bool TREE, int FORM, bool FP4 = false>
 __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __restrict__ Q, int row_blocks, int splits, int chunk) {
   constexpr bool kRaw = FORM == kRawScore || FORM == kRawBiased, kBiased = FORM == kRawBiased || FORM == kAnyBiased;
   constexpr int KB = 64 * KS, RG = 4 / KS, TB = D / 32;
@@ -302,6 +305,52 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
     }
   };
 
+  // ---- a tile of a cache of 4 bits: kShare features of key tid / kSharers
+  constexpr int kSharers = 256 / KB, kShare = D / kSharers, kShareWords = kShare / 8, kShareScales = kShare > kFp4Group ? kShare / kFp4Group : 1;
+  const int my_key = tid / kSharers, my_first = tid % kSharers * kShare;
+  const int code_row = fp4_code_bytes(a.d), scale_row = fp4_scale_bytes(a.d);
+  uint32_t codes[2][kShareWords], scales[2][kShareScales];
+  auto issue_fp4 = [&](int j0) {
+    const int limit = L - j0;
+    if (keyed && tid < KB) {
+      const int there = j0 + min(tid, limit - 1);
+      key_reg = a.pos ? a.pos[head * a.C + there] : there;
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      // resources that end with the cache's last entry: what lies behind it comes back as 0
+      const auto rc = __builtin_amdgcn_make_buffer_rsrc((void*)((const uint8_t*)(t ? a.Vc : a.Kc) + (head * a.C + j0) * code_row), 0, min(limit, KB) * code_row, 0x00020000);
+      const auto rs = __builtin_amdgcn_make_buffer_rsrc((void*)((t ? a.Vs : a.Ks) + (head * a.C + j0) * scale_row), 0, min(limit, KB) * scale_row, 0x00020000);
+#pragma unroll
+      for (int w = 0; w < kShareWords; w += 4) {
+        const int off = my_first / 2 + w * 4 < code_row ? my_key * code_row + my_first / 2 + w * 4 : (int)kDecOob;
+        if constexpr (kShareWords == 2) {
+          const dec_u32x2_t v = __builtin_amdgcn_raw_buffer_load_b64(rc, off, 0, 0);
+          codes[t][0] = v.x;
+          codes[t][1] = v.y;
+        } else {
+          const uint4 v = rows_load16(rc, off);
+          codes[t][w] = v.x; codes[t][w + 1] = v.y; codes[t][w + 2] = v.z; codes[t][w + 3] = v.w;
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < kShareScales; ++x) {
+        const int grp = my_first / kFp4Group + x;
+        scales[t][x] = __builtin_amdgcn_raw_buffer_load_b8(rs, grp < scale_row ? my_key * scale_row + grp : (int)kDecOob, 0, 0);
+      }
+    }
+  };
+  auto open_fp4 = [&](int stage) {
+#pragma unroll
+    for (int w = 0; w < kShareWords; ++w) {
+      const int c = my_first / 8 + w;
+      *(lds_u32x4_t*)(Ks + stage * Lds::kTile + my_key * Lds::kRow + (c ^ Lds::swz_k(my_key)) * 16) =
+          __builtin_bit_cast(u32x4_t, fp4_values_bf16(codes[0][w], fp4_scale_value(scales[0][kShareScales > 1 ? w / 4 : 0])));
+      *(lds_u32x4_t*)(Vs + stage * Lds::kTile + my_key * Lds::kRow + (c ^ Lds::swz_v(my_key)) * 16) =
+          __builtin_bit_cast(u32x4_t, fp4_values_bf16(codes[1][w], fp4_scale_value(scales[1][kShareScales > 1 ? w / 4 : 0])));
+    }
+  };
+
   f32x16_t o_acc[TB];
   float mrun, lrun;
   mrun = kLowestScore;
@@ -321,7 +370,12 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
   // ---- one tile is on its way while one is worked on
   int tile = seek(TREE ? split * chunk : 0), seen = look_over(tile);
   if (tile != kNoTile) {
-    issue(tile, 0);
+    if (FP4 && tile != kTreeTile) {
+      issue_fp4(tile);
+      open_fp4(0);
+    } else {
+      issue(tile, 0);
+    }
     if (keyed && tid < KB) Key[tid] = key_reg;
   }
   int cur = 0, number = 1;
@@ -334,7 +388,9 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
     asm volatile("" ::: "memory");
     const int next = tile < 0 ? kNoTile : seek(tile + KB), fresh = 1 - cur;
     const int next_seen = look_over(next);
-    if (next != kNoTile) issue(next, fresh);
+    const bool next_held = FP4 && next >= 0;
+    if (next_held) issue_fp4(next);
+    else if (next != kNoTile) issue(next, fresh);
 
     const bool mask = seen & kMineLeaveOut;
     bool odd_tile = false;
@@ -625,6 +681,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
           }
       keep_ahead<NSB * 2 * TB, 2>();
     }
+    if (next_held) open_fp4(fresh);
     if (next != kNoTile && keyed && tid < KB) Key[fresh * KB + tid] = key_reg;
     cur = fresh;
     ++number;
@@ -700,9 +757,9 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
   if (TREE && a.lse && quad0 == 0 && half == 0) a.lse[(mb * a.N + token) * a.heads + h] = none ? -INFINITY : (mtot + __builtin_amdgcn_logf(ltot)) * kLn2;
 }
 
-template <int D, int KS, bool TREE, int FORM>
-__global__ __launch_bounds__(256, D == 64 ? 3 : D == 128 ? 2 : 1) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
-  decoder_tiles<D, KS, TREE, FORM>(a, (const bf16_t*)a.Q, row_blocks, splits, chunk);
+template <int D, int KS, bool TREE, int FORM, bool FP4 = false>
+__global__ __launch_bounds__(256, D == 64 ? (FP4 ? 2 : 3) : D == 128 ? 2 : 1) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
+  decoder_tiles<D, KS, TREE, FORM, FP4>(a, (const bf16_t*)a.Q, row_blocks, splits, chunk);
 }
 
 // Sums of the chunks of one row: D / 4 lanes hold its features, 4 each, and SHARE such groups of lanes take every SHARE-th chunk.  Maxima and sums in log2

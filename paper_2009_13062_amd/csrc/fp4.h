@@ -4,7 +4,8 @@
 //
 // The scale is the smallest power of two with |x| <= 7 * scale in the whole group, exponents -125 ... 125: up to 7 an element rounds to 6, off by no more than elsewhere
 // between two codes (1 / 7), and a smaller scale than the usual floor(log2 max) - 2 gives from 6 to 7 is never taken, so none is cut by more.  Multiplying by a power of two is
-// exact, so rounding to the nearest code (halfway to the even one) has one answer, which the hardware's conversions give: all 256 scales and both directions were checked.
+// exact, so rounding to the nearest code (halfway to the even one) has one answer, which the hardware's conversions give: all 256 scales and both directions were checked.  Of a
+// scale they look at the exponent alone.
 // A group that holds an infinity or NaN gets the byte 255, which reads as NaN throughout.
 #pragma once
 #include "nf_common.h"

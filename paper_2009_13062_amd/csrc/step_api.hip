@@ -164,7 +164,7 @@ nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc,
 long long netfuse_attention_tree_fp4_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt) {
   if (M <= 0 || B <= 0 || T <= 0 || T > 64 || C <= 0 || C > kMostEntries || !heads_ok(heads, kv_heads, d) || d > 256 || !is_dtype(dt)) return -1;
   if (!pieces_sizes(T, heads, kv_heads, d, dt)) return 0;
-  const int chunk = tree_fp4_chunk(T * (heads / kv_heads), dt), splits = (int)(((long long)C + chunk - 1) / chunk);
+  const int splits = (int)(((long long)C + kTreeFp4Chunk - 1) / kTreeFp4Chunk);
   if (splits == 1) return 0;                               // no cache is shared out
   const long long bytes = prod({M, B, heads, T, splits, 4LL * (tree_features(d) + 2)});
   return bytes >= kMaxElems ? -1 : bytes;
@@ -197,9 +197,12 @@ nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V
   a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.kv_stride_m = kv_stride_m; a.kv_stride_row = kv_stride_row;
   a.scale = scale; a.cap = cap; a.inv_cap = cap != 0.f ? 1.f / cap : 0.f;
   if (pieces_ok(a, dt)) {
-    const int chunk = tree_fp4_chunk(T * (heads / kv_heads), dt), splits = (int)(((long long)C + chunk - 1) / chunk);
+    const int chunk = kTreeFp4Chunk, splits = (int)(((long long)C + chunk - 1) / chunk), rows = T * (heads / kv_heads);
     if (splits > 1 && !grid_fits(tree_join_blocks(a, splits), 256)) return NF_EUNSUPPORTED;      // before the first of the two is enqueued
-    const nf_status st = launch_tree_fp4_stream(a, chunk, splits, dt, (hipStream_t)stream);
+    // Rows that go through LDS: as with caches of bfloat16, but from 65 up where heads are large (36 rows of 256 features over 8 caches of 4096, us, registers / LDS 64 / 79, 104 rows - / 88; of
+    // 128, 36 rows over 16 51 / 48, 32 over 32 84 / 115; of 64, 20 rows over 16 32.7 / 31.5).
+    const bool tiles = dt == NF_BF16 && rows > (d <= 64 ? 16 : d <= 128 ? 32 : 64);
+    const nf_status st = tiles ? launch_tree_fp4_tiles(a, chunk, splits, (hipStream_t)stream) : launch_tree_fp4_stream(a, chunk, splits, dt, (hipStream_t)stream);
     return st != NF_OK || splits == 1 ? st : launch_tree_join(a, chunk, splits, dt, (hipStream_t)stream);
   }
   return launch_fp4_rows(a, dt, (hipStream_t)stream);
