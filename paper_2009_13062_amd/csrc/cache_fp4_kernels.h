@@ -12,78 +12,120 @@ struct AppendFp4Args {
   long stride_m, stride_row;
 };
 
-// Eight features of a row from feature f on, those past d as 0.  WIDE: d, strides and pointers in 16-byte pieces.
-template <typename T, bool WIDE> __device__ __forceinline__ void fp4_load8(const T* row, int f, int d, float (&x)[8]) {
-  if constexpr (WIDE) {
-#pragma unroll
-    for (int h = 0; h < 8; h += 4) {
-      const float4 v = f + h < d ? *reinterpret_cast<const float4*>(row + f + h) : make_float4(0.f, 0.f, 0.f, 0.f);
-      x[h] = v.x; x[h + 1] = v.y; x[h + 2] = v.z; x[h + 3] = v.w;
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = f + e < d ? load_f32(row + f + e) : 0.f;
-  }
-}
-
 // The largest magnitude over the four lanes of a group: each has eight of its features.
 __device__ __forceinline__ uint32_t group_top(uint32_t top) {
   top = max(top, (uint32_t)dpp<kQuadXor1>((int)top));
   return max(top, (uint32_t)dpp<kQuadXor2>((int)top));
 }
 
-// Eight features of a lane to their codes; the scale of the lane's group comes along.  Every lane of a quad has to come here.
-template <typename T, bool WIDE> __device__ __forceinline__ uint32_t fp4_quantise8(const T* row, int f, int d, uint32_t& scale) {
-  if constexpr (WIDE && sizeof(T) == 2) {
-    const uint4 w = f < d ? *reinterpret_cast<const uint4*>(row + f) : make_uint4(0, 0, 0, 0);
-    uint32_t top = 0;
-    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+// Eight features of a row from feature f on, those past d as 0, and their codes; the scale of the lane's group comes along (every lane of a quad has to come there).  WIDE: d, strides and
+// pointers in 16-byte pieces.
+template <typename T, bool WIDE> struct Eight {
+  float x[8];
+  __device__ __forceinline__ void load(const T* row, int f, int d) {
+    if constexpr (WIDE) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) top = max(top, max(ws[e] << 16 & 0x7fffffffu, ws[e] & 0x7fff0000u));
-    scale = fp4_scale(group_top(top));
-    return fp4_codes(w, scale);
-  } else {
-    float x[8];
-    fp4_load8<T, WIDE>(row, f, d, x);
+      for (int h = 0; h < 8; h += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(row + (f + h < d ? f + h : 0));
+        const bool in = f + h < d;
+        x[h] = in ? v.x : 0.f; x[h + 1] = in ? v.y : 0.f; x[h + 2] = in ? v.z : 0.f; x[h + 3] = in ? v.w : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const float v = load_f32(row + (f + e < d ? f + e : 0));
+        x[e] = f + e < d ? v : 0.f;
+      }
+    }
+  }
+  __device__ __forceinline__ uint32_t codes(uint32_t& scale) const {
     uint32_t top = 0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
     scale = fp4_scale(group_top(top));
     return fp4_codes(x, scale);
   }
+};
+template <> struct Eight<bf16_t, true> {
+  uint4 w;
+  __device__ __forceinline__ void load(const bf16_t* row, int f, int d) {
+    w = *reinterpret_cast<const uint4*>(row + (f < d ? f : 0));
+    if (f >= d) w = make_uint4(0, 0, 0, 0);
+  }
+  __device__ __forceinline__ uint32_t codes(uint32_t& scale) const {
+    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
+    uint32_t top = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top = max(top, max(ws[e] << 16 & 0x7fffffffu, ws[e] & 0x7fff0000u));
+    scale = fp4_scale(group_top(top));
+    return fp4_codes(w, scale);
+  }
+};
+
+// The scales of a head's groups, a byte each in lanes 0, 4, .. of the head's, to one number in the first of them (2 or 4 groups: the lanes of a head lie in a row of 16).
+template <int G> __device__ __forceinline__ uint32_t gather_scales(uint32_t s) {
+  constexpr int kRowShl = 0x100;
+  uint32_t all = s | (uint32_t)dpp<kRowShl + 4>((int)s) << 8;
+  if constexpr (G == 4) all |= (uint32_t)dpp<kRowShl + 8>((int)s) << 16 | (uint32_t)dpp<kRowShl + 12>((int)s) << 24;
+  return all;
 }
 
-// A lane takes eight features of a key and its value, four lanes a group, so a head's row is read and written in one run.  A workgroup takes `rows` new rows of one sequence.
-template <typename T, bool WIDE>
-__global__ __launch_bounds__(256) void cache_append_fp4_kernel(AppendFp4Args a, int rows, int blocks_per_seq) {
-  const unsigned umb = blockIdx.x / blocks_per_seq;
-  const long mb = umb, m = umb / a.B;
-  const int i0 = (int)(blockIdx.x % blocks_per_seq) * rows, b = (int)(umb % a.B);
+// A workgroup takes rows of one head of one sequence, so what it writes is one run of codes, of scales, of positions and of weights; a lane takes eight features of a key and its value, four
+// lanes a group, kAppendRows rows at a time.  G: the groups of a head where these are 2 or 4, 0 for others.
+constexpr int kAppendRows = 4;
+template <typename T, bool WIDE, int G>
+__global__ __launch_bounds__(256) void cache_append_fp4_kernel(AppendFp4Args a, int blocks_per_head) {
+  const int groups = G ? G : fp4_groups(a.d), S = G ? G : fp4_scale_bytes(a.d), units = 4 * groups, at_once = 256 / units;
+  const unsigned uhead = blockIdx.x / blocks_per_head, umb = uhead / a.kv;
+  const int g = (int)(uhead - umb * a.kv), b = (int)(umb % a.B);
+  const long mb = umb, m = umb / a.B, head = uhead;
   const int cnt = a.count ? clamp_len(a.count[mb], a.n) : a.n, L = clamp_len(a.len[mb], a.C);
-  const int end = min(min(i0 + rows, cnt), a.C - L);       // entries past the capacity are not written
-  const int G = fp4_groups(a.d), S = fp4_scale_bytes(a.d), units = 4 * G, per_row = a.kv * units;
-  for (int i = i0 + (int)threadIdx.x / per_row, c = (int)threadIdx.x % per_row; i < end;) {      // the lanes of a quad stay together: per_row is a multiple of 4
-    const int row = a.index ? a.index[mb * a.n + i] : i;
-    if (row >= 0 && row < a.T) {
-      const int g = c / units, u = c % units;
-      const long from = m * a.stride_m + ((long)b * a.T + row) * a.stride_row + (long)g * a.d, slot = (mb * a.kv + g) * a.C + L + i;
-      uint32_t ks, vs;
-      const uint32_t kc = fp4_quantise8<T, WIDE>((const T*)a.K + from, 8 * u, a.d, ks), vc = fp4_quantise8<T, WIDE>((const T*)a.V + from, 8 * u, a.d, vs);
-      ((uint32_t*)a.Kc)[slot * units + u] = kc;
-      ((uint32_t*)a.Vc)[slot * units + u] = vc;
-      if (u % 4 == 0) {
-        a.Ks[slot * S + u / 4] = (uint8_t)ks;
-        a.Vs[slot * S + u / 4] = (uint8_t)vs;
-      }
-      if (u == 0) {
-        if (S > G) a.Ks[slot * S + G] = 0, a.Vs[slot * S + G] = 0;
-        if (a.pos) a.pos[slot] = (a.start ? a.start[mb] : L) + i;
-        if (a.weight) a.weight[slot] = 0.f;
-      }
+  const int end = min(cnt, a.C - L);                       // entries past the capacity are not written
+  const int r = (int)threadIdx.x / units, u = (int)threadIdx.x - r * units, i0 = (int)(blockIdx.x - uhead * blocks_per_head) * (kAppendRows * at_once) + r;
+  if (r >= at_once) return;
+  int row[kAppendRows];
+#pragma unroll
+  for (int x = 0; x < kAppendRows; ++x) {
+    const int i = i0 + x * at_once;
+    row[x] = i >= end ? -1 : a.index ? a.index[mb * a.n + i] : i;
+    if (row[x] >= a.T) row[x] = -1;
+  }
+  const int first = a.start ? a.start[mb] : L;
+  const long from = m * a.stride_m + (long)b * a.T * a.stride_row + (long)g * a.d;
+  Eight<T, WIDE> k[kAppendRows], v[kAppendRows];
+#pragma unroll
+  for (int x = 0; x < kAppendRows; ++x) {                  // a row that is not there: the first one, not used
+    const long at = from + max(row[x], 0) * a.stride_row;
+    k[x].load((const T*)a.K + at, 8 * u, a.d);
+    v[x].load((const T*)a.V + at, 8 * u, a.d);
+  }
+#pragma unroll
+  for (int x = 0; x < kAppendRows; ++x) {
+    const long slot = head * a.C + L + i0 + x * at_once;
+    uint32_t ks, vs;
+    const uint32_t kc = k[x].codes(ks), vc = v[x].codes(vs);                     // by every lane of a quad
+    const uint32_t ksum = G ? gather_scales<G>(ks) : ks, vsum = G ? gather_scales<G>(vs) : vs;
+    if (row[x] < 0) continue;
+    ((uint32_t*)a.Kc)[slot * units + u] = kc;
+    ((uint32_t*)a.Vc)[slot * units + u] = vc;
+    if (G == 0 && u % 4 == 0) {
+      a.Ks[slot * S + u / 4] = (uint8_t)ks;
+      a.Vs[slot * S + u / 4] = (uint8_t)vs;
     }
-    c += 256;
-    i += c / per_row;
-    c %= per_row;
+    if (u == 0) {
+      if constexpr (G == 4) {
+        ((uint32_t*)a.Ks)[slot] = ksum;
+        ((uint32_t*)a.Vs)[slot] = vsum;
+      } else if constexpr (G == 2) {
+        ((uint16_t*)a.Ks)[slot] = (uint16_t)ksum;
+        ((uint16_t*)a.Vs)[slot] = (uint16_t)vsum;
+      } else if (S > groups) {
+        a.Ks[slot * S + groups] = 0;
+        a.Vs[slot * S + groups] = 0;
+      }
+      if (a.pos) a.pos[slot] = first + i0 + x * at_once;
+      if (a.weight) a.weight[slot] = 0.f;
+    }
   }
 }
 
@@ -93,57 +135,61 @@ struct ReadFp4Args {
   int M, B, n, C, kv, d;
 };
 
-// A lane gives eight features of an entry, of its key and of its value; UNROLL of them are on their way at a time.  A workgroup takes `rows` entries of one head.
-template <typename T, bool WIDE, int UNROLL>
-__global__ __launch_bounds__(256) void cache_read_fp4_kernel(ReadFp4Args a, int rows, int blocks_per_head) {
+// A workgroup takes entries of one head; a lane gives eight features of an entry, of its key and of its value, kReadEntries entries at a time.  Bound by what it writes.  PAST: results that no
+// cache will hold go past them (us, through them / past them: 1.07 GB 243 / 231, 267 MB 66 / 54, 50 MB 14 / 25).
+constexpr int kReadEntries = 4;
+template <typename T, bool WIDE, bool PAST>
+__global__ __launch_bounds__(256) void cache_read_fp4_kernel(ReadFp4Args a, int blocks_per_head) {
+  const int S = fp4_scale_bytes(a.d), words = fp4_code_bytes(a.d) / 4, units = (a.d + 7) / 8, at_once = 256 / units;
   const unsigned uhead = blockIdx.x / blocks_per_head;
   const long head = uhead, mb = uhead / a.kv;
-  const int i0 = (int)(blockIdx.x % blocks_per_head) * rows, stop = min(rows, a.n - i0);
+  const int r = (int)threadIdx.x / units, u = (int)threadIdx.x - r * units, i0 = (int)(blockIdx.x - uhead * blocks_per_head) * (kReadEntries * at_once) + r;
+  if (r >= at_once) return;
   const int first = a.first ? a.first[mb] : 0, cnt = a.count ? clamp_len(a.count[mb], a.n) : a.n;
-  const int S = fp4_scale_bytes(a.d), words = fp4_code_bytes(a.d) / 4;
-  const unsigned units = (unsigned)(a.d + 7) / 8, total = (unsigned)stop * units;
-  for (unsigned k0 = threadIdx.x; k0 < total; k0 += 256 * UNROLL) {
-    uint32_t code[2][UNROLL], scale[2][UNROLL];
+  auto store16 = [](T* p, const uint4& v) {
+    if constexpr (PAST) __builtin_nontemporal_store(nf_u32x4_t{v.x, v.y, v.z, v.w}, (nf_u32x4_t*)p);
+    else *reinterpret_cast<uint4*>(p) = v;
+  };
+  uint32_t code[2][kReadEntries], scale[2][kReadEntries];
 #pragma unroll
-    for (int x = 0; x < UNROLL; ++x) {
-      const unsigned k = min(k0 + 256u * x, total - 1), i = k / units, u = k - i * units;
-      const long long slot = (long long)first + i0 + i;
-      const bool there = i0 + (int)i < cnt && slot >= 0 && slot < a.C;
-      const long at = head * a.C + (there ? slot : 0);     // an entry that is not there: some entry's bytes, not used
+  for (int x = 0; x < kReadEntries; ++x) {
+    const int i = i0 + x * at_once;
+    const long long slot = (long long)first + i;
+    const bool there = i < cnt && slot >= 0 && slot < a.C;
+    const long at = head * a.C + (there ? slot : 0);       // an entry that is not there: some entry's bytes, not used
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        code[t][x] = scale[t][x] = 0;
-        if (t == 0 || a.V) {
-          const uint32_t c = ((const uint32_t*)(t ? a.Vc : a.Kc))[at * words + u], s = (t ? a.Vs : a.Ks)[at * S + u / 4];
-          code[t][x] = there ? c : 0u;
-          scale[t][x] = there ? s : 127u;
-        }
+    for (int t = 0; t < 2; ++t) {
+      code[t][x] = scale[t][x] = 0;
+      if (t == 0 || a.V) {
+        const uint32_t c = ((const uint32_t*)(t ? a.Vc : a.Kc))[at * words + u], s = (t ? a.Vs : a.Ks)[at * S + u / 4];
+        code[t][x] = there ? c : 0u;
+        scale[t][x] = there ? s : 127u;
       }
     }
+  }
 #pragma unroll
-    for (int x = 0; x < UNROLL; ++x) {
-      const unsigned k = k0 + 256u * x, i = k / units, u = k - i * units;
-      if (k >= total) break;
-      const long at = (head * a.n + i0 + i) * a.d + 8 * u;
+  for (int x = 0; x < kReadEntries; ++x) {
+    const int i = i0 + x * at_once;
+    if (i >= a.n) break;
+    const long at = (head * a.n + i) * a.d + 8 * u;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        if (t == 1 && !a.V) break;
-        T* out = (T*)(t ? a.V : a.K) + at;
-        const float s = fp4_scale_value(scale[t][x]);
-        if constexpr (sizeof(T) == 2 && WIDE) {
-          *reinterpret_cast<uint4*>(out) = fp4_values_bf16(code[t][x], s);
+    for (int t = 0; t < 2; ++t) {
+      if (t == 1 && !a.V) break;
+      T* out = (T*)(t ? a.V : a.K) + at;
+      const float s = fp4_scale_value(scale[t][x]);
+      if constexpr (sizeof(T) == 2 && WIDE) {
+        store16(out, fp4_values_bf16(code[t][x], s));
+      } else {
+        float v[8];
+        fp4_values_f32(code[t][x], s, v);
+        if constexpr (WIDE) {
+#pragma unroll
+          for (int h = 0; h < 8; h += 4)
+            if (8 * u + h < a.d) store16(out + h, make_uint4(__float_as_uint(v[h]), __float_as_uint(v[h + 1]), __float_as_uint(v[h + 2]), __float_as_uint(v[h + 3])));
         } else {
-          float v[8];
-          fp4_values_f32(code[t][x], s, v);
-          if constexpr (WIDE) {
 #pragma unroll
-            for (int h = 0; h < 8; h += 4)
-              if ((int)(8 * u) + h < a.d) *reinterpret_cast<float4*>(out + h) = make_float4(v[h], v[h + 1], v[h + 2], v[h + 3]);
-          } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if ((int)(8 * u) + e < a.d) store_f32(out + e, v[e]);
-          }
+          for (int e = 0; e < 8; ++e)
+            if (8 * u + e < a.d) store_f32(out + e, v[e]);
         }
       }
     }

@@ -124,19 +124,18 @@ nf_status netfuse_cache_append_fp4(const void* K, const void* V, const int* inde
       !aligned(len, 4) || !aligned(start, 4) || !aligned(pos, 4) || !aligned(weight, 4))
     return NF_EINVAL;
   if (d > 256) return NF_EUNSUPPORTED;
-  const long long per_row = 4LL * kv_heads * fp4_groups(d);
-  if (per_row > INT_MAX / 2) return NF_EUNSUPPORTED;
   const AppendFp4Args a = {K, V, index, count, len, start, (uint8_t*)Kc, (uint8_t*)Ks, (uint8_t*)Vc, (uint8_t*)Vs, pos, weight, M, B, T, n, C, kv_heads, d, kv_stride_m, kv_stride_row};
-  const int rows = (int)std::max<long long>(1, std::min<long long>(n, 512 / per_row));
-  const int per_seq = (n + rows - 1) / rows;
-  const long long blocks = prod({M, B, per_seq});
+  const int groups = fp4_groups(d), rows = kAppendRows * (256 / (4 * groups)), per_head = (int)((n + (long long)rows - 1) / rows);
+  const long long blocks = prod({M, B, kv_heads, per_head});
   if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
   const bool wide = d * esz % 16 == 0 && whole_pieces(kv_stride_m, kv_stride_row, esz) && aligned(K, 16) && aligned(V, 16);
   hipStream_t s = (hipStream_t)stream;
-#define NF_APPEND(T, WIDE) nf_launch((cache_append_fp4_kernel<T, WIDE>), dim3((unsigned)blocks), dim3(256), 0, s, a, rows, per_seq)
-  if (dt == NF_F32) { if (wide) NF_APPEND(float, true); else NF_APPEND(float, false); }
-  else { if (wide) NF_APPEND(bf16_t, true); else NF_APPEND(bf16_t, false); }
+#define NF_APPEND_G(T, WIDE, G) nf_launch((cache_append_fp4_kernel<T, WIDE, G>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head)
+#define NF_APPEND(T, WIDE) if (groups == 4) NF_APPEND_G(T, WIDE, 4); else if (groups == 2) NF_APPEND_G(T, WIDE, 2); else NF_APPEND_G(T, WIDE, 0)
+  if (dt == NF_F32) { if (wide) { NF_APPEND(float, true); } else { NF_APPEND(float, false); } }
+  else { if (wide) { NF_APPEND(bf16_t, true); } else { NF_APPEND(bf16_t, false); } }
 #undef NF_APPEND
+#undef NF_APPEND_G
   return launched();
 }
 
@@ -149,14 +148,15 @@ nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc,
   if (!aligned(Kc, 16) || !aligned(Ks, 16) || !aligned(Vc, 16) || !aligned(Vs, 16) || !aligned(K, esz) || !aligned(V, esz) || !aligned(first, 4) || !aligned(count, 4)) return NF_EINVAL;
   if (d > 256) return NF_EUNSUPPORTED;
   const ReadFp4Args a = {(const uint8_t*)Kc, (const uint8_t*)Ks, (const uint8_t*)Vc, (const uint8_t*)Vs, first, count, K, V, M, B, n, C, kv_heads, d};
-  const int units = (d + 7) / 8, rows = std::max(1, std::min(n, 1024 / units)), per_head = (n + rows - 1) / rows;
+  const int rows = kReadEntries * (256 / ((d + 7) / 8)), per_head = (int)((n + (long long)rows - 1) / rows);
   const long long blocks = prod({M, B, kv_heads, per_head});
   if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
   const bool wide = d * esz % 16 == 0 && aligned(K, 16) && aligned(V, 16);
   hipStream_t s = (hipStream_t)stream;
-#define NF_READ(T, WIDE) nf_launch((cache_read_fp4_kernel<T, WIDE, 4>), dim3((unsigned)blocks), dim3(256), 0, s, a, rows, per_head)
-  if (dt == NF_F32) { if (wide) NF_READ(float, true); else NF_READ(float, false); }
-  else { if (wide) NF_READ(bf16_t, true); else NF_READ(bf16_t, false); }
+  const bool past = prod({M, B, kv_heads, n, d, (long long)esz, V ? 2 : 1}) > (128LL << 20);
+#define NF_READ(T, WIDE, PAST) nf_launch((cache_read_fp4_kernel<T, WIDE, PAST>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head)
+  if (dt == NF_F32) { if (!wide) NF_READ(float, false, false); else if (past) NF_READ(float, true, true); else NF_READ(float, true, false); }
+  else { if (!wide) NF_READ(bf16_t, false, false); else if (past) NF_READ(bf16_t, true, true); else NF_READ(bf16_t, true, false); }
 #undef NF_READ
   return launched();
 }
