@@ -52,18 +52,6 @@ __device__ __forceinline__ uint32_t weight_order(float w) {
   return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-// Inclusive sum over a wavefront: within rows of 16 lanes, then each row's last lane into the next row, then lane 31 into the upper half.
-template <int CTRL, int ROWS> __device__ __forceinline__ int add_from(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true); }
-__device__ __forceinline__ int wave_scan(int x) {
-  constexpr int kRowShr = 0x110, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
-  x = add_from<kRowShr + 1, 0xf>(x);
-  x = add_from<kRowShr + 2, 0xf>(x);
-  x = add_from<kRowShr + 4, 0xf>(x);
-  x = add_from<kRowShr + 8, 0xf>(x);
-  x = add_from<kRowBcast15, 0xa>(x);
-  return add_from<kRowBcast31, 0xc>(x);
-}
-
 // Exclusive sum over the NT threads of a workgroup, `total` their sum.  Every thread has to come here; wave_sums must not be in use by another sum.
 template <int NT> __device__ __forceinline__ int block_sum(int v, int* wave_sums, int& total) {
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;

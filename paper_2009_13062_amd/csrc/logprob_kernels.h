@@ -5,8 +5,8 @@
 // Both terms of the entropy are positive, and top + log S is never formed, so nothing is lost to large logits.  f grows with its argument and scale is positive, so the order of
 // the logits is that of the probabilities, and it is taken from the logits as they are stored: no two that differ become equal.
 //
-// A wavefront takes a chunk of a row, each lane 16 bytes at a time of it, and keeps all of them in registers.  The chunks of a row and the join of their results follow from V
-// alone, so a row's bits do not depend on what is merged with it.  Bound by the logits' bytes.
+// A wavefront takes some chunks of a row, one after the other, each lane 16 bytes at a time of it, and keeps a chunk in registers.  Each chunk leaves sums of its own, whose join follows from V
+// alone, and alternatives are exact, so a row's bits depend neither on what is merged with it nor on how many chunks a wavefront takes.
 #pragma once
 #include "decoder.h"
 #include "decoder_tiles.h"
@@ -18,7 +18,7 @@ constexpr int kMostAlternatives = 32;
 struct LogprobArgs {
   const void* logits; const int* token; const int* vocab; const int* nodes;
   float* logp; float* entropy; int* top; float* top_logp; float* ws;
-  int M, B, T, V, n, k, chunks;
+  int M, B, T, V, n, k, chunks, per_wave, groups;          // chunks of a row, of a wavefront, wavefronts of a row
   long stride_m, stride_row;
   float scale, cap, inv_cap;
 };
@@ -29,6 +29,8 @@ __device__ __forceinline__ uint32_t logit_order(float v) {
   return v > -INFINITY ? (u & 0x80000000u ? ~u : u | 0x80000000u) : 0u;
 }
 __device__ __forceinline__ float logit_of(uint32_t order) { return order == 0u ? -INFINITY : __uint_as_float(order & 0x80000000u ? order & 0x7fffffffu : ~order); }
+
+constexpr uint32_t kLowestOrder = 0x00800000u;             // of the lowest finite number: what lies below is no candidate
 
 // x of a logit under a cap, in units of log2 (tanh within 2^-20)
 __device__ __forceinline__ float capped_logit(float v, const LogprobArgs& a) { return tanh_either(v * (a.scale * a.inv_cap)) * (a.cap * kLog2e); }
@@ -41,10 +43,12 @@ struct FromTop {
 };
 
 constexpr int kLogprobList = 64;                           // candidates of a wavefront
+constexpr int kFewLanes = 16, kSlack = 8;                  // lanes that reach the border for which a higher one is not looked for; candidates past k that the list may keep
 constexpr int logprob_chunk(size_t bytes) { return bytes == 2 ? 4096 : 2048; }   // logits of a wavefront, by the size of one
 
-// What a chunk leaves in the workspace: its largest logit and the two sums at it (of 1 and of x - top, that in units of log2), then k pairs (order, token), the most likely first.
-constexpr int logprob_words(int k) { return 4 + 2 * k; }
+// The workspace: four numbers of each chunk -- its largest logit and the two sums at it (of 1 and of x - top, that in units of log2) -- then k pairs (order, token) of each wavefront, the
+// most likely first.
+constexpr int kChunkWords = 4;
 
 // An alternative as one number: the larger order wins, then the lower token.
 __device__ __forceinline__ uint64_t alternative(uint32_t order, int token) { return (uint64_t)order << 32 | (uint32_t)~token; }
@@ -58,15 +62,15 @@ __device__ __forceinline__ uint64_t wave_best(uint64_t v) {
   return v;
 }
 
-// An order that at least k lanes' own best ones reach, and few others of a wavefront's do: the k-th largest of the 64, its upper 16 bits found one by one with ballots.
-__device__ __forceinline__ uint32_t few_above(uint32_t best, int k) {
+// An order that at least k lanes' own best ones reach, and few others of a wavefront's do: the k-th largest of the 64, its upper BITS bits found one by one with ballots.
+template <int BITS> __device__ __forceinline__ uint32_t few_above(uint32_t best, int k) {
   uint32_t found = 0;
 #pragma unroll
-  for (int bit = 15; bit >= 0; --bit) {
+  for (int bit = BITS - 1; bit >= 0; --bit) {
     const uint32_t trial = found | 1u << bit;
-    if (__popcll(__ballot(best >> 16 >= trial)) >= k) found = trial;             // uniform
+    if (__popcll(__ballot(best >> (32 - BITS) >= trial)) >= k) found = trial;    // uniform
   }
-  return max(found << 16, 0x00800000u);                    // the order of the lowest finite number: -infinity and NaN are no candidates
+  return max(found << (32 - BITS), kLowestOrder);
 }
 // A lane's candidates go into the list, which holds kList; `count` goes on past that.
 template <class What> __device__ __forceinline__ void list_if(bool in, uint64_t* list, int& count, What&& what) {
@@ -105,6 +109,19 @@ template <> struct Logits<bf16_t> {
   static constexpr uint32_t kNone = 0xff80ff80u;
 };
 
+// The largest of three, and of the sizes of the last two, in one instruction (from the function the compiler first quiets each operand: twice the instructions of a chunk's maximum).  A
+// signalling NaN may come out as NaN.
+__device__ __forceinline__ float largest(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float largest_size(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, |%2|, |%3|" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 // tanh(u) / u on u^2: minimax fits of the relative error, 2^-23 in float32, up to kTanhNear and kTanhWide
 constexpr float kTanhNear = 0.35f, kTanhWide = 0.8f;
 
@@ -114,17 +131,17 @@ __global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
   constexpr int kChunk = logprob_chunk(sizeof(T)), P = L::kN, N = kChunk / kWave / P;
   __shared__ uint64_t lists[4][kLogprobList];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const unsigned wid = blockIdx.x * 4 + wave, row = wid / a.chunks;              // fewer than 2^26 and 2^31
+  const unsigned wid = blockIdx.x * 4 + wave, row = wid / a.groups;              // fewer than 2^26 and 2^31
   if (row >= (unsigned)(a.M * a.B) * (unsigned)a.T) return;                      // uniform per wavefront, as the next ones
-  const int chunk = (int)(wid - row * a.chunks);
+  const int group = (int)(wid - row * a.groups);
   const unsigned mb = row / a.T, m = mb / a.B;
   const int t = (int)(row - mb * a.T);
   const int V = a.vocab ? clamp_len(a.vocab[m], a.V) : a.V;
-  const int base = chunk * kChunk, left = V - base;
-  if (left <= 0 || (a.nodes && t >= a.nodes[mb])) return;
-  const T* p = (const T*)a.logits + m * a.stride_m + (long)(row - m * a.B * a.T) * a.stride_row + base;
+  const int chunk0 = group * a.per_wave, chunk1 = min(chunk0 + a.per_wave, (V + kChunk - 1) / kChunk);
+  if (chunk0 >= chunk1 || (a.nodes && t >= a.nodes[mb])) return;
+  const T* const logits = (const T*)a.logits + m * a.stride_m + (long)(row - m * a.B * a.T) * a.stride_row;
   // 16 bytes of each lane, -infinity where the row has ended; whether a piece is whole for all of them is the same for all of them
-  auto piece = [&](int i) -> uint4 {
+  auto piece = [&](const T* p, int left, int i) -> uint4 {
     const int j = (i * kWave + lane) * P;
     if ((i + 1) * kWave * P <= left) return load_at<uint4>(p + j);
     uint32_t x[4] = {L::kNone, L::kNone, L::kNone, L::kNone};
@@ -142,128 +159,199 @@ __global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
     return make_uint4(x[0], x[1], x[2], x[3]);
   };
   uint4 w[N];
-  if (left >= kChunk) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = load_at<uint4>(p + (i * kWave + lane) * P);
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = piece(i);
-  }
   // The logits stay as they came: each pass opens them again.  (Left to itself the compiler keeps what it made of them in the pass before, all 64 of it.)
   auto as_they_came = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(w[i].x), "+v"(w[i].y), "+v"(w[i].z), "+v"(w[i].w));
   };
-  float piece_top[N], mine = -INFINITY, low = INFINITY;
+  uint64_t* const list = lists[wave];
+  int count = 0;                                           // candidates in the list
+  uint32_t border = kLowestOrder;                          // the order that one of this wavefront's has to have
+  bool flooded = false;
+  for (int chunk = chunk0; chunk < chunk1; ++chunk) {
+    const int base = chunk * kChunk, left = V - base;
+    const T* const p = logits + base;
+    int at_lane = lane;                                    // made new for every chunk: the 64 token numbers of a lane would be kept in a register each
+    asm volatile("" : "+v"(at_lane));
+    if (left >= kChunk) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    piece_top[i] = L::at(w[i], 0);
+      for (int i = 0; i < N; ++i) w[i] = load_at<uint4>(p + (i * kWave + at_lane) * P);
+    } else {
 #pragma unroll
-    for (int e = 1; e < P; ++e) piece_top[i] = fmaxf(piece_top[i], L::at(w[i], e));
-    mine = fmaxf(mine, piece_top[i]);
-    if (CAP) {
-#pragma unroll
-      for (int e = 0; e < P; ++e) low = fminf(low, L::at(w[i], e));
+      for (int i = 0; i < N; ++i) w[i] = piece(p, left, i);
     }
-    __builtin_amdgcn_sched_barrier(0);
-  }
-  const float top = wave_max(mine);
-  as_they_came();
-  const FromTop from_top(top, a);
-  float sum = 0.f, first = 0.f;
-  bool plain = !CAP;                                       // each x from one polynomial of its logit
-  const float x1 = a.scale * kLog2e;
-  auto add = [&](float x) __attribute__((always_inline)) {
-    const float e = __builtin_amdgcn_exp2f(x);
-    sum += e;
-    first = fmaf(e, x, first);
-  };
-  if constexpr (!CAP) {
+    float piece_top[N], mine = -INFINITY, reach = 0.f;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+      piece_top[i] = -INFINITY;
 #pragma unroll
-      for (int e = 0; e < P; ++e) add((L::at(w[i], e) - top) * x1);
-      __builtin_amdgcn_sched_barrier(0);                   // one piece's numbers at a time: more would take registers from other wavefronts
-    }
-  } else {
-    const float u1 = a.scale * a.inv_cap, reach = fmaxf(fabsf(top), fabsf(wave_max(-low))) * u1, u2 = u1 * u1;
-    const bool sane = u1 > 1e-4f && u1 < 1e4f;                     // powers of the factor that float32 holds
-    const float most = from_top.most;
-    if (sane && reach <= kTanhNear) {
-      plain = true;
-      const float c0 = x1 * 0.9999999403953552f, c1 = x1 * u2 * -0.33332422375679016f, c2 = x1 * u2 * u2 * 0.13295799493789673f, c3 = x1 * u2 * u2 * u2 * -0.04895823076367378f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-#pragma unroll
-        for (int e = 0; e < P; ++e) {
-          const float v = L::at(w[i], e), q = v * v;
-          add(fmaf(v, fmaf(fmaf(fmaf(c3, q, c2), q, c1), q, c0), -most));
-        }
-        __builtin_amdgcn_sched_barrier(0);
+      for (int e = 0; e < P; e += 2) {
+        const float x = L::at(w[i], e), y = L::at(w[i], e + 1);
+        piece_top[i] = largest(piece_top[i], x, y);
+        if (CAP) reach = largest_size(reach, x, y);
       }
-    } else if (sane && reach <= kTanhWide) {
-      plain = true;
-      const float c0 = x1 * 0.9999999403953552f, c1 = x1 * u2 * -0.3333267569541931f, c2 = x1 * u2 * u2 * 0.13321048021316528f, c3 = x1 * u2 * u2 * u2 * -0.05311431363224983f,
-                  c4 = x1 * u2 * u2 * u2 * u2 * 0.01909330114722252f, c5 = x1 * u2 * u2 * u2 * u2 * u2 * -0.004355299286544323f;
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-#pragma unroll
-        for (int e = 0; e < P; ++e) {
-          const float v = L::at(w[i], e), q = v * v;
-          add(fmaf(v, fmaf(fmaf(fmaf(fmaf(fmaf(c5, q, c4), q, c3), q, c2), q, c1), q, c0), -most));
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
+      mine = fmaxf(mine, piece_top[i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
-  }
-  if (!plain || __any(first != first)) {                   // logits of -infinity (0 times it), NaN, or under a cap large ones: with more care
-    sum = first = 0.f;
+    float top = wave_max(mine);
     as_they_came();
+    FromTop from_top(top, a);
+    float sum = 0.f, first = 0.f;
+    bool plain = !CAP;                                       // each x from one polynomial of its logit
+    const float x1 = a.scale * kLog2e;
+    auto add = [&](float x) __attribute__((always_inline)) {
+      const float e = __builtin_amdgcn_exp2f(x);
+      sum += e;
+      first = fmaf(e, x, first);
+    };
+    if constexpr (!CAP) {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+      for (int i = 0; i < N; ++i) {
 #pragma unroll
-      for (int e = 0; e < P; ++e) {
-        const float y = L::at(w[i], e), x = CAP ? capped_logit(y, a) - from_top.most : (y - top) * x1, f = y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x);
-        sum += f;
-        first += f != 0.f ? x * f : 0.f;
-        if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);                       // more of them at a time would take registers from every chunk
+        for (int e = 0; e < P; ++e) add((L::at(w[i], e) - top) * x1);
+        __builtin_amdgcn_sched_barrier(0);                   // one piece's numbers at a time: more would take registers from other wavefronts
       }
-  }
-  sum = wave_sum(sum);
-  first = wave_sum(first);
-  float* const out = a.ws + ((long)row * a.chunks + chunk) * logprob_words(a.k);
-  if (lane == 0) *reinterpret_cast<float2*>(out) = make_float2(top, sum), out[2] = first;
-  if (a.k == 0) return;
+    } else {
+      const float u1 = a.scale * a.inv_cap, u2 = u1 * u1;
+      reach = wave_max(reach) * u1;
+      const bool sane = u1 > 1e-4f && u1 < 1e4f;                     // powers of the factor that float32 holds
+      const float most = from_top.most;
+      if (sane && reach <= kTanhNear) {
+        plain = true;
+        const float c0 = x1 * 0.9999999403953552f, c1 = x1 * u2 * -0.33332422375679016f, c2 = x1 * u2 * u2 * 0.13295799493789673f, c3 = x1 * u2 * u2 * u2 * -0.04895823076367378f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+#pragma unroll
+          for (int e = 0; e < P; ++e) {
+            const float v = L::at(w[i], e), q = v * v;
+            add(fmaf(v, fmaf(fmaf(fmaf(c3, q, c2), q, c1), q, c0), -most));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else if (sane && reach <= kTanhWide) {
+        plain = true;
+        const float c0 = x1 * 0.9999999403953552f, c1 = x1 * u2 * -0.3333267569541931f, c2 = x1 * u2 * u2 * 0.13321048021316528f, c3 = x1 * u2 * u2 * u2 * -0.05311431363224983f,
+                    c4 = x1 * u2 * u2 * u2 * u2 * 0.01909330114722252f, c5 = x1 * u2 * u2 * u2 * u2 * u2 * -0.004355299286544323f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+#pragma unroll
+          for (int e = 0; e < P; ++e) {
+            const float v = L::at(w[i], e), q = v * v;
+            add(fmaf(v, fmaf(fmaf(fmaf(fmaf(fmaf(c5, q, c4), q, c3), q, c2), q, c1), q, c0), -most));
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    if (!plain || __any(first != first)) {                   // logits of -infinity (0 times it), NaN, or under a cap large ones: with more care
+      as_they_came();
+      mine = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        piece_top[i] = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < P; ++e) piece_top[i] = fmaxf(piece_top[i], L::at(w[i], e));        // whatever kind of NaN there is
+        mine = fmaxf(mine, piece_top[i]);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      top = wave_max(mine);
+      from_top = FromTop(top, a);
+      sum = first = 0.f;
+      as_they_came();
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+          const float y = L::at(w[i], e), x = CAP ? capped_logit(y, a) - from_top.most : (y - top) * x1, f = y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x);
+          sum += f;
+          first += f != 0.f ? x * f : 0.f;
+          if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);                     // more of them at a time would take registers from every chunk
+        }
+    }
+    sum = wave_sum(sum);
+    first = wave_sum(first);
+    if (lane == 0) *reinterpret_cast<float4*>(a.ws + ((long)row * a.chunks + chunk) * kChunkWords) = make_float4(top, sum, first, 0.f);
 
-  auto put = [&](int r, uint64_t x) { *reinterpret_cast<uint2*>(out + 4 + 2 * r) = make_uint2((uint32_t)(x >> 32), ~(uint32_t)x); };
-  const float border = logit_of(few_above(logit_order(mine), a.k));
-  int count = 0;
-  as_they_came();
+    // ---- alternatives: what reaches the border joins the list, which is cut back to the best k when it has grown
+    const uint64_t hot = __ballot(mine >= logit_of(border));
+    if (a.k == 0 || hot == 0 || flooded) continue;         // uniform
+    uint32_t from = border;
+    if (__popcll(hot) > kFewLanes) from = max(from, few_above<16>(logit_order(mine), a.k));
+    const int before = count;
+    bool all_of = true;                                    // of the border's equals too
+    for (;;) {
+      as_they_came();
+      asm volatile("" : "+v"(at_lane));
+      const float least = logit_of(from + !all_of);
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (!__any(piece_top[i] >= border)) continue;          // uniform
+      for (int i = 0; i < N; ++i) {
+        if (!__any(piece_top[i] >= least)) continue;       // uniform
 #pragma unroll
-    for (int e = 0; e < P; ++e) {
-      const float v = L::at(w[i], e);
-      list_if(v >= border, lists[wave], count, [&] { return alternative(logit_order(v), base + (i * kWave + lane) * P + e); });
+        for (int e = 0; e < P; ++e) {
+          const float v = L::at(w[i], e);
+          list_if(v >= least, list, count, [&] { return alternative(logit_order(v), base + (i * kWave + at_lane) * P + e); });
+        }
+      }
+      flooded = !all_of && count > kLogprobList;
+      if (flooded || count <= kLogprobList) break;
+      // many alike: those above the k-th lane's best, then of its equals the first ones, k at most
+      count = before;
+      from = max(border, few_above<32>(logit_order(mine), a.k));
+      all_of = false;
+    }
+    if (flooded) continue;
+    if (!all_of) {
+      const float least = logit_of(from);
+      int need = a.k - (count - before);
+      if (count + max(need, 0) > kLogprobList) {
+        flooded = true;
+        continue;
+      }
+#pragma unroll 1
+      for (int i = 0; i < N && need > 0; ++i) {
+        const uint4 v = piece(p, left, i);                 // again from memory: numbered registers would have to be there for it
+        int alike = 0;
+#pragma unroll
+        for (int e = 0; e < P; ++e) alike += L::at(v, e) == least;
+        const int upto = wave_scan(alike);
+        int at = upto - alike;
+#pragma unroll
+        for (int e = 0; e < P; ++e)
+          if (L::at(v, e) == least) {
+            if (at < need) list[count + at] = alternative(from, base + (i * kWave + at_lane) * P + e);
+            ++at;
+          }
+        const int found = min(__shfl(upto, kWave - 1, kWave), need);
+        count += found;
+        need -= found;
+      }
+    }
+    if (count >= a.k + kSlack && chunk + 1 < chunk1) {
+      rank_list(list, count, a.k, [&](int r, uint64_t x) { list[r] = x; });
+      count = a.k;
+      border = (uint32_t)(list[a.k - 1] >> 32) + 1;        // of two alike the earlier one stays
     }
   }
-  if (count <= kLogprobList) {
-    rank_list(lists[wave], count, a.k, put);
+  if (a.k == 0) return;
+  uint2* const out = reinterpret_cast<uint2*>(a.ws + (long)a.M * a.B * a.T * a.chunks * kChunkWords) + ((long)row * a.groups + group) * a.k;
+  auto put = [&](int r, uint64_t x) { out[r] = make_uint2((uint32_t)(x >> 32), ~(uint32_t)x); };
+  if (!flooded) {
+    rank_list(list, count, a.k, put);
     return;
   }
-  // many alike: the best one that is left, k times
+  // The best one that is left, k times: so many logits of few lanes that no border of lanes' best ones tells them apart.
   uint64_t last = ~0ull;
 #pragma unroll 1
   for (int r = 0; r < a.k; ++r) {
     uint64_t best = 0;
 #pragma unroll 1
-    for (int i = 0; i < N; ++i) {
-      const uint4 v = piece(i);                            // again from memory: numbered registers would have to be there for it
+    for (int x = chunk0 * N; x < chunk1 * N; ++x) {
+      const int chunk = x / N, i = x - chunk * N;
+      const uint4 v = piece(logits + chunk * kChunk, V - chunk * kChunk, i);
 #pragma unroll
       for (int e = 0; e < P; ++e) {
-        const uint64_t x = alternative(logit_order(L::at(v, e)), base + (i * kWave + lane) * P + e);
-        best = x < last && x > best ? x : best;
+        const uint64_t y = alternative(logit_order(L::at(v, e)), chunk * kChunk + (i * kWave + lane) * P + e);
+        best = y < last && y > best ? y : best;
       }
     }
     last = wave_best(best);
@@ -280,24 +368,25 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
   const unsigned row = blockIdx.x, mb = row / a.T, m = mb / a.B;
   const int t = (int)(row - mb * a.T);
   const int V = a.nodes && t >= a.nodes[mb] ? 0 : a.vocab ? clamp_len(a.vocab[m], a.V) : a.V;
-  const int chunks = (V + kChunk - 1) / kChunk, words = logprob_words(a.k);
-  const float* const ws = a.ws + (long)row * a.chunks * words;
+  const int chunks = (V + kChunk - 1) / kChunk, groups = (chunks + a.per_wave - 1) / a.per_wave;
+  const float4* const ws = reinterpret_cast<const float4*>(a.ws) + (long)row * a.chunks;
+  const uint2* const lists = reinterpret_cast<const uint2*>(a.ws + (long)a.M * a.B * a.T * a.chunks * kChunkWords) + (long)row * a.groups * a.k;
   const T* const p = (const T*)a.logits + m * a.stride_m + (long)(row - m * a.B * a.T) * a.stride_row;
   // what the first lanes need, all on its way at once
   const int token0 = lane < a.n ? a.token[(long)row * a.n + lane] : -1;
   const bool known0 = token0 >= 0 && token0 < V;
   const float logit0 = known0 ? load_f32(p + token0) : -INFINITY;
   float top = -INFINITY;
-  for (int c = lane; c < chunks; c += kWave) top = fmaxf(top, ws[(long)c * words]);
+  for (int c = lane; c < chunks; c += kWave) top = fmaxf(top, ws[c].x);
   top = wave_max(top);
   const FromTop from_top(top, a);
   float sum = 0.f, first = 0.f;
   for (int c = lane; c < chunks; c += kWave) {
-    const float2 w = *reinterpret_cast<const float2*>(ws + (long)c * words);
-    const float z = ws[(long)c * words + 2], x = from_top(w.x, a), f = __builtin_amdgcn_exp2f(x);
+    const float4 w = ws[c];
+    const float x = from_top(w.x, a), f = __builtin_amdgcn_exp2f(x);
     if (w.y != 0.f) {                                      // a chunk of -infinity alone adds nothing
       sum = fmaf(w.y, f, sum);
-      first += f != 0.f ? f * fmaf(x, w.y, z) : 0.f;
+      first += f != 0.f ? f * fmaf(x, w.y, w.z) : 0.f;
     }
   }
   sum = wave_sum(sum);
@@ -313,13 +402,9 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
   }
   if (a.k == 0) return;
 
-  // The same choice among the chunks' alternatives, candidate i being number i % k of chunk i / k.
-  const int all = chunks * a.k;
-  auto candidate = [&](int i) -> uint64_t {
-    const int c = i / a.k;
-    const uint2 w = *reinterpret_cast<const uint2*>(ws + (long)c * words + 4 + 2 * (i - c * a.k));
-    return alternative(w.x, (int)w.y);
-  };
+  // The same choice among the wavefronts' alternatives.
+  const int all = groups * a.k;
+  auto candidate = [&](int i) { return alternative(lists[i].x, (int)lists[i].y); };
   auto put = [&](int r, uint64_t x) {
     const uint32_t order = (uint32_t)(x >> 32);
     a.top[(long)row * a.k + r] = order ? (int)~(uint32_t)x : -1;
@@ -330,7 +415,7 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
     const uint64_t x = candidate(i);
     mine = x > mine ? x : mine;
   }
-  const uint32_t border = few_above((uint32_t)(mine >> 32), a.k);
+  const uint32_t border = few_above<16>((uint32_t)(mine >> 32), a.k);
   int count = 0;
   for (int i0 = 0; i0 < all; i0 += kWave) {
     const uint64_t x = i0 + lane < all ? candidate(i0 + lane) : 0;

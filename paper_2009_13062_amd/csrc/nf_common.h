@@ -119,6 +119,18 @@ struct MaxOp { __device__ __forceinline__ float operator()(float a, float b) con
 __device__ __forceinline__ float wave_sum(float v) { return wave_reduce(v, AddOp{}); }
 __device__ __forceinline__ float wave_max(float v) { return wave_reduce(v, MaxOp{}); }
 
+// Inclusive sum over a wavefront: within rows of 16 lanes, then each row's last lane into the next row, then lane 31 into the upper half.
+template <int CTRL, int ROWS> __device__ __forceinline__ int add_from(int x) { return x + __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, true); }
+__device__ __forceinline__ int wave_scan(int x) {
+  constexpr int kRowShr = 0x110, kRowBcast15 = 0x142, kRowBcast31 = 0x143;
+  x = add_from<kRowShr + 1, 0xf>(x);
+  x = add_from<kRowShr + 2, 0xf>(x);
+  x = add_from<kRowShr + 4, 0xf>(x);
+  x = add_from<kRowShr + 8, 0xf>(x);
+  x = add_from<kRowBcast15, 0xa>(x);
+  return add_from<kRowBcast31, 0xc>(x);
+}
+
 // Workgroups are handed to the 8 XCDs round-robin (id % 8), and each XCD has its own L2.  This
 // maps the hardware id to a logical id such that consecutive logical ids run on the same XCD, so
 // tiles that share operands (the tiles of one model) share an L2.  Bijective for any total.

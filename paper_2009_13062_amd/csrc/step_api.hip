@@ -210,7 +210,7 @@ nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V
 
 long long netfuse_token_logprobs_workspace(int M, int B, int T, int V, int k) {
   if (M <= 0 || B <= 0 || T <= 0 || V <= 0 || V > kMostEntries || k < 0 || k > kMostAlternatives) return -1;
-  const long long bytes = prod({M, B, T, logprob_chunks(V, NF_F32), 4LL * logprob_words(k)});
+  const long long bytes = prod({M, B, T, logprob_chunks(V, NF_F32), 4LL * kChunkWords + 8LL * k});        // for a wavefront per chunk of either type
   return bytes >= kMaxElems ? -1 : bytes;
 }
 
@@ -230,9 +230,14 @@ nf_status netfuse_token_logprobs(const void* logits, const int* token, const int
   if (k > kMostAlternatives) return NF_EUNSUPPORTED;
   const long long need = netfuse_token_logprobs_workspace(M, B, T, V, k);
   if (need < 0 || workspace_bytes < need) return NF_EINVAL;
-  const LogprobArgs a = {logits, token, vocab, nodes, logp, entropy, top, top_logp, (float*)workspace, M, B, T, V, n, k, logprob_chunks(V, dt),
+  const long long rows = prod({M, B, T});
+  const int chunks = logprob_chunks(V, dt);
+  // As many chunks to a wavefront as leave two wavefronts for each that the device holds: its alternatives then are few and soon have a high border (4084 rows of 50001 in float32, 20 alternatives,
+  // chunks and join, us: a wavefront per chunk 174 + 13, 8 chunks 164 + 8, 16 168 + 8, 32 188 + 8).
+  const int per_wave = (int)std::max<long long>(1, std::min<long long>(16, prod({rows, chunks}) / 8192)), groups = (chunks + per_wave - 1) / per_wave;
+  const LogprobArgs a = {logits, token, vocab, nodes, logp, entropy, top, top_logp, (float*)workspace, M, B, T, V, n, k, chunks, per_wave, groups,
                          stride_m, stride_row, scale, cap, cap != 0.f ? 1.f / cap : 0.f};
-  const long long rows = prod({M, B, T}), blocks = (prod({rows, a.chunks}) + 3) / 4;
+  const long long blocks = (prod({rows, groups}) + 3) / 4;
   if (!grid_fits(blocks, 256) || !grid_fits(rows, 64)) return NF_EUNSUPPORTED;          // before the first of the two is enqueued
   hipStream_t s = (hipStream_t)stream;
 #define NF_CHUNKS(T, CAP) nf_launch((logprob_chunks_kernel<T, CAP>), dim3((unsigned)blocks), dim3(256), 0, s, a)

@@ -481,6 +481,45 @@ def test_logprobs_of_equal_logits(nf, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [1, 4000])
+def test_logprobs_of_floods(nf, dtype, rows):
+    """More candidates than a wavefront's list holds, whether it takes one chunk (few rows) or several: equal ones past the border, a few masked rows' lowest values, and
+    large ones that lie in a few lanes (those of the same 8 neighbouring tokens of each 512)."""
+    V = 9000 if rows == 1 else 13000
+    kinds = torch.zeros(4, V)
+    kinds[0, ::3] = 1.0
+    kinds[0, 4000:4010] = 2.0
+    kinds[1] = torch.finfo(dtype).min
+    kinds[1, [7, 4500, 8999]] = torch.tensor([1.0, 3.0, 2.0])
+    lane = torch.arange(V) % 512 // 8
+    kinds[2] = torch.where(lane < 3, 5.0 + torch.rand(V, generator=gen(1)), torch.rand(V, generator=gen(2)))
+    kinds[3] = torch.where(lane < 3, 5.0, 1.0)
+    x = kinds.to(dtype).cuda()[None].expand(rows, 4, V).reshape(1, 4 * rows, V)
+    kw = dict(k=20, vocab=None, nodes=None, scale=1.0, cap=0.0)
+    got = nf.token_logprobs(x, **kw)
+    for r in (0, rows - 1):
+        part = [None if t is None else t[:, 4 * r:4 * r + 4] for t in got]
+        check_logprobs(part, x[:, 4 * r:4 * r + 4], None, kw)
+    for t in got[1:]:
+        assert torch.equal(t.view(rows, -1), t.view(rows, -1)[:1].expand(rows, -1))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_logprobs_bits_do_not_depend_on_the_other_rows(nf, dtype):
+    """Rows whose chunks are one wavefront's each give the bits that they give among thousands, several chunks to a wavefront."""
+    V, g = 20011, gen(31)
+    x = (torch.randn(1, 6000, V, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda") * 3).to(dtype)
+    for cap in (0.0, 25.0):
+        kw = dict(k=12, cap=cap)
+        token = torch.randint(0, V, (1, 6000, 2), generator=g).to(I32).cuda()
+        many = nf.token_logprobs(x, token, **kw)
+        for r in (0, 2999, 5999):
+            for a, b in zip(many, nf.token_logprobs(x[:, r:r + 1], token[:, r:r + 1].contiguous(), **kw)):
+                assert torch.equal(a[:, r:r + 1], b)
+        check_logprobs([t[:, :2] for t in many], x[:, :2], token[:, :2], dict(kw, vocab=None, nodes=None, scale=1.0))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("cap", [0.0, 20.0])
 def test_logprobs_of_odd_logits(nf, dtype, cap):
     """Tokens that are masked with -infinity or the type's lowest value, rows of nothing else, +infinity, NaN; what lies past the vocabulary."""
@@ -495,6 +534,7 @@ def test_logprobs_of_odd_logits(nf, dtype, cap):
     x[0, 6, ::2] = -math.inf
     x[0, 7] = torch.finfo(dtype).min
     x[0, 8, :4096] = -math.inf
+    x[0, 4].view(torch.int16 if dtype == BF else I32)[6001] = 0x7f81 if dtype == BF else 0x7f800001      # a signalling NaN
     token = ints([[[3, 11, 100]] * 9])
     kw = dict(k=12, vocab=None, nodes=None, scale=1.0, cap=cap)
     check_logprobs(nf.token_logprobs(x, token, **kw), x, token, kw)
