@@ -12,13 +12,20 @@
 #include "decoder_tiles.h"
 
 namespace nf {
+// 16 bytes of logits, from any element on; they are read once, and past the caches that is faster (4084 rows of 50001 in float32 164 -> 143 us).
+template <class T> __device__ __forceinline__ uint4 load_once(const T* p) {
+  typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  const words_t v = __builtin_nontemporal_load((const words_t*)p);
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+
 
 constexpr int kMostAlternatives = 32;
 
 struct LogprobArgs {
   const void* logits; const int* token; const int* vocab; const int* nodes;
   float* logp; float* entropy; int* top; float* top_logp; float* ws;
-  int M, B, T, V, n, k, chunks, per_wave, groups;          // chunks of a row, of a wavefront, wavefronts of a row
+  int M, B, T, V, n, k, chunks, groups;                    // chunks and wavefronts of a row
   long stride_m, stride_row;
   float scale, cap, inv_cap;
 };
@@ -125,8 +132,11 @@ __device__ __forceinline__ float largest_size(float a, float b, float c) {
 // tanh(u) / u on u^2: minimax fits of the relative error, 2^-23 in float32, up to kTanhNear and kTanhWide
 constexpr float kTanhNear = 0.35f, kTanhWide = 0.8f;
 
+// Four wavefronts per SIMD in float32, which is bound by the reads (143 us of the rows above, 5.7 TB/s; 5 of them 143, 6 160), five in bfloat16, which is bound by vector instructions: about
+// 8 for each logit, with a cap 12, and an exponential of a quarter of their rate (832 rows of 131072, 8 alternatives, us: 3 wavefronts 56, under a cap 69, 4 53 and 61, 5 52 and 61, 6 51 and 59;
+// rows of 131071, which begin at odd elements, 58 and 67 with 5).
 template <typename T, bool CAP>
-__global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_kernel(LogprobArgs a) {
   using L = Logits<T>;
   constexpr int kChunk = logprob_chunk(sizeof(T)), P = L::kN, N = kChunk / kWave / P;
   __shared__ uint64_t lists[4][kLogprobList];
@@ -137,13 +147,13 @@ __global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
   const unsigned mb = row / a.T, m = mb / a.B;
   const int t = (int)(row - mb * a.T);
   const int V = a.vocab ? clamp_len(a.vocab[m], a.V) : a.V;
-  const int chunk0 = group * a.per_wave, chunk1 = min(chunk0 + a.per_wave, (V + kChunk - 1) / kChunk);
-  if (chunk0 >= chunk1 || (a.nodes && t >= a.nodes[mb])) return;
+  const int chunks = (V + kChunk - 1) / kChunk;           // this wavefront's are every a.groups-th, so that neighbours read what lies together
+  if (group >= chunks || (a.nodes && t >= a.nodes[mb])) return;
   const T* const logits = (const T*)a.logits + m * a.stride_m + (long)(row - m * a.B * a.T) * a.stride_row;
   // 16 bytes of each lane, -infinity where the row has ended; whether a piece is whole for all of them is the same for all of them
   auto piece = [&](const T* p, int left, int i) -> uint4 {
     const int j = (i * kWave + lane) * P;
-    if ((i + 1) * kWave * P <= left) return load_at<uint4>(p + j);
+    if ((i + 1) * kWave * P <= left) return load_once(p + j);
     uint32_t x[4] = {L::kNone, L::kNone, L::kNone, L::kNone};
     if (i * kWave * P < left) {
       uint32_t v[P];
@@ -168,17 +178,20 @@ __global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
   int count = 0;                                           // candidates in the list
   uint32_t border = kLowestOrder;                          // the order that one of this wavefront's has to have
   bool flooded = false;
-  for (int chunk = chunk0; chunk < chunk1; ++chunk) {
+  for (int chunk = group; chunk < chunks; chunk += a.groups) {
     const int base = chunk * kChunk, left = V - base;
     const T* const p = logits + base;
     int at_lane = lane;                                    // made new for every chunk: the 64 token numbers of a lane would be kept in a register each
     asm volatile("" : "+v"(at_lane));
     if (left >= kChunk) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) w[i] = load_at<uint4>(p + (i * kWave + at_lane) * P);
+      for (int i = 0; i < N; ++i) w[i] = load_once(p + (i * kWave + at_lane) * P);
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i) w[i] = piece(p, left, i);
+      for (int i = 0; i < N; ++i) {
+        w[i] = piece(p, left, i);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
     float piece_top[N], mine = -INFINITY, reach = 0.f;
 #pragma unroll
@@ -204,12 +217,17 @@ __global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
       sum += e;
       first = fmaf(e, x, first);
     };
+    // One piece's numbers at a time, the sum's too (which could wait, all terms of it in registers, for a path that uses it): more would take registers from other wavefronts
+    auto added = [&]() __attribute__((always_inline)) {
+      asm volatile("" : "+v"(sum), "+v"(first));
+      __builtin_amdgcn_sched_barrier(0);
+    };
     if constexpr (!CAP) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
 #pragma unroll
         for (int e = 0; e < P; ++e) add((L::at(w[i], e) - top) * x1);
-        __builtin_amdgcn_sched_barrier(0);                   // one piece's numbers at a time: more would take registers from other wavefronts
+        added();
       }
     } else {
       const float u1 = a.scale * a.inv_cap, u2 = u1 * u1;
@@ -226,7 +244,7 @@ __global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
             const float v = L::at(w[i], e), q = v * v;
             add(fmaf(v, fmaf(fmaf(fmaf(c3, q, c2), q, c1), q, c0), -most));
           }
-          __builtin_amdgcn_sched_barrier(0);
+          added();
         }
       } else if (sane && reach <= kTanhWide) {
         plain = true;
@@ -239,7 +257,7 @@ __global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
             const float v = L::at(w[i], e), q = v * v;
             add(fmaf(v, fmaf(fmaf(fmaf(fmaf(fmaf(c5, q, c4), q, c3), q, c2), q, c1), q, c0), -most));
           }
-          __builtin_amdgcn_sched_barrier(0);
+          added();
         }
       }
     }
@@ -326,7 +344,7 @@ __global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
         need -= found;
       }
     }
-    if (count >= a.k + kSlack && chunk + 1 < chunk1) {
+    if (count >= a.k + kSlack && chunk + a.groups < chunks) {
       rank_list(list, count, a.k, [&](int r, uint64_t x) { list[r] = x; });
       count = a.k;
       border = (uint32_t)(list[a.k - 1] >> 32) + 1;        // of two alike the earlier one stays
@@ -345,8 +363,7 @@ __global__ __launch_bounds__(256, 4) void logprob_chunks_kernel(LogprobArgs a) {
   for (int r = 0; r < a.k; ++r) {
     uint64_t best = 0;
 #pragma unroll 1
-    for (int x = chunk0 * N; x < chunk1 * N; ++x) {
-      const int chunk = x / N, i = x - chunk * N;
+    for (int chunk = group, i = 0; chunk < chunks; i = i + 1 < N ? i + 1 : 0, chunk += i == 0 ? a.groups : 0) {
       const uint4 v = piece(logits + chunk * kChunk, V - chunk * kChunk, i);
 #pragma unroll
       for (int e = 0; e < P; ++e) {
@@ -368,7 +385,7 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
   const unsigned row = blockIdx.x, mb = row / a.T, m = mb / a.B;
   const int t = (int)(row - mb * a.T);
   const int V = a.nodes && t >= a.nodes[mb] ? 0 : a.vocab ? clamp_len(a.vocab[m], a.V) : a.V;
-  const int chunks = (V + kChunk - 1) / kChunk, groups = (chunks + a.per_wave - 1) / a.per_wave;
+  const int chunks = (V + kChunk - 1) / kChunk, groups = min(chunks, a.groups);
   const float4* const ws = reinterpret_cast<const float4*>(a.ws) + (long)row * a.chunks;
   const uint2* const lists = reinterpret_cast<const uint2*>(a.ws + (long)a.M * a.B * a.T * a.chunks * kChunkWords) + (long)row * a.groups * a.k;
   const T* const p = (const T*)a.logits + m * a.stride_m + (long)(row - m * a.B * a.T) * a.stride_row;

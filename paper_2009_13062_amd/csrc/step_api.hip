@@ -235,7 +235,7 @@ nf_status netfuse_token_logprobs(const void* logits, const int* token, const int
   // As many chunks to a wavefront as leave two wavefronts for each that the device holds: its alternatives then are few and soon have a high border (4084 rows of 50001 in float32, 20 alternatives,
   // chunks and join, us: a wavefront per chunk 174 + 13, 8 chunks 164 + 8, 16 168 + 8, 32 188 + 8).
   const int per_wave = (int)std::max<long long>(1, std::min<long long>(16, prod({rows, chunks}) / 8192)), groups = (chunks + per_wave - 1) / per_wave;
-  const LogprobArgs a = {logits, token, vocab, nodes, logp, entropy, top, top_logp, (float*)workspace, M, B, T, V, n, k, chunks, per_wave, groups,
+  const LogprobArgs a = {logits, token, vocab, nodes, logp, entropy, top, top_logp, (float*)workspace, M, B, T, V, n, k, chunks, groups,
                          stride_m, stride_row, scale, cap, cap != 0.f ? 1.f / cap : 0.f};
   const long long blocks = (prod({rows, groups}) + 3) / 4;
   if (!grid_fits(blocks, 256) || !grid_fits(rows, 64)) return NF_EUNSUPPORTED;          // before the first of the two is enqueued
