@@ -13,8 +13,8 @@
 
 namespace nf {
 // 16 bytes of logits, from any element on; they are read once, and past the caches that is faster (4084 rows of 50001 in float32 164 -> 143 us).
+typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(2)));
 template <class T> __device__ __forceinline__ uint4 load_once(const T* p) {
-  typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(sizeof(T))));
   const words_t v = __builtin_nontemporal_load((const words_t*)p);
   return make_uint4(v.x, v.y, v.z, v.w);
 }
