@@ -664,6 +664,7 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
       }
+      if (next_held) open_fp4(fresh);                      // trees leave no tile out
       // O^T += V^T P^T.  In a 16-lane group, lane i points at key row i / 4, features 4 (i % 4) .. + 3 of a 4 x 16 block and receives the
       // 4 keys of feature i; slots 0-3 of step (sb, st) are keys 32 sb + 16 st + 4 half + 0..3, slots 4-7 the same + 8.
 #pragma unroll
@@ -681,7 +682,6 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
           }
       keep_ahead<NSB * 2 * TB, 2>();
     }
-    if (next_held) open_fp4(fresh);
     if (next != kNoTile && keyed && tid < KB) Key[fresh * KB + tid] = key_reg;
     cur = fresh;
     ++number;
