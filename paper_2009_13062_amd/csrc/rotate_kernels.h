@@ -3,7 +3,8 @@
 //   y = x / sqrt(mean x^2 + eps) * gamma;   pair i of the first `rot` features: (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),  t = position * freq[i]
 //
 // pairs (i, i + rot / 2) or (2 i, 2 i + 1).  The angle is a product in 64 bits, taken in whole turns before it becomes a float32: an angle is
-// off by 2^-51 of itself, a far position's bits are not lost to a float32.  Bound by the rows' bytes.
+// off by 2^-51 of itself, a far position's bits are not lost to a float32.  Bound by the rows' bytes (16 prompts of up to 2039 tokens, 32 heads over 8 of 128, normed, three axes: 103 us, 4.84 TB/s where a copy
+// reaches 4.94), a few tokens by latency (8 of them 5 us).
 #pragma once
 #include "decoder.h"
 
@@ -54,27 +55,30 @@ template <int LPH> __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
+// Four neighbouring features of a row in one load: 16 bytes of float32, 8 of bfloat16.  (Eight of bfloat16 hold twice the registers: 16 prompts of up to 2039 tokens, 32 heads over 8 of 128, 106 us
+// and 103; 32 of 512, 12 heads of 64, 26.5 and 22.6.  And 80 features of which 40 turn are no whole pieces of 16: one by one 525 us, so 81.)
 template <typename T> struct Piece;
 template <> struct Piece<float> {
-  static constexpr int kN = 4;
+  typedef uint4 words_t;
   __device__ static __forceinline__ void open(const uint4& w, float* x) { x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w); }
   __device__ static __forceinline__ uint4 close(const float* x) { return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])); }
 };
 template <> struct Piece<bf16_t> {
-  static constexpr int kN = 8;
-  __device__ static __forceinline__ void open(const uint4& w, float* x) {
-    const uint32_t ws[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[2 * e] = __uint_as_float(ws[e] << 16), x[2 * e + 1] = __uint_as_float(ws[e] & 0xffff0000u);
+  typedef uint2 words_t;
+  __device__ static __forceinline__ void open(const uint2& w, float* x) {
+    x[0] = __uint_as_float(w.x << 16); x[1] = __uint_as_float(w.x & 0xffff0000u); x[2] = __uint_as_float(w.y << 16); x[3] = __uint_as_float(w.y & 0xffff0000u);
   }
-  __device__ static __forceinline__ uint4 close(const float* x) { return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])); }
+  __device__ static __forceinline__ uint2 close(const float* x) { return make_uint2(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3])); }
 };
+constexpr int kPieceFeatures = 4;
 
-// A wavefront takes one token.  Its lanes work out the token's angles once, a pair each; then LPH lanes take a head, each the two pieces of 16 bytes whose features turn with
+// A wavefront takes one token, or `per_wave` steps of it.  Its lanes work out the token's angles once, a pair each; then LPH lanes take a head, each the two pieces whose features turn with
 // each other (or, past `rot`, two neighbouring ones), so 64 / LPH heads are read and written at a time and a lane keeps its angles and weights over all of them.
 template <typename T, int LPH>
 __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int parts, int per_wave) {
-  constexpr int P = Piece<T>::kN, kHeads = kWave / LPH, kAhead = 4;
+  using Pc = Piece<T>;
+  typedef typename Pc::words_t words_t;
+  constexpr int P = kPieceFeatures, kHeads = kWave / LPH, kAhead = 4;
   __shared__ float2 angle[4][128];
   const int lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -97,17 +101,18 @@ __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int pa
   T* const ko = (T*)a.Ko + m * a.ko_stride_m + row * a.ko_stride_row;
 
   // Every lane loads, from some row that is there where it has none of its own: a load under a condition is waited for before the next one.
-  uint4 x0[kAhead], x1[kAhead];
+  words_t x0[kAhead], x1[kAhead];
   const int at0 = f0 < a.d ? f0 : 0, at1 = f1 < a.d ? f1 : 0;
   auto load = [&](int step) {
 #pragma unroll
     for (int t = 0; t < kAhead; ++t) {
-      const int st = min(step + t, step1 - 1);
+      if (step + t >= step1) break;                        // uniform
+      const int st = step + t;
       const bool key = st >= q_steps;                      // uniform
       const int h = min((st - (key ? q_steps : 0)) * kHeads + sub, (key ? a.kv : a.heads) - 1);
       const T* p = (key ? k : q) + (long)h * a.d;
-      x0[t] = *reinterpret_cast<const uint4*>(p + at0);
-      x1[t] = *reinterpret_cast<const uint4*>(p + at1);
+      x0[t] = *reinterpret_cast<const words_t*>(p + at0);
+      x1[t] = *reinterpret_cast<const words_t*>(p + at1);
     }
   };
   load(step0);
@@ -130,8 +135,8 @@ __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int pa
       const int h = (step + t - (key ? q_steps : 0)) * kHeads + sub;
       const float* const gamma = key ? a.gamma_k : a.gamma_q;
       float x[2 * P];
-      Piece<T>::open(x0[t], x);
-      Piece<T>::open(x1[t], x + P);
+      Pc::open(x0[t], x);
+      Pc::open(x1[t], x + P);
       if (gamma) {
         if (gamma_of != key) {
           gamma_of = key;
@@ -168,8 +173,8 @@ __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int pa
       }
       if (h < (key ? a.kv : a.heads)) {
         T* o = (key ? ko : qo) + (long)h * a.d;
-        if (f0 < a.d) *reinterpret_cast<uint4*>(o + f0) = Piece<T>::close(x);
-        if (f1 < a.d) *reinterpret_cast<uint4*>(o + f1) = Piece<T>::close(x + P);
+        if (f0 < a.d) *reinterpret_cast<words_t*>(o + f0) = Pc::close(x);
+        if (f1 < a.d) *reinterpret_cast<words_t*>(o + f1) = Pc::close(x + P);
       }
     }
     if (step + kAhead < step1) load(step + kAhead);

@@ -23,20 +23,23 @@ inline nf_status launched() { return hipGetLastError() == hipSuccess ? NF_OK : N
 inline bool whole_pieces(long stride_m, long stride_row, size_t esz) { return stride_m * (long)esz % 16 == 0 && stride_row * (long)esz % 16 == 0; }
 
 template <typename T>
-nf_status launch_rotate(const RotateArgs& a, bool pieces, hipStream_t s) {
-  const long long tokens = prod({a.M, a.B, a.S});
-  if (!pieces) {
-    const long long blocks = (prod({tokens, a.heads + (long long)a.kv}) + 3) / 4;
-    if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
-    nf_launch((rotate_rows_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, s, a);
-    return launched();
-  }
-  constexpr int P = Piece<T>::kN;
+nf_status launch_rotate_rows(const RotateArgs& a, hipStream_t s) {
+  const long long blocks = (prod({a.M, a.B, a.S, a.heads + (long long)a.kv}) + 3) / 4;
+  if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
+  nf_launch((rotate_rows_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, s, a);
+  return launched();
+}
+
+template <typename T>
+nf_status launch_rotate(const RotateArgs& a, hipStream_t s) {
+  constexpr int P = kPieceFeatures;
   const int units = (a.d + 2 * P - 1) / (2 * P);
   int lph = 1;
   while (lph < units) lph *= 2;
   const int at_once = kWave / lph, steps = (a.heads + at_once - 1) / at_once + (a.kv + at_once - 1) / at_once;
-  const int parts = 1, per_wave = steps;
+  // a token's steps are shared out where there are few tokens (32 heads over 8 of 128: 8 tokens 5.4 us, by one wavefront each 7.3)
+  const long long tokens = prod({a.M, a.B, a.S});
+  const int most = (int)std::max<long long>(1, std::min<long long>(steps, 2048 / tokens)), per_wave = (steps + most - 1) / most, parts = (steps + per_wave - 1) / per_wave;
   const long long blocks = (prod({tokens, parts}) + 3) / 4;
   if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
 #define NF_ROTATE(LPH) nf_launch((rotate_pieces_kernel<T, LPH>), dim3((unsigned)blocks), dim3(256), 0, s, a, parts, per_wave)
@@ -104,11 +107,14 @@ nf_status netfuse_rotate_heads(const void* Q, const void* K, const float* gamma_
   a.q_stride_m = q_stride_m; a.q_stride_row = q_stride_row; a.k_stride_m = k_stride_m; a.k_stride_row = k_stride_row;
   a.qo_stride_m = qo_stride_m; a.qo_stride_row = qo_stride_row; a.ko_stride_m = ko_stride_m; a.ko_stride_row = ko_stride_row;
   a.eps = eps;
-  const int P = 16 / (int)esz;
-  const bool pieces = d % P == 0 && rot % (2 * P) == 0 && whole_pieces(q_stride_m, q_stride_row, esz) && whole_pieces(qo_stride_m, qo_stride_row, esz) &&
-                      (!K || (whole_pieces(k_stride_m, k_stride_row, esz) && whole_pieces(ko_stride_m, ko_stride_row, esz))) && aligned(Q, 16) && aligned(K, 16) && aligned(Qo, 16) &&
-                      aligned(Ko, 16);
-  return dt == NF_F32 ? launch_rotate<float>(a, pieces, (hipStream_t)stream) : launch_rotate<bf16_t>(a, pieces, (hipStream_t)stream);
+  // rows, strides and pointers of whole pieces
+  const int P = kPieceFeatures;
+  auto whole = [&](const void* p, long stride_m, long stride_row) { return !p || (stride_m % P == 0 && stride_row % P == 0 && aligned(p, P * esz)); };
+  const bool pieces = d % P == 0 && rot % (2 * P) == 0 && whole(Q, q_stride_m, q_stride_row) && whole(K, k_stride_m, k_stride_row) && whole(Qo, qo_stride_m, qo_stride_row) &&
+                      whole(Ko, ko_stride_m, ko_stride_row);
+  hipStream_t s = (hipStream_t)stream;
+  if (dt == NF_F32) return pieces ? launch_rotate<float>(a, s) : launch_rotate_rows<float>(a, s);
+  return pieces ? launch_rotate<bf16_t>(a, s) : launch_rotate_rows<bf16_t>(a, s);
 }
 
 nf_status netfuse_cache_append_fp4(const void* K, const void* V, const int* index, const int* count, const int* len, const int* start, void* Kc,
