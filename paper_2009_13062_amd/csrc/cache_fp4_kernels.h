@@ -135,21 +135,19 @@ struct ReadFp4Args {
   int M, B, n, C, kv, d;
 };
 
-// A workgroup takes entries of one head; a lane gives eight features of an entry, of its key and of its value, kReadEntries entries at a time.  Bound by what it writes.  PAST: results that no
-// cache will hold go past them (us, through them / past them: 1.07 GB 243 / 231, 267 MB 66 / 54, 50 MB 14 / 25).
+// A workgroup takes entries of one head; a lane gives 16 bytes of an entry, of its key and of its value (two of codes for four features of float32, four for eight of bfloat16), kReadEntries entries at
+// a time.  Bound by what it writes.  PAST: results that no cache will hold go past them (us, through them / past them: 1.07 GB 243 / 231, 267 MB 66 / 54, 50 MB 14 / 25).
 constexpr int kReadEntries = 4;
 template <typename T, bool WIDE, bool PAST>
 __global__ __launch_bounds__(256) void cache_read_fp4_kernel(ReadFp4Args a, int blocks_per_head) {
-  const int S = fp4_scale_bytes(a.d), words = fp4_code_bytes(a.d) / 4, units = (a.d + 7) / 8, at_once = 256 / units;
+  constexpr int F = 16 / (int)sizeof(T);                   // features of a lane
+  using Codes = std::conditional_t<F == 8, uint32_t, uint16_t>;
+  const int S = fp4_scale_bytes(a.d), row = fp4_code_bytes(a.d) / (int)sizeof(Codes), units = (a.d + F - 1) / F, at_once = 256 / units;
   const unsigned uhead = blockIdx.x / blocks_per_head;
   const long head = uhead, mb = uhead / a.kv;
   const int r = (int)threadIdx.x / units, u = (int)threadIdx.x - r * units, i0 = (int)(blockIdx.x - uhead * blocks_per_head) * (kReadEntries * at_once) + r;
   if (r >= at_once) return;
   const int first = a.first ? a.first[mb] : 0, cnt = a.count ? clamp_len(a.count[mb], a.n) : a.n;
-  auto store16 = [](T* p, const uint4& v) {
-    if constexpr (PAST) __builtin_nontemporal_store(nf_u32x4_t{v.x, v.y, v.z, v.w}, (nf_u32x4_t*)p);
-    else *reinterpret_cast<uint4*>(p) = v;
-  };
   uint32_t code[2][kReadEntries], scale[2][kReadEntries];
 #pragma unroll
   for (int x = 0; x < kReadEntries; ++x) {
@@ -161,7 +159,7 @@ __global__ __launch_bounds__(256) void cache_read_fp4_kernel(ReadFp4Args a, int 
     for (int t = 0; t < 2; ++t) {
       code[t][x] = scale[t][x] = 0;
       if (t == 0 || a.V) {
-        const uint32_t c = ((const uint32_t*)(t ? a.Vc : a.Kc))[at * words + u], s = (t ? a.Vs : a.Ks)[at * S + u / 4];
+        const uint32_t c = ((const Codes*)(t ? a.Vc : a.Kc))[at * row + u], s = (t ? a.Vs : a.Ks)[at * S + u * F / kFp4Group];
         code[t][x] = there ? c : 0u;
         scale[t][x] = there ? s : 127u;
       }
@@ -171,26 +169,29 @@ __global__ __launch_bounds__(256) void cache_read_fp4_kernel(ReadFp4Args a, int 
   for (int x = 0; x < kReadEntries; ++x) {
     const int i = i0 + x * at_once;
     if (i >= a.n) break;
-    const long at = (head * a.n + i) * a.d + 8 * u;
+    const long at = (head * a.n + i) * a.d + F * u;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       if (t == 1 && !a.V) break;
       T* out = (T*)(t ? a.V : a.K) + at;
       const float s = fp4_scale_value(scale[t][x]);
-      if constexpr (sizeof(T) == 2 && WIDE) {
-        store16(out, fp4_values_bf16(code[t][x], s));
+      uint4 w;
+      if constexpr (F == 8) {
+        w = fp4_values_bf16(code[t][x], s);
       } else {
-        float v[8];
-        fp4_values_f32(code[t][x], s, v);
-        if constexpr (WIDE) {
+        const f32x2_t lo = fp4_pair_f32<0>(code[t][x], s), hi = fp4_pair_f32<1>(code[t][x], s);
+        w = make_uint4(__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x), __float_as_uint(hi.y));
+      }
+      if constexpr (WIDE && PAST) {
+        __builtin_nontemporal_store(nf_u32x4_t{w.x, w.y, w.z, w.w}, (nf_u32x4_t*)out);
+      } else if constexpr (WIDE) {
+        *reinterpret_cast<uint4*>(out) = w;
+      } else {
+        T v[F];
+        __builtin_memcpy(v, &w, 16);
 #pragma unroll
-          for (int h = 0; h < 8; h += 4)
-            if (8 * u + h < a.d) store16(out + h, make_uint4(__float_as_uint(v[h]), __float_as_uint(v[h + 1]), __float_as_uint(v[h + 2]), __float_as_uint(v[h + 3])));
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (8 * u + e < a.d) store_f32(out + e, v[e]);
-        }
+        for (int e = 0; e < F; ++e)
+          if (F * u + e < a.d) out[e] = v[e];
       }
     }
   }

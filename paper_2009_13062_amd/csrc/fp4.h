@@ -48,15 +48,10 @@ template <int SEL> __device__ __forceinline__ uint32_t fp4_pair_bf16(uint32_t co
   return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
 }
 template <int SEL> __device__ __forceinline__ f32x2_t fp4_pair_f32(uint32_t codes, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes, scale, SEL); }
-// A dword of codes to eight values: 16 bytes of bfloat16, 32 of float32
+// A dword of codes to eight values
 __device__ __forceinline__ uint4 fp4_values_bf16(uint32_t codes, float scale) {
   return make_uint4(fp4_pair_bf16<0>(codes, scale), fp4_pair_bf16<1>(codes, scale), fp4_pair_bf16<2>(codes, scale), fp4_pair_bf16<3>(codes, scale));
 }
-__device__ __forceinline__ void fp4_values_f32(uint32_t codes, float scale, float (&x)[8]) {
-  const f32x2_t a = fp4_pair_f32<0>(codes, scale), b = fp4_pair_f32<1>(codes, scale), c = fp4_pair_f32<2>(codes, scale), d = fp4_pair_f32<3>(codes, scale);
-  x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y; x[4] = c.x; x[5] = c.y; x[6] = d.x; x[7] = d.y;
-}
-
 // One element of a row, for the kernels that take any size
 __device__ __forceinline__ float fp4_value(const uint8_t* codes, const uint8_t* scales, int t) {
   const f32x2_t v = fp4_pair_f32<0>(codes[t / 2], fp4_scale_value(scales[t / kFp4Group]));

@@ -51,7 +51,8 @@ struct FromTop {
 
 constexpr int kLogprobList = 64;                           // candidates of a wavefront
 constexpr int kFewLanes = 16, kSlack = 8;                  // lanes that reach the border for which a higher one is not looked for; candidates past k that the list may keep
-constexpr int logprob_chunk(size_t bytes) { return bytes == 2 ? 4096 : 2048; }   // logits of a wavefront, by the size of one
+// Logits of a chunk, by their size and number: a short row of bfloat16 is shared out among twice the wavefronts (8 rows of 32000 11.8 us with chunks of 4096, 10.2 with 2048; 832 rows of 131071 58 and 62)
+__host__ __device__ constexpr int logprob_chunk(size_t bytes, int V) { return bytes == 2 && V > 65536 ? 4096 : 2048; }
 
 // The workspace: four numbers of each chunk -- its largest logit and the two sums at it (of 1 and of x - top, that in units of log2) -- then k pairs (order, token) of each wavefront, the
 // most likely first.
@@ -135,10 +136,10 @@ constexpr float kTanhNear = 0.35f, kTanhWide = 0.8f;
 // Four wavefronts per SIMD in float32, which is bound by the reads (143 us of the rows above, 5.7 TB/s; 5 of them 143, 6 160), five in bfloat16, which is bound by vector instructions: about
 // 8 for each logit, with a cap 12, and an exponential of a quarter of their rate (832 rows of 131072, 8 alternatives, us: 3 wavefronts 56, under a cap 69, 4 53 and 61, 5 52 and 61, 6 51 and 59;
 // rows of 131071, which begin at odd elements, 58 and 67 with 5).
-template <typename T, bool CAP>
+template <typename T, bool CAP, int kChunk>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_kernel(LogprobArgs a) {
   using L = Logits<T>;
-  constexpr int kChunk = logprob_chunk(sizeof(T)), P = L::kN, N = kChunk / kWave / P;
+  constexpr int P = L::kN, N = kChunk / kWave / P;
   __shared__ uint64_t lists[4][kLogprobList];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const unsigned wid = blockIdx.x * 4 + wave, row = wid / a.groups;              // fewer than 2^26 and 2^31
@@ -379,7 +380,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
 // A row's chunks: one wavefront.
 template <typename T>
 __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
-  constexpr int kChunk = logprob_chunk(sizeof(T));
+  const int kChunk = logprob_chunk(sizeof(T), a.V);
   __shared__ uint64_t list[kLogprobList];
   const int lane = threadIdx.x;
   const unsigned row = blockIdx.x, mb = row / a.T, m = mb / a.B;

@@ -68,7 +68,7 @@ nf_status launch_fp4_rows(const DecArgs& a, nf_dtype dt, hipStream_t s) {
   return launched();
 }
 
-int logprob_chunks(int V, nf_dtype dt) { return (int)(((long long)V + logprob_chunk(dt == NF_F32 ? 4 : 2) - 1) / logprob_chunk(dt == NF_F32 ? 4 : 2)); }
+int logprob_chunks(int V, int chunk) { return (int)(((long long)V + chunk - 1) / chunk); }
 
 }  // namespace
 
@@ -154,10 +154,10 @@ nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc,
   if (!aligned(Kc, 16) || !aligned(Ks, 16) || !aligned(Vc, 16) || !aligned(Vs, 16) || !aligned(K, esz) || !aligned(V, esz) || !aligned(first, 4) || !aligned(count, 4)) return NF_EINVAL;
   if (d > 256) return NF_EUNSUPPORTED;
   const ReadFp4Args a = {(const uint8_t*)Kc, (const uint8_t*)Ks, (const uint8_t*)Vc, (const uint8_t*)Vs, first, count, K, V, M, B, n, C, kv_heads, d};
-  const int rows = kReadEntries * (256 / ((d + 7) / 8)), per_head = (int)((n + (long long)rows - 1) / rows);
+  const int features = 16 / (int)esz, rows = kReadEntries * (256 / ((d + features - 1) / features)), per_head = (int)((n + (long long)rows - 1) / rows);
   const long long blocks = prod({M, B, kv_heads, per_head});
   if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
-  const bool wide = d * esz % 16 == 0 && aligned(K, 16) && aligned(V, 16);
+  const bool wide = d % features == 0 && aligned(K, 16) && aligned(V, 16);
   hipStream_t s = (hipStream_t)stream;
   const bool past = prod({M, B, kv_heads, n, d, (long long)esz, V ? 2 : 1}) > (128LL << 20);
 #define NF_READ(T, WIDE, PAST) nf_launch((cache_read_fp4_kernel<T, WIDE, PAST>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head)
@@ -216,7 +216,7 @@ nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V
 
 long long netfuse_token_logprobs_workspace(int M, int B, int T, int V, int k) {
   if (M <= 0 || B <= 0 || T <= 0 || V <= 0 || V > kMostEntries || k < 0 || k > kMostAlternatives) return -1;
-  const long long bytes = prod({M, B, T, logprob_chunks(V, NF_F32), 4LL * kChunkWords + 8LL * k});        // for a wavefront per chunk of either type
+  const long long bytes = prod({M, B, T, logprob_chunks(V, logprob_chunk(4, V)), 4LL * kChunkWords + 8LL * k});        // a wavefront per chunk, of either type's
   return bytes >= kMaxElems ? -1 : bytes;
 }
 
@@ -237,7 +237,7 @@ nf_status netfuse_token_logprobs(const void* logits, const int* token, const int
   const long long need = netfuse_token_logprobs_workspace(M, B, T, V, k);
   if (need < 0 || workspace_bytes < need) return NF_EINVAL;
   const long long rows = prod({M, B, T});
-  const int chunks = logprob_chunks(V, dt);
+  const int chunk = logprob_chunk(esz, V), chunks = logprob_chunks(V, chunk);
   // As many chunks to a wavefront as leave two wavefronts for each that the device holds: its alternatives then are few and soon have a high border (4084 rows of 50001 in float32, 20 alternatives,
   // chunks and join, us: a wavefront per chunk 174 + 13, 8 chunks 164 + 8, 16 168 + 8, 32 188 + 8).
   const int per_wave = (int)std::max<long long>(1, std::min<long long>(16, prod({rows, chunks}) / 8192)), groups = (chunks + per_wave - 1) / per_wave;
@@ -246,9 +246,10 @@ nf_status netfuse_token_logprobs(const void* logits, const int* token, const int
   const long long blocks = (prod({rows, groups}) + 3) / 4;
   if (!grid_fits(blocks, 256) || !grid_fits(rows, 64)) return NF_EUNSUPPORTED;          // before the first of the two is enqueued
   hipStream_t s = (hipStream_t)stream;
-#define NF_CHUNKS(T, CAP) nf_launch((logprob_chunks_kernel<T, CAP>), dim3((unsigned)blocks), dim3(256), 0, s, a)
-  if (dt == NF_F32) { if (cap != 0.f) NF_CHUNKS(float, true); else NF_CHUNKS(float, false); }
-  else { if (cap != 0.f) NF_CHUNKS(bf16_t, true); else NF_CHUNKS(bf16_t, false); }
+#define NF_CHUNKS(T, CHUNK)                                                                                                 \
+  if (cap != 0.f) nf_launch((logprob_chunks_kernel<T, true, CHUNK>), dim3((unsigned)blocks), dim3(256), 0, s, a);           \
+  else nf_launch((logprob_chunks_kernel<T, false, CHUNK>), dim3((unsigned)blocks), dim3(256), 0, s, a)
+  if (dt == NF_F32) { NF_CHUNKS(float, 2048); } else if (chunk == 2048) { NF_CHUNKS(bf16_t, 2048); } else { NF_CHUNKS(bf16_t, 4096); }
 #undef NF_CHUNKS
   const nf_status st = launched();
   if (st != NF_OK) return st;
