@@ -10,13 +10,13 @@
 namespace nf {
 namespace {
 
-template <typename T, int D, int RT, int KS, bool EXACT>
+template <typename T, int D, int RT, int KS, bool EXACT, bool FOLD>
 nf_status go_rows(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   constexpr int kRows = 4 / KS * RT * 16, kBytes = stream_lds_bytes(RT, KS, D / 16);
   const long long R = (long long)a.N * (a.heads / a.kv), row_blocks = (R + kRows - 1) / kRows;
   const long long total = prod({a.M, a.B, a.kv, row_blocks, splits});
   if (!grid_fits(total, 256)) return NF_EUNSUPPORTED;
-  const auto kernel = decoder_stream_kernel<T, D, RT, KS, true, true, EXACT>;
+  const auto kernel = decoder_stream_kernel<T, D, RT, KS, true, true, EXACT, FOLD>;
   static std::atomic<bool> opted_in{false};                // more than 64 KB of LDS: one opt-in per process (idempotent)
   if (kBytes > 64 * 1024 && !opted_in.load(std::memory_order_acquire)) {
     if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, kBytes) != hipSuccess) return NF_ELAUNCH;
@@ -26,9 +26,9 @@ nf_status go_rows(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH;
 }
 
-template <typename T, int D, int RT, int KS>
+template <typename T, int D, int RT, int KS, bool FOLD = false>
 nf_status go(const DecArgs& a, int splits, int chunk, hipStream_t s) {
-  return a.d == D ? go_rows<T, D, RT, KS, true>(a, splits, chunk, s) : go_rows<T, D, RT, KS, false>(a, splits, chunk, s);
+  return a.d == D ? go_rows<T, D, RT, KS, true, FOLD>(a, splits, chunk, s) : go_rows<T, D, RT, KS, false, FOLD>(a, splits, chunk, s);
 }
 
 template <typename T, int D>
@@ -36,6 +36,7 @@ nf_status tree(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   const int R = a.N * (a.heads / a.kv);
   // 32 rows per wavefront would open keys and values once for both halves, but hold few other registers (8 tokens of groups of 4 over 32 caches of 4096, 8 key heads of 128: 58 us,
   // 32 rows 61; float32 84 and 314).
+  if constexpr (D <= 128) if (R <= 4) return go<T, D, 1, 4, true>(a, splits, chunk, s);
   if (R <= 16) return go<T, D, 1, 4>(a, splits, chunk, s);
   if (R <= 32) return go<T, D, 1, 2>(a, splits, chunk, s);
   return go<T, D, 1, 1>(a, splits, chunk, s);

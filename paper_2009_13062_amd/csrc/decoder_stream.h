@@ -43,10 +43,10 @@ constexpr int stream_lds_bytes(int RT, int KS, int NB) { return KS > 1 ? (256 * 
 
 template <int W> struct Words { uint32_t w[W]; };
 
-// Eight float32 values in bfloat16 parts of 8 bits each, a pair to a dword: N = 2 of them, which hold 15 bits (the last part is rounded), or 3, which hold all.
-template <int N> __device__ __forceinline__ void to_parts(const float (&v)[8], uint32_t (&w)[N][4]) {
+// C float32 values in bfloat16 parts of 8 bits each, a pair to a dword: N = 2 of them, which hold 15 bits (the last part is rounded), or 3, which hold all.
+template <int N, int C> __device__ __forceinline__ void to_parts(const float (&v)[C], uint32_t (&w)[N][C / 2]) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
+  for (int e = 0; e < C / 2; ++e) {
     float x = v[2 * e], y = v[2 * e + 1];
 #pragma unroll
     for (int p = 0; p < N - 1; ++p) {
@@ -66,7 +66,7 @@ __device__ __forceinline__ void to_parts_any(const float (&v)[8], uint32_t (&w)[
     finite[e] = fabsf(v[e]) < INFINITY ? v[e] : 0.f;
     odd |= !(fabsf(v[e]) < INFINITY);
   }
-  to_parts<3>(finite, w);
+  to_parts<3, 8>(finite, w);
   if (odd) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
@@ -95,9 +95,11 @@ template <typename T, int D> struct Fp4Shape {
 };
 
 // FP4: the cache is one of 4 bits (TREE); EXACT: of D features, so that rows lie a known number of bytes apart and a step's loads differ in their immediate offsets.
-template <typename T, int D, int RT, int KS, bool TREE, bool FP4 = false, bool EXACT = false>
+// FOLD: with up to 4 rows 4 lanes share a row's scores of a step (FP4).
+template <typename T, int D, int RT, int KS, bool TREE, bool FP4 = false, bool EXACT = false, bool FOLD = false>
 __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void decoder_stream_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
   static_assert(TREE || !FP4, "prompts have no cache");
+  static_assert(!FOLD || (FP4 && RT == 1 && KS == 4 && D <= 128), "a block of keys for each of the lanes");
   using Sh = StreamShape<T, D>;
   using Q4 = Fp4Shape<T, D>;
   constexpr bool kBf = Sh::kBf;
@@ -308,7 +310,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
   uint4 qf[RT][SL];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const int r = r0 + (rg * RT + rt) * 16 + l16;
+    const int r = r0 + (rg * RT + rt) * 16 + (FOLD ? l16 % 4 : l16);
     const int i = min(r, R - 1) / group, h = g * group + (min(r, R - 1) - i * group);
     token[rt] = i;
     const T* q = (const T*)a.Q + m * a.q_stride_m + ((long)b * a.N + i) * a.q_stride_row + (long)h * a.d;
@@ -584,6 +586,7 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
         }
       }
     key_reg = key_first;
+    if (FOLD && l16 >= 4) lrun[0] = 0.f;                      // the tree's own sums, which all four lanes have, are the first one's
     while (st4 < cached_steps) {
       const int base = key_start + st4 * Q4::kStep, limit = key_end - base, key_now = key_reg;
       asm volatile("" : "+v"(fp4_lane));
@@ -608,52 +611,71 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
       const int next = st4 + KS;
       if (next < cached_steps) load_fp4_keys(next);
 
-      // element r of block k: key base + 16 k + 4 g4 + r of row l16.  Each question is asked once, not for each score.
+      // Element r of block k: key base + 16 k + 4 g4 + r of row l16.  Where 4 rows fill only a quarter of the columns, the other columns hold the same rows again, and lane 4 j + i takes block j of row i:
+      // what follows is then done for a quarter of the scores (one token, 8 key heads of 128, groups of 4, us: two caches of up to 100003 49.6 / 47.4, float32 71 / 64, 32 of 4096 under a cap 37.8 / 32).
+      constexpr int NT = FOLD ? 1 : NK4;                   // blocks of a lane
+      const int part = FOLD ? l16 / 4 : 0;
+      f32x4_t x[RT][NT];
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int k = 0; k < NT; ++k) {
+          if constexpr (FOLD) {
+#pragma unroll
+            for (int r = 0; r < 4; ++r) x[rt][k][r] = part & 2 ? (part & 1 ? s[rt][3][r] : s[rt][2][r]) : (part & 1 ? s[rt][1][r] : s[rt][0][r]);
+          } else {
+            x[rt][k] = s[rt][k];
+          }
+        }
+      const int first_key = 16 * NT * part + 4 * g4;       // of a lane
+      // each question is asked once, not for each score
       auto every = [&](auto&& f) __attribute__((always_inline)) {
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-          for (int k = 0; k < NK4; ++k)
+          for (int k = 0; k < NT; ++k)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) s[rt][k][r] = f(s[rt][k][r], rt, 16 * k + 4 * g4 + r);
+            for (int r = 0; r < 4; ++r) x[rt][k][r] = f(x[rt][k][r], rt, 16 * k + r);
       };
       if (capped_scores) {
-        if constexpr (kBf) every([&](float x, int, int) { return tanh_either(x * (a.scale * a.inv_cap)) * (a.cap * kLog2e); });
-        else every([&](float x, int, int) { return a.cap * tanhf(x * a.scale * a.inv_cap); });
+        if constexpr (kBf) every([&](float y, int, int) { return tanh_either(y * (a.scale * a.inv_cap)) * (a.cap * kLog2e); });
+        else every([&](float y, int, int) { return a.cap * tanhf(y * a.scale * a.inv_cap); });
       } else {
-        every([&](float x, int, int) { return x * sc; });
+        every([&](float y, int, int) { return y * sc; });
       }
       if (biased) {
         float away[RT];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) away[rt] = (float)(mine[rt] - base - 4 * g4);
-        if (a.pos) every([&](float x, int rt, int key) { return fmaf(-slope[rt], fabsf((float)(mine[rt] - __shfl(key_now, key, kWave))), x); });
-        else every([&](float x, int rt, int key) { return fmaf(-slope[rt], fabsf(away[rt] - (float)(key - 4 * g4)), x); });
+        for (int rt = 0; rt < RT; ++rt) away[rt] = (float)(mine[rt] - base - first_key);
+        if (a.pos) every([&](float y, int rt, int key) { return fmaf(-slope[rt], fabsf((float)(mine[rt] - __shfl(key_now, first_key + key, kWave))), y); });
+        else every([&](float y, int rt, int key) { return fmaf(-slope[rt], fabsf(away[rt] - (float)key), y); });
+      }
+      if (limit < Q4::kStep) {                             // every row sees every entry that is there
+        const int there_are = limit - first_key;
+        every([&](float y, int, int key) { return key < there_are ? y : -INFINITY; });
       }
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt) {
-        if (limit < Q4::kStep) {                           // every row sees every entry that is there
-#pragma unroll
-          for (int k = 0; k < NK4; ++k)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) s[rt][k][r] = 16 * k + 4 * g4 + r < limit ? s[rt][k][r] : -INFINITY;
-        }
         float top = -INFINITY;
 #pragma unroll
-        for (int k = 0; k < NK4; ++k)
+        for (int k = 0; k < NT; ++k)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) top = fmaxf(top, s[rt][k][r]);
+          for (int r = 0; r < 4; ++r) top = fmaxf(top, x[rt][k][r]);
         top = across_halves(across_rows(top, MaxOp{}), MaxOp{});
+        if constexpr (FOLD) {
+          top = fmaxf(top, dpp<kRowRor8>(top));
+          top = fmaxf(top, dpp<kRowRor4>(top));
+        }
         const float mnew = fmaxf(mrun[rt], top);
         const float corr = kBf ? __builtin_amdgcn_exp2f(mrun[rt] - mnew) : expf(mrun[rt] - mnew);
         mrun[rt] = mnew;
         float sum = 0.f;
 #pragma unroll
-        for (int k = 0; k < NK4; ++k)
+        for (int k = 0; k < NT; ++k)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            s[rt][k][r] = kBf ? __builtin_amdgcn_exp2f(s[rt][k][r] - mnew) : expf(s[rt][k][r] - mnew);
-            sum += s[rt][k][r];
+            x[rt][k][r] = kBf ? __builtin_amdgcn_exp2f(x[rt][k][r] - mnew) : expf(x[rt][k][r] - mnew);
+            sum += x[rt][k][r];
           }
         lrun[rt] = fmaf(lrun[rt], corr, sum);
         if (__any(corr != 1.0f)) {
@@ -664,19 +686,47 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
         }
       }
 
+      // weights of the lane's 8 keys of each pair of blocks, in parts of 8 bits (no cached value is infinite, so a part may be 0)
+      uint32_t weight[NK4 / 2][WP][RT][4];
+      if constexpr (FOLD) {
+        constexpr int kRowShl = 0x100;
+        float v[4];
+        uint32_t w[WP][2];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = x[0][0][e];
+        to_parts<WP, 4>(v, w);
+#pragma unroll
+        for (int p = 0; p < WP; ++p)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {                    // the first lanes collect the others'; the columns behind them are not looked at
+            weight[0][p][0][e] = w[p][e];
+            weight[0][p][0][2 + e] = (uint32_t)dpp<kRowShl + 4>((int)w[p][e]);
+            weight[1][p][0][e] = (uint32_t)dpp<kRowShl + 8>((int)w[p][e]);
+            weight[1][p][0][2 + e] = (uint32_t)dpp<kRowShl + 12>((int)w[p][e]);
+          }
+      } else {
+#pragma unroll
+        for (int k = 0; k < NT; k += 2)
+#pragma unroll
+          for (int rt = 0; rt < RT; ++rt) {
+            float v[8];
+            uint32_t w[WP][4];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = x[rt][k + e / 4][e % 4];
+            to_parts<WP, 8>(v, w);
+#pragma unroll
+            for (int p = 0; p < WP; ++p)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) weight[k / 2][p][rt][e] = w[p][e];
+          }
+      }
 #pragma unroll
       for (int k = 0; k < NK4; k += 2) {
-        bf16x8_t wp[WP][RT];                               // weights of the lane's 8 keys in parts of 8 bits
+        bf16x8_t wp[WP][RT];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-          float v[8];
-          uint32_t w[WP][4];
+        for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) v[e] = s[rt][k + e / 4][e % 4];
-          to_parts<WP>(v, w);                                 // no cached value is infinite, so a part may be 0
-#pragma unroll
-          for (int p = 0; p < WP; ++p) wp[p][rt] = __builtin_bit_cast(bf16x8_t, make_uint4(w[p][0], w[p][1], w[p][2], w[p][3]));
-        }
+          for (int p = 0; p < WP; ++p) wp[p][rt] = __builtin_bit_cast(bf16x8_t, make_uint4(weight[k / 2][p][rt][0], weight[k / 2][p][rt][1], weight[k / 2][p][rt][2], weight[k / 2][p][rt][3]));
         Words<VF / 2> vw[8][VC];
 #pragma unroll
         for (int e = 0; e < 8; ++e)
@@ -726,6 +776,10 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
   lds_f32_t* const sum_of = max_of + RT * 256;
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) lrun[rt] = across_halves(across_rows(lrun[rt], AddOp{}), AddOp{});
+  if constexpr (FOLD) {
+    lrun[0] += dpp<kRowRor8>(lrun[0]);
+    lrun[0] += dpp<kRowRor4>(lrun[0]);
+  }
   if constexpr (KS > 1) {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {

@@ -687,3 +687,15 @@ def test_given_streams(nf):
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("T,heads,kv,d", [(1, 4, 1, 64), (1, 3, 1, 128), (2, 2, 1, 96), (4, 2, 2, 64), (1, 5, 1, 128), (2, 4, 1, 32), (1, 1, 1, 128)])
+def test_tree_fp4_of_few_rows(nf, T, heads, kv, d, dtype):
+    """Up to four rows to a key head, whose scores several lanes share: every rest of a step, one step and several, caps, slopes and positions, the tree's own rows beside them."""
+    for n in (0, 1, 15, 16, 17, 63, 64, 65, 200, 255, 256, 257, 700, 1024, 1025, 1300):
+        case = (1, 1, T, n + 5, heads, kv, d, 12.0 if n % 2 else 0.0, n % 3 != 0, n % 4 == 1, False, T > 1 and n % 5 == 0, "tree" if T > 1 else "chain", [[n]])
+        rows, cache, L, kw = tree_case(nf, case, dtype, seed=n)
+        lse = torch.empty(1, T, heads, device="cuda")
+        O = nf.attention_tree_fp4(*rows, *cache, L, lse=lse, **kw)
+        check_tree(case, dtype, rows, cache, L, kw, O, lse)
