@@ -303,7 +303,8 @@ nf_status netfuse_rotate_heads(const void* Q, const void* K, const float* gamma_
  * A cache of 4 bits per element.  32 neighbouring features share a scale 2^e; an element is one of +-{0, 0.5, 1, 1.5, 2, 3, 4, 6} * 2^e, the code of the value's place in that
  * list and 8 for the sign.  With G = ceil(d / 32):
  *   Kc, Vc: bytes [M][B][kv_heads][C][16 G], feature 2 i in the lower half of byte i, features past d as 0.
- *   Ks, Vs: bytes [M][B][kv_heads][C][G, or G + 1 where G is odd], byte e + 127 of each group (the byte behind an odd number of them is 0).   All four 16-byte aligned.
+ *   Ks, Vs: bytes [M][B][kv_heads][C][G, or G + 1 where G is odd], byte e + 127 of each group (the byte behind an odd number of them is 0).
+ *   Codes are 16-byte aligned, scales to their rows of 2 (d up to 64) or 4 bytes (up to 128).
  * Appending takes the smallest e of -125 ... 125 with |x| <= 7 * 2^e in the whole group and rounds to the nearest code, halfway to the even one (magnitudes past 7 * 2^125 to
  * 6 * 2^125); a group that holds an infinity or NaN gets the byte 255 and reads as NaN.  Readers take any byte 0 ... 254 as 2^(byte - 127).
  * Rows of codes and rows of scales are rows like any others to netfuse_cache_evict (as bfloat16 of half as many elements: a head's codes, then, from the same
@@ -320,7 +321,8 @@ nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc,
                                  int M, int B, int n, int C, int kv_heads, int d, nf_dtype dt, void* stream);
 
 /*
- * netfuse_attention_tree over a cache of 4 bits; the new tokens' own K and V are of type dt.  Cached elements enter the products exactly.
+ * netfuse_attention_tree over a cache of 4 bits; the new tokens' own K and V are of type dt.  Cached elements enter the products exactly; float32 queries and attention weights meet
+ * them in three bfloat16 parts that hold all of their bits (fewer below 2^-102), bfloat16 ones as with caches of bfloat16.
  */
 long long netfuse_attention_tree_fp4_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt);
 nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V, const void* Kc, const void* Ks, const void* Vc, const void* Vs,

@@ -40,8 +40,8 @@ __device__ __forceinline__ float2 cos_sin_turns(double t) {
 
 __device__ __forceinline__ float2 rotate_angle(const RotateArgs& a, long mb, int s, int pair) {
   const int axis = (pair >= a.axis_end[0]) + (pair >= a.axis_end[1]) + (pair >= a.axis_end[2]);
-  const int p = a.pos ? a.pos[(mb * a.S + s) * a.axes + axis] : (a.start ? a.start[mb] : 0) + s;
-  return cos_sin_turns((double)p * (double)a.freq[pair] * 0.15915494309189535);
+  const double p = a.pos ? (double)a.pos[(mb * a.S + s) * a.axes + axis] : (double)(a.start ? a.start[mb] : 0) + s;
+  return cos_sin_turns(p * (double)a.freq[pair] * 0.15915494309189535);
 }
 
 // Sum over LPH neighbouring lanes, in all of them

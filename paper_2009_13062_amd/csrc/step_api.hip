@@ -68,6 +68,12 @@ nf_status launch_fp4_rows(const DecArgs& a, nf_dtype dt, hipStream_t s) {
   return launched();
 }
 
+// Codes come in rows of 16 bytes, scales in rows of 2, 4 or (over 128 features) single bytes.
+bool cache_fp4_aligned(const void* Kc, const void* Ks, const void* Vc, const void* Vs, int d) {
+  const size_t n = d <= 64 ? 2 : d <= 128 ? 4 : 1;
+  return aligned(Kc, 16) && aligned(Vc, 16) && aligned(Ks, n) && aligned(Vs, n);
+}
+
 int logprob_chunks(int V, int chunk) { return (int)(((long long)V + chunk - 1) / chunk); }
 
 }  // namespace
@@ -126,7 +132,7 @@ nf_status netfuse_cache_append_fp4(const void* K, const void* V, const int* inde
   if (prod({B, T}) > INT_MAX / 2 || prod({B, n}) > INT_MAX / 2 || prod({M, B, kv_heads, C, d}) >= kMaxElems) return NF_EINVAL;
   if (!rows_ok(M, (long long)B * T, (long long)kv_heads * d, kv_stride_m, kv_stride_row)) return NF_EINVAL;
   const size_t esz = dt == NF_F32 ? 4 : 2;
-  if (!aligned(K, esz) || !aligned(V, esz) || !aligned(Kc, 16) || !aligned(Ks, 16) || !aligned(Vc, 16) || !aligned(Vs, 16) || !aligned(index, 4) || !aligned(count, 4) ||
+  if (!aligned(K, esz) || !aligned(V, esz) || !cache_fp4_aligned(Kc, Ks, Vc, Vs, d) || !aligned(index, 4) || !aligned(count, 4) ||
       !aligned(len, 4) || !aligned(start, 4) || !aligned(pos, 4) || !aligned(weight, 4))
     return NF_EINVAL;
   if (d > 256) return NF_EUNSUPPORTED;
@@ -151,7 +157,7 @@ nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc,
   if (M <= 0 || B <= 0 || n <= 0 || C <= 0 || C > kMostEntries || n > kMostEntries || kv_heads <= 0 || d <= 0 || !is_dtype(dt)) return NF_EINVAL;
   if (prod({M, B, kv_heads, C, d}) >= kMaxElems || prod({M, B, kv_heads, n, d}) >= kMaxElems) return NF_EINVAL;
   const size_t esz = dt == NF_F32 ? 4 : 2;
-  if (!aligned(Kc, 16) || !aligned(Ks, 16) || !aligned(Vc, 16) || !aligned(Vs, 16) || !aligned(K, esz) || !aligned(V, esz) || !aligned(first, 4) || !aligned(count, 4)) return NF_EINVAL;
+  if (!cache_fp4_aligned(Kc, Ks, Vc, Vs, d) || !aligned(K, esz) || !aligned(V, esz) || !aligned(first, 4) || !aligned(count, 4)) return NF_EINVAL;
   if (d > 256) return NF_EUNSUPPORTED;
   const ReadFp4Args a = {(const uint8_t*)Kc, (const uint8_t*)Ks, (const uint8_t*)Vc, (const uint8_t*)Vs, first, count, K, V, M, B, n, C, kv_heads, d};
   const int features = 16 / (int)esz, rows = kReadEntries * (256 / ((d + features - 1) / features)), per_head = (int)((n + (long long)rows - 1) / rows);
@@ -189,7 +195,7 @@ nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V
       !rows_ok(M, (long long)B * T, (long long)kv_heads * d, kv_stride_m, kv_stride_row))
     return NF_EINVAL;
   const size_t esz = dt == NF_F32 ? 4 : 2;
-  if (!aligned(Q, esz) || !aligned(K, esz) || !aligned(V, esz) || !aligned(Kc, 16) || !aligned(Ks, 16) || !aligned(Vc, 16) || !aligned(Vs, 16) || !aligned(O, esz) ||
+  if (!aligned(Q, esz) || !aligned(K, esz) || !aligned(V, esz) || !cache_fp4_aligned(Kc, Ks, Vc, Vs, d) || !aligned(O, esz) ||
       !aligned(pos, 4) || !aligned(len, 4) || !aligned(start, 4) || !aligned(parent, 4) || !aligned(nodes, 4) || !aligned(slope, 4) || !aligned(lse, 4) || !aligned(workspace, 16))
     return NF_EINVAL;
   if (T > 64 || d > 256) return NF_EUNSUPPORTED;

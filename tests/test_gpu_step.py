@@ -114,6 +114,19 @@ def test_rotate_into_rows_of_a_larger_tensor(nf, case):
     assert bool((into[:, :, :2] == 7).all()) and bool((into[:, :, 2 + (heads + kv) * d:] == 7).all())
 
 
+def test_rotate_of_the_last_positions(nf):
+    """A start so far that its rows' positions leave 32 bits goes on counting."""
+    Q, freq = torch.randn(1, 4, 32, device="cuda"), torch.tensor([1.0] + [0.01] * 15, device="cuda")
+    start = 2 ** 31 - 2
+    q, _ = nf.rotate_heads(Q, None, 1, 4, 1, freq=freq, start=ints([[start]]))
+    where = (start + torch.arange(4)).double()
+    angle = where[:, None] * freq.cpu().double()
+    a, b = Q[0].cpu().double().chunk(2, 1)
+    want = torch.cat((a * angle.cos() - b * angle.sin(), a * angle.sin() + b * angle.cos()), 1)
+    room = (a.abs() + b.abs()) * (2.0 ** -21 + 2.0 ** -23 + 2.0 ** -51 * angle)
+    P.near(q[0], want, torch.cat((room, room), 1) + 2.0 ** -24 * want.abs())
+
+
 def test_rotate_keeps_rows_apart(nf):
     """Infinities and NaN in one head reach no other one; rows past the length are not read into anything."""
     case = (2, 2, 4, 4, 2, 64, 32, None, False, True, "start", True)
@@ -293,6 +306,11 @@ TREE = [
     (1, 1, 1, 64, 1, 1, 8, 0.0, False, False, False, False, "chain", [[0]]),         # the token alone
     (1, 1, 10, 300, 2, 2, 96, 0.0, False, False, False, False, "tree", [[257]]),
     (1, 1, 17, 1030, 8, 4, 40, 0.0, True, False, False, False, "tree", [[1030]]),
+    (1, 1, 1, 90, 2, 2, 36, 0.0, True, False, False, False, "chain", [[88]]),       # features that are no whole pieces of bfloat16
+    (1, 1, 6, 200, 4, 1, 132, 9.0, False, True, True, False, "tree", [[177]]),
+    (1, 1, 3, 150, 2, 1, 200, 0.0, True, True, False, False, "tree", [[149]]),      # seven groups
+    (1, 1, 30, 300, 4, 1, 168, 0.0, True, False, False, False, "tree", [[291]]),    # six groups, many rows
+    (1, 1, 35, 1100, 2, 1, 64, 0.0, False, True, True, False, "tree", [[1029]]),
 ]
 
 
@@ -358,6 +376,28 @@ def test_tree_fp4_general_kernel_agrees(nf, case, dtype):
     lse = torch.empty(M, B * T, heads, device="cuda")
     O = nf.attention_tree_fp4(*moved, *cache, L, lse=lse, **kw)
     check_tree(case, dtype, rows, cache, L, kw, O, lse)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("d", [64, 128, 80, 40, 200])
+def test_fp4_caches_of_single_models(nf, d, dtype):
+    """Slices of a merged cache of odd capacity: each model's is a cache as good as any, and the merged calls are the models' own."""
+    M, B, T, C, heads, kv = 3, 1, 2, 37, 4, 2
+    case = (M, B, T, C, heads, kv, d, 0.0, True, False, False, False, "chain", [[30], [5], [37]])
+    rows, cache, L, kw = tree_case(nf, case, dtype, packed=False)
+    O = nf.attention_tree_fp4(*rows, *cache, L, **kw)
+    k, v = nf.cache_read_fp4(*cache, d, dtype=dtype)
+    after = [t.clone() for t in cache]
+    nf.cache_append_fp4(rows[1], rows[2], *after, None, None, L)
+    for m in range(M):
+        one, held, l = [t[m:m + 1] for t in rows], [t[m:m + 1] for t in cache], L[m:m + 1].clone()
+        assert torch.equal(nf.attention_tree_fp4(*one, *held, l, slope=kw["slope"][m:m + 1].clone()), O[m:m + 1])
+        k1, v1 = nf.cache_read_fp4(*held, d, dtype=dtype)
+        assert torch.equal(k1, k[m:m + 1]) and torch.equal(v1, v[m:m + 1])
+    for m in range(M):
+        nf.cache_append_fp4(*[t[m:m + 1] for t in rows[1:]], *[t[m:m + 1] for t in cache], None, None, L[m:m + 1].clone())
+    for a, b in zip(cache, after):
+        assert torch.equal(a, b)
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])

@@ -53,7 +53,7 @@ def test_append_fp4_refuses(nf):
     call = caller(nf.lib.netfuse_cache_append_fp4, ok)
     for bad in [dict([(k, None)]) for k in ("K", "V", "length", "Kc", "Ks", "Vc", "Vs")] + [
             dict(M=0), dict(B=-1), dict(T=0), dict(n=0), dict(C=0), dict(C=2 ** 30 + 1), dict(kv=0), dict(d=0), dict(dt=-1), dict(index=None), dict(sr=100), dict(sm=100), dict(K=P + 1), dict(Kc=P + 8),
-            dict(Ks=P + 4), dict(Vc=P + 1), dict(Vs=P + 2), dict(pos=P + 2), dict(weight=P + 1), dict(B=2 ** 30, T=2 ** 30)]:
+            dict(Ks=P + 1), dict(Vc=P + 1), dict(Vs=P + 1), dict(pos=P + 2), dict(weight=P + 1), dict(B=2 ** 30, T=2 ** 30)]:
         assert call(**bad) == EINVAL, bad
     assert call(d=288, sr=2 * 288, sm=6 * 2 * 288) == EUNSUPPORTED
 
@@ -62,7 +62,7 @@ def test_read_fp4_refuses(nf):
     ok = dict(Kc=P, Ks=P, Vc=P, Vs=P, first=P, count=P, K=P, V=P, M=2, B=2, n=5, C=8, kv=2, d=64, dt=1)
     call = caller(nf.lib.netfuse_cache_read_fp4, ok)
     for bad in [dict([(k, None)]) for k in ("Kc", "Ks", "Vc", "Vs", "K", "V")] + [
-            dict(Vc=None, V=None), dict(Vc=None, Vs=None), dict(M=0), dict(B=0), dict(n=0), dict(n=2 ** 30 + 1), dict(C=0), dict(kv=0), dict(d=-1), dict(dt=9), dict(Kc=P + 4), dict(Vs=P + 8), dict(K=P + 1), dict(V=P + 1),
+            dict(Vc=None, V=None), dict(Vc=None, Vs=None), dict(M=0), dict(B=0), dict(n=0), dict(n=2 ** 30 + 1), dict(C=0), dict(kv=0), dict(d=-1), dict(dt=9), dict(Kc=P + 4), dict(Vs=P + 3), dict(d=128, Ks=P + 2), dict(K=P + 1), dict(V=P + 1),
             dict(first=P + 2), dict(count=P + 1), dict(M=2 ** 31 - 1, B=2 ** 31 - 1)]:
         assert call(**bad) == EINVAL, bad
     assert call(d=257) == EUNSUPPORTED
@@ -74,7 +74,7 @@ def test_tree_fp4_refuses(nf):
     call = caller(nf.lib.netfuse_attention_tree_fp4, ok)
     for bad in [dict([(k, None)]) for k in ("Q", "K", "V", "Kc", "Ks", "Vc", "Vs", "length", "O")] + [
             dict(M=0), dict(B=0), dict(T=0), dict(C=0), dict(C=2 ** 30 + 1), dict(heads=3), dict(kv=0), dict(d=0), dict(dt=4), dict(scale=float("inf")), dict(cap=-1.0), dict(cap=float("nan")), dict(qr=255),
-            dict(kr=100), dict(qm=7), dict(Kc=P + 2), dict(Ks=P + 8), dict(O=P + 1), dict(lse=P + 2), dict(ws=P + 4), dict(slope=P + 1)]:
+            dict(kr=100), dict(qm=7), dict(Kc=P + 2), dict(Ks=P + 3), dict(O=P + 1), dict(lse=P + 2), dict(ws=P + 4), dict(slope=P + 1)]:
         assert call(**bad) == EINVAL, bad
     assert call(T=65, qm=130 * 256, km=130 * 128) == EUNSUPPORTED and call(d=260, qr=1040, kr=520, qm=6 * 1040, km=6 * 520) == EUNSUPPORTED
     size = nf.lib.netfuse_attention_tree_fp4_workspace
