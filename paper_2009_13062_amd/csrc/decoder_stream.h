@@ -20,6 +20,11 @@
 // float32: scores in natural units, expf and tanhf, weights unrounded.  bfloat16: log2 units, weights in two bfloat16 parts that hold 15 bits, each a product of
 // its own (the loads hide it: two caches of up to 100003 entries 120.4 us with one part, 120.6 with two; 2 % at most, where caches are short).
 // Masks, chunks of a cache and workspace as in decoder_tiles.h.
+//
+// A cache of 4 bits (FP4) is streamed as it is held, a byte of scale with 16 of codes, and opened in registers: an element is exact in bfloat16, so float32 rows meet it in three
+// bfloat16 parts of theirs, which is exact too.  What the bytes gain goes into opening them: of some 330 vector instructions of a step of 64 keys two thirds are conversions and the
+// permutes that turn values into operands (one token over two caches of up to 100003 entries, 8 key heads of 128: 41 us and 5 to join, where the same cache in bfloat16 takes 114 and 6; 167 MB at
+// 3.6 TB/s, vector units busy 49 %, matrix units 19 %, 39 % of the wavefronts' time waits, 6 us of a workgroup's time before its first step and after its last).
 #pragma once
 #include "decoder.h"
 #include "decoder_tiles.h"

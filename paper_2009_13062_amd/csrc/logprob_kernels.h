@@ -6,19 +6,22 @@
 // the logits is that of the probabilities, and it is taken from the logits as they are stored: no two that differ become equal.
 //
 // A wavefront takes some chunks of a row, one after the other, each lane 16 bytes at a time of it, and keeps a chunk in registers.  Each chunk leaves sums of its own, whose join follows from V
-// alone, and alternatives are exact, so a row's bits depend neither on what is merged with it nor on how many chunks a wavefront takes.
+// alone, and alternatives are exact, so a row's bits depend neither on the other rows nor on how many chunks a wavefront takes.
+//
+// Bound by the reads in float32 (4084 rows of 50001, 20 alternatives: 147 us with the join's 7, 818 MB at 5.7 TB/s), by vector instructions in bfloat16 (832 rows of up to 131071 under a cap, 8
+// alternatives: 58 us with the join's 5, vector units busy 96 %), a few rows by two launches (8 of 32000: 10.2 us).
 #pragma once
 #include "decoder.h"
 #include "decoder_tiles.h"
 
 namespace nf {
+
 // 16 bytes of logits, from any element on; they are read once, and past the caches that is faster (4084 rows of 50001 in float32 164 -> 143 us).
 typedef uint32_t words_t __attribute__((ext_vector_type(4), aligned(2)));
 template <class T> __device__ __forceinline__ uint4 load_once(const T* p) {
   const words_t v = __builtin_nontemporal_load((const words_t*)p);
   return make_uint4(v.x, v.y, v.z, v.w);
 }
-
 
 constexpr int kMostAlternatives = 32;
 

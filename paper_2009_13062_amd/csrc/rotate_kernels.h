@@ -3,8 +3,8 @@
 //   y = x / sqrt(mean x^2 + eps) * gamma;   pair i of the first `rot` features: (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),  t = position * freq[i]
 //
 // pairs (i, i + rot / 2) or (2 i, 2 i + 1).  The angle is a product in 64 bits, taken in whole turns before it becomes a float32: an angle is
-// off by 2^-51 of itself, a far position's bits are not lost to a float32.  Bound by the rows' bytes (16 prompts of up to 2039 tokens, 32 heads over 8 of 128, normed, three axes: 103 us, 4.84 TB/s where a copy
-// reaches 4.94), a few tokens by latency (8 of them 5 us).
+// off by 2^-51 of itself, a far position's bits are not lost to a float32.  Bound by the rows' bytes (16 prompts of up to 2039 tokens, 32 heads over 8 of 128, normed, three axes: 104 us, 4.8 TB/s where a copy
+// reaches 4.94), a few tokens by latency (8 of them, 32 heads over 8 of 128, 5.4 us; 12 heads of 64 4.0).
 #pragma once
 #include "decoder.h"
 
