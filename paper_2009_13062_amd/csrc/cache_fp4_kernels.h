@@ -1,7 +1,7 @@
 // A cache held in 4 bits: rows quantised as they are appended, entries read back.
 //
-// Bound by bytes in large calls (32 prompts of up to 2039 rows, 8 heads of 128, bfloat16: 261 MB read and written in 55 us, 4.7 TB/s, and read back in 55; 16 caches of up to 16384 read
-// back: 0.2 GB read and 1.07 written, the 0 past the counts too, in 232 us, 5.6 TB/s), by the launch in small ones (3 us each).
+// Bound by bytes in large calls (32 prompts of up to 2039 rows, 8 heads of 128, bfloat16: 261 MB read and written, then read back, 465 MB in 96 us together; 16 caches of up to
+// 16384 read back: 0.2 GB read and 1.07 written, the 0 past the counts too, in 206 us, 6.2 TB/s), by the launch in small ones (3 us each).
 #pragma once
 #include "decoder.h"
 #include "fp4.h"
@@ -22,7 +22,8 @@ __device__ __forceinline__ uint32_t group_top(uint32_t top) {
 }
 
 // Eight features of a row from feature f on, those past d as 0, and their codes; the scale of the lane's group comes along (every lane of a quad has to come there).  WIDE: d, strides and
-// pointers in 16-byte pieces.
+// pointers in 16-byte pieces.  A piece of bfloat16 is read once, past the caches (append and read back of the prompts above 102 us, so 96); of float32 two lie in a line (97 us of the same
+// rows of 64 features, past the caches 107).
 template <typename T, bool WIDE> struct Eight {
   float x[8];
   __device__ __forceinline__ void load(const T* row, int f, int d) {
@@ -52,7 +53,7 @@ template <typename T, bool WIDE> struct Eight {
 template <> struct Eight<bf16_t, true> {
   uint4 w;
   __device__ __forceinline__ void load(const bf16_t* row, int f, int d) {
-    w = *reinterpret_cast<const uint4*>(row + (f < d ? f : 0));
+    w = ldnt16(row + (f < d ? f : 0));
     if (f >= d) w = make_uint4(0, 0, 0, 0);
   }
   __device__ __forceinline__ uint32_t codes(uint32_t& scale) const {
@@ -74,8 +75,7 @@ template <int G> __device__ __forceinline__ uint32_t gather_scales(uint32_t s) {
 }
 
 // A workgroup takes rows of one head of one sequence, so what it writes is one run of codes, of scales, of positions and of weights; a lane takes eight features of a key and its value, four
-// lanes a group, kAppendRows rows at a time.  G: the groups of a head where these are 2 or 4, 0 for others.
-constexpr int kAppendRows = 4;
+// lanes a group.  G: the groups of a head where these are 2 or 4, 0 for others.  (A lane that takes four rows, all their loads on their way at once, leaves fewer wavefronts: append and read back 109 us, so 102.)
 template <typename T, bool WIDE, int G>
 __global__ __launch_bounds__(256) void cache_append_fp4_kernel(AppendFp4Args a, int blocks_per_head) {
   const int groups = G ? G : fp4_groups(a.d), S = G ? G : fp4_scale_bytes(a.d), units = 4 * groups, at_once = 256 / units;
@@ -84,51 +84,38 @@ __global__ __launch_bounds__(256) void cache_append_fp4_kernel(AppendFp4Args a, 
   const long mb = umb, m = umb / a.B, head = uhead;
   const int cnt = a.count ? clamp_len(a.count[mb], a.n) : a.n, L = clamp_len(a.len[mb], a.C);
   const int end = min(cnt, a.C - L);                       // entries past the capacity are not written
-  const int r = (int)threadIdx.x / units, u = (int)threadIdx.x - r * units, i0 = (int)(blockIdx.x - uhead * blocks_per_head) * (kAppendRows * at_once) + r;
-  if (r >= at_once) return;
-  int row[kAppendRows];
-#pragma unroll
-  for (int x = 0; x < kAppendRows; ++x) {
-    const int i = i0 + x * at_once;
-    row[x] = i >= end ? -1 : a.index ? a.index[mb * a.n + i] : i;
-    if (row[x] >= a.T) row[x] = -1;
-  }
-  const int first = a.start ? a.start[mb] : L;
-  const long from = m * a.stride_m + (long)b * a.T * a.stride_row + (long)g * a.d;
-  Eight<T, WIDE> k[kAppendRows], v[kAppendRows];
-#pragma unroll
-  for (int x = 0; x < kAppendRows; ++x) {                  // a row that is not there: the first one, not used
-    const long at = from + max(row[x], 0) * a.stride_row;
-    k[x].load((const T*)a.K + at, 8 * u, a.d);
-    v[x].load((const T*)a.V + at, 8 * u, a.d);
-  }
-#pragma unroll
-  for (int x = 0; x < kAppendRows; ++x) {
-    const long slot = head * a.C + L + i0 + x * at_once;
-    uint32_t ks, vs;
-    const uint32_t kc = k[x].codes(ks), vc = v[x].codes(vs);                     // by every lane of a quad
-    const uint32_t ksum = G ? gather_scales<G>(ks) : ks, vsum = G ? gather_scales<G>(vs) : vs;
-    if (row[x] < 0) continue;
-    ((uint32_t*)a.Kc)[slot * units + u] = kc;
-    ((uint32_t*)a.Vc)[slot * units + u] = vc;
-    if (G == 0 && u % 4 == 0) {
+  const int r = (int)threadIdx.x / units, u = (int)threadIdx.x - r * units, i = (int)(blockIdx.x - uhead * blocks_per_head) * at_once + r;
+  if (r >= at_once || i >= end) return;                    // whole groups of lanes
+  const int row = a.index ? a.index[mb * a.n + i] : i, first = a.start ? a.start[mb] : L;
+  if (row < 0 || row >= a.T) return;
+  const long at = m * a.stride_m + ((long)b * a.T + row) * a.stride_row + (long)g * a.d, slot = head * a.C + L + i;
+  Eight<T, WIDE> k, v;
+  k.load((const T*)a.K + at, 8 * u, a.d);
+  v.load((const T*)a.V + at, 8 * u, a.d);
+  uint32_t ks, vs;
+  const uint32_t kc = k.codes(ks), vc = v.codes(vs);
+  ((uint32_t*)a.Kc)[slot * units + u] = kc;
+  ((uint32_t*)a.Vc)[slot * units + u] = vc;
+  if constexpr (G == 4 || G == 2) {
+    using Scales = std::conditional_t<G == 4, uint32_t, uint16_t>;
+    const uint32_t ksum = gather_scales<G>(ks), vsum = gather_scales<G>(vs);
+    if (u == 0) {
+      ((Scales*)a.Ks)[slot] = (Scales)ksum;
+      ((Scales*)a.Vs)[slot] = (Scales)vsum;
+    }
+  } else {
+    if (u % 4 == 0) {
       a.Ks[slot * S + u / 4] = (uint8_t)ks;
       a.Vs[slot * S + u / 4] = (uint8_t)vs;
     }
-    if (u == 0) {
-      if constexpr (G == 4) {
-        ((uint32_t*)a.Ks)[slot] = ksum;
-        ((uint32_t*)a.Vs)[slot] = vsum;
-      } else if constexpr (G == 2) {
-        ((uint16_t*)a.Ks)[slot] = (uint16_t)ksum;
-        ((uint16_t*)a.Vs)[slot] = (uint16_t)vsum;
-      } else if (S > groups) {
-        a.Ks[slot * S + groups] = 0;
-        a.Vs[slot * S + groups] = 0;
-      }
-      if (a.pos) a.pos[slot] = first + i0 + x * at_once;
-      if (a.weight) a.weight[slot] = 0.f;
+    if (u == 0 && S > groups) {
+      a.Ks[slot * S + groups] = 0;
+      a.Vs[slot * S + groups] = 0;
     }
+  }
+  if (u == 0) {
+    if (a.pos) a.pos[slot] = first + i;
+    if (a.weight) a.weight[slot] = 0.f;
   }
 }
 
@@ -138,9 +125,9 @@ struct ReadFp4Args {
   int M, B, n, C, kv, d;
 };
 
-// A workgroup takes entries of one head; a lane gives 16 bytes of an entry, of its key and of its value (two of codes for four features of float32, four for eight of bfloat16), kReadEntries entries at
-// a time.  Bound by what it writes.  PAST: results that no cache will hold go past them (us, through them / past them: 1.07 GB 243 / 231, 267 MB 66 / 54, 50 MB 14 / 25).
-constexpr int kReadEntries = 4;
+// A workgroup takes entries of one head; a lane gives 16 bytes of an entry, of its key and of its value (two of codes for four features of float32, four for eight of bfloat16).  (Four
+// entries to a lane: 231 us of the 16 caches above, so 206; keys and values in workgroups of their own 288.)  PAST: results that the second caches do not hold go past
+// them (us, through them / past them: 1.07 GB 215 / 206, 268 MB 59 / 49, 134 MB 32 / 26, 50 MB 11.2 / 9.9, 17 MB 5.8 / 5.0, which whoever reads them next would pay for).
 template <typename T, bool WIDE, bool PAST>
 __global__ __launch_bounds__(256) void cache_read_fp4_kernel(ReadFp4Args a, int blocks_per_head) {
   constexpr int F = 16 / (int)sizeof(T);                   // features of a lane
@@ -148,54 +135,42 @@ __global__ __launch_bounds__(256) void cache_read_fp4_kernel(ReadFp4Args a, int 
   const int S = fp4_scale_bytes(a.d), row = fp4_code_bytes(a.d) / (int)sizeof(Codes), units = (a.d + F - 1) / F, at_once = 256 / units;
   const unsigned uhead = blockIdx.x / blocks_per_head;
   const long head = uhead, mb = uhead / a.kv;
-  const int r = (int)threadIdx.x / units, u = (int)threadIdx.x - r * units, i0 = (int)(blockIdx.x - uhead * blocks_per_head) * (kReadEntries * at_once) + r;
-  if (r >= at_once) return;
+  const int r = (int)threadIdx.x / units, u = (int)threadIdx.x - r * units, i = (int)(blockIdx.x - uhead * blocks_per_head) * at_once + r;
+  if (r >= at_once || i >= a.n) return;
   const int first = a.first ? a.first[mb] : 0, cnt = a.count ? clamp_len(a.count[mb], a.n) : a.n;
-  uint32_t code[2][kReadEntries], scale[2][kReadEntries];
+  const long long slot = (long long)first + i;
+  const bool there = i < cnt && slot >= 0 && slot < a.C;
+  const long at = head * a.C + (there ? slot : 0), to = (head * a.n + i) * a.d + F * u;          // an entry that is not there: some entry's bytes, not used
+  uint32_t code[2] = {}, scale[2] = {};
 #pragma unroll
-  for (int x = 0; x < kReadEntries; ++x) {
-    const int i = i0 + x * at_once;
-    const long long slot = (long long)first + i;
-    const bool there = i < cnt && slot >= 0 && slot < a.C;
-    const long at = head * a.C + (there ? slot : 0);       // an entry that is not there: some entry's bytes, not used
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      code[t][x] = scale[t][x] = 0;
-      if (t == 0 || a.V) {
-        const uint32_t c = ((const Codes*)(t ? a.Vc : a.Kc))[at * row + u], s = (t ? a.Vs : a.Ks)[at * S + u * F / kFp4Group];
-        code[t][x] = there ? c : 0u;
-        scale[t][x] = there ? s : 127u;
-      }
+  for (int t = 0; t < 2; ++t)
+    if (t == 0 || a.V) {
+      code[t] = ((const Codes*)(t ? a.Vc : a.Kc))[at * row + u];
+      scale[t] = (t ? a.Vs : a.Ks)[at * S + u * F / kFp4Group];
     }
-  }
 #pragma unroll
-  for (int x = 0; x < kReadEntries; ++x) {
-    const int i = i0 + x * at_once;
-    if (i >= a.n) break;
-    const long at = (head * a.n + i) * a.d + F * u;
+  for (int t = 0; t < 2; ++t) {
+    if (t == 1 && !a.V) break;
+    T* out = (T*)(t ? a.V : a.K) + to;
+    const uint32_t c = there ? code[t] : 0u;
+    const float s = fp4_scale_value(there ? scale[t] : 127u);
+    uint4 w;
+    if constexpr (F == 8) {
+      w = fp4_values_bf16(c, s);
+    } else {
+      const f32x2_t lo = fp4_pair_f32<0>(c, s), hi = fp4_pair_f32<1>(c, s);
+      w = make_uint4(__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x), __float_as_uint(hi.y));
+    }
+    if constexpr (WIDE && PAST) {
+      __builtin_nontemporal_store(nf_u32x4_t{w.x, w.y, w.z, w.w}, (nf_u32x4_t*)out);
+    } else if constexpr (WIDE) {
+      *reinterpret_cast<uint4*>(out) = w;
+    } else {
+      T v[F];
+      __builtin_memcpy(v, &w, 16);
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      if (t == 1 && !a.V) break;
-      T* out = (T*)(t ? a.V : a.K) + at;
-      const float s = fp4_scale_value(scale[t][x]);
-      uint4 w;
-      if constexpr (F == 8) {
-        w = fp4_values_bf16(code[t][x], s);
-      } else {
-        const f32x2_t lo = fp4_pair_f32<0>(code[t][x], s), hi = fp4_pair_f32<1>(code[t][x], s);
-        w = make_uint4(__float_as_uint(lo.x), __float_as_uint(lo.y), __float_as_uint(hi.x), __float_as_uint(hi.y));
-      }
-      if constexpr (WIDE && PAST) {
-        __builtin_nontemporal_store(nf_u32x4_t{w.x, w.y, w.z, w.w}, (nf_u32x4_t*)out);
-      } else if constexpr (WIDE) {
-        *reinterpret_cast<uint4*>(out) = w;
-      } else {
-        T v[F];
-        __builtin_memcpy(v, &w, 16);
-#pragma unroll
-        for (int e = 0; e < F; ++e)
-          if (F * u + e < a.d) out[e] = v[e];
-      }
+      for (int e = 0; e < F; ++e)
+        if (F * u + e < a.d) out[e] = v[e];
     }
   }
 }

@@ -137,7 +137,7 @@ nf_status netfuse_cache_append_fp4(const void* K, const void* V, const int* inde
     return NF_EINVAL;
   if (d > 256) return NF_EUNSUPPORTED;
   const AppendFp4Args a = {K, V, index, count, len, start, (uint8_t*)Kc, (uint8_t*)Ks, (uint8_t*)Vc, (uint8_t*)Vs, pos, weight, M, B, T, n, C, kv_heads, d, kv_stride_m, kv_stride_row};
-  const int groups = fp4_groups(d), rows = kAppendRows * (256 / (4 * groups)), per_head = (int)((n + (long long)rows - 1) / rows);
+  const int groups = fp4_groups(d), rows = 256 / (4 * groups), per_head = (int)((n + (long long)rows - 1) / rows);
   const long long blocks = prod({M, B, kv_heads, per_head});
   if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
   const bool wide = d * esz % 16 == 0 && whole_pieces(kv_stride_m, kv_stride_row, esz) && aligned(K, 16) && aligned(V, 16);
@@ -160,12 +160,12 @@ nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc,
   if (!cache_fp4_aligned(Kc, Ks, Vc, Vs, d) || !aligned(K, esz) || !aligned(V, esz) || !aligned(first, 4) || !aligned(count, 4)) return NF_EINVAL;
   if (d > 256) return NF_EUNSUPPORTED;
   const ReadFp4Args a = {(const uint8_t*)Kc, (const uint8_t*)Ks, (const uint8_t*)Vc, (const uint8_t*)Vs, first, count, K, V, M, B, n, C, kv_heads, d};
-  const int features = 16 / (int)esz, rows = kReadEntries * (256 / ((d + features - 1) / features)), per_head = (int)((n + (long long)rows - 1) / rows);
+  const int features = 16 / (int)esz, rows = 256 / ((d + features - 1) / features), per_head = (int)((n + (long long)rows - 1) / rows);
   const long long blocks = prod({M, B, kv_heads, per_head});
   if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
   const bool wide = d % features == 0 && aligned(K, 16) && aligned(V, 16);
   hipStream_t s = (hipStream_t)stream;
-  const bool past = prod({M, B, kv_heads, n, d, (long long)esz, V ? 2 : 1}) > (128LL << 20);
+  const bool past = prod({M, B, kv_heads, n, d, (long long)esz, V ? 2 : 1}) > (32LL << 20);      // what the second caches hold together
 #define NF_READ(T, WIDE, PAST) nf_launch((cache_read_fp4_kernel<T, WIDE, PAST>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head)
   if (dt == NF_F32) { if (!wide) NF_READ(float, false, false); else if (past) NF_READ(float, true, true); else NF_READ(float, true, false); }
   else { if (!wide) NF_READ(bf16_t, false, false); else if (past) NF_READ(bf16_t, true, true); else NF_READ(bf16_t, true, false); }
