@@ -3,7 +3,7 @@
 //   y = x / sqrt(mean x^2 + eps) * gamma;   pair i of the first `rot` features: (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),  t = position * freq[i]
 //
 // pairs (i, i + rot / 2) or (2 i, 2 i + 1).  The angle is a product in 64 bits, taken in whole turns before it becomes a float32: an angle is
-// off by 2^-51 of itself, a far position's bits are not lost to a float32.  Bound by the rows' bytes (16 prompts of up to 2039 tokens, 32 heads over 8 of 128, normed, three axes: 104 us, 4.8 TB/s where a copy
+// off by 2^-51 of itself, a far position's bits are not lost to a float32.  Bound by the rows' bytes (16 prompts of up to 2039 tokens, 32 heads over 8 of 128, normed, three axes: 98 us, 5.1 TB/s where a copy
 // reaches 4.94), a few tokens by latency (8 of them, 32 heads over 8 of 128, 5.4 us; 12 heads of 64 4.0).
 #pragma once
 #include "decoder.h"
@@ -60,11 +60,13 @@ template <int LPH> __device__ __forceinline__ float lanes_sum(float v) {
 template <typename T> struct Piece;
 template <> struct Piece<float> {
   typedef uint4 words_t;
+  typedef nf_u32x4_t store_t;
   __device__ static __forceinline__ void open(const uint4& w, float* x) { x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y); x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w); }
   __device__ static __forceinline__ uint4 close(const float* x) { return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])); }
 };
 template <> struct Piece<bf16_t> {
   typedef uint2 words_t;
+  typedef uint32_t store_t __attribute__((ext_vector_type(2)));
   __device__ static __forceinline__ void open(const uint2& w, float* x) {
     x[0] = __uint_as_float(w.x << 16); x[1] = __uint_as_float(w.x & 0xffff0000u); x[2] = __uint_as_float(w.y << 16); x[3] = __uint_as_float(w.y & 0xffff0000u);
   }
@@ -74,7 +76,8 @@ constexpr int kPieceFeatures = 4;
 
 // A wavefront takes one token, or `per_wave` steps of it.  Its lanes work out the token's angles once, a pair each; then LPH lanes take a head, each the two pieces whose features turn with
 // each other (or, past `rot`, two neighbouring ones), so 64 / LPH heads are read and written at a time and a lane keeps its angles and weights over all of them.
-template <typename T, int LPH>
+// PAST: results that the second caches do not hold go past them (rows of the 16 prompts above 105 us, so 98; 32 of 512, 12 heads of 64, 22.5 and 19.9).
+template <typename T, int LPH, bool PAST>
 __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int parts, int per_wave) {
   using Pc = Piece<T>;
   typedef typename Pc::words_t words_t;
@@ -173,8 +176,12 @@ __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int pa
       }
       if (h < (key ? a.kv : a.heads)) {
         T* o = (key ? ko : qo) + (long)h * a.d;
-        if (f0 < a.d) *reinterpret_cast<words_t*>(o + f0) = Pc::close(x);
-        if (f1 < a.d) *reinterpret_cast<words_t*>(o + f1) = Pc::close(x + P);
+        auto put = [&](T* p, const float* v) __attribute__((always_inline)) {
+          if constexpr (PAST) __builtin_nontemporal_store(__builtin_bit_cast(typename Pc::store_t, Pc::close(v)), (typename Pc::store_t*)p);
+          else *reinterpret_cast<words_t*>(p) = Pc::close(v);
+        };
+        if (f0 < a.d) put(o + f0, x);
+        if (f1 < a.d) put(o + f1, x + P);
       }
     }
     if (step + kAhead < step1) load(step + kAhead);

@@ -20,6 +20,7 @@ using namespace nf;
 namespace {
 
 inline nf_status launched() { return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH; }
+constexpr long long kSecondCaches = 32LL << 20;            // bytes that they hold together
 inline bool whole_pieces(long stride_m, long stride_row, size_t esz) { return stride_m * (long)esz % 16 == 0 && stride_row * (long)esz % 16 == 0; }
 
 template <typename T>
@@ -42,7 +43,10 @@ nf_status launch_rotate(const RotateArgs& a, hipStream_t s) {
   const int most = (int)std::max<long long>(1, std::min<long long>(steps, 2048 / tokens)), per_wave = (steps + most - 1) / most, parts = (steps + per_wave - 1) / per_wave;
   const long long blocks = (prod({tokens, parts}) + 3) / 4;
   if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
-#define NF_ROTATE(LPH) nf_launch((rotate_pieces_kernel<T, LPH>), dim3((unsigned)blocks), dim3(256), 0, s, a, parts, per_wave)
+  const bool past = prod({tokens, a.heads + (long long)a.kv, a.d, (long long)sizeof(T)}) > kSecondCaches;
+#define NF_ROTATE(LPH)                                                                                                        \
+  if (past) nf_launch((rotate_pieces_kernel<T, LPH, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, parts, per_wave);     \
+  else nf_launch((rotate_pieces_kernel<T, LPH, false>), dim3((unsigned)blocks), dim3(256), 0, s, a, parts, per_wave)
   switch (lph) {
     case 1: NF_ROTATE(1); break;
     case 2: NF_ROTATE(2); break;
@@ -165,7 +169,7 @@ nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc,
   if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
   const bool wide = d % features == 0 && aligned(K, 16) && aligned(V, 16);
   hipStream_t s = (hipStream_t)stream;
-  const bool past = prod({M, B, kv_heads, n, d, (long long)esz, V ? 2 : 1}) > (32LL << 20);      // what the second caches hold together
+  const bool past = prod({M, B, kv_heads, n, d, (long long)esz, V ? 2 : 1}) > kSecondCaches;
 #define NF_READ(T, WIDE, PAST) nf_launch((cache_read_fp4_kernel<T, WIDE, PAST>), dim3((unsigned)blocks), dim3(256), 0, s, a, per_head)
   if (dt == NF_F32) { if (!wide) NF_READ(float, false, false); else if (past) NF_READ(float, true, true); else NF_READ(float, true, false); }
   else { if (!wide) NF_READ(bf16_t, false, false); else if (past) NF_READ(bf16_t, true, true); else NF_READ(bf16_t, true, false); }

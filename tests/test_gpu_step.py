@@ -127,6 +127,21 @@ def test_rotate_of_the_last_positions(nf):
     P.near(q[0], want, torch.cat((room, room), 1) + 2.0 ** -24 * want.abs())
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_rotate_of_large_results(nf, dtype):
+    """Rows of more than 32 MB, which are stored past the caches, are those that calls of fewer tokens give; in place and into tensors of their own."""
+    S, heads, kv, d, cut = 2100, 40, 24, 128, 1050
+    Q, K, _, _, _, _, kw = rotate_case((2, 1, S, heads, kv, d, d, None, False, True, "start", False), dtype)
+    Q, K = Q.contiguous(), K.contiguous()
+    q, k = nf.rotate_heads(Q, K, 1, S, heads, kv, **kw)
+    for at in (0, cut):
+        part = dict(kw, start=kw["start"] + at)
+        one = nf.rotate_heads(Q[:, at:at + cut], K[:, at:at + cut], 1, cut, heads, kv, **part)
+        assert torch.equal(one[0], q[:, at:at + cut]) and torch.equal(one[1], k[:, at:at + cut])
+    nf.rotate_heads(Q, K, 1, S, heads, kv, out_q=Q, out_k=K, **kw)
+    assert torch.equal(Q, q) and torch.equal(K, k)
+
+
 def test_rotate_keeps_rows_apart(nf):
     """Infinities and NaN in one head reach no other one; rows past the length are not read into anything."""
     case = (2, 2, 4, 4, 2, 64, 32, None, False, True, "start", True)
@@ -271,6 +286,20 @@ def test_read_fp4_of_any_bytes(nf, d, n, C, dtype):
             assert torch.equal(torch.isnan(got.cpu()), torch.isnan(want)) and torch.equal(got.cpu().nan_to_num(0.0), want.nan_to_num(0.0))
         only, none = nf.cache_read_fp4(cache[0], cache[1], None, None, d, n=n, first=first, count=count, dtype=dtype)
         assert none is None and torch.equal(only.view(I32 if dtype == F32 else torch.int16), k.view(I32 if dtype == F32 else torch.int16))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_read_fp4_of_large_results(nf, dtype):
+    """Entries of more than 32 MB, which are stored past the caches, are those that calls of fewer entries give."""
+    M, B, kv, C, d = 2, 2, 4, 2500, 128
+    g = gen(8)
+    cache = [torch.randint(0, 252, t.shape, generator=g, dtype=torch.int64).to(U8).cuda() for t in nf.cache_fp4(M, B, kv, C, d)]
+    count = ints([[2500, 7], [0, 1999]])
+    k, v = nf.cache_read_fp4(*cache, d, count=count, dtype=dtype)
+    for at in range(0, C, 500):
+        few = nf.cache_read_fp4(*cache, d, n=500, first=torch.full((M, B), at, dtype=I32, device="cuda"), count=(count - at).clamp(0, 500), dtype=dtype)
+        for got, want in zip(few, (k, v)):
+            assert torch.equal(got, want[:, :, :, at:at + 500])
 
 
 def test_fp4_rows_past_four_gigabytes(nf):
