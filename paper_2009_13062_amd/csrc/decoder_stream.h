@@ -112,7 +112,9 @@ __global__ __launch_bounds__(256, D > 128 ? 1 : RT == 1 && !FP4 ? 3 : 2) void de
   constexpr int kRows = RG * RT * 16;                      // per workgroup
   // A cache that one workgroup's rows are all of is read once: its values go past the caches (two of 100003 keys 131 -> 122 us; keys, whose 128-byte lines take
   // two loads, do not: one token over 8192 110 -> 119).
-  constexpr int kOnce = TREE && KS > 1 ? 2 : 0;
+  // Of a cache of 4 bits (through them / past them, us): bfloat16, 128 features, one token over the two caches 48.9 / 46.2, 32 of 4096 32.8 / 30.6, 256 features, 5 tokens over 8 of 4096 37.1 / 40.6;
+  // float32 the two caches 61.8 / 63.5, 8 of 1024 12.2 / 13.3, 5 tokens over 32 of 4096 79.8 / 81.4.
+  constexpr int kOnce = TREE && KS > 1 && !(FP4 && (!kBf || D > 128)) ? 2 : 0;
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int g4 = lane / 16, l16 = lane % 16, rg = wave % RG, share = wave / RG;
