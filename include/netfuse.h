@@ -306,7 +306,8 @@ nf_status netfuse_rotate_heads(const void* Q, const void* K, const float* gamma_
  *   Ks, Vs: bytes [M][B][kv_heads][C][G, or G + 1 where G is odd], byte e + 127 of each group (the byte behind an odd number of them is 0).
  *   Codes are 16-byte aligned, scales to their rows of 2 (d up to 64) or 4 bytes (up to 128).
  * Appending takes the smallest e of -125 ... 125 with |x| <= 7 * 2^e in the whole group and rounds to the nearest code, halfway to the even one (magnitudes past 7 * 2^125 to
- * 6 * 2^125); a group that holds an infinity or NaN gets the byte 255 and reads as NaN.  Readers take any byte 0 ... 254 as 2^(byte - 127).
+ * 6 * 2^125); a group that holds an infinity or NaN gets the byte 255 and reads as NaN.  Readers take any byte 0 ... 254 as 2^(byte - 127); under 253 and 254, which
+ * appending does not write, elements may leave float32 and read as infinite, as NaN to attention.
  * Rows of codes and rows of scales are rows like any others to netfuse_cache_evict (as bfloat16 of half as many elements: a head's codes, then, from the same
  * pos and weight into the same pos_out and weight_out, its scales), and netfuse_cache_weigh takes the keys that netfuse_cache_read_fp4 gives.
  *
