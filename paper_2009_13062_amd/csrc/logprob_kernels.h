@@ -52,7 +52,8 @@ struct FromTop {
   __device__ __forceinline__ float natural(float v, const LogprobArgs& a) const { return a.cap != 0.f ? (capped_logit(v, a) - most) * kLn2 : (v - top) * a.scale; }
 };
 
-constexpr int kLogprobList = 64;                           // candidates of a wavefront
+// Candidates of a wavefront: of 32 alternatives a list of 64 holds what two chunks of random logits bring less often than not
+constexpr int kLogprobList = 2 * kWave;
 constexpr int kFewLanes = 16, kSlack = 8;                  // lanes that reach the border for which a higher one is not looked for; candidates past k that the list may keep
 // Logits of a chunk, by their size and number: a short row of bfloat16 is shared out among twice the wavefronts (8 rows of 32000 11.8 us with chunks of 4096, 10.2 with 2048; 832 rows of 131071 58 and 62)
 __host__ __device__ constexpr int logprob_chunk(size_t bytes, int V) { return bytes == 2 && V > 65536 ? 4096 : 2048; }
@@ -63,15 +64,6 @@ constexpr int kChunkWords = 4;
 
 // An alternative as one number: the larger order wins, then the lower token.
 __device__ __forceinline__ uint64_t alternative(uint32_t order, int token) { return (uint64_t)order << 32 | (uint32_t)~token; }
-__device__ __forceinline__ uint64_t wave_best(uint64_t v) {
-#pragma unroll
-  for (int o = 1; o < kWave; o *= 2) {
-    const uint32_t x = __shfl_xor((uint32_t)v, o, kWave), y = __shfl_xor((uint32_t)(v >> 32), o, kWave);
-    const uint64_t w = (uint64_t)y << 32 | x;
-    v = w > v ? w : v;
-  }
-  return v;
-}
 
 // An order that at least k lanes' own best ones reach, and few others of a wavefront's do: the k-th largest of the 64, its upper BITS bits found one by one with ballots.
 template <int BITS> __device__ __forceinline__ uint32_t few_above(uint32_t best, int k) {
@@ -91,13 +83,24 @@ template <class What> __device__ __forceinline__ void list_if(bool in, uint64_t*
   if (in && at < kLogprobList) list[at] = what();
   count += __popcll(who);
 }
-// The list's place r for r < k: lane i ranks candidate i among all.  put(r, alternative), 0 where there are fewer.
+// The list's place r for r < k: lane i ranks candidates i and i + 64 among all.  put(r, alternative), 0 where there are fewer.
 template <class Put> __device__ __forceinline__ void rank_list(const uint64_t* list, int count, int k, Put&& put) {
   const int lane = threadIdx.x % kWave;
   __builtin_amdgcn_wave_barrier();
   const uint64_t mine = lane < count ? list[lane] : 0;
   int rank = 0;
-  for (int i = 0; i < count; ++i) rank += list[i] > mine;
+  if (count <= kWave) {                                    // uniform
+    for (int i = 0; i < count; ++i) rank += list[i] > mine;
+  } else {
+    const uint64_t more = lane + kWave < count ? list[lane + kWave] : 0;
+    int rank_more = 0;
+    for (int i = 0; i < count; ++i) {
+      const uint64_t x = list[i];
+      rank += x > mine;
+      rank_more += x > more;
+    }
+    if (lane + kWave < count && rank_more < k) put(rank_more, more);
+  }
   if (lane < count && rank < k) put(rank, mine);
   if (lane >= count && lane < k) put(lane, (uint64_t)0);
   __builtin_amdgcn_wave_barrier();
@@ -181,7 +184,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
   uint64_t* const list = lists[wave];
   int count = 0;                                           // candidates in the list
   uint32_t border = kLowestOrder;                          // the order that one of this wavefront's has to have
-  bool flooded = false;
   for (int chunk = group; chunk < chunks; chunk += a.groups) {
     const int base = chunk * kChunk, left = V - base;
     const T* const p = logits + base;
@@ -296,7 +298,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
 
     // ---- alternatives: what reaches the border joins the list, which is cut back to the best k when it has grown
     const uint64_t hot = __ballot(mine >= logit_of(border));
-    if (a.k == 0 || hot == 0 || flooded) continue;         // uniform
+    if (a.k == 0 || hot == 0) continue;                    // uniform
     uint32_t from = border;
     if (__popcll(hot) > kFewLanes) from = max(from, few_above<16>(logit_order(mine), a.k));
     const int before = count;
@@ -314,24 +316,37 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
           list_if(v >= least, list, count, [&] { return alternative(logit_order(v), base + (i * kWave + at_lane) * P + e); });
         }
       }
-      flooded = !all_of && count > kLogprobList;
-      if (flooded || count <= kLogprobList) break;
+      if (count <= kLogprobList || !all_of) break;
       // many alike: those above the k-th lane's best, then of its equals the first ones, k at most
       count = before;
       from = max(border, few_above<32>(logit_order(mine), a.k));
       all_of = false;
     }
-    if (flooded) continue;
-    if (!all_of) {
-      const float least = logit_of(from);
-      int need = a.k - (count - before);
-      if (count + max(need, 0) > kLogprobList) {
-        flooded = true;
-        continue;
-      }
+    const int need = all_of ? 0 : max(a.k - (count - before), 0);
+    if (count + need > kLogprobList) {
+      // Many of few lanes: one of each lane at a time, and the list is cut back before it is full (2000 rows of 50001 in float32, whose logits rise, 20 alternatives: 98 us where random ones take 86;
+      // the best one that is left, looked for in all of them, k times: 1470).
+      count = before;
 #pragma unroll 1
-      for (int i = 0; i < N && need > 0; ++i) {
+      for (int i = 0; i < N; ++i) {
         const uint4 v = piece(p, left, i);                 // again from memory: numbered registers would have to be there for it
+#pragma unroll
+        for (int e = 0; e < P; ++e) {
+          const float y = L::at(v, e);
+          list_if(y >= logit_of(from), list, count, [&] { return alternative(logit_order(y), base + (i * kWave + at_lane) * P + e); });
+          if (count > kLogprobList - kWave) {              // uniform
+            rank_list(list, count, a.k, [&](int r, uint64_t x) { list[r] = x; });
+            count = a.k;
+            from = (uint32_t)(list[a.k - 1] >> 32);        // of this chunk's equals an earlier one may still come
+          }
+        }
+      }
+    } else if (need > 0) {
+      const float least = logit_of(from);
+      int left_over = need;
+#pragma unroll 1
+      for (int i = 0; i < N && left_over > 0; ++i) {
+        const uint4 v = piece(p, left, i);
         int alike = 0;
 #pragma unroll
         for (int e = 0; e < P; ++e) alike += L::at(v, e) == least;
@@ -340,12 +355,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
 #pragma unroll
         for (int e = 0; e < P; ++e)
           if (L::at(v, e) == least) {
-            if (at < need) list[count + at] = alternative(from, base + (i * kWave + at_lane) * P + e);
+            if (at < left_over) list[count + at] = alternative(from, base + (i * kWave + at_lane) * P + e);
             ++at;
           }
-        const int found = min(__shfl(upto, kWave - 1, kWave), need);
+        const int found = min(__shfl(upto, kWave - 1, kWave), left_over);
         count += found;
-        need -= found;
+        left_over -= found;
       }
     }
     if (count >= a.k + kSlack && chunk + a.groups < chunks) {
@@ -357,27 +372,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
   if (a.k == 0) return;
   uint2* const out = reinterpret_cast<uint2*>(a.ws + (long)a.M * a.B * a.T * a.chunks * kChunkWords) + ((long)row * a.groups + group) * a.k;
   auto put = [&](int r, uint64_t x) { out[r] = make_uint2((uint32_t)(x >> 32), ~(uint32_t)x); };
-  if (!flooded) {
-    rank_list(list, count, a.k, put);
-    return;
-  }
-  // The best one that is left, k times: so many logits of few lanes that no border of lanes' best ones tells them apart.
-  uint64_t last = ~0ull;
-#pragma unroll 1
-  for (int r = 0; r < a.k; ++r) {
-    uint64_t best = 0;
-#pragma unroll 1
-    for (int chunk = group, i = 0; chunk < chunks; i = i + 1 < N ? i + 1 : 0, chunk += i == 0 ? a.groups : 0) {
-      const uint4 v = piece(logits + chunk * kChunk, V - chunk * kChunk, i);
-#pragma unroll
-      for (int e = 0; e < P; ++e) {
-        const uint64_t y = alternative(logit_order(L::at(v, e)), chunk * kChunk + (i * kWave + lane) * P + e);
-        best = y < last && y > best ? y : best;
-      }
-    }
-    last = wave_best(best);
-    if (lane == 0) put(r, last);
-  }
+  rank_list(list, count, a.k, put);
 }
 
 // A row's chunks: one wavefront.
@@ -423,9 +418,12 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
   }
   if (a.k == 0) return;
 
-  // The same choice among the wavefronts' alternatives.
+  // The same choice among the wavefronts' alternatives, everyone's first ones first.
   const int all = groups * a.k;
-  auto candidate = [&](int i) { return alternative(lists[i].x, (int)lists[i].y); };
+  auto candidate = [&](int j) {
+    const int place = (int)((unsigned)j / (unsigned)groups), i = (j - place * groups) * a.k + place;
+    return alternative(lists[i].x, (int)lists[i].y);
+  };
   auto put = [&](int r, uint64_t x) {
     const uint32_t order = (uint32_t)(x >> 32);
     a.top[(long)row * a.k + r] = order ? (int)~(uint32_t)x : -1;
@@ -436,26 +434,18 @@ __global__ __launch_bounds__(64) void logprob_join_kernel(LogprobArgs a) {
     const uint64_t x = candidate(i);
     mine = x > mine ? x : mine;
   }
-  const uint32_t border = few_above<16>((uint32_t)(mine >> 32), a.k);
+  uint32_t border = few_above<16>((uint32_t)(mine >> 32), a.k);
   int count = 0;
   for (int i0 = 0; i0 < all; i0 += kWave) {
     const uint64_t x = i0 + lane < all ? candidate(i0 + lane) : 0;
     list_if((uint32_t)(x >> 32) >= border, list, count, [&] { return x; });
-  }
-  if (count <= kLogprobList) {
-    rank_list(list, count, a.k, put);
-    return;
-  }
-  uint64_t last = ~0ull;
-  for (int r = 0; r < a.k; ++r) {
-    uint64_t best = 0;
-    for (int i = lane; i < all; i += kWave) {
-      const uint64_t x = candidate(i);
-      best = x < last && x > best ? x : best;
+    if (count > kLogprobList - kWave && i0 + kWave < all) {                      // uniform
+      rank_list(list, count, a.k, [&](int r, uint64_t y) { list[r] = y; });
+      count = a.k;
+      border = (uint32_t)(list[a.k - 1] >> 32);            // an equal one of a lower token may still come
     }
-    last = wave_best(best);
-    if (lane == 0) put(r, last);
   }
+  rank_list(list, count, a.k, put);
 }
 
 }  // namespace nf

@@ -574,6 +574,26 @@ def test_logprobs_of_floods(nf, dtype, rows):
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [1, 3000])
+def test_logprobs_of_lists_that_fill(nf, dtype, rows):
+    """The most alternatives that there are, of rows whose candidates fill a wavefront's list from chunk to chunk: random, rising and falling ones, steps of many equals, and those of a few lanes."""
+    V = 13000
+    j = torch.arange(V)
+    g = gen(5)
+    kinds = torch.stack([torch.randn(V, generator=g) * 3, j.float() / 256, -j.float() / 256, (j // 300).float(), -(j // 300).float(),
+                         torch.where(j % 512 // 8 < 3, 5.0 + torch.rand(V, generator=g), torch.rand(V, generator=g)),
+                         torch.where(j % 256 // 4 < 2, 5.0 + j / 4096, torch.rand(V, generator=g))])
+    n = kinds.shape[0]
+    x = kinds.to(dtype).cuda()[None].expand(rows, n, V).reshape(1, n * rows, V)
+    for k in (17, 32):
+        kw = dict(k=k, vocab=None, nodes=None, scale=1.0, cap=0.0)
+        got = nf.token_logprobs(x, **kw)
+        check_logprobs([None if t is None else t[:, :n] for t in got], x[:, :n], None, kw)
+        for t in got[1:]:
+            assert torch.equal(t.view(rows, -1), t.view(rows, -1)[:1].expand(rows, -1))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
 def test_logprobs_bits_do_not_depend_on_the_other_rows(nf, dtype):
     """Rows whose chunks are one wavefront's each give the bits that they give among thousands, several chunks to a wavefront."""
     V, g = 20011, gen(31)
