@@ -74,8 +74,8 @@ template <> struct Piece<bf16_t> {
 };
 constexpr int kPieceFeatures = 4;
 
-// A wavefront takes one token, or `per_wave` steps of it.  Its lanes work out the token's angles once, a pair each; then LPH lanes take a head, each the two pieces whose features turn with
-// each other (or, past `rot`, two neighbouring ones), so 64 / LPH heads are read and written at a time and a lane keeps its angles and weights over all of them.
+// A wavefront takes one token, or `per_wave` steps of it.  Its lanes work out the token's angles once, a pair each; then LPH lanes take a head, each two pieces, whose features turn with
+// each other or within each (or, past `rot`, not at all), so 64 / LPH heads are read and written at a time and a lane keeps its angles and weights over all of them.
 // PAST: results that the second caches do not hold go past them (rows of the 16 prompts above 105 us, so 98; 32 of 512, 12 heads of 64, 22.5 and 19.9).
 template <typename T, int LPH, bool PAST>
 __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int parts, int per_wave) {
@@ -95,8 +95,10 @@ __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int pa
   const int step0 = (int)(wid - token * parts) * per_wave, step1 = min(steps, step0 + per_wave);
   const int u = lane % LPH, sub = lane / LPH, pairs = a.rot / 2, turning = a.rot / (2 * P);
   const bool turns = u < turning;
-  const int f0 = turns ? (a.interleaved ? 2 * P * u : P * u) : a.rot + 2 * P * (u - turning);
-  const int f1 = turns && !a.interleaved ? pairs + P * u : f0 + P;
+  // pieces of the two halves, of what turns and of the rest: neighbouring lanes have neighbouring pieces, so each load and store covers whole lines (pairs of neighbours, their two pieces side by
+  // side, 123 us of the rows above, so 98)
+  const int rest = (a.d - a.rot) / P, half = (rest + 1) / 2, v = u - turning;
+  const int f0 = turns ? P * u : v < half ? a.rot + P * v : a.d, f1 = f0 + (turns ? pairs : P * half);
   const long row = (long)b * a.S + s;
   const T* const q = (const T*)a.Q + m * a.q_stride_m + row * a.q_stride_row;
   const T* const k = (const T*)a.K + m * a.k_stride_m + row * a.k_stride_row;
@@ -124,9 +126,11 @@ __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int pa
   float c[P], sn[P];
 #pragma unroll
   for (int e = 0; e < P; ++e) {
-    const float2 v = turns ? angle[wave][P * u + e] : make_float2(1.f, 0.f);
-    c[e] = v.x;
-    sn[e] = v.y;
+    // pairs of neighbours: two of each piece
+    const int pair = !a.interleaved ? P * u + e : e < P / 2 ? P / 2 * u + e : pairs / 2 + P / 2 * (u - 1) + e;
+    const float2 t = turns ? angle[wave][pair] : make_float2(1.f, 0.f);
+    c[e] = t.x;
+    sn[e] = t.y;
   }
   float g[2 * P];
   int gamma_of = -1;
