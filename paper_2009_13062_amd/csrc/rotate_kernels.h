@@ -3,7 +3,7 @@
 //   y = x / sqrt(mean x^2 + eps) * gamma;   pair i of the first `rot` features: (y_a, y_b) -> (y_a cos t - y_b sin t, y_a sin t + y_b cos t),  t = position * freq[i]
 //
 // pairs (i, i + rot / 2) or (2 i, 2 i + 1).  The angle is a product in 64 bits, taken in whole turns before it becomes a float32: an angle is
-// off by 2^-51 of itself, a far position's bits are not lost to a float32.  Bound by the rows' bytes (16 prompts of up to 2039 tokens, 32 heads over 8 of 128, normed, three axes: 98 us, 5.1 TB/s where a copy
+// off by 2^-51 of itself, a far position's bits are not lost to a float32.  Bound by the rows' bytes (16 prompts of up to 2039 tokens, 32 heads over 8 of 128, normed, three axes: 97 us, 5.1 TB/s where a copy
 // reaches 4.94), a few tokens by latency (8 of them, 32 heads over 8 of 128, 5.4 us; 12 heads of 64 4.0).
 #pragma once
 #include "decoder.h"
@@ -56,7 +56,7 @@ template <int LPH> __device__ __forceinline__ float lanes_sum(float v) {
 }
 
 // Four neighbouring features of a row in one load: 16 bytes of float32, 8 of bfloat16.  (Eight of bfloat16 hold twice the registers: 16 prompts of up to 2039 tokens, 32 heads over 8 of 128, 106 us
-// and 103; 32 of 512, 12 heads of 64, 26.5 and 22.6.  And 80 features of which 40 turn are no whole pieces of 16: one by one 525 us, so 81.)
+// and 103; 32 of 512, 12 heads of 64, 26.5 and 22.6, both with results in the caches.  And 80 features of which 40 turn are no whole pieces of 16: one by one 525 us, so 81.)
 template <typename T> struct Piece;
 template <> struct Piece<float> {
   typedef uint4 words_t;
