@@ -42,8 +42,8 @@ __device__ __forceinline__ float logit_of(uint32_t order) { return order == 0u ?
 
 constexpr uint32_t kLowestOrder = 0x00800000u;             // of the lowest finite number: what lies below is no candidate
 
-// x of a logit under a cap, in units of log2 (tanh within 2^-20)
-__device__ __forceinline__ float capped_logit(float v, const LogprobArgs& a) { return tanh_either(v * (a.scale * a.inv_cap)) * (a.cap * kLog2e); }
+// x of a logit under a cap, in units of log2 (tanh within 2^-20).  One factor after the other: scale / cap itself may be infinite, which would make a logit of 0 NaN, or 0.
+__device__ __forceinline__ float capped_logit(float v, const LogprobArgs& a) { return tanh_either(v * a.scale * a.inv_cap) * (a.cap * kLog2e); }
 // x - x(top), in units of log2.  Without a cap the difference comes first: the types' lowest values, which stand for masks, do not leave float32.
 struct FromTop {
   float top, most;

@@ -1,0 +1,39 @@
+"""Log probabilities under caps and scales of any size: quotients of them that are no float32 number."""
+import pytest
+import torch
+
+import step_plain as P
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(scope="module")
+def nf():
+    import paper_2009_13062_amd as nf
+    return nf
+
+
+def check(nf, x, scale, cap, k=4):
+    x = x.cuda()
+    token = torch.randint(0, x.shape[2], (*x.shape[:2], 3), generator=torch.Generator().manual_seed(1)).to(torch.int32).cuda()
+    want = P.logprobs(x, token, k, None, None, scale, cap)
+    logp, entropy, top, top_logp = nf.token_logprobs(x, token, k=k, scale=scale, cap=cap)
+    P.near(logp, want[0], want[1])
+    P.near(entropy, want[2], want[3])
+    assert torch.equal(top.cpu(), want[4])
+    P.near(top_logp, want[5], want[6])
+
+
+# scale / cap: infinite, largest, smallest, 0 in float32.  `size` is that of the logits, so that scale * logit is about 3 or the cap decides.
+RATIOS = [(1e20, 1e-20, 1.0), (1e10, 1e-30, 3.0), (1e30, 1e-30, 1e-30), (1e-20, 1e30, 3e20), (1e-30, 1e30, 3e30), (1e-8, 1e30, 3e8), (1e-30, 1e-30, 1.0)]
+
+
+@pytest.mark.parametrize("scale,cap,size", RATIOS, ids=str)
+@pytest.mark.parametrize("dtype", [BF, F32], ids=str)
+def test_scale_over_cap_of_any_size(nf, dtype, scale, cap, size):
+    """Every third logit is 0, and so is what it stands for."""
+    x = torch.randn(1, 3, 4500, generator=torch.Generator().manual_seed(2)) * size
+    x[:, :, ::3] = 0
+    x[0, 2] = 0
+    check(nf, x.to(dtype), scale, cap)
