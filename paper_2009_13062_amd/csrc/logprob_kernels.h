@@ -238,24 +238,26 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
     } else {
       const float u1 = a.scale * a.inv_cap, u2 = u1 * u1;
       reach = wave_max(reach) * u1;
-      const bool sane = u1 > 1e-4f && u1 < 1e4f;                     // powers of the factor that float32 holds
       const float most = from_top.most;
-      if (sane && reach <= kTanhNear) {
+      // Coefficients of the logit itself, whose powers of scale / cap are in them: they run evenly from c0, which is a normal number, to the last one, so that one says whether all of them are
+      auto held = [](float last) { return fabsf(last) >= 0x1p-126f && fabsf(last) < INFINITY; };
+      const float c0 = x1 * 0.9999999403953552f;
+      const float n1 = x1 * u2 * -0.33332422375679016f, n2 = x1 * u2 * u2 * 0.13295799493789673f, n3 = x1 * u2 * u2 * u2 * -0.04895823076367378f;
+      const float c1 = x1 * u2 * -0.3333267569541931f, c2 = x1 * u2 * u2 * 0.13321048021316528f, c3 = x1 * u2 * u2 * u2 * -0.05311431363224983f,
+                  c4 = x1 * u2 * u2 * u2 * u2 * 0.01909330114722252f, c5 = x1 * u2 * u2 * u2 * u2 * u2 * -0.004355299286544323f;
+      if (reach <= kTanhNear && held(n3)) {
         plain = true;
-        const float c0 = x1 * 0.9999999403953552f, c1 = x1 * u2 * -0.33332422375679016f, c2 = x1 * u2 * u2 * 0.13295799493789673f, c3 = x1 * u2 * u2 * u2 * -0.04895823076367378f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
 #pragma unroll
           for (int e = 0; e < P; ++e) {
             const float v = L::at(w[i], e), q = v * v;
-            add(fmaf(v, fmaf(fmaf(fmaf(c3, q, c2), q, c1), q, c0), -most));
+            add(fmaf(v, fmaf(fmaf(fmaf(n3, q, n2), q, n1), q, c0), -most));
           }
           added();
         }
-      } else if (sane && reach <= kTanhWide) {
+      } else if (reach <= kTanhWide && held(c5)) {
         plain = true;
-        const float c0 = x1 * 0.9999999403953552f, c1 = x1 * u2 * -0.3333267569541931f, c2 = x1 * u2 * u2 * 0.13321048021316528f, c3 = x1 * u2 * u2 * u2 * -0.05311431363224983f,
-                    c4 = x1 * u2 * u2 * u2 * u2 * 0.01909330114722252f, c5 = x1 * u2 * u2 * u2 * u2 * u2 * -0.004355299286544323f;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
 #pragma unroll

@@ -1,4 +1,4 @@
-"""Log probabilities under caps and scales of any size: quotients of them that are no float32 number."""
+"""Log probabilities under caps and scales of any size: quotients and powers of them that are no float32 number."""
 import pytest
 import torch
 
@@ -36,4 +36,18 @@ def test_scale_over_cap_of_any_size(nf, dtype, scale, cap, size):
     x = torch.randn(1, 3, 4500, generator=torch.Generator().manual_seed(2)) * size
     x[:, :, ::3] = 0
     x[0, 2] = 0
+    check(nf, x.to(dtype), scale, cap)
+
+
+# Powers of scale / cap times scale that float32 does not hold, too small (the first four) and too large ones.
+POWERS = [(1e-3, 9.9), (0.01, 90.0), (0.003, 28.0), (1e-4, 0.9), (100.0, 0.02), (9000.0, 1.0), (1e5, 30.0), (1e10, 1e7)]
+
+
+@pytest.mark.parametrize("reach", [0.3, 0.7])
+@pytest.mark.parametrize("scale,cap", POWERS, ids=str)
+@pytest.mark.parametrize("dtype", [BF, F32], ids=str)
+def test_powers_that_leave_float32(nf, dtype, scale, cap, reach):
+    """Logits up to `reach` caps, of either sign and all negative, in a row of a few whole chunks."""
+    x = (torch.rand(1, 2, 8192, generator=torch.Generator().manual_seed(3)) * 2 - 1) * (reach * cap / scale)
+    x[0, 1] = -x[0, 1].abs()
     check(nf, x.to(dtype), scale, cap)
