@@ -43,13 +43,19 @@ __device__ __forceinline__ float logit_of(uint32_t order) { return order == 0u ?
 constexpr uint32_t kLowestOrder = 0x00800000u;             // of the lowest finite number: what lies below is no candidate
 
 // x of a logit under a cap, in units of log2 (tanh within 2^-20).  One factor after the other: scale / cap itself may be infinite, which would make a logit of 0 NaN, or 0.
-__device__ __forceinline__ float capped_logit(float v, const LogprobArgs& a) { return tanh_either(v * a.scale * a.inv_cap) * (a.cap * kLog2e); }
-// x - x(top), in units of log2.  Without a cap the difference comes first: the types' lowest values, which stand for masks, do not leave float32.
+// The product is rounded, never one with the difference that it goes into: equal logits have equal x, and the largest's difference to itself is 0.
+__device__ __forceinline__ float capped_logit(float v, const LogprobArgs& a) {
+#pragma clang fp contract(off)
+  return tanh_either(v * a.scale * a.inv_cap) * (a.cap * kLog2e);
+}
+// x - x(top), in units of log2.  Without a cap the difference comes first: the types' lowest values, which stand for masks, do not leave float32.  With one it is never above 0, as
+// by tanh's error, which grows with the cap, it could be.
+__device__ __forceinline__ float below_top(float x) { return x > 0.f ? 0.f : x; }          // NaN stays
 struct FromTop {
   float top, most;
   __device__ __forceinline__ FromTop(float t, const LogprobArgs& a) : top(t), most(a.cap != 0.f ? capped_logit(t, a) : 0.f) {}
-  __device__ __forceinline__ float operator()(float v, const LogprobArgs& a) const { return a.cap != 0.f ? capped_logit(v, a) - most : (v - top) * (a.scale * kLog2e); }
-  __device__ __forceinline__ float natural(float v, const LogprobArgs& a) const { return a.cap != 0.f ? (capped_logit(v, a) - most) * kLn2 : (v - top) * a.scale; }
+  __device__ __forceinline__ float operator()(float v, const LogprobArgs& a) const { return a.cap != 0.f ? below_top(capped_logit(v, a) - most) : (v - top) * (a.scale * kLog2e); }
+  __device__ __forceinline__ float natural(float v, const LogprobArgs& a) const { return a.cap != 0.f ? below_top(capped_logit(v, a) - most) * kLn2 : (v - top) * a.scale; }
 };
 
 // Candidates of a wavefront: of 32 alternatives a list of 64 holds what two chunks of random logits bring less often than not
@@ -137,7 +143,7 @@ __device__ __forceinline__ float largest_size(float a, float b, float c) {
 }
 
 // tanh(u) / u on u^2: minimax fits of the relative error, 2^-23 in float32, up to kTanhNear and kTanhWide
-constexpr float kTanhNear = 0.35f, kTanhWide = 0.8f;
+constexpr float kTanhNear = 0.35f, kTanhWide = 0.8f, kCapPlain = 0x1p19f;
 
 // Four wavefronts per SIMD in float32, which is bound by the reads (143 us of the rows above, 5.7 TB/s; 5 of them 143, 6 160), five in bfloat16, which is bound by vector instructions: about
 // 8 for each logit, with a cap 12, and an exponential of a quarter of their rate (832 rows of 131072, 8 alternatives, us: 3 wavefronts 56, under a cap 69, 4 53 and 61, 5 52 and 61, 6 51 and 59;
@@ -214,7 +220,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
     }
     float top = wave_max(mine);
     as_they_came();
-    FromTop from_top(top, a);
     float sum = 0.f, first = 0.f;
     bool plain = !CAP;                                       // each x from one polynomial of its logit
     const float x1 = a.scale * kLog2e;
@@ -238,38 +243,35 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
     } else {
       const float u1 = a.scale * a.inv_cap, u2 = u1 * u1;
       reach = wave_max(reach) * u1;
-      const float most = from_top.most;
       // Coefficients of the logit itself, whose powers of scale / cap are in them: they run evenly from c0, which is a normal number, to the last one, so that one says whether all of them are
       auto held = [](float last) { return fabsf(last) >= 0x1p-126f && fabsf(last) < INFINITY; };
       const float c0 = x1 * 0.9999999403953552f;
       const float n1 = x1 * u2 * -0.33332422375679016f, n2 = x1 * u2 * u2 * 0.13295799493789673f, n3 = x1 * u2 * u2 * u2 * -0.04895823076367378f;
       const float c1 = x1 * u2 * -0.3333267569541931f, c2 = x1 * u2 * u2 * 0.13321048021316528f, c3 = x1 * u2 * u2 * u2 * -0.05311431363224983f,
                   c4 = x1 * u2 * u2 * u2 * u2 * 0.01909330114722252f, c5 = x1 * u2 * u2 * u2 * u2 * u2 * -0.004355299286544323f;
-      if (reach <= kTanhNear && held(n3)) {
+      // The largest logit's x from the same polynomial as the others': within 2^-23 of a cap up to kCapPlain no x lies far above it
+      auto all_by = [&](auto&& tanh_of) __attribute__((always_inline)) {
         plain = true;
+        const float most = top * tanh_of(top * top);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
 #pragma unroll
           for (int e = 0; e < P; ++e) {
-            const float v = L::at(w[i], e), q = v * v;
-            add(fmaf(v, fmaf(fmaf(fmaf(n3, q, n2), q, n1), q, c0), -most));
+            const float v = L::at(w[i], e);
+            add(fmaf(v, tanh_of(v * v), -most));
           }
           added();
         }
+      };
+      if (a.cap > kCapPlain) {
+      } else if (reach <= kTanhNear && held(n3)) {
+        all_by([&](float q) __attribute__((always_inline)) { return fmaf(fmaf(fmaf(n3, q, n2), q, n1), q, c0); });
       } else if (reach <= kTanhWide && held(c5)) {
-        plain = true;
-#pragma unroll
-        for (int i = 0; i < N; ++i) {
-#pragma unroll
-          for (int e = 0; e < P; ++e) {
-            const float v = L::at(w[i], e), q = v * v;
-            add(fmaf(v, fmaf(fmaf(fmaf(fmaf(fmaf(c5, q, c4), q, c3), q, c2), q, c1), q, c0), -most));
-          }
-          added();
-        }
+        all_by([&](float q) __attribute__((always_inline)) { return fmaf(fmaf(fmaf(fmaf(fmaf(c5, q, c4), q, c3), q, c2), q, c1), q, c0); });
       }
     }
-    if (!plain || __any(first != first)) {                   // logits of -infinity (0 times it), NaN, or under a cap large ones: with more care
+    const bool careful = !plain || __any(first != first);
+    if (careful) {                                           // logits of -infinity (0 times it), NaN, or under a cap large ones: with more care
       as_they_came();
       mine = -INFINITY;
 #pragma unroll
@@ -281,14 +283,14 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
         __builtin_amdgcn_sched_barrier(0);
       }
       top = wave_max(mine);
-      from_top = FromTop(top, a);
+      const FromTop from_top(top, a);
       sum = first = 0.f;
       as_they_came();
 #pragma unroll
       for (int i = 0; i < N; ++i)
 #pragma unroll
         for (int e = 0; e < P; ++e) {
-          const float y = L::at(w[i], e), x = CAP ? capped_logit(y, a) - from_top.most : (y - top) * x1, f = y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x);
+          const float y = L::at(w[i], e), x = CAP ? below_top(capped_logit(y, a) - from_top.most) : (y - top) * x1, f = y == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(x);
           sum += f;
           first += f != 0.f ? x * f : 0.f;
           if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);                     // more of them at a time would take registers from every chunk
@@ -296,6 +298,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
     }
     sum = wave_sum(sum);
     first = wave_sum(first);
+    if (CAP && !careful) sum = fmaxf(sum, 1.f);              // the largest logit's own term, up to a rounding
     if (lane == 0) *reinterpret_cast<float4*>(a.ws + ((long)row * a.chunks + chunk) * kChunkWords) = make_float4(top, sum, first, 0.f);
 
     // ---- alternatives: what reaches the border joins the list, which is cut back to the best k when it has grown

@@ -1,4 +1,4 @@
-"""Log probabilities under caps and scales of any size: quotients and powers of them that are no float32 number."""
+"""Log probabilities under caps and scales of any size: quotients and powers of them that are no float32 number, and caps so large that tanh's error is large."""
 import pytest
 import torch
 
@@ -51,3 +51,16 @@ def test_powers_that_leave_float32(nf, dtype, scale, cap, reach):
     x = (torch.rand(1, 2, 8192, generator=torch.Generator().manual_seed(3)) * 2 - 1) * (reach * cap / scale)
     x[0, 1] = -x[0, 1].abs()
     check(nf, x.to(dtype), scale, cap)
+
+
+@pytest.mark.parametrize("reach", [0.3, 0.7, 3.0])
+@pytest.mark.parametrize("cap", [1e6, 1e9, 1e30])
+@pytest.mark.parametrize("dtype", [BF, F32], ids=str)
+def test_caps_whose_error_is_large(nf, dtype, cap, reach):
+    """The largest logit has the largest x, whatever the errors of tanh are: half a million of units of a cap of 1e12, say.  No probability is above 1."""
+    x = (torch.rand(1, 40, 4500, generator=torch.Generator().manual_seed(4)) * 2 - 1) * reach
+    x[0, 20:, 1::2] = 0.2499                                          # on either side of where the form of tanh changes
+    x[0, 20:, 0] = torch.linspace(0.2501, 0.26, 20)
+    check(nf, x.to(dtype), min(cap, 1e30), cap)
+    logp = nf.token_logprobs(x.to(dtype).cuda(), k=8, scale=cap, cap=cap)[3]
+    assert (logp <= 0).all()
