@@ -361,10 +361,11 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
 #pragma unroll
     for (int r = 0; r < 16; ++r) o_acc[tb][r] = 0.f;
   const float sc = a.scale * kLog2e, slope_raw = slope / sc;
-  // series of the capped score: used within these bounds, not at all for caps and scales whose powers leave float32 (nor without a cap: 0)
+  // series of the capped score: used within these bounds, not at all for caps and scales whose powers leave float32 (nor without a cap: 0).  cap3 may be too large where scale / cap is not;
+  // too small it is with scores below 2e-9 alone, whose weights do not show it.
   const float to_u = uniform(a.scale * a.inv_cap), back = uniform(a.cap * kLog2e), u2 = to_u * to_u;
   const float cap1 = uniform(sc * u2 * -0.3333333333333333f), cap2 = uniform(sc * u2 * u2 * 0.13333333333333333f), cap3 = uniform(sc * u2 * u2 * u2 * -0.05396825396825397f);
-  const bool series = fabsf(to_u) > 1e-4f && fabsf(to_u) < 1e4f;
+  const bool series = fabsf(to_u) > 1e-4f && fabsf(to_u) < 1e4f && fabsf(cap3) < INFINITY;
   const float cap_short = uniform(series ? kTanhShort / fabsf(to_u) : 0.f), cap_small = uniform(series ? kTanhSeries / fabsf(to_u) : 0.f);
   const float w_short = uniform(cap_short * cap_short), cap23 = uniform(fmaf(w_short, cap3, cap2));
 
