@@ -1,4 +1,6 @@
 // Attention of drafted trees over a cache of 4 bits on the matrix pipe: instances and launches of decoder_stream.h and decoder_tiles.h.
+#include <limits.h>
+
 #include <atomic>
 
 #include "decoder_launch.h"
@@ -37,10 +39,11 @@ nf_status tree(const DecArgs& a, int splits, int chunk, hipStream_t s) {
   // 32 rows per wavefront would open keys and values once for both halves, but hold few other registers (8 tokens of groups of 4 over 32 caches of 4096, 8 key heads of 128: 58 us,
   // 32 rows 61; float32 84 and 314).
   // Up to 4 rows share their scores among four lanes (one token of groups of 4 over the two long caches 49 us, shared 46; of 8 rows among two the gain was 2 % at most).
+  constexpr int kMost = sizeof(T) == 4 ? INT_MAX : tree_fp4_streamed(D);                // rows that come here
   if constexpr (D <= 128) if (R <= 4) return go<T, D, 1, 4, true>(a, splits, chunk, s);
-  if (R <= 16) return go<T, D, 1, 4>(a, splits, chunk, s);
-  if (R <= 32) return go<T, D, 1, 2>(a, splits, chunk, s);
-  return go<T, D, 1, 1>(a, splits, chunk, s);
+  if constexpr (kMost > 32) if (R > 32) return go<T, D, 1, 1>(a, splits, chunk, s);
+  if constexpr (kMost > 16) if (R > 16) return go<T, D, 1, 2>(a, splits, chunk, s);
+  return go<T, D, 1, 4>(a, splits, chunk, s);
 }
 
 template <int D, int KS, int FORM>

@@ -16,6 +16,9 @@ inline int tree_features(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 // Of a cache of 4 bits, whose chunks are shorter in bytes (us, 512 / 1024 / 2048 keys, 8 key heads of 128, bfloat16: one token of groups of 4 over two caches of up to 100003 57 / 49 / 47,
 // 32 of 4096 37 / 32 / 31, one of 8192 11.5 / 14 / 22; 5 tokens over 16 of 4096 36 / 32 / 40; 26 over 32 of 4096 141 / 120 / 112; 9 over 16 of 4096 55 / 48 / 71)
 constexpr int kTreeFp4Chunk = 1024;
+// Rows of bfloat16 up to which it is streamed; more go through LDS, as with caches of bfloat16, but from 65 up where heads are large (36 rows of 256 features over 8 caches of 4096, us, registers /
+// LDS 64 / 79, 104 rows - / 88; of 128, 36 rows over 16 51 / 48, 32 over 32 84 / 115; of 64, 20 rows over 16 32.7 / 31.5).
+constexpr int tree_fp4_streamed(int d) { return d <= 64 ? 16 : d <= 128 ? 32 : 64; }
 nf_status launch_tree_fp4_tiles(const DecArgs& a, int chunk, int splits, hipStream_t s);        // bfloat16
 nf_status launch_tree_fp4_stream(const DecArgs& a, int chunk, int splits, nf_dtype dt, hipStream_t s);
 

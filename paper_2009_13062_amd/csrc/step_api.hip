@@ -215,9 +215,7 @@ nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V
   if (pieces_ok(a, dt)) {
     const int chunk = kTreeFp4Chunk, splits = (int)(((long long)C + chunk - 1) / chunk), rows = T * (heads / kv_heads);
     if (splits > 1 && !grid_fits(tree_join_blocks(a, splits), 256)) return NF_EUNSUPPORTED;      // before the first of the two is enqueued
-    // Rows that go through LDS: as with caches of bfloat16, but from 65 up where heads are large (36 rows of 256 features over 8 caches of 4096, us, registers / LDS 64 / 79, 104 rows - / 88; of
-    // 128, 36 rows over 16 51 / 48, 32 over 32 84 / 115; of 64, 20 rows over 16 32.7 / 31.5).
-    const bool tiles = dt == NF_BF16 && rows > (d <= 64 ? 16 : d <= 128 ? 32 : 64);
+    const bool tiles = dt == NF_BF16 && rows > tree_fp4_streamed(d);
     const nf_status st = tiles ? launch_tree_fp4_tiles(a, chunk, splits, (hipStream_t)stream) : launch_tree_fp4_stream(a, chunk, splits, dt, (hipStream_t)stream);
     return st != NF_OK || splits == 1 ? st : launch_tree_join(a, chunk, splits, dt, (hipStream_t)stream);
   }
