@@ -12,7 +12,7 @@ from typing import Optional, Tuple
 import torch
 
 import paper_2009_13062_amd as nf
-from .decoder import _dense, _head_size, _key_value_rows, _output, _own, _rows, _workspace
+from .decoder import _dense, _head_size, _key_value_rows, _output, _rows, _workspace
 
 
 def _rows_out(out: Optional[torch.Tensor], name, M, N, width, dtype, device, stream, whole):
