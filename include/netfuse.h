@@ -323,7 +323,8 @@ nf_status netfuse_cache_read_fp4(const void* Kc, const void* Ks, const void* Vc,
 
 /*
  * netfuse_attention_tree over a cache of 4 bits; the new tokens' own K and V are of type dt.  Cached elements enter the products exactly; float32 queries and attention weights meet
- * them in three bfloat16 parts that hold all of their bits (fewer below 2^-102), bfloat16 ones as with caches of bfloat16.
+ * them in three bfloat16 parts that hold all of their bits (fewer below 2^-102), bfloat16 ones as with caches of bfloat16 (weights
+ * rounded to bfloat16 from 17 rows to a key head on up to 64 features, 33 up to 128, 65 above).
  */
 long long netfuse_attention_tree_fp4_workspace(int M, int B, int T, int C, int heads, int kv_heads, int d, nf_dtype dt);
 nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V, const void* Kc, const void* Ks, const void* Vc, const void* Vs,
@@ -334,13 +335,15 @@ nf_status netfuse_attention_tree_fp4(const void* Q, const void* K, const void* V
 
 /*
  * Log probabilities of tokens.  Row (b, t) of model m has the logits ptr[m*stride_m + (b*T + t)*stride_row + j], j < V, of which the first vocab[m] are that model's tokens
- * (vocab: int[M] or NULL: all V); what lies behind them is not read.  With x_j = f(scale * logit_j), scale (one over a temperature) 1e-30 ... 1e30, f and cap as for scores:
+ * (vocab: int[M] or NULL: all V); what lies behind them is not read.  With x_j = f(scale * logit_j), scale 1e-30 ... 1e30, f and cap as for scores:
  *   logp[m][b*T + t][i] = x_j - log sum exp(x) for j = token[m][b*T + t][i], i < n (-infinity for a number that is not one of the row's tokens);   n = 0: token and logp NULL
  *   entropy[m][b*T + t] = - sum p_j log p_j
  *   top, top_logp [m][b*T + t][k]: the k <= 32 tokens of the largest logits, the lower one first among equals, and their log probabilities;   k = 0: both NULL
  * A logit of -infinity has probability 0 under a cap too and is no alternative; where a row has fewer than k alternatives the rest are -1 with -infinity.  A row without
  * any token (and the rows of nodes that are not there: nodes int[M][B] or NULL) has logp -infinity, entropy 0 and no alternatives.  NaN, and +infinity without a cap, make
  * every log probability that is not -infinity and the entropy of their row NaN; the order of the alternatives stands, without the NaN ones.
+ * Temperature: without a cap scale is one over it.  f takes scale * logit, so of a model that caps its logits first, c * tanh(logit / c), and divides by a temperature t afterwards the
+ * probabilities are those of scale 1 / t AND cap c / t; scale 1 / t under the cap c caps what was divided.   Under a cap x is within 2^-20 of itself.
  * Results are float.  NF_EUNSUPPORTED for k > 32.   workspace: as for netfuse_attention_tree, of netfuse_token_logprobs_workspace(...) bytes (never 0).
  */
 long long netfuse_token_logprobs_workspace(int M, int B, int T, int V, int k);

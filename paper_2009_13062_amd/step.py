@@ -189,6 +189,7 @@ def token_logprobs(logits, token=None, k=0, vocab=None, nodes=None, scale=1.0, c
     scale*logit): -> (logp[M, N, n], entropy[M, N], top[M, N, k], top_logp[M, N, k]); logp is None without token, the last two with k = 0.
 
     top: the k <= 32 tokens of the largest logits, the lower first among equals, -1 where there are no more.  vocab[m]: tokens that model m has (None: V).
+    A temperature t is scale 1/t; where the model caps its logits at c before they are divided by it, scale 1/t and cap c/t.
     nodes[M, B]: how many of the T rows of a sequence are there; the others are as rows without tokens.  out: the four results to write into.
     workspace: token_logprobs_workspace(...) bytes, a call's own if None."""
     if nf._native is not None and stream is None and type(logits) is nf._Tensor and logits.is_cuda:

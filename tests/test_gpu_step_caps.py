@@ -64,3 +64,20 @@ def test_caps_whose_error_is_large(nf, dtype, cap, reach):
     check(nf, x.to(dtype), min(cap, 1e30), cap)
     logp = nf.token_logprobs(x.to(dtype).cuda(), k=8, scale=cap, cap=cap)[3]
     assert (logp <= 0).all()
+
+
+@pytest.mark.parametrize("c,t", [(30.0, 0.7), (15.0, 2.5), (50.0, 1.0)])
+@pytest.mark.parametrize("dtype", [BF, F32], ids=str)
+def test_temperature_after_a_cap(nf, dtype, c, t):
+    """Logits capped by the model and divided by a temperature afterwards are scale 1 / t under the cap c / t; under the cap c they are another distribution."""
+    x = (torch.randn(1, 3, 5000, generator=torch.Generator().manual_seed(6)) * 8).to(dtype)
+    z = (c * torch.tanh(x.double() / c) / t)
+    want = torch.log_softmax(z, -1)
+    token = z.topk(5, -1).indices.to(torch.int32)
+    room = P.logprobs(x, token, 0, None, None, 1 / t, c / t)[1]      # the operator's own bound of its own definition
+    logp = nf.token_logprobs(x.cuda(), token.cuda(), scale=1 / t, cap=c / t)[0]
+    # 1 / t and c / t are rounded to float32: the quotient by 2^-23, the factor outside by 2^-24, of x and of the largest x
+    P.near(logp, want.gather(-1, token.long()), room + 2.0 ** -22 * 2 * z.abs().amax())
+    if t != 1:
+        other = nf.token_logprobs(x.cuda(), token.cuda(), scale=1 / t, cap=c)[0].cpu().double()
+        assert ((other - want.gather(-1, token.long())).abs() > 100 * room).any()
