@@ -142,8 +142,10 @@ __device__ __forceinline__ float largest_size(float a, float b, float c) {
   return r;
 }
 
-// tanh(u) / u on u^2: minimax fits of the relative error, 2^-23 in float32, up to kTanhNear and kTanhWide
+// tanh(u) / u on u^2: minimax fits of the relative error up to kTanhNear and kTanhWide (tanh_fit.py; 2^-24, with float32's roundings 2^-22); used for caps up to kCapPlain
 constexpr float kTanhNear = 0.35f, kTanhWide = 0.8f, kCapPlain = 0x1p19f;
+constexpr float kTanhNearFit[4] = {0.9999999403953552f, -0.33332422375679016f, 0.13295799493789673f, -0.04895823076367378f};
+constexpr float kTanhWideFit[6] = {0.9999999403953552f, -0.3333267569541931f, 0.13321048021316528f, -0.05311431363224983f, 0.01909330114722252f, -0.004355299286544323f};
 
 // Four wavefronts per SIMD in float32, which is bound by the reads (143 us of the rows above, 5.7 TB/s; 5 of them 143, 6 160), five in bfloat16, which is bound by vector instructions: about
 // 8 for each logit, with a cap 12, and an exponential of a quarter of their rate (832 rows of 131072, 8 alternatives, us: 3 wavefronts 56, under a cap 69, 4 53 and 61, 5 52 and 61, 6 51 and 59;
@@ -245,11 +247,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
       reach = wave_max(reach) * u1;
       // Coefficients of the logit itself, whose powers of scale / cap are in them: they run evenly from c0, which is a normal number, to the last one, so that one says whether all of them are
       auto held = [](float last) { return fabsf(last) >= 0x1p-126f && fabsf(last) < INFINITY; };
-      const float c0 = x1 * 0.9999999403953552f;
-      const float n1 = x1 * u2 * -0.33332422375679016f, n2 = x1 * u2 * u2 * 0.13295799493789673f, n3 = x1 * u2 * u2 * u2 * -0.04895823076367378f;
-      const float c1 = x1 * u2 * -0.3333267569541931f, c2 = x1 * u2 * u2 * 0.13321048021316528f, c3 = x1 * u2 * u2 * u2 * -0.05311431363224983f,
-                  c4 = x1 * u2 * u2 * u2 * u2 * 0.01909330114722252f, c5 = x1 * u2 * u2 * u2 * u2 * u2 * -0.004355299286544323f;
-      // The largest logit's x from the same polynomial as the others': within 2^-23 of a cap up to kCapPlain no x lies far above it
+      constexpr auto& kN = kTanhNearFit;
+      constexpr auto& kW = kTanhWideFit;
+      static_assert(kN[0] == kW[0], "one c0");
+      const float c0 = x1 * kN[0], n1 = x1 * u2 * kN[1], n2 = x1 * u2 * u2 * kN[2], n3 = x1 * u2 * u2 * u2 * kN[3];
+      const float c1 = x1 * u2 * kW[1], c2 = x1 * u2 * u2 * kW[2], c3 = x1 * u2 * u2 * u2 * kW[3], c4 = x1 * u2 * u2 * u2 * u2 * kW[4], c5 = x1 * u2 * u2 * u2 * u2 * u2 * kW[5];
+      // The largest logit's x from the same polynomial as the others': within 2^-22 of a cap up to kCapPlain no x lies far above it
       auto all_by = [&](auto&& tanh_of) __attribute__((always_inline)) {
         plain = true;
         const float most = top * tanh_of(top * top);
