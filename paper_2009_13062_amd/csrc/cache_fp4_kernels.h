@@ -128,6 +128,8 @@ struct ReadFp4Args {
 // A workgroup takes entries of one head; a lane gives 16 bytes of an entry, of its key and of its value (two of codes for four features of float32, four for eight of bfloat16).  (Four
 // entries to a lane: 231 us of the 16 caches above, so 206; keys and values in workgroups of their own 288.)  PAST: results that the second caches do not hold go past
 // them (us, through them / past them: 1.07 GB 215 / 206, 268 MB 59 / 49, 134 MB 32 / 26, 50 MB 11.2 / 9.9, 17 MB 5.8 / 5.0, which whoever reads them next would pay for).
+// Above 32 MB it depends on the reader (read back and read, us, through / past: one token over keys and values of bfloat16, 67 MB 39 / 40, 134 MB 54 / 57, 268 MB 105 / 99, 537 MB 207 / 202; keys
+// alone and their weighing, 67 MB 33 / 29, 100 MB 44 / 42, 134 MB 54 / 53).
 template <typename T, bool WIDE, bool PAST>
 __global__ __launch_bounds__(256) void cache_read_fp4_kernel(ReadFp4Args a, int blocks_per_head) {
   constexpr int F = 16 / (int)sizeof(T);                   // features of a lane

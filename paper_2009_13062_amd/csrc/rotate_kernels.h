@@ -76,7 +76,9 @@ constexpr int kPieceFeatures = 4;
 
 // A wavefront takes one token, or `per_wave` steps of it.  Its lanes work out the token's angles once, a pair each; then LPH lanes take a head, each two pieces, whose features turn with
 // each other or within each (or, past `rot`, not at all), so 64 / LPH heads are read and written at a time and a lane keeps its angles and weights over all of them.
-// PAST: results that the second caches do not hold go past them (rows of the 16 prompts above 105 us, so 98; 32 of 512, 12 heads of 64, 22.5 and 19.9).
+// PAST: results that the last cache does not hold go past them all (rows of the 16 prompts above 105 us, so 98).  Smaller ones would leave this call earlier too, but the attention that reads them next
+// pays for more than that (rotation alone, then with the attention, us, through the caches / past them: 16 prompts of 1024, 32 heads over 8 of 128, 168 MB, 72 / 53, 269 / 275; 8 of them 30 / 30,
+// 134 / 138; 64 of 512, 12 heads of 64, 101 MB, 40 / 38, 127 / 131; and above, 32 of 1024, 336 MB, 135 / 129, 530 / 532).
 template <typename T, int LPH, bool PAST>
 __global__ __launch_bounds__(256) void rotate_pieces_kernel(RotateArgs a, int parts, int per_wave) {
   using Pc = Piece<T>;

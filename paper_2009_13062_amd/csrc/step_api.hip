@@ -20,7 +20,7 @@ using namespace nf;
 namespace {
 
 inline nf_status launched() { return hipGetLastError() == hipSuccess ? NF_OK : NF_ELAUNCH; }
-constexpr long long kSecondCaches = 32LL << 20;            // bytes that they hold together
+constexpr long long kSecondCaches = 32LL << 20, kLastCache = 256LL << 20;                // bytes that the second ones hold together, and the last one
 inline bool whole_pieces(long stride_m, long stride_row, size_t esz) { return stride_m * (long)esz % 16 == 0 && stride_row * (long)esz % 16 == 0; }
 
 template <typename T>
@@ -43,7 +43,7 @@ nf_status launch_rotate(const RotateArgs& a, hipStream_t s) {
   const int most = (int)std::max<long long>(1, std::min<long long>(steps, 2048 / tokens)), per_wave = (steps + most - 1) / most, parts = (steps + per_wave - 1) / per_wave;
   const long long blocks = (prod({tokens, parts}) + 3) / 4;
   if (!grid_fits(blocks, 256)) return NF_EUNSUPPORTED;
-  const bool past = prod({tokens, a.heads + (long long)a.kv, a.d, (long long)sizeof(T)}) > kSecondCaches;
+  const bool past = prod({tokens, a.heads + (long long)a.kv, a.d, (long long)sizeof(T)}) > kLastCache;
 #define NF_ROTATE(LPH)                                                                                                        \
   if (past) nf_launch((rotate_pieces_kernel<T, LPH, true>), dim3((unsigned)blocks), dim3(256), 0, s, a, parts, per_wave);     \
   else nf_launch((rotate_pieces_kernel<T, LPH, false>), dim3((unsigned)blocks), dim3(256), 0, s, a, parts, per_wave)
