@@ -759,8 +759,11 @@ __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __
   if (TREE && a.lse && quad0 == 0 && half == 0) a.lse[(mb * a.N + token) * a.heads + h] = none ? -INFINITY : (mtot + __builtin_amdgcn_logf(ltot)) * kLn2;
 }
 
+// Of a cache of 4 bits and 64 features three workgroups to a compute unit leave 168 registers, where a thread holds codes and scales too: up to 64 rows, whose tiles are twice as long, 10 to 27 of them are
+// spilled, so there are two; above 64 rows 0 to 14, and three are faster (32 caches of 4096, 8 key heads, groups of 4, us, two / three: 13 tokens 52 / 55, biased 59 / 63, capped 57 / 61; 26 tokens 66 / 66,
+// 82 / 79, 82 / 78; 64 tokens 128 / 115, 158 / 140, 158 / 141).
 template <int D, int KS, bool TREE, int FORM, bool FP4 = false>
-__global__ __launch_bounds__(256, D == 64 ? (FP4 ? 2 : 3) : D == 128 ? 2 : 1) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
+__global__ __launch_bounds__(256, D == 64 ? (FP4 && KS == 2 ? 2 : 3) : D == 128 ? 2 : 1) void decoder_tiles_kernel(DecArgs a, int row_blocks, int splits, int chunk) {
   decoder_tiles<D, KS, TREE, FORM, FP4>(a, (const bf16_t*)a.Q, row_blocks, splits, chunk);
 }
 
