@@ -48,14 +48,15 @@ __device__ __forceinline__ float capped_logit(float v, const LogprobArgs& a) {
 #pragma clang fp contract(off)
   return tanh_either(v * a.scale * a.inv_cap) * (a.cap * kLog2e);
 }
-// x - x(top), in units of log2.  Without a cap the difference comes first: the types' lowest values, which stand for masks, do not leave float32.  With one it is never above 0, as
+// x - x(top), in units of log2 or natural ones.  Without a cap the difference comes first: the types' lowest values, which stand for masks, do not leave float32; natural ones, which are results, of the
+// halves: the same bits, and from the lowest to the largest value the difference is one too (as a power of 2 it is 0 in either form).  With one it is never above 0, as
 // by tanh's error, which grows with the cap, it could be.
 __device__ __forceinline__ float below_top(float x) { return x > 0.f ? 0.f : x; }          // NaN stays
 struct FromTop {
   float top, most;
   __device__ __forceinline__ FromTop(float t, const LogprobArgs& a) : top(t), most(a.cap != 0.f ? capped_logit(t, a) : 0.f) {}
   __device__ __forceinline__ float operator()(float v, const LogprobArgs& a) const { return a.cap != 0.f ? below_top(capped_logit(v, a) - most) : (v - top) * (a.scale * kLog2e); }
-  __device__ __forceinline__ float natural(float v, const LogprobArgs& a) const { return a.cap != 0.f ? below_top(capped_logit(v, a) - most) * kLn2 : (v - top) * a.scale; }
+  __device__ __forceinline__ float natural(float v, const LogprobArgs& a) const { return a.cap != 0.f ? below_top(capped_logit(v, a) - most) * kLn2 : (0.5f * v - 0.5f * top) * (2.f * a.scale); }
 };
 
 // Candidates of a wavefront: of 32 alternatives a list of 64 holds what two chunks of random logits bring less often than not

@@ -81,3 +81,18 @@ def test_temperature_after_a_cap(nf, dtype, c, t):
     if t != 1:
         other = nf.token_logprobs(x.cuda(), token.cuda(), scale=1 / t, cap=c)[0].cpu().double()
         assert ((other - want.gather(-1, token.long())).abs() > 100 * room).any()
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 0.25, 0.5])
+@pytest.mark.parametrize("dtype", [BF, F32], ids=str)
+def test_largest_and_lowest_logits_in_a_row(nf, dtype, scale):
+    """Their difference leaves float32, times the scale it does not."""
+    x = torch.randn(1, 3, 2600, generator=torch.Generator().manual_seed(7)).to(dtype)
+    x[0, :, 100], x[0, 0, 200:], x[0, 1, 2500] = torch.finfo(dtype).max, torch.finfo(dtype).min, torch.finfo(dtype).min
+    token = torch.tensor([100, 250, 2500, 7], dtype=torch.int32).expand(1, 3, 4).contiguous()
+    want = P.logprobs(x, token, 3, None, None, scale, 0.0)
+    logp, entropy, top, top_logp = nf.token_logprobs(x.cuda(), token.cuda(), k=3, scale=scale)
+    P.near(logp, want[0], want[1])
+    P.near(entropy, want[2], want[3])
+    assert torch.equal(top.cpu(), want[4])
+    P.near(top_logp, want[5], want[6])
