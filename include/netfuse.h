@@ -286,6 +286,7 @@ nf_status netfuse_cache_evict(void* Kc, void* Vc, const int* pos, const float* w
  * Queries and keys normed head by head and rotated by position, in one pass:  y = x / sqrt(mean(x^2) + eps) * gamma  over the d features of a head (gamma_q, gamma_k:
  * float[M][d]; NULL: y = x), then pair i of the first `rot` features turns by the angle position * freq[i]:
  *   (y_a, y_b) -> (y_a cos - y_b sin, y_a sin + y_b cos),   a, b = i, i + rot/2, or with interleaved != 0  2 i, 2 i + 1;   the other d - rot features stay y.
+ *   The mean is float32, as are its squares: a head with magnitudes above some 1e19 has an infinite one and becomes 0.
  *   rot: even, 0 ... d.   freq: float[rot/2] (NULL with rot = 0).   Angles are formed in 64 bits (off by 2^-51 of themselves), cosines and sines are within 2^-21.
  *   axes: 1 ... 4 positions per token (time, height, width).  sections: HOST array of `axes` numbers of pairs that add up to rot/2, the first pairs being axis 0's; NULL with one axis.
  *   pos: int[M][B][S][axes], or NULL with one axis: start[m][b] + s (start: int[M][B], or NULL: 0).   Any position of 32 bits.

@@ -13,8 +13,11 @@ namespace nf {
 inline int tree_chunk(int rows, nf_dtype dt) { return rows > (dt == NF_F32 ? 64 : 32) ? 1024 : 512; }
 inline int tree_features(int d) { return d <= 64 ? 64 : d <= 128 ? 128 : 256; }
 
-// Of a cache of 4 bits, whose chunks are shorter in bytes (us, 512 / 1024 / 2048 keys, 8 key heads of 128, bfloat16: one token of groups of 4 over two caches of up to 100003 57 / 49 / 47,
-// 32 of 4096 37 / 32 / 31, one of 8192 11.5 / 14 / 22; 5 tokens over 16 of 4096 36 / 32 / 40; 26 over 32 of 4096 141 / 120 / 112; 9 over 16 of 4096 55 / 48 / 71)
+// Of a cache of 4 bits, whose chunks are shorter in bytes: one length for any rows and either type, between what few caches and what many would have (8 key heads of 128, groups of 4, caches of 4096
+// unless said, us, 512 / 1024 / 2048 keys.  bfloat16, one token over 1 cache 11.6 / 13.6 / 18.2, over 32 40 / 34 / 30, over two of 100000 54 / 48 / 47; 5 tokens over 8 22.8 / 23.3 / 35, over 32
+// 66 / 58 / 55; 9 over 16 57 / 49 / 71; 26 over 1 28 / 42 / 71, over 8 39 / 46 / 74, over 32 132 / 108 / 103; 64 over 32 267 / 215 / 195.  float32, one token over 1 14 / 18 / 24, over 32
+// 53 / 43 / 40; 5 over 1 20 / 28 / 43, over 8 30 / 30 / 48, over 32 88 / 77 / 76; 26 over 1 30 / 45 / 76, over 8 87 / 79 / 87, over 32 301 / 268 / 250).  The caches that are merged may not choose
+// it, as a sequence's bits would follow from them.
 constexpr int kTreeFp4Chunk = 1024;
 // Rows of bfloat16 up to which it is streamed; more go through LDS, as with caches of bfloat16, but from 65 up where heads are large (36 rows of 256 features over 8 caches of 4096, us, registers /
 // LDS 64 / 79, 104 rows - / 88; of 128, 36 rows over 16 51 / 48, 32 over 32 84 / 115; of 64, 20 rows over 16 32.7 / 31.5).

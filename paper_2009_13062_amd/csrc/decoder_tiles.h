@@ -96,8 +96,9 @@ constexpr std::false_type kNoShift;
 
 // `Q` is a.Q once more: a pointer that is declared not to alias is what keeps the compiler from waiting for every load into LDS before a transposing read.
 // FP4: the cache is one of 4 bits (TREE): a thread loads a few neighbouring features of a key and of its value as they are held, and opens them into the stage, bfloat16 then,
-// before the product with the values of the tile before (after it: 120 us, where this takes 117: trees of 26 over 32 caches of 4096, 8 key heads of 128; vector units busy 49 %, matrix
-// units 25 %, a third of the wavefronts' time waits, as with the cache in bfloat16, whose bytes were not what bound them).
+// before the product with the values of the tile before (trees of 26 over 32 caches of 4096, 8 key heads, groups of 4, us, before it / after it: 128 features 106 / 107, capped 124 / 126, biased 114 / 112; 64
+// features, two workgroups to a compute unit, 66 / 67, 82 / 84, 82 / 81; 256 features over 16 171 / 172, 178 / 179, 170 / 169).  Of 128 features under a cap vector units are busy 49 %, matrix units 25 %,
+// a third of the wavefronts' time waits, as with the cache in bfloat16, whose bytes were not what bound them.
 template <int D, int KS, bool TREE, int FORM, bool FP4 = false>
 __device__ __forceinline__ void decoder_tiles(const DecArgs& a, const bf16_t* __restrict__ Q, int row_blocks, int splits, int chunk) {
   constexpr bool kRaw = FORM == kRawScore || FORM == kRawBiased, kBiased = FORM == kRawBiased || FORM == kAnyBiased;

@@ -9,7 +9,7 @@
 // alone, and alternatives are exact, so a row's bits depend neither on the other rows nor on how many chunks a wavefront takes.
 //
 // Bound by the reads in float32 (4084 rows of 50001, 20 alternatives: 147 us with the join's 7, 818 MB at 5.7 TB/s), by vector instructions in bfloat16 (832 rows of up to 131071 under a cap, 8
-// alternatives: 58 us with the join's 5, vector units busy 96 %), a few rows by two launches (8 of 32000: 10.2 us).
+// alternatives: 58 us with the join's 5, vector units full), a few rows by two launches (8 of 32000: 10.4 us).
 #pragma once
 #include "decoder.h"
 #include "decoder_tiles.h"
@@ -62,7 +62,9 @@ struct FromTop {
 // Candidates of a wavefront: of 32 alternatives a list of 64 holds what two chunks of random logits bring less often than not
 constexpr int kLogprobList = 2 * kWave;
 constexpr int kFewLanes = 16, kSlack = 8;                  // lanes that reach the border for which a higher one is not looked for; candidates past k that the list may keep
-// Logits of a chunk, by their size and number: a short row of bfloat16 is shared out among twice the wavefronts (8 rows of 32000 11.8 us with chunks of 4096, 10.2 with 2048; 832 rows of 131071 58 and 62)
+// Logits of a chunk, by their size and number, as a row's bits may follow from V but not from how many rows there are.  bfloat16, 8 alternatives, us with chunks of 4096 / 2048: 8 rows of 32000 (5
+// alternatives) 11.8 / 10.2; of 65537 8 rows 12.8 / 11.8, 128 16.7 / 15.5, 832 37 / 40; of 131071 8 rows 14.8 / 13.3, 32 15.1 / 14.2, 128 21.6 / 23.2, 832 60 / 64; of 131072 12.9 / 12.4, 12.8 / 13.1,
+// 16.6 / 20.1, 53 / 61; of 151936 13.5 / 13.6, 14.4 / 15.2, 19.8 / 23.2, 61 / 68: above 65536 many rows gain more than few ones lose.
 __host__ __device__ constexpr int logprob_chunk(size_t bytes, int V) { return bytes == 2 && V > 65536 ? 4096 : 2048; }
 
 // The workspace: four numbers of each chunk -- its largest logit and the two sums at it (of 1 and of x - top, that in units of log2) -- then k pairs (order, token) of each wavefront, the
@@ -148,9 +150,9 @@ constexpr float kTanhNear = 0.35f, kTanhWide = 0.8f, kCapPlain = 0x1p19f;
 constexpr float kTanhNearFit[4] = {0.9999999403953552f, -0.33332422375679016f, 0.13295799493789673f, -0.04895823076367378f};
 constexpr float kTanhWideFit[6] = {0.9999999403953552f, -0.3333267569541931f, 0.13321048021316528f, -0.05311431363224983f, 0.01909330114722252f, -0.004355299286544323f};
 
-// Four wavefronts per SIMD in float32, which is bound by the reads (143 us of the rows above, 5.7 TB/s; 5 of them 143, 6 160), five in bfloat16, which is bound by vector instructions: about
-// 8 for each logit, with a cap 12, and an exponential of a quarter of their rate (832 rows of 131072, 8 alternatives, us: 3 wavefronts 56, under a cap 69, 4 53 and 61, 5 52 and 61, 6 51 and 59;
-// rows of 131071, which begin at odd elements, 58 and 67 with 5).
+// Four wavefronts per SIMD in float32, which is bound by the reads (143 us of the rows above, 5.7 TB/s; 5 of them 143, 6 160), five in bfloat16, which is bound by vector instructions: for
+// each logit 9.6 counted, with a cap 15.4, 4.3 more for 8 alternatives and 7.8 for 20 (8.3, 14.2, 4.8 and 8.9 in float32), an exponential of a quarter of their rate among them
+// (832 rows of 131072, 8 alternatives, us: 3 wavefronts 56, under a cap 69, 4 53 and 61, 5 52 and 61, 6 51 and 59; rows of 131071, which begin at odd elements, 58 and 67 with 5).
 template <typename T, bool CAP, int kChunk>
 __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_kernel(LogprobArgs a) {
   using L = Logits<T>;
@@ -246,13 +248,6 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
     } else {
       const float u1 = a.scale * a.inv_cap, u2 = u1 * u1;
       reach = wave_max(reach) * u1;
-      // Coefficients of the logit itself, whose powers of scale / cap are in them: they run evenly from c0, which is a normal number, to the last one, so that one says whether all of them are
-      auto held = [](float last) { return fabsf(last) >= 0x1p-126f && fabsf(last) < INFINITY; };
-      constexpr auto& kN = kTanhNearFit;
-      constexpr auto& kW = kTanhWideFit;
-      static_assert(kN[0] == kW[0], "one c0");
-      const float c0 = x1 * kN[0], n1 = x1 * u2 * kN[1], n2 = x1 * u2 * u2 * kN[2], n3 = x1 * u2 * u2 * u2 * kN[3];
-      const float c1 = x1 * u2 * kW[1], c2 = x1 * u2 * u2 * kW[2], c3 = x1 * u2 * u2 * u2 * kW[3], c4 = x1 * u2 * u2 * u2 * u2 * kW[4], c5 = x1 * u2 * u2 * u2 * u2 * u2 * kW[5];
       // The largest logit's x from the same polynomial as the others': within 2^-22 of a cap up to kCapPlain no x lies far above it
       auto all_by = [&](auto&& tanh_of) __attribute__((always_inline)) {
         plain = true;
@@ -267,11 +262,17 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
           added();
         }
       };
+      // Coefficients of the logit itself, whose powers of scale / cap are in them: they run evenly from c0, which is a normal number, to the last one, so that one says whether all of them are
+      auto held = [](float last) { return fabsf(last) >= 0x1p-126f && fabsf(last) < INFINITY; };
       if (a.cap > kCapPlain) {
-      } else if (reach <= kTanhNear && held(n3)) {
-        all_by([&](float q) __attribute__((always_inline)) { return fmaf(fmaf(fmaf(n3, q, n2), q, n1), q, c0); });
-      } else if (reach <= kTanhWide && held(c5)) {
-        all_by([&](float q) __attribute__((always_inline)) { return fmaf(fmaf(fmaf(fmaf(fmaf(c5, q, c4), q, c3), q, c2), q, c1), q, c0); });
+      } else if (reach <= kTanhNear) {
+        constexpr auto& k = kTanhNearFit;
+        const float c0 = x1 * k[0], c1 = x1 * u2 * k[1], c2 = x1 * u2 * u2 * k[2], c3 = x1 * u2 * u2 * u2 * k[3];
+        if (held(c3)) all_by([&](float q) __attribute__((always_inline)) { return fmaf(fmaf(fmaf(c3, q, c2), q, c1), q, c0); });
+      } else if (reach <= kTanhWide) {
+        constexpr auto& k = kTanhWideFit;
+        const float c0 = x1 * k[0], c1 = x1 * u2 * k[1], c2 = x1 * u2 * u2 * k[2], c3 = x1 * u2 * u2 * u2 * k[3], c4 = x1 * u2 * u2 * u2 * u2 * k[4], c5 = x1 * u2 * u2 * u2 * u2 * u2 * k[5];
+        if (held(c5)) all_by([&](float q) __attribute__((always_inline)) { return fmaf(fmaf(fmaf(fmaf(fmaf(c5, q, c4), q, c3), q, c2), q, c1), q, c0); });
       }
     }
     const bool careful = !plain || __any(first != first);
