@@ -264,12 +264,12 @@ __global__ __launch_bounds__(256, sizeof(T) == 4 ? 4 : 5) void logprob_chunks_ke
       };
       // Coefficients of the logit itself, whose powers of scale / cap are in them: they run evenly from c0, which is a normal number, to the last one, so that one says whether all of them are
       auto held = [](float last) { return fabsf(last) >= 0x1p-126f && fabsf(last) < INFINITY; };
-      if (a.cap > kCapPlain) {
-      } else if (reach <= kTanhNear) {
+      const bool exact = a.cap > kCapPlain;                  // each by the form that the join takes too
+      if (!exact && reach <= kTanhNear) {
         constexpr auto& k = kTanhNearFit;
         const float c0 = x1 * k[0], c1 = x1 * u2 * k[1], c2 = x1 * u2 * u2 * k[2], c3 = x1 * u2 * u2 * u2 * k[3];
         if (held(c3)) all_by([&](float q) __attribute__((always_inline)) { return fmaf(fmaf(fmaf(c3, q, c2), q, c1), q, c0); });
-      } else if (reach <= kTanhWide) {
+      } else if (!exact && reach <= kTanhWide) {
         constexpr auto& k = kTanhWideFit;
         const float c0 = x1 * k[0], c1 = x1 * u2 * k[1], c2 = x1 * u2 * u2 * k[2], c3 = x1 * u2 * u2 * u2 * k[3], c4 = x1 * u2 * u2 * u2 * u2 * k[4], c5 = x1 * u2 * u2 * u2 * u2 * u2 * k[5];
         if (held(c5)) all_by([&](float q) __attribute__((always_inline)) { return fmaf(fmaf(fmaf(fmaf(fmaf(c5, q, c4), q, c3), q, c2), q, c1), q, c0); });
